@@ -213,6 +213,8 @@ def prepare(case, seed):
             s["D"] = normal(M, N, type=kind)
             s["dA"] = torch.empty(M, K, dtype=out, device=dev)
             s["dB"] = torch.empty_like(s["B"], dtype=out)
+            # (lent to the sums over many rows that few outputs have)
+            s["workspace"] = torch.empty(64 << 20, dtype=torch.uint8, device=dev)
         else:
             s["R"] = torch.empty(M, N, dtype=out, device=dev)
     elif op == "quantize":
@@ -341,7 +343,7 @@ def run(s):
             return [s["R"]]
         # dA = D B^T, row by row; dB = A^T D, expert by expert, in B's layout
         am.amulet_grouped_mm(s["D"], s["B"], s["offsets"], s["dA"], trans_b=not s["trans_b"])
-        am.amulet_grouped_mm_wgrad(s["A"], s["D"], s["offsets"], s["dB"], rows=s["rows"], trans_r=s["trans_b"])
+        am.amulet_grouped_mm_wgrad(s["A"], s["D"], s["offsets"], s["dB"], s["workspace"], rows=s["rows"], trans_r=s["trans_b"])
         return [s["dA"], s["dB"]]
     if op == "quantize":
         if s["rows"] == 1:
