@@ -67,7 +67,8 @@ typedef enum {
     AMULET_ERR_LAUNCH = -5, /* HIP reported an error at launch                */
     AMULET_ERR_SHAPE = -6,  /* unknown tile-shape id, or one the task lacks   */
     AMULET_ERR_RANGE = -7,  /* a dimension exceeds what the kernels index     */
-    AMULET_ERR_WORKSPACE = -8 /* the workspace lent to the call is too small   */
+    AMULET_ERR_WORKSPACE = -8, /* the workspace lent to the call is too small  */
+    AMULET_ERR_TYPE = -9    /* an element type the operator does not take      */
 } amulet_status_t;
 
 /*
@@ -603,6 +604,129 @@ int amulet_tile_of_workgroup(int64_t block, int64_t tiles_m, int64_t tiles_n, in
  * scratch buffer and blocks.  Returns AMULET_OK or a negative status.
  */
 int amulet_probe_mfma_i8(int waves_per_simd, double *macs_per_second, void *stream);
+
+/*
+ * ---- Operators of a mixture-of-experts layer ---------------------------------
+ *
+ * The same triple loop with the rows of A in groups, each with a matrix of its own:
+ *
+ *     R[i][j] = sum_k A[row(i)][k] * B[g(i)][k][j]
+ *
+ * for operands of 16 bits (bf16, fp16) or 8 (e4m3 with a scale for each block of
+ * 128), the router that makes the groups, and the sum that brings their rows
+ * back to the tokens; each with its gradients.  What a layer calls:
+ *
+ *     amulet_route            logits -> experts, weights, rows in order of expert
+ *     amulet_grouped_mm       tokens' rows x experts' matrices (rows = tokens)
+ *     amulet_combine          experts' rows -> tokens
+ *     ... and backward: amulet_combine_grad, amulet_grouped_mm with B read the other
+ *     way (the rows' gradients), amulet_grouped_mm_wgrad, amulet_combine without weights (the
+ *     rows' gradients back to the tokens), amulet_route_grad
+ *     amulet_quantize_fp8 / _blocks, then amulet_grouped_mm_fp8 or amulet_mm_fp8
+ *
+ * Conventions of the calls above hold (device pointers, row-major, pitches in
+ * elements, enqueue and return, nothing allocated, no host synchronisation), except:
+ *  - results are WRITTEN, not accumulated, and every element of them is: a sum over
+ *    nothing is 0 (K = 0, a group without rows, rows outside every group).  Only
+ *    amulet_combine_grad leaves the rows of dY that no pair names as they are.
+ *  - sums are fp32 whatever the operands' type and rounded once to the result's.  Their
+ *    order is fixed by the sizes: two calls on the same inputs give the same bits.
+ *  - NaN and infinities spread through the products as in any sum of products, to the
+ *    outputs that they belong to and no others.
+ *  - any alignment of elements and any pitch that holds a row is accepted.
+ *  - `offsets`: int32, G + 1 values in device memory, ascending; rows offsets[g] to
+ *    offsets[g+1] - 1 belong to group g.  They are read on the device only.  Values
+ *    outside 0..M count as the nearest of the two; where they do not ascend, results are
+ *    unspecified (and nothing outside the operands is read or written).
+ */
+typedef enum { AMULET_FP32 = 0, AMULET_BF16 = 1, AMULET_FP16 = 2 } amulet_type_t;
+
+/*
+ * The router.  logits: T x E of `type` (fp32, bf16, fp16), pitch ldx; 1 <= k <= min(E, 64), E <= 1024.
+ *   experts[t*k + j]  the expert with the j-th highest logit of token t; equal logits: the lower
+ *                     index first (0 and -0 are equal).  -inf and NaN are never chosen: -1 where
+ *                     nothing is left (mask an expert with -inf; the type's lowest value is an ordinary one)
+ *   weights[t*k + j]  fp32: norm != 0: exp(x) over the sum of the chosen ones'; else over the sum of all
+ *                     E (of an infinite maximum's equals each has the same share); 0 where experts is -1
+ *   place[t*k + j]    the pair's row: rows lie in order of expert, then of token; -1 where experts is -1
+ *   tokens[row]       the token of a row (T * k values; -1 past the last row)
+ *   offsets[e]        first row of expert e (E + 1 values; the last is the number of rows)
+ * The workspace (amulet_route_workspace_bytes, 0 up to 64 tokens) holds counts during the call.
+ * One kernel up to 64 tokens, two for more.
+ */
+size_t amulet_route_workspace_bytes(int64_t T, int64_t E);
+int amulet_route(int type, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldx, int norm,
+                 int32_t *experts, float *weights, int32_t *place, int32_t *tokens, int32_t *offsets,
+                 void *workspace, size_t workspace_bytes, void *stream);
+/* Its gradient: dlogits[t][e] = p_e (up_e - sum p up), up_e = dweights at a chosen expert and 0
+ * elsewhere, p = the weights (norm) or the softmax over all E; 0 for masked logits.  `experts`,
+ * `weights`: what amulet_route wrote.  `logits` is read only where norm is 0 (else it may be NULL). */
+int amulet_route_grad(int type, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldx, int norm,
+                      const int32_t *experts, const float *weights, const float *dweights,
+                      void *dlogits, int64_t lddx, void *stream);
+
+/* R[t] = sum_j weights[t*k+j] Y[place[t*k+j]], rows of H values of `type`; places outside
+ * 0..rows-1 (dropped pairs) add nothing; weights NULL: ones.  Y has `rows` rows. */
+int amulet_combine(int type, int64_t T, int64_t k, int64_t H, int64_t rows, const void *Y, int64_t ldy,
+                   const float *weights, const int32_t *place, void *R, int64_t ldr, void *stream);
+/* dY[place] = weights dR[t]; dweights = <dR[t], Y[place]> (0 for a dropped pair).  No two pairs may
+ * have the same place.  dweights NULL: not wanted (Y is then not read). */
+int amulet_combine_grad(int type, int64_t T, int64_t k, int64_t H, int64_t rows, const void *Y, int64_t ldy,
+                        const float *weights, const int32_t *place, const void *dR, int64_t lddr,
+                        void *dY, int64_t lddy, float *dweights, void *stream);
+
+/*
+ * Products by groups of rows: for row i of group g, R[i] = A[r] B[g], r = i, or rows[i] where `rows` is
+ * given (int32, M values; A then has a_rows rows, and a value that names none of them stands for a row of zeros).
+ *   A  bf16 or fp16 (`type`), lda >= K        B  G matrices, group_b elements apart:
+ *   K x N (ldb >= N), or N x K with trans_b (ldb >= K)        R  M x N, fp32 or the operands' type (`out_type`)
+ * The rows' gradients are the same call: D x (B read the other way).
+ */
+int amulet_grouped_mm(int type, int out_type, int trans_b, int64_t M, int64_t N, int64_t K, int64_t G,
+                      const void *A, int64_t lda, const int32_t *rows, int64_t a_rows,
+                      const void *B, int64_t ldb, int64_t group_b, const int32_t *offsets,
+                      void *R, int64_t ldr, void *stream);
+/*
+ * The matrices' gradients: R[g] = sum over the rows i of g of A[r]^T D[i], K x N, or its transpose
+ * (N x K) with trans_r; A: M (or a_rows, with `rows`) x K, D: M x N, R: G matrices, group_r elements apart.
+ * The workspace (any size, also none) lets sums over many rows that few outputs have run
+ * as parts on more of the chip; amulet_grouped_mm_wgrad_workspace_bytes: all that it could use.
+ */
+size_t amulet_grouped_mm_wgrad_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t G);
+int amulet_grouped_mm_wgrad(int type, int out_type, int trans_r, int64_t M, int64_t N, int64_t K, int64_t G,
+                            const void *A, int64_t lda, const int32_t *rows, int64_t a_rows,
+                            const void *D, int64_t ldd, const int32_t *offsets,
+                            void *R, int64_t ldr, int64_t group_r,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * 8-bit operands (e4m3: 4 exponent bits, 3 of mantissa, no infinities, largest value 448):
+ * scale = max(amax / 448, 2^-126) of a block, value = e4m3(x * (1 / scale)), to the nearest, ties to even.
+ *   amulet_quantize_fp8         blocks of 1 x 128: X is M x K, Q M x K, scales[b * lds + i] for block b of row i
+ *                               (ceil(K / 128) rows of M scales, lds >= M)
+ *   amulet_quantize_fp8_blocks  blocks of 128 x 128 of G matrices M x K: scales[g * group_s + (i / 128) * lds + k / 128]
+ * X: fp32, bf16 or fp16.  A NaN stays one; an infinity makes its block's scale infinite.
+ */
+int amulet_quantize_fp8(int type, int64_t M, int64_t K, const void *X, int64_t ldx,
+                        void *Q, int64_t ldq, float *scales, int64_t lds, void *stream);
+int amulet_quantize_fp8_blocks(int type, int64_t G, int64_t M, int64_t K, const void *X, int64_t ldx, int64_t group_x,
+                               void *Q, int64_t ldq, int64_t group_q, float *scales, int64_t lds, int64_t group_s,
+                               void *stream);
+/*
+ * As amulet_grouped_mm with 8-bit operands: scales_a as amulet_quantize_fp8 writes them for A's rows (lds_a apart per
+ * block of K, read at r), scales_b as amulet_quantize_fp8_blocks for the matrices as they are stored (K x N, or N x K
+ * with trans_b).  R: fp32, bf16 or fp16.  The products of 128 k are summed by the matrix instruction, whose
+ * sum drops what is below some 2^-17 of its largest product, and added up in fp32 times both scales.
+ * amulet_mm_fp8: one matrix, all rows.
+ */
+int amulet_grouped_mm_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K, int64_t G,
+                          const void *A, int64_t lda, const float *scales_a, int64_t lds_a, const int32_t *rows, int64_t a_rows,
+                          const void *B, int64_t ldb, int64_t group_b, const float *scales_b, int64_t lds_b, int64_t group_sb,
+                          const int32_t *offsets, void *R, int64_t ldr, void *stream);
+int amulet_mm_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K,
+                  const void *A, int64_t lda, const float *scales_a, int64_t lds_a,
+                  const void *B, int64_t ldb, const float *scales_b, int64_t lds_b,
+                  void *R, int64_t ldr, void *stream);
 
 /* Printable text for a status code (static storage). */
 const char *amulet_strerror(int code);

@@ -15,6 +15,7 @@ import os
 
 AMULET_IDENTITY, AMULET_DISCOUNT, AMULET_BOOST, AMULET_COUNT_GT = 0, 1, 2, 3
 AMULET_TASK_COUNT_I8 = 100
+AMULET_FP32, AMULET_BF16, AMULET_FP16 = 0, 1, 2
 AMULET_THRES_COL, AMULET_THRES_ROW, AMULET_THRES_CONST, AMULET_THRES_ELEM = 0, 1, 2, 3
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -26,6 +27,8 @@ _raw_stream = None
 # the compiled marshalling of the calls that a program makes most often (csrc/marshal.cpp); None before the
 # library is loaded and where it was not built for this Python and torch: the functions below do the same
 _marshal = None
+# torch's element types as the operators of a mixture-of-experts layer name them; filled with the library
+_types = {}
 
 
 class AmuletError(RuntimeError):
@@ -156,6 +159,34 @@ def load_library():
     lib.amulet_debug_fail_launches.argtypes = [i32]
     lib.amulet_version.restype = ctypes.c_char_p
     lib.amulet_version.argtypes = []
+    sz = ctypes.c_size_t
+    lib.amulet_route_workspace_bytes.restype = sz
+    lib.amulet_route_workspace_bytes.argtypes = [i64, i64]
+    lib.amulet_route.restype = i32
+    lib.amulet_route.argtypes = [i32, i64, i64, i64, vp, i64, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.amulet_route_grad.restype = i32
+    lib.amulet_route_grad.argtypes = [i32, i64, i64, i64, vp, i64, i32, vp, vp, vp, vp, i64, vp]
+    lib.amulet_combine.restype = i32
+    lib.amulet_combine.argtypes = [i32, i64, i64, i64, i64, vp, i64, vp, vp, vp, i64, vp]
+    lib.amulet_combine_grad.restype = i32
+    lib.amulet_combine_grad.argtypes = [i32, i64, i64, i64, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, vp]
+    lib.amulet_grouped_mm.restype = i32
+    lib.amulet_grouped_mm.argtypes = [i32, i32, i32, i64, i64, i64, i64, vp, i64, vp, i64, vp, i64, i64, vp, vp, i64, vp]
+    lib.amulet_grouped_mm_wgrad_workspace_bytes.restype = sz
+    lib.amulet_grouped_mm_wgrad_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    lib.amulet_grouped_mm_wgrad.restype = i32
+    lib.amulet_grouped_mm_wgrad.argtypes = [i32, i32, i32, i64, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, i64,
+                                            vp, sz, vp]
+    lib.amulet_quantize_fp8.restype = i32
+    lib.amulet_quantize_fp8.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.amulet_quantize_fp8_blocks.restype = i32
+    lib.amulet_quantize_fp8_blocks.argtypes = [i32, i64, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp]
+    lib.amulet_grouped_mm_fp8.restype = i32
+    lib.amulet_grouped_mm_fp8.argtypes = [i32, i32, i64, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, i64, vp, i64, i64,
+                                          vp, vp, i64, vp]
+    lib.amulet_mm_fp8.restype = i32
+    lib.amulet_mm_fp8.argtypes = [i32, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    _types.update({torch.float32: AMULET_FP32, torch.bfloat16: AMULET_BF16, torch.float16: AMULET_FP16})
     _torch, _raw_stream = torch, getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _marshal = _compiled_marshalling()
     _lib = lib
@@ -623,6 +654,215 @@ def amulet_probe_mfma_i8(waves_per_simd: int, stream=None) -> float:
     _check(load_library().amulet_probe_mfma_i8(waves_per_simd, ctypes.byref(out), _stream_ptr(stream)),
            "amulet_probe_mfma_i8")
     return out.value
+
+
+# ---- operators of a mixture-of-experts layer --------------------------------------------------------------------------
+
+def _vec(t, dtype, n, what: str):
+    """data_ptr of a contiguous device tensor of n values (any shape)."""
+    if not t.is_cuda or t.dtype is not dtype or not t.is_contiguous() or t.numel() != n:
+        raise ValueError("%s must hold %d contiguous %s values on the device" % (what, n, dtype))
+    return t.data_ptr()
+
+
+def _typed(t, what: str):
+    """(type code, data_ptr, rows, cols, leading dimension) of a 2-D device tensor of fp32, bf16 or fp16."""
+    if t.dtype not in _types:
+        raise ValueError("%s must be fp32, bf16 or fp16" % what)
+    return (_types[t.dtype],) + _mat(t, t.dtype, what)
+
+
+def _groups(t, dtype, what: str):
+    """(data_ptr, groups, rows, cols, leading dimension, elements between groups) of a 3-D device tensor."""
+    if not t.is_cuda or t.dim() != 3 or t.dtype is not dtype:
+        raise ValueError("%s must be a 3-D %s tensor on the GPU" % (what, dtype))
+    G, rows, cols = t.shape
+    gs, ld, step = t.stride()
+    if cols > 1 and step != 1:
+        raise ValueError("%s must have unit column stride" % what)
+    if rows <= 1:
+        ld = cols
+    return t.data_ptr(), G, rows, cols, ld if ld > 0 else 1, gs if G > 1 else rows * max(ld, 1)
+
+
+def _bytes(t, what: str):
+    if t is None:
+        return None, 0
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous device tensor" % what)
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def amulet_route_workspace_bytes(T: int, E: int) -> int:
+    """Bytes of workspace that amulet_route needs for T tokens and E experts (0 up to 64 tokens)."""
+    return int(load_library().amulet_route_workspace_bytes(T, E))
+
+
+def amulet_route(logits, experts, weights, place, tokens, offsets, workspace=None, *, norm: bool = True, stream=None):
+    """The k experts with the highest logits of every token, their weights, and the rows of all (token, expert) pairs
+    in order of expert.  logits: T x E (fp32, bf16, fp16; -inf masks).  Written: experts, place (T x k int32), weights
+    (T x k fp32: over the chosen with norm, else over all), tokens (T * k int32), offsets (E + 1 int32)."""
+    lib = load_library()
+    kind, px, T, E, ldx = _typed(logits, "logits")
+    if experts.dim() != 2 or experts.shape[0] != T:
+        raise ValueError("experts must be T x k")
+    k = experts.shape[1]
+    n, i32 = T * k, _torch.int32
+    pe, pw = _vec(experts, i32, n, "experts"), _vec(weights, _torch.float32, n, "weights")
+    pp, pt, po = _vec(place, i32, n, "place"), _vec(tokens, i32, n, "tokens"), _vec(offsets, i32, E + 1, "offsets")
+    ws, nw = _bytes(workspace, "workspace")
+    _check(lib.amulet_route(kind, T, E, k, px, ldx, int(norm), pe, pw, pp, pt, po, ws, nw, _stream_ptr(stream)), "amulet_route")
+
+
+def amulet_route_grad(logits, experts, weights, dweights, dlogits, *, norm: bool = True, stream=None):
+    """dlogits (T x E, written) from the weights' gradients; experts and weights as amulet_route wrote them.  logits is
+    read without norm only (None will do with it)."""
+    lib = load_library()
+    kind, pd, T, E, ldd = _typed(dlogits, "dlogits")
+    if experts.dim() != 2 or experts.shape[0] != T:
+        raise ValueError("experts must be T x k")
+    k, f32 = experts.shape[1], _torch.float32
+    px, ldx = None, E
+    if logits is not None and not norm:
+        px, T2, E2, ldx = _mat(logits, dlogits.dtype, "logits")
+        if (T2, E2) != (T, E):
+            raise ValueError("logits and dlogits must have one shape")
+    _check(lib.amulet_route_grad(kind, T, E, k, px, ldx, int(norm), _vec(experts, _torch.int32, T * k, "experts"),
+                                 _vec(weights, f32, T * k, "weights"), _vec(dweights, f32, T * k, "dweights"), pd, ldd,
+                                 _stream_ptr(stream)), "amulet_route_grad")
+
+
+def amulet_combine(Y, weights, place, R, *, stream=None):
+    """R[t] = sum_j weights[t, j] Y[place[t, j]]; a place outside Y adds nothing; weights None: ones."""
+    lib = load_library()
+    kind, pr, T, H, ldr = _typed(R, "R")
+    py, rows, H2, ldy = _mat(Y, R.dtype, "Y")
+    if H2 != H or place.dim() != 2 or place.shape[0] != T:
+        raise ValueError("shape mismatch: Y is rows x H, place T x k, R T x H")
+    k = place.shape[1]
+    pw = None if weights is None else _vec(weights, _torch.float32, T * k, "weights")
+    _check(lib.amulet_combine(kind, T, k, H, rows, py, ldy, pw, _vec(place, _torch.int32, T * k, "place"), pr, ldr,
+                              _stream_ptr(stream)), "amulet_combine")
+
+
+def amulet_combine_grad(Y, weights, place, dR, dY, dweights=None, *, stream=None):
+    """dY[place[t, j]] = weights[t, j] dR[t] (rows of dY that no pair names stay as they are), and dweights[t, j] =
+    <dR[t], Y[place[t, j]]> where dweights is given (else Y may be None)."""
+    lib = load_library()
+    kind, pd, T, H, ldd = _typed(dR, "dR")
+    pdy, rows, H2, lddy = _mat(dY, dR.dtype, "dY")
+    if H2 != H or place.dim() != 2 or place.shape[0] != T:
+        raise ValueError("shape mismatch: dY is rows x H, place T x k, dR T x H")
+    k = place.shape[1]
+    py, ldy, pdw = None, H, None
+    if dweights is not None:
+        py, rows2, H2, ldy = _mat(Y, dR.dtype, "Y")
+        if (rows2, H2) != (rows, H):
+            raise ValueError("Y and dY must have one shape")
+        pdw = _vec(dweights, _torch.float32, T * k, "dweights")
+    pw = None if weights is None else _vec(weights, _torch.float32, T * k, "weights")
+    _check(lib.amulet_combine_grad(kind, T, k, H, rows, py, ldy, pw, _vec(place, _torch.int32, T * k, "place"), pd, ldd, pdy, lddy,
+                                   pdw, _stream_ptr(stream)), "amulet_combine_grad")
+
+
+def _rows_of(rows, M):
+    return None if rows is None else _vec(rows, _torch.int32, M, "rows")
+
+
+def amulet_grouped_mm(A, B, offsets, R, *, rows=None, trans_b: bool = False, stream=None):
+    """R[i] = A[i] B[g] for the rows i of group g, offsets[g] <= i < offsets[g + 1] (A[rows[i]] where rows is given); rows of
+    no group are 0.  A bf16 or fp16; B G x K x N, or G x N x K with trans_b; R of A's type or fp32."""
+    lib = load_library()
+    kind, pa, Ra, K, lda = _typed(A, "A")
+    pb, G, b0, b1, ldb, gb = _groups(B, A.dtype, "B")
+    out, pr, M, N, ldr = _typed(R, "R")
+    if (b0, b1) != ((N, K) if trans_b else (K, N)) or (rows is None and Ra != M):
+        raise ValueError("shape mismatch between A, B and R")
+    _check(lib.amulet_grouped_mm(kind, out, int(trans_b), M, N, K, G, pa, lda, _rows_of(rows, M), Ra, pb, ldb, gb,
+                                 _vec(offsets, _torch.int32, G + 1, "offsets"), pr, ldr, _stream_ptr(stream)), "amulet_grouped_mm")
+
+
+def amulet_grouped_mm_wgrad_workspace_bytes(M: int, N: int, K: int, G: int) -> int:
+    """All the workspace that amulet_grouped_mm_wgrad can use for these sizes (it runs with less, or none)."""
+    return int(load_library().amulet_grouped_mm_wgrad_workspace_bytes(M, N, K, G))
+
+
+def amulet_grouped_mm_wgrad(A, D, offsets, R, workspace=None, *, rows=None, trans_r: bool = False, stream=None):
+    """R[g] = sum over the rows i of group g of A[i]^T D[i] (A[rows[i]] where rows is given): G x K x N, or G x N x K with
+    trans_r; 0 for a group without rows.  A, D bf16 or fp16; R of their type or fp32."""
+    lib = load_library()
+    kind, pa, Ra, K, lda = _typed(A, "A")
+    pd, M, N, ldd = _mat(D, A.dtype, "D")
+    if R.dtype not in _types:
+        raise ValueError("R must be fp32, bf16 or fp16")
+    pr, G, r0, r1, ldr, gr = _groups(R, R.dtype, "R")
+    if (r0, r1) != ((N, K) if trans_r else (K, N)) or (rows is None and Ra != M):
+        raise ValueError("shape mismatch between A, D and R")
+    ws, nw = _bytes(workspace, "workspace")
+    _check(lib.amulet_grouped_mm_wgrad(kind, _types[R.dtype], int(trans_r), M, N, K, G, pa, lda, _rows_of(rows, M), Ra, pd, ldd,
+                                       _vec(offsets, _torch.int32, G + 1, "offsets"), pr, ldr, gr, ws, nw, _stream_ptr(stream)),
+           "amulet_grouped_mm_wgrad")
+
+
+def amulet_quantize_fp8(X, Q, scales, *, stream=None):
+    """e4m3 values Q of X (M x K; fp32, bf16, fp16), one scale to 128 values of a row: scales[k // 128, i], ceil(K / 128) x M."""
+    lib = load_library()
+    kind, px, M, K, ldx = _typed(X, "X")
+    pq, M2, K2, ldq = _mat(Q, _torch.float8_e4m3fn, "Q")
+    ps, KB, M3, lds = _mat(scales, _torch.float32, "scales")
+    if (M2, K2) != (M, K) or (KB, M3) != ((K + 127) // 128, M):
+        raise ValueError("shape mismatch: Q has X's shape, scales are ceil(K / 128) x M")
+    _check(lib.amulet_quantize_fp8(kind, M, K, px, ldx, pq, ldq, ps, lds, _stream_ptr(stream)), "amulet_quantize_fp8")
+
+
+def amulet_quantize_fp8_blocks(X, Q, scales, *, stream=None):
+    """e4m3 values Q of X (G x M x K; fp32, bf16, fp16), one scale to 128 x 128: scales[g, i // 128, k // 128]."""
+    lib = load_library()
+    if X.dtype not in _types:
+        raise ValueError("X must be fp32, bf16 or fp16")
+    px, G, M, K, ldx, gx = _groups(X, X.dtype, "X")
+    pq, G2, M2, K2, ldq, gq = _groups(Q, _torch.float8_e4m3fn, "Q")
+    ps, G3, MB, KB, lds, gs = _groups(scales, _torch.float32, "scales")
+    if (G2, M2, K2) != (G, M, K) or (G3, MB, KB) != (G, (M + 127) // 128, (K + 127) // 128):
+        raise ValueError("shape mismatch: Q has X's shape, scales are G x ceil(M / 128) x ceil(K / 128)")
+    _check(lib.amulet_quantize_fp8_blocks(_types[X.dtype], G, M, K, px, ldx, gx, pq, ldq, gq, ps, lds, gs, _stream_ptr(stream)),
+           "amulet_quantize_fp8_blocks")
+
+
+def amulet_grouped_mm_fp8(A, scales_a, B, scales_b, offsets, R, *, rows=None, trans_b: bool = False, stream=None):
+    """amulet_grouped_mm of e4m3 operands: scales_a ceil(K / 128) x rows of A (amulet_quantize_fp8), scales_b one to 128 x 128
+    of B as it is stored (amulet_quantize_fp8_blocks).  R fp32, bf16 or fp16."""
+    lib = load_library()
+    f8 = _torch.float8_e4m3fn
+    pa, Ra, K, lda = _mat(A, f8, "A")
+    psa, KB, Rs, lsa = _mat(scales_a, _torch.float32, "scales_a")
+    pb, G, b0, b1, ldb, gb = _groups(B, f8, "B")
+    psb, G2, s0, s1, lsb, gsb = _groups(scales_b, _torch.float32, "scales_b")
+    out, pr, M, N, ldr = _typed(R, "R")
+    if (b0, b1) != ((N, K) if trans_b else (K, N)) or (rows is None and Ra != M):
+        raise ValueError("shape mismatch between A, B and R")
+    if (KB, Rs) != ((K + 127) // 128, Ra) or (G2, s0, s1) != (G, (b0 + 127) // 128, (b1 + 127) // 128):
+        raise ValueError("shape mismatch between operands and scales")
+    _check(lib.amulet_grouped_mm_fp8(out, int(trans_b), M, N, K, G, pa, lda, psa, lsa if KB > 1 else Ra, _rows_of(rows, M), Ra,
+                                     pb, ldb, gb, psb, lsb, gsb, _vec(offsets, _torch.int32, G + 1, "offsets"), pr, ldr,
+                                     _stream_ptr(stream)), "amulet_grouped_mm_fp8")
+
+
+def amulet_mm_fp8(A, scales_a, B, scales_b, R, *, trans_b: bool = False, stream=None):
+    """amulet_grouped_mm_fp8 with one matrix B (K x N, or N x K with trans_b) for all rows."""
+    lib = load_library()
+    f8, f32 = _torch.float8_e4m3fn, _torch.float32
+    pa, M, K, lda = _mat(A, f8, "A")
+    psa, KB, Ms, lsa = _mat(scales_a, f32, "scales_a")
+    pb, b0, b1, ldb = _mat(B, f8, "B")
+    psb, s0, s1, lsb = _mat(scales_b, f32, "scales_b")
+    out, pr, M2, N, ldr = _typed(R, "R")
+    if (b0, b1) != ((N, K) if trans_b else (K, N)) or M2 != M:
+        raise ValueError("shape mismatch between A, B and R")
+    if (KB, Ms) != ((K + 127) // 128, M) or (s0, s1) != ((b0 + 127) // 128, (b1 + 127) // 128):
+        raise ValueError("shape mismatch between operands and scales")
+    _check(lib.amulet_mm_fp8(out, int(trans_b), M, N, K, pa, lda, psa, lsa, pb, ldb, psb, lsb, pr, ldr, _stream_ptr(stream)),
+           "amulet_mm_fp8")
 
 
 def amulet_strerror(code: int) -> str:

@@ -14,6 +14,7 @@
 
 #include "amulet.h"
 #include "amulet_internal.h"
+#include "experts_internal.h"
 
 namespace amulet {
 
@@ -171,6 +172,7 @@ struct KernelNote {
     int critical;                  // (rows of a tile of the kernel by critical values, which has no shape id either)
     int groups;                    // (fp64 identity: groups of waves that share a tile's K)
     CountRan ran;                  // (join count by a shape id)
+    const char *name;              // (an operator of a mixture-of-experts layer: the whole name)
 };
 constexpr unsigned KERNEL_NOTES = 16;
 static thread_local KernelNote g_notes[KERNEL_NOTES];
@@ -178,12 +180,19 @@ static thread_local unsigned g_notes_made = 0;
 static KernelNote &new_note(int task, int f64, int shape, int64_t rows)
 {
     KernelNote &n = g_notes[g_notes_made++ % KERNEL_NOTES];
-    n = KernelNote{task, f64, shape, 0, 1, 0, 0, 0, 0, 0, 0, rows, 0, 0, 1, CountRan()};
+    n = KernelNote{task, f64, shape, 0, 1, 0, 0, 0, 0, 0, 0, rows, 0, 0, 1, CountRan(), nullptr};
     return n;
 }
 
 // text of the last HIP error a launch reported (diagnostics for AMULET_ERR_LAUNCH)
 static thread_local hipError_t g_last_hip_error = hipSuccess;
+
+void note_kernel(const char *name, int64_t rows) { new_note(-1, 0, -1, rows).name = name; }
+int launch_status(hipError_t e)
+{
+    g_last_hip_error = e;
+    return e == hipSuccess ? AMULET_OK : AMULET_ERR_LAUNCH;
+}
 
 static const int64_t kMaxDim = 2147483647LL - 65536LL;
 
@@ -1768,7 +1777,9 @@ const char *amulet_recent_kernel(int back)
     if (back < 0 || back >= (int)KERNEL_NOTES || (unsigned)back >= g_notes_made) return text;
     const KernelNote &n = g_notes[(g_notes_made - 1 - (unsigned)back) % KERNEL_NOTES];
     const long long rows = (long long)n.rows;
-    if (n.shape >= 0) {
+    if (n.name) {
+        snprintf(text, sizeof(text), "%s rows %lld", n.name, rows);
+    } else if (n.shape >= 0) {
         const char *name = !n.f64 ? amulet_shape_name(n.task, n.shape)
                            : n.task != TASK_IDENTITY ? amulet_f64_shape_name(n.shape)
                            : n.shape % F64_TILES == 0 ? "mfma_f64_64x64_dma4" : "mfma_f64_128x128_dma4";
@@ -1830,6 +1841,7 @@ const char *amulet_strerror(int code)
     case AMULET_ERR_SHAPE: return "unknown tile shape";
     case AMULET_ERR_RANGE: return "dimension too large for the kernels' 32-bit indexing";
     case AMULET_ERR_WORKSPACE: return "workspace too small for the packed copy";
+    case AMULET_ERR_TYPE: return "unknown element type, or one the operator does not take";
     default: return "unknown status code";
     }
 }

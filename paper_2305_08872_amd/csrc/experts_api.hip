@@ -1,0 +1,320 @@
+// C ABI of a mixture-of-experts layer's operators: argument checks, the choice of tiles, launches.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "amulet.h"
+#include "experts_internal.h"
+
+namespace amulet {
+
+static const int64_t kMostRows = 2147483647LL - 65536LL;   // of a dimension, as in the other calls
+static const int64_t kMostGroups = 1 << 20;
+static const int64_t kMostBlocks = 0xffffffffLL / 512;     // workgroups of a launch (a grid holds 2^32 - 1 work-items)
+
+static bool known16(int type) { return type == AMULET_BF16 || type == AMULET_FP16; }
+static bool known(int type) { return type == AMULET_FP32 || known16(type); }
+
+// Tiles by rows.  A tile's rows follow the average group's: rows past a group's end are work for nothing, and a tile
+// of fewer rows reads the group's matrix more often.
+static int rows_tile(int64_t M, int64_t N, int64_t G)
+{
+    const int64_t per = (M + G - 1) / G;
+    if (per <= 16) return N >= 8192 ? EXPERTS_16x64 : EXPERTS_16x32;
+    if (per <= 32) return EXPERTS_32x64;
+    if (per <= 64) return EXPERTS_64x128;
+    const int64_t tiles = (M / 256 + G) * ((N + 255) / 256);
+    return per >= 192 && tiles >= compute_units() ? EXPERTS_256x256 : EXPERTS_128x128;
+}
+// Workgroups that are enough for any offsets: a group's last tile may hold one row only, and the rows outside the groups
+// are two regions more.
+static int64_t rows_blocks(int tile, int64_t M, int64_t N, int64_t G, bool grouped)
+{
+    const int64_t bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
+    const int64_t regions = !grouped ? 1 : G + 2 < M ? G + 2 : M;
+    const int64_t tiles = (M + regions * (bm - 1)) / bm * ((N + bn - 1) / bn);
+    return (tiles + 7) / 8 * 8;
+}
+
+static int check_rows(int64_t M, int64_t N, int64_t K, int64_t G, int trans_b, const void *A, int64_t lda, const int32_t *rows, int64_t a_rows,
+                      const void *B, int64_t ldb, int64_t group_b, const int32_t *offsets, bool grouped, const void *R, int64_t ldr)
+{
+    if (M < 0 || N < 0 || K < 0 || G < 0 || a_rows < 0) return AMULET_ERR_DIM;
+    if (M > kMostRows || N > kMostRows || K > kMostRows || a_rows > kMostRows || G > kMostGroups) return AMULET_ERR_RANGE;
+    if (M == 0 || N == 0) return 1;   // nothing to write
+    if (!R || (grouped && !offsets)) return AMULET_ERR_NULL;
+    if (ldr < N) return AMULET_ERR_LD;
+    if (K == 0 || G == 0 || (rows && a_rows == 0)) return AMULET_OK;   // zeros: the operands are not read
+    if (!A || !B) return AMULET_ERR_NULL;
+    if (lda < K || ldb < (trans_b ? K : N) || (G > 1 && group_b < 0)) return AMULET_ERR_LD;
+    return AMULET_OK;
+}
+
+static int run_rows(const char *const *names, int type, int trans_b, ExpertsArgs &a, int64_t M, int64_t N, int64_t G, void *stream)
+{
+    const int tile = rows_tile(M, N, G < 1 ? 1 : G);
+    const int64_t blocks = rows_blocks(tile, M, N, G, a.offsets != nullptr);
+    if (blocks > kMostBlocks) return AMULET_ERR_RANGE;
+    note_kernel(names[tile], M);
+    hipStream_t s = (hipStream_t)stream;
+    switch (type) {
+    case EXPERTS_BF16: return launch_status(launch_experts_rows_bf16(tile, !trans_b, a, blocks, s));
+    case EXPERTS_FP16: return launch_status(launch_experts_rows_fp16(tile, !trans_b, a, blocks, s));
+    default: return launch_status(launch_experts_rows_fp8(tile, !trans_b, a, blocks, s));
+    }
+}
+
+static const char *const kRowsNames[EXPERTS_TILES] = {"grouped_mm_256x256", "grouped_mm_128x128", "grouped_mm_64x128", "grouped_mm_32x64", "grouped_mm_16x64", "grouped_mm_16x32"};
+static const char *const kFp8Names[EXPERTS_TILES] = {"mm_fp8_256x256", "mm_fp8_128x128", "mm_fp8_64x128", "mm_fp8_32x64", "mm_fp8_16x64", "mm_fp8_16x32"};
+
+// The weights' gradients: tiles, and the parts that a group's rows are summed in.  A part is a workgroup of its own that
+// writes its fp32 sums to the workspace, so there are only as many as bring the workgroups to two per compute unit, of at
+// least 512 rows of an average group each, and as the workspace holds.
+static int sums_tile(int64_t rows_r, int64_t cols_r, int64_t G)
+{
+    const int64_t tiles = ((rows_r + 255) / 256) * ((cols_r + 255) / 256) * G;
+    return tiles >= compute_units() ? EXPERTS_256x256 : EXPERTS_128x128;
+}
+static int64_t sums_parts(int tile, int64_t rows_r, int64_t cols_r, int64_t G, int64_t M, size_t bytes)
+{
+    const int64_t bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
+    const int64_t tiles = ((rows_r + bm - 1) / bm) * ((cols_r + bn - 1) / bn) * G;
+    int64_t parts = 2 * (int64_t)compute_units() / tiles;
+    const int64_t most = M / (512 * G), room = (int64_t)(bytes / 4 / (size_t)(bm * bn)) / tiles;
+    if (parts > most) parts = most;
+    if (parts > room) parts = room;
+    return parts < 1 ? 1 : parts;
+}
+
+}  // namespace amulet
+
+using namespace amulet;
+
+extern "C" {
+
+size_t amulet_route_workspace_bytes(int64_t T, int64_t E)
+{
+    if (T <= 64 || E <= 0 || T > kMostRows || E > 1024) return 0;
+    return (size_t)(route_blocks(T) * E * 4);
+}
+
+static int check_route(int type, int64_t T, int64_t E, int64_t k, int64_t ldx)
+{
+    if (!known(type)) return AMULET_ERR_TYPE;
+    if (T < 0 || E < 1 || k < 1 || k > E) return AMULET_ERR_DIM;
+    if (E > 1024 || k > 64 || T > kMostRows / k) return AMULET_ERR_RANGE;
+    if (ldx < E) return AMULET_ERR_LD;
+    return AMULET_OK;
+}
+
+int amulet_route(int type, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldx, int norm,
+                 int32_t *experts, float *weights, int32_t *place, int32_t *tokens, int32_t *offsets,
+                 void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_route(type, T, E, k, ldx);
+    if (rc != AMULET_OK) return rc;
+    if (!offsets || (T > 0 && (!logits || !experts || !weights || !place || !tokens))) return AMULET_ERR_NULL;
+    const size_t need = amulet_route_workspace_bytes(T, E);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return AMULET_ERR_WORKSPACE;
+    if (((uintptr_t)workspace & 3) != 0) return AMULET_ERR_WORKSPACE;
+    RouteArgs a = {};
+    a.logits = logits; a.ldx = ldx; a.type = type;
+    a.T = (int)T; a.E = (int)E; a.k = (int)k; a.norm = norm;
+    a.experts = experts; a.weights = weights; a.place = place; a.tokens = tokens; a.offsets = offsets;
+    a.counts = (int32_t *)workspace;
+    note_kernel("route", T);
+    return launch_status(launch_route(a, (hipStream_t)stream));
+}
+
+int amulet_route_grad(int type, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldx, int norm,
+                      const int32_t *experts, const float *weights, const float *dweights,
+                      void *dlogits, int64_t lddx, void *stream)
+{
+    const int rc = check_route(type, T, E, k, norm ? E : ldx);
+    if (rc != AMULET_OK) return rc;
+    if (T == 0) return AMULET_OK;
+    if ((!norm && !logits) || !experts || !weights || !dweights || !dlogits) return AMULET_ERR_NULL;
+    if (lddx < E) return AMULET_ERR_LD;
+    RouteArgs a = {};
+    a.logits = logits; a.ldx = ldx; a.type = type;
+    a.T = (int)T; a.E = (int)E; a.k = (int)k; a.norm = norm;
+    a.experts = (int32_t *)experts; a.weights = (float *)weights; a.dweights = dweights;
+    a.dlogits = dlogits; a.lddx = lddx;
+    note_kernel("route_grad", T);
+    return launch_status(launch_route_grad(a, (hipStream_t)stream));
+}
+
+static int check_combine(int type, int64_t T, int64_t k, int64_t H, int64_t rows)
+{
+    if (!known(type)) return AMULET_ERR_TYPE;
+    if (T < 0 || k < 0 || H < 0 || rows < 0) return AMULET_ERR_DIM;
+    if (H > kMostRows || rows > kMostRows || k > kMostRows || T > kMostRows / (k > 0 ? k : 1)) return AMULET_ERR_RANGE;
+    if (T == 0 || H == 0) return 1;
+    // (four waves to a workgroup of 256 threads)
+    const int64_t chunks = (H + 255) / 256, waves = T * (k > chunks ? k : chunks);
+    return (waves + 3) / 4 > kMostBlocks ? AMULET_ERR_RANGE : AMULET_OK;
+}
+
+int amulet_combine(int type, int64_t T, int64_t k, int64_t H, int64_t rows, const void *Y, int64_t ldy,
+                   const float *weights, const int32_t *place, void *R, int64_t ldr, void *stream)
+{
+    const int rc = check_combine(type, T, k, H, rows);
+    if (rc != AMULET_OK) return rc > 0 ? AMULET_OK : rc;
+    if (!R || (k > 0 && !place) || (k > 0 && rows > 0 && !Y)) return AMULET_ERR_NULL;
+    if (ldr < H || (k > 0 && rows > 0 && ldy < H)) return AMULET_ERR_LD;
+    CombineArgs a = {};
+    a.Y = Y; a.ldy = ldy; a.weights = weights; a.place = place; a.R = R; a.ldr = ldr;
+    a.T = (int)T; a.k = (int)k; a.H = (int)H; a.type = type; a.rows = rows;
+    note_kernel("combine", T);
+    return launch_status(launch_combine(a, (hipStream_t)stream));
+}
+
+int amulet_combine_grad(int type, int64_t T, int64_t k, int64_t H, int64_t rows, const void *Y, int64_t ldy,
+                        const float *weights, const int32_t *place, const void *dR, int64_t lddr,
+                        void *dY, int64_t lddy, float *dweights, void *stream)
+{
+    const int rc = check_combine(type, T, k, H > 0 ? H : 1, rows);
+    if (rc != AMULET_OK) return rc > 0 ? AMULET_OK : rc;
+    if (H < 0) return AMULET_ERR_DIM;
+    if (k == 0) return AMULET_OK;
+    if (!place || (H > 0 && (!dR || (rows > 0 && (!dY || (dweights && !Y)))))) return AMULET_ERR_NULL;
+    if (lddr < H || (rows > 0 && (lddy < H || (dweights && ldy < H)))) return AMULET_ERR_LD;
+    CombineArgs a = {};
+    a.Y = Y; a.ldy = ldy; a.weights = weights; a.place = place; a.R = (void *)dR; a.ldr = lddr;
+    a.dY = dY; a.lddy = lddy; a.dweights = dweights;
+    a.T = (int)T; a.k = (int)k; a.H = (int)H; a.type = type; a.rows = rows;
+    note_kernel("combine_grad", T);
+    return launch_status(launch_combine_grad(a, (hipStream_t)stream));
+}
+
+int amulet_grouped_mm(int type, int out_type, int trans_b, int64_t M, int64_t N, int64_t K, int64_t G,
+                      const void *A, int64_t lda, const int32_t *rows, int64_t a_rows,
+                      const void *B, int64_t ldb, int64_t group_b, const int32_t *offsets,
+                      void *R, int64_t ldr, void *stream)
+{
+    if (!known16(type) || (out_type != AMULET_FP32 && out_type != type)) return AMULET_ERR_TYPE;
+    const int rc = check_rows(M, N, K, G, trans_b, A, lda, rows, a_rows, B, ldb, group_b, offsets, true, R, ldr);
+    if (rc != AMULET_OK) return rc > 0 ? AMULET_OK : rc;
+    ExpertsArgs a = {};
+    a.A = A; a.B = B; a.R = R; a.offsets = offsets; a.rows = rows;
+    a.lda = lda; a.ldb = ldb; a.ldr = ldr; a.group_b = group_b;
+    a.M = (int)M; a.N = (int)N; a.K = G == 0 || (rows && a_rows == 0) ? 0 : (int)K; a.G = (int)G; a.a_rows = (int)a_rows;
+    a.out = out_type;
+    return run_rows(kRowsNames, type, trans_b, a, M, N, G, stream);
+}
+
+size_t amulet_grouped_mm_wgrad_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t G)
+{
+    if (M <= 0 || N <= 0 || K <= 0 || G <= 0 || M > kMostRows || N > kMostRows || K > kMostRows || G > kMostGroups) return 0;
+    const int tile = sums_tile(K, N, G);
+    const int64_t bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
+    const int64_t tiles = ((K + bm - 1) / bm) * ((N + bn - 1) / bn) * G, parts = sums_parts(tile, K, N, G, M, ~(size_t)0 >> 1);
+    return parts < 2 ? 0 : (size_t)(tiles * parts * bm * bn * 4);
+}
+
+int amulet_grouped_mm_wgrad(int type, int out_type, int trans_r, int64_t M, int64_t N, int64_t K, int64_t G,
+                            const void *A, int64_t lda, const int32_t *rows, int64_t a_rows,
+                            const void *D, int64_t ldd, const int32_t *offsets,
+                            void *R, int64_t ldr, int64_t group_r,
+                            void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!known16(type) || (out_type != AMULET_FP32 && out_type != type)) return AMULET_ERR_TYPE;
+    if (M < 0 || N < 0 || K < 0 || G < 0 || a_rows < 0) return AMULET_ERR_DIM;
+    if (M > kMostRows || N > kMostRows || K > kMostRows || a_rows > kMostRows || G > kMostGroups) return AMULET_ERR_RANGE;
+    if (G == 0 || N == 0 || K == 0) return AMULET_OK;
+    if (!R || !offsets) return AMULET_ERR_NULL;
+    if (ldr < (trans_r ? K : N) || (G > 1 && group_r / ldr < (trans_r ? N : K))) return AMULET_ERR_LD;
+    const bool some = M > 0 && !(rows && a_rows == 0);   // else: zeros, and the operands are not read
+    if (some && (!A || !D)) return AMULET_ERR_NULL;
+    if (some && (lda < K || ldd < N)) return AMULET_ERR_LD;
+    ExpertsArgs a = {};
+    a.R = R; a.offsets = offsets; a.rows = rows; a.ldr = ldr; a.group_r = group_r;
+    a.G = (int)G; a.a_rows = (int)a_rows; a.k_rows = some ? (int)M : 0; a.out = out_type;
+    // lines of the first operand are R's rows
+    if (trans_r) { a.A = D; a.lda = ldd; a.B = A; a.ldb = lda; a.M = (int)N; a.N = (int)K; a.rows_of_b = 1; }
+    else { a.A = A; a.lda = lda; a.B = D; a.ldb = ldd; a.M = (int)K; a.N = (int)N; }
+    const int tile = sums_tile(a.M, a.N, G);
+    if (((uintptr_t)workspace & 15) != 0) return AMULET_ERR_WORKSPACE;
+    a.workspace = (float *)workspace;
+    a.parts = (int)sums_parts(tile, a.M, a.N, G, M, workspace ? workspace_bytes : 0);
+    const int64_t bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
+    const int64_t tiles = ((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn) * G;
+    if (tiles * a.parts > kMostBlocks || tiles * (bm * bn / 1024) > kMostBlocks) return AMULET_ERR_RANGE;
+    note_kernel(tile == EXPERTS_256x256 ? "grouped_mm_wgrad_256x256" : "grouped_mm_wgrad_128x128", M);
+    hipStream_t s = (hipStream_t)stream;
+    const int rc = launch_status(launch_experts_sums(type, tile, a, (tiles * a.parts + 7) / 8 * 8, s));
+    if (rc != AMULET_OK || a.parts == 1) return rc;
+    return launch_status(launch_experts_join(tile, a, s));
+}
+
+int amulet_quantize_fp8(int type, int64_t M, int64_t K, const void *X, int64_t ldx,
+                        void *Q, int64_t ldq, float *scales, int64_t lds, void *stream)
+{
+    if (!known(type)) return AMULET_ERR_TYPE;
+    if (M < 0 || K < 0) return AMULET_ERR_DIM;
+    if (M > kMostRows || K > kMostRows || (M + 15) / 16 * ((K + 127) / 128) > kMostBlocks) return AMULET_ERR_RANGE;
+    if (M == 0 || K == 0) return AMULET_OK;
+    if (!X || !Q || !scales) return AMULET_ERR_NULL;
+    if (ldx < K || ldq < K || lds < M) return AMULET_ERR_LD;
+    QuantizeArgs a = {};
+    a.X = X; a.ldx = ldx; a.Q = (uint8_t *)Q; a.ldq = ldq; a.scales = scales; a.lds = lds;
+    a.G = 1; a.M = (int)M; a.K = (int)K; a.type = type;
+    note_kernel("quantize_fp8", M);
+    return launch_status(launch_quantize_rows(a, (hipStream_t)stream));
+}
+
+int amulet_quantize_fp8_blocks(int type, int64_t G, int64_t M, int64_t K, const void *X, int64_t ldx, int64_t group_x,
+                               void *Q, int64_t ldq, int64_t group_q, float *scales, int64_t lds, int64_t group_s,
+                               void *stream)
+{
+    if (!known(type)) return AMULET_ERR_TYPE;
+    if (G < 0 || M < 0 || K < 0) return AMULET_ERR_DIM;
+    if (M > kMostRows || K > kMostRows || G > kMostGroups) return AMULET_ERR_RANGE;
+    if (G == 0 || M == 0 || K == 0) return AMULET_OK;
+    const int64_t MB = (M + 127) / 128, KB = (K + 127) / 128;
+    if (MB * KB > kMostBlocks / G) return AMULET_ERR_RANGE;
+    if (!X || !Q || !scales) return AMULET_ERR_NULL;
+    if (ldx < K || ldq < K || lds < KB || (G > 1 && (group_x < 0 || group_q / ldq < M || group_s / lds < MB))) return AMULET_ERR_LD;
+    QuantizeArgs a = {};
+    a.X = X; a.ldx = ldx; a.group_x = group_x; a.Q = (uint8_t *)Q; a.ldq = ldq; a.group_q = group_q;
+    a.scales = scales; a.lds = lds; a.group_s = group_s;
+    a.G = (int)G; a.M = (int)M; a.K = (int)K; a.type = type;
+    note_kernel("quantize_fp8_blocks", G * M);
+    return launch_status(launch_quantize_blocks(a, (hipStream_t)stream));
+}
+
+static int run_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K, int64_t G,
+                   const void *A, int64_t lda, const float *scales_a, int64_t lds_a, const int32_t *rows, int64_t a_rows,
+                   const void *B, int64_t ldb, int64_t group_b, const float *scales_b, int64_t lds_b, int64_t group_sb,
+                   const int32_t *offsets, bool grouped, void *R, int64_t ldr, void *stream)
+{
+    if (!known(out_type)) return AMULET_ERR_TYPE;
+    const int rc = check_rows(M, N, K, G, trans_b, A, lda, rows, a_rows, B, ldb, group_b, offsets, grouped, R, ldr);
+    if (rc != AMULET_OK) return rc > 0 ? AMULET_OK : rc;
+    const bool some = K > 0 && G > 0 && !(rows && a_rows == 0);
+    if (some && (!scales_a || !scales_b)) return AMULET_ERR_NULL;
+    if (some && (lds_a < (rows ? a_rows : M) || lds_b < ((trans_b ? K : N) + 127) / 128 || (G > 1 && group_sb < 0))) return AMULET_ERR_LD;
+    ExpertsArgs a = {};
+    a.A = A; a.B = B; a.R = R; a.offsets = offsets; a.rows = rows; a.scale_a = scales_a; a.scale_b = scales_b;
+    a.lda = lda; a.ldb = ldb; a.ldr = ldr; a.group_b = group_b; a.ld_sa = lds_a; a.ld_sb = lds_b; a.group_sb = group_sb;
+    a.M = (int)M; a.N = (int)N; a.K = some ? (int)K : 0; a.G = (int)G; a.a_rows = (int)a_rows;
+    a.out = out_type;
+    return run_rows(kFp8Names, EXPERTS_FP8, trans_b, a, M, N, G, stream);
+}
+
+int amulet_grouped_mm_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K, int64_t G,
+                          const void *A, int64_t lda, const float *scales_a, int64_t lds_a, const int32_t *rows, int64_t a_rows,
+                          const void *B, int64_t ldb, int64_t group_b, const float *scales_b, int64_t lds_b, int64_t group_sb,
+                          const int32_t *offsets, void *R, int64_t ldr, void *stream)
+{
+    return run_fp8(out_type, trans_b, M, N, K, G, A, lda, scales_a, lds_a, rows, a_rows, B, ldb, group_b, scales_b, lds_b, group_sb, offsets, true, R, ldr, stream);
+}
+
+int amulet_mm_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K,
+                  const void *A, int64_t lda, const float *scales_a, int64_t lds_a,
+                  const void *B, int64_t ldb, const float *scales_b, int64_t lds_b,
+                  void *R, int64_t ldr, void *stream)
+{
+    return run_fp8(out_type, trans_b, M, N, K, 1, A, lda, scales_a, lds_a, nullptr, 0, B, ldb, 0, scales_b, lds_b, 0, nullptr, false, R, ldr, stream);
+}
+
+}  // extern "C"

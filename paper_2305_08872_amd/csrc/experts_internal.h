@@ -1,0 +1,88 @@
+// Declarations shared by the translation units of a mixture-of-experts layer's operators: the router, the products by
+// groups of rows, the fp8 quantiser.  Not part of the C ABI.
+#ifndef AMULET_EXPERTS_INTERNAL_H
+#define AMULET_EXPERTS_INTERNAL_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "amulet_internal.h"
+
+namespace amulet {
+
+// types of elements, as in the C ABI (amulet_type_t)
+enum { EXPERTS_FP32 = 0, EXPERTS_BF16 = 1, EXPERTS_FP16 = 2, EXPERTS_FP8 = 3 };
+
+// A product by groups of rows, checked on the host.  Pitches and strides in elements.
+struct ExpertsArgs {
+    const void *A, *B;
+    void *R;
+    const int32_t *offsets;          // G + 1 first rows, or null: one group of all rows
+    const int32_t *rows;             // storage row of A (by sums: of A or D) for each row, or null
+    const float *scale_a, *scale_b;  // fp8: [k block][row of A]; [block of B's storage rows][block of its columns]
+    float *workspace;                // by sums, parts > 1: fp32 sums of tiles
+    int64_t lda, ldb, ldr, group_b, group_r, ld_sa, ld_sb, group_sb;
+    int M, N, K, G;                  // by sums: M, N are the columns of A's and D's storage
+    int a_rows;                      // rows that `rows` may name
+    int k_rows;                      // by sums: rows of all groups
+    int parts;                       // by sums: ranges of a group's rows, each a workgroup's
+    int rows_of_b;                   // by sums: `rows` names D's rows
+    int out;                         // type of R
+};
+
+// tiles of R by rows (experts_mm_*.hip): rows x columns
+enum { EXPERTS_256x256 = 0, EXPERTS_128x128 = 1, EXPERTS_64x128 = 2, EXPERTS_32x64 = 3, EXPERTS_16x64 = 4, EXPERTS_16x32 = 5, EXPERTS_TILES = 6 };
+constexpr int kExpertsTileRows[EXPERTS_TILES] = {256, 128, 64, 32, 16, 16};
+constexpr int kExpertsTileCols[EXPERTS_TILES] = {256, 128, 128, 64, 64, 32};
+
+// `blocks` workgroups of tile shape `tile`; b_across: B's storage has k across its rows (K x N), else N x K
+hipError_t launch_experts_rows_bf16(int tile, bool b_across, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
+hipError_t launch_experts_rows_fp16(int tile, bool b_across, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
+hipError_t launch_experts_rows_fp8(int tile, bool b_across, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
+// by sums: tile EXPERTS_256x256 or EXPERTS_128x128
+hipError_t launch_experts_sums(int type, int tile, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
+// R = the parts' sums, added up in order
+hipError_t launch_experts_join(int tile, const ExpertsArgs &a, hipStream_t s);
+
+struct RouteArgs {
+    const void *logits; int64_t ldx; int type;
+    int T, E, k, norm;
+    int32_t *experts, *place, *tokens, *offsets;
+    float *weights;
+    int32_t *counts;                 // workspace: [block of tokens][expert]
+    const float *dweights;           // gradient only
+    void *dlogits; int64_t lddx;
+};
+hipError_t launch_route(const RouteArgs &a, hipStream_t s);
+hipError_t launch_route_grad(const RouteArgs &a, hipStream_t s);
+int64_t route_blocks(int64_t T);     // blocks of tokens whose experts are counted apart
+
+struct CombineArgs {
+    const void *Y; int64_t ldy;
+    const float *weights;            // null: ones
+    const int32_t *place;
+    void *R; int64_t ldr;            // the sum (gradient: its gradient, read)
+    void *dY; int64_t lddy;
+    float *dweights;
+    int T, k, H, type;
+    int64_t rows;                    // of Y
+};
+hipError_t launch_combine(const CombineArgs &a, hipStream_t s);
+hipError_t launch_combine_grad(const CombineArgs &a, hipStream_t s);
+
+struct QuantizeArgs {
+    const void *X; int64_t ldx, group_x;
+    uint8_t *Q; int64_t ldq, group_q;
+    float *scales; int64_t lds, group_s;
+    int G, M, K, type;
+};
+// a scale for each row and 128 columns; for each 128 x 128
+hipError_t launch_quantize_rows(const QuantizeArgs &a, hipStream_t s);
+hipError_t launch_quantize_blocks(const QuantizeArgs &a, hipStream_t s);
+
+// the calling thread's note of a launch (amulet_recent_kernel), and the status of a launch's error (amulet_last_launch_error)
+void note_kernel(const char *name, int64_t rows);
+int launch_status(hipError_t e);
+
+}  // namespace amulet
+#endif

@@ -1,0 +1,657 @@
+// Matrix products by groups of rows, 16-bit and 8-bit floating point operands, on the matrix cores:
+//     R[i][:] = A[row(i)][:] B[g(i)]                        by rows  (experts' products and their rows' gradients)
+//     R[g]    = sum over the rows i of g of A[row(i)]^T D[i]  by sums (the gradients of the experts' weights)
+// One kernel body for both; the translation units experts_mm_*.hip hold its instances.
+//
+// A stage of an operand is 128 bytes of k per line (64 k of 16 bits, 128 of 8), streamed global -> LDS by
+// global_load_lds_dwordx4 (64 lanes x 16 bytes, any byte alignment) through a ring of S stages.  Two storages:
+//   k along the rows (KC): LDS keeps [line][8 units of 16 bytes]; a lane's fragment is one ds_read_b128.
+//   k across them   (KS): LDS keeps [k][line], and ds_read_b64_tr_b16 / _b8 hand a lane the k of its line.
+// Both are XOR-swizzled by unit so that the lanes of an LDS clock fall on distinct banks (unit_of below).  A stage that
+// does not lie wholly inside its operand (the last k, lines past the edge that end inside a unit) goes through registers
+// instead, element by element, with zeros past the end: nothing outside an operand is read.
+//
+// The matrix instruction takes B's lines as its rows and A's as its columns, so that a lane ends up with neighbouring
+// columns of one row of R.  Sums are fp32; fp8 operands have one scale per 128 k, so an instruction's 16 x 16 x 128 products
+// are summed alone and then added to the accumulators times both scales.
+#ifndef AMULET_EXPERTS_TILE_H
+#define AMULET_EXPERTS_TILE_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "experts_internal.h"
+
+// the LDS-DMA asm below sets M0 itself and says so in its clobber list
+#pragma clang diagnostic ignored "-Winline-asm"
+
+namespace amulet {
+
+typedef float xt_f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t xt_u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t xt_u2 __attribute__((ext_vector_type(2)));
+typedef int xt_i8 __attribute__((ext_vector_type(8)));
+typedef short xt_s4 __attribute__((ext_vector_type(4)));
+typedef int xt_i2 __attribute__((ext_vector_type(2)));
+typedef __bf16 xt_bf8 __attribute__((ext_vector_type(8)));
+typedef _Float16 xt_h8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) xt_s4 *xt_lds_s4;
+typedef __attribute__((address_space(3))) xt_i2 *xt_lds_i2;
+typedef __attribute__((address_space(3))) void *xt_lds_void;
+
+extern __shared__ __attribute__((aligned(16))) char xt_smem[];
+
+template <int ELEM_, int BM_, int BN_, int WM_, int WN_, int WK_, int S_, bool AKS_, bool BKS_>
+struct ExpertTile {
+    static constexpr int ELEM = ELEM_;                       // EXPERTS_BF16, _FP16, _FP8
+    static constexpr int ES = ELEM == EXPERTS_FP8 ? 1 : 2;   // bytes of an element
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WK = WK_, S = S_;
+    static constexpr bool AKS = AKS_, BKS = BKS_;
+    static constexpr int BK = 128 / ES;                      // k of a stage
+    static constexpr int NW = WM * WN, NT = 64 * NW * WK;    // waves of a k group; threads
+    static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
+    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;
+    static constexpr int SA_BYTES = ELEM == EXPERTS_FP8 ? (BM < 64 ? 256 : BM * 4) : 0;   // scales of A's rows
+    static constexpr int STAGE = A_BYTES + B_BYTES + SA_BYTES;
+    static constexpr int LDS = S * STAGE * WK;
+    // neighbouring fragments of B interleave their columns, so that a lane's values of both are 8 in a row
+    static constexpr bool PERM = !BKS && NI % 2 == 0;
+};
+
+// Position of 16-byte unit `u` of LDS line `line` (RB bytes long); see the two storages above.  256 bytes hold 16 units,
+// the banks of one clock:
+//   KC, natural fragments (lines 0..15 at one u): 2 lines per 256 bytes, so bits 1..3 of the line;
+//   KC, interleaved (lines 8 a + c, a, c = 0..3, or + 4): bits 1 and 3, 4;
+//   KS: 16-bit reads take 32 bytes of rows {0..3, 8..11} at a time, 8-bit reads 16 of rows {0..7, 16..23}.
+template <int RB, bool KS, bool PERM, int ES>
+__device__ __forceinline__ int unit_of(int line, int u)
+{
+    if constexpr (!KS) return u ^ (PERM ? ((line >> 2) & 6) | ((line >> 1) & 1) : (line >> 1) & 7);
+    else if constexpr (ES == 2) {
+        if constexpr (RB >= 256) return u ^ (((line & 3) | ((line >> 1) & 4)) << 1);
+        else if constexpr (RB == 128) return u ^ ((((line >> 1) & 1) | ((line >> 2) & 2)) << 1);
+        else if constexpr (RB == 64) return u ^ (((line >> 3) & 1) << 1);
+        else return u;
+    } else {
+        if constexpr (RB >= 256) return u ^ ((line & 7) | ((line >> 1) & 8));
+        else if constexpr (RB == 128) return u ^ (((line >> 1) & 3) | ((line >> 2) & 4));
+        else if constexpr (RB == 64) return u ^ (((line >> 2) & 1) | ((line >> 3) & 2));
+        else if constexpr (RB == 32) return u ^ ((line >> 4) & 1);
+        else return u;
+    }
+}
+
+__device__ __forceinline__ void dma16(const char *p, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(const char *p, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
+}
+
+// what an index that names no row stands for
+__device__ const xt_u4 xt_zeros = {0, 0, 0, 0};
+
+// `n` (1..) elements from p, zeros behind them
+template <int ES>
+__device__ __forceinline__ xt_u4 load_some(const char *p, int n)
+{
+    xt_u4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 16 / ES; ++i) {
+        const uint32_t x = i >= n ? 0u : ES == 2 ? (uint32_t) * (const uint16_t *)(p + 2 * i) : (uint32_t) * (const uint8_t *)(p + i);
+        v[i * ES / 4] |= x << (8 * ((i * ES) % 4));
+    }
+    return v;
+}
+
+// One operand on its way into LDS: LINES lines (rows of A, columns of B), one stage at a time, by the NW waves of a k group.
+// The LDS units of a stage are loaded 64 by a wave instruction: instruction j of the stage, j = wave + NW q.
+template <int LINES, int ES, bool KS, bool PERM, int NW>
+struct Staged {
+    static constexpr int BYTES = LINES * 128, LOADS = LINES / 8;             // instructions of a stage, all waves
+    static constexpr int Q = (LOADS + NW - 1) / NW;                           // ... of one wave (the last waves may repeat others')
+    static constexpr int RB = KS ? LINES * ES : 128, UR = RB / 16;            // bytes, units of an LDS line
+    static constexpr int BK = 128 / ES, E = 16 / ES;
+
+    const char *base;        // storage at the group's first k (KS) or at line 0 (KC)
+    int64_t pitch;           // bytes between storage rows
+    const int32_t *index;    // KS: storage row of a k, or null: the k itself
+    const char *p[Q];        // KC, and KS without an index: each lane's next unit
+    int lines, line0;        // lines of the operand, the tile's first
+    int k, storage_rows;     // k of the group; rows that an index may name
+
+    static __device__ __forceinline__ int slot(int q, int wave, int lane) { return ((wave + NW * q) % LOADS) * 64 + lane; }
+
+    // KC: `row_of(line)` gives the storage row of a line that is inside
+    template <class RowOf>
+    __device__ __forceinline__ void start_kc(const char *b, int64_t pitch_bytes, int first, int n, int k_all, int k0, int wave, int lane, RowOf row_of)
+    {
+        base = b; pitch = pitch_bytes; lines = n; line0 = first; k = k_all; index = nullptr; storage_rows = 0;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const int s = slot(q, wave, lane), line = s / 8, u = unit_of<128, false, PERM, ES>(line, s % 8);
+            const int in = first + line < n ? first + line : n - 1;
+            p[q] = b + (int64_t)row_of(in) * pitch_bytes + (int64_t)(k0 * ES + u * 16);
+        }
+    }
+    __device__ __forceinline__ void start_ks(const char *b, int64_t pitch_bytes, const int32_t *idx, int rows, int first, int n, int k_all, int k0, int wave, int lane)
+    {
+        base = b; pitch = pitch_bytes; lines = n; line0 = first; k = k_all; index = idx; storage_rows = rows;
+        if (idx) return;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const int s = slot(q, wave, lane), row = s / UR;
+            p[q] = b + (int64_t)(k0 + row) * pitch_bytes + column_of(row, s % UR);
+        }
+    }
+    // byte offset in a storage row of the unit at LDS place `place` of line `row` (past the edge: the last whole unit, whose values nobody stores)
+    __device__ __forceinline__ int64_t column_of(int row, int place) const
+    {
+        int c = line0 + unit_of<RB, KS, PERM, ES>(row, place) * E;
+        c = c < lines ? c : (lines - 1) / E * E;
+        return (int64_t)c * ES;
+    }
+    // whether some unit of the tile holds lines on both sides of the edge: read whole it ends outside its row
+    __device__ __forceinline__ bool cut() const { return KS && line0 + LINES > lines && lines % E != 0; }
+
+    // the whole stage at k0 into `lds`; then on to the stage `ahead` k further
+    __device__ __forceinline__ void load(uint32_t lds, int k0, int ahead, int wave, int lane)
+    {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const uint32_t to = lds + (uint32_t)((wave + NW * q) % LOADS) * 1024u;
+            if (KS && index) {
+                const int row = slot(q, wave, lane) / UR;
+                const int r = index[k0 + row];
+                const char *const from = base + (int64_t)r * pitch + column_of(row, slot(q, wave, lane) % UR);
+                dma16((unsigned)r < (unsigned)storage_rows ? from : (const char *)&xt_zeros, to);
+            } else {
+                dma16(p[q], to);
+                p[q] += KS ? (int64_t)ahead * pitch : (int64_t)ahead * ES;
+            }
+        }
+    }
+    // the stage at k0, of which `left` k are there (any number, also none), through registers
+    template <class RowOf>
+    __device__ __forceinline__ void load_cut(char *lds, int k0, int wave, int lane, RowOf row_of)
+    {
+#pragma unroll 1
+        for (int q = 0; q < Q; ++q) {
+            const int s = slot(q, wave, lane);
+            xt_u4 v = {0, 0, 0, 0};
+            if constexpr (!KS) {
+                const int line = s / 8, at = k0 + unit_of<128, false, PERM, ES>(line, s % 8) * E;
+                const int in = line0 + line < lines ? line0 + line : lines - 1;
+                if (at < k) v = load_some<ES>(base + (int64_t)row_of(in) * pitch + (int64_t)at * ES, k - at);
+            } else {
+                const int row = s / UR, c = line0 + unit_of<RB, KS, PERM, ES>(row, s % UR) * E;
+                if (k0 + row < k && c < lines) {
+                    int r = k0 + row;
+                    bool there = true;
+                    if (index) { r = index[r]; there = (unsigned)r < (unsigned)storage_rows; }
+                    if (there) v = load_some<ES>(base + (int64_t)r * pitch + (int64_t)c * ES, lines - c);
+                }
+            }
+            *(xt_u4 *)(lds + s * 16) = v;
+        }
+    }
+};
+
+// Fragments: a lane's 16 bytes of half `h` of a stage, of the fragment that starts at line f (KC) or at its columns (KS).
+template <int ES>
+__device__ __forceinline__ xt_u4 read_kc(const char *at) { return *(const xt_u4 *)at; }
+
+template <class T, int LINES, bool KS, bool PERM>
+struct FragReader {
+    static constexpr int ES = T::ES, RB = KS ? LINES * ES : 128, UR = RB / 16;
+    int at;          // KC: byte offset at half 0
+    int row, part;   // KS: this lane's first row; half unit (16 bits: 8 bytes of four)
+    int wave0;       // the wave's first line
+    // i: fragment line of the lane, b: k block of the lane
+    __device__ __forceinline__ void start(int first_line, int lane)
+    {
+        const int i = lane & 15, b = lane >> 4;
+        wave0 = first_line;
+        if constexpr (!KS) {
+            const int line = first_line + (PERM ? 8 * (i >> 2) + (i & 3) : i);
+            at = line * 128 + unit_of<128, false, PERM, ES>(line, b) * 16;
+        } else if constexpr (ES == 2) {
+            row = 8 * b + (i >> 2);
+            part = i & 3;
+        } else {
+            row = 16 * b + (i >> 1);
+            part = i & 1;
+        }
+    }
+    // half h (64 bytes of k) of fragment f
+    __device__ __forceinline__ xt_u4 read(const char *lds, int f, int h) const
+    {
+        if constexpr (!KS) {
+            // (units b and b + 4: the swizzle changes neither with the fragment nor in bit 2 with the half)
+            const int line = PERM ? (f >> 1) * 32 + (f & 1) * 4 : f * 16;
+            return *(const xt_u4 *)(lds + ((at + line * 128) ^ (h * 64)));
+        } else if constexpr (ES == 2) {
+            xt_u4 v;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int r = row + 4 * t + 32 * h;
+                const int u = unit_of<RB, true, false, 2>(r, (wave0 + 16 * f) / 8 + (part >> 1));
+                const xt_s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((xt_lds_s4)(lds + r * RB + u * 16 + (part & 1) * 8));
+                const xt_u2 y = __builtin_bit_cast(xt_u2, x);
+                v[2 * t] = y[0];
+                v[2 * t + 1] = y[1];
+            }
+            return v;
+        } else {
+            xt_u4 v;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int r = row + 8 * t + 64 * h;
+                const int u = unit_of<RB, true, false, 1>(r, (wave0 + 16 * f) / 16);
+                const xt_i2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((xt_lds_i2)(lds + r * RB + u * 16 + part * 8));
+                v[2 * t] = (uint32_t)x[0];
+                v[2 * t + 1] = (uint32_t)x[1];
+            }
+            return v;
+        }
+    }
+};
+
+template <int ELEM>
+__device__ __forceinline__ xt_f4 mma16(xt_u4 a, xt_u4 b, xt_f4 c)
+{
+    if constexpr (ELEM == EXPERTS_BF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(xt_bf8, a), __builtin_bit_cast(xt_bf8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(xt_h8, a), __builtin_bit_cast(xt_h8, b), c, 0, 0, 0);
+}
+
+// `v` consecutive values of R from column c on, of which those below `cols` exist; rounded once, to the output's type.
+template <int V>
+__device__ __forceinline__ void store_out(void *R, int out, int64_t row_at, int c, int cols, const float *x)
+{
+    if (out == EXPERTS_FP32) {
+        float *p = (float *)R + row_at + c;
+        if (c + V <= cols && ((uintptr_t)p & 15) == 0) {
+#pragma unroll
+            for (int i = 0; i < V; i += 4) *(xt_f4 *)(p + i) = xt_f4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (c + i < cols) p[i] = x[i];
+        }
+        return;
+    }
+    uint32_t w[V / 2];
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+        uint16_t lo, hi;
+        if (out == EXPERTS_BF16) {
+            lo = __builtin_bit_cast(uint16_t, (__bf16)x[i]);
+            hi = __builtin_bit_cast(uint16_t, (__bf16)x[i + 1]);
+        } else {
+            lo = __builtin_bit_cast(uint16_t, (_Float16)x[i]);
+            hi = __builtin_bit_cast(uint16_t, (_Float16)x[i + 1]);
+        }
+        w[i / 2] = lo | ((uint32_t)hi << 16);
+    }
+    uint16_t *p = (uint16_t *)R + row_at + c;
+    if (c + V <= cols && ((uintptr_t)p & (2 * V - 1)) == 0) {
+        if constexpr (V == 8) *(xt_u4 *)p = xt_u4{w[0], w[1], w[2], w[3]};
+        else *(xt_u2 *)p = xt_u2{w[0], w[1]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (c + i < cols) p[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+    }
+}
+
+// Which tile a workgroup has.  Row tiles of the groups in order, then those of the rows before the first group and behind
+// the last one, which are zeros (group -1).  Every wave finds it for itself: lane l looks at group l.
+struct RowTile {
+    int group, row0, row1, tm, tn;
+};
+__device__ __forceinline__ int clamp_row(int x, int M) { return x < 0 ? 0 : x > M ? M : x; }
+template <int BM>
+__device__ __forceinline__ bool find_row_tile(const ExpertsArgs &a, int tiles_n, int block, RowTile &t)
+{
+    const int lane = threadIdx.x & 63;
+    const int regions = a.offsets ? a.G + 2 : 1;
+    auto region = [&](int g, int &lo, int &hi) {
+        if (!a.offsets) { lo = 0; hi = g == 0 ? a.M : 0; }
+        else if (g < a.G) { lo = clamp_row(a.offsets[g], a.M); hi = clamp_row(a.offsets[g + 1], a.M); }
+        else if (g == a.G) { lo = 0; hi = clamp_row(a.offsets[0], a.M); }
+        else if (g == a.G + 1) { lo = clamp_row(a.offsets[a.G], a.M); hi = a.M; }
+        else lo = hi = 0;
+    };
+    auto scan = [&](int c, int &lo, int &hi, int &n) {   // row tiles of regions c .. c + lane
+        region(c + lane, lo, hi);
+        n = hi > lo ? (hi - lo + BM - 1) / BM : 0;
+        int sum = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int up = __shfl_up(sum, d);
+            if (lane >= d) sum += up;
+        }
+        return sum;
+    };
+    int lo, hi, n, total = 0;
+    int first = scan(0, lo, hi, n);
+    total = __shfl(first, 63);
+    for (int c = 64; c < regions; c += 64) {
+        int l2, h2, n2;
+        total += __shfl(scan(c, l2, h2, n2), 63);
+    }
+    // XCD x (workgroup b runs on XCD b % 8) takes an eighth of the tiles, neighbours in the order below
+    const int64_t tiles = (int64_t)total * tiles_n;
+    const int xcd = block & 7, slot = block >> 3;
+    const int64_t begin = tiles * xcd / 8, end = tiles * (xcd + 1) / 8;
+    if (slot >= end - begin) return false;
+    const int64_t at = begin + slot;
+    // the region that holds tile `at`
+    int before = 0, c = 0;
+    for (;;) {
+        const uint64_t past = __ballot((int64_t)(before + first) * tiles_n > at);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            const int nl = __shfl(n, l), upto = __shfl(first, l);
+            t.group = c + l;
+            t.row0 = __shfl(lo, l);
+            t.row1 = __shfl(hi, l);
+            // within a region: panels of 8 row tiles, column by column
+            const int64_t in = at - (int64_t)(before + upto - nl) * tiles_n;
+            const int panel = (int)(in / (8 * (int64_t)tiles_n));
+            const int high = nl - panel * 8 < 8 ? nl - panel * 8 : 8;
+            const int rem = (int)(in - (int64_t)panel * 8 * tiles_n);
+            t.tm = panel * 8 + rem % high;
+            t.tn = rem / high;
+            break;
+        }
+        before += __shfl(first, 63);
+        c += 64;
+        first = scan(c, lo, hi, n);
+    }
+    t.group = __builtin_amdgcn_readfirstlane(t.group);
+    t.row0 = __builtin_amdgcn_readfirstlane(t.row0);
+    t.row1 = __builtin_amdgcn_readfirstlane(t.row1);
+    t.tm = __builtin_amdgcn_readfirstlane(t.tm);
+    t.tn = __builtin_amdgcn_readfirstlane(t.tn);
+    if (t.group >= a.G) t.group = -1;
+    return true;
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vm()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+
+// The sums of a tile: acc[mi][ni] of this wave, over the k of [k0, k1) of the group; k-group waves each their stages, joined
+// at the end.  True for the waves that hold the result.
+template <class T, class ARow>
+__device__ __forceinline__ bool tile_sums(const ExpertsArgs &a, Staged<T::BM, T::ES, T::AKS, false, T::NW> &sa, Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW> &sb,
+                                          const int k0, const int k1, const int wave, const int kg, const int lane, ARow a_row, const char *scale_at, int64_t scale_step,
+                                          const float *scale_b, int64_t scale_b_step, xt_f4 (&acc)[T::MI][T::NI])
+{
+    constexpr int S = T::S, BK = T::BK;
+    constexpr int LOADS = Staged<T::BM, T::ES, T::AKS, false, T::NW>::Q + Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW>::Q + (T::ELEM == EXPERTS_FP8 ? 1 : 0);
+    static_assert(LOADS * (S - 2) <= 63, "the wait count is a 6-bit field");
+    const int wm = wave / T::WN, wn = wave % T::WN;
+    char *const ring = xt_smem + kg * (S * T::STAGE);
+    const uint32_t ring_at = (uint32_t)(uintptr_t)(xt_lds_void)ring;
+    FragReader<T, T::BM, T::AKS, false> fa;
+    FragReader<T, T::BN, T::BKS, T::PERM> fb;
+    fa.start(wm * (T::BM / T::WM), lane);
+    fb.start(wn * (T::BN / T::WN), lane);
+#pragma unroll
+    for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = xt_f4{0, 0, 0, 0};
+
+    const int k = k1 - k0;
+    const int stages = k > 0 ? (k + BK - 1) / BK : 0;
+    // stages that lie wholly inside both operands
+    const bool a_cut = sa.cut(), b_cut = sb.cut();
+    int whole = k > 0 ? k / BK : 0;
+    if (whole == stages && whole > 0 && (a_cut || b_cut)) --whole;
+    if ((T::AKS && a_cut && sa.index) || (T::BKS && b_cut && sb.index)) whole = 0;   // (any k may name the storage's last row)
+    const int rounds = (stages + T::WK - 1) / T::WK;
+    auto request = [&](int r) {
+        const int s = r * T::WK + kg, slot = r % S;
+        if (s < whole) {
+            const uint32_t to = ring_at + (uint32_t)(slot * T::STAGE);
+            sa.load(to, k0 + s * BK, BK * T::WK, wave, lane);
+            sb.load(to + T::A_BYTES, k0 + s * BK, BK * T::WK, wave, lane);
+        } else if (s < stages) {
+            char *const to = ring + slot * T::STAGE;
+            sa.load_cut(to, k0 + s * BK, wave, lane, a_row);
+            sb.load_cut(to + T::A_BYTES, k0 + s * BK, wave, lane, [](int r2) { return r2; });
+        }
+        if constexpr (T::ELEM == EXPERTS_FP8) {
+            // (64 rows a wave; the last waves repeat others')
+            if (s < stages) dma4(scale_at + (int64_t)s * scale_step, ring_at + (uint32_t)(slot * T::STAGE + T::A_BYTES + T::B_BYTES + (wave * 64 % (T::BM < 64 ? 64 : T::BM)) * 4));
+        }
+    };
+#pragma unroll
+    for (int r = 0; r < S - 1; ++r)
+        if (r < rounds) request(r);
+    for (int r = 0; r < rounds; ++r) {
+        // stage r has landed: only the requests of the S - 2 rounds behind it may be under way
+        if (S > 2 && r + S - 2 < rounds && (r + S - 2) * T::WK + kg < whole) wait_vm<LOADS * (S - 2)>();
+        else wait_vm<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (r + S - 1 < rounds) request(r + S - 1);   // into the slot that round r - 1 has left
+        const int s = r * T::WK + kg;
+        if (s >= stages) continue;
+        const char *const la = ring + (r % S) * T::STAGE, *const lb = la + T::A_BYTES;
+        if constexpr (T::ELEM != EXPERTS_FP8) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                xt_u4 xa[T::MI], xb[T::NI];
+#pragma unroll
+                for (int ni = 0; ni < T::NI; ++ni) xb[ni] = fb.read(lb, ni, h);
+#pragma unroll
+                for (int mi = 0; mi < T::MI; ++mi) xa[mi] = fa.read(la, mi, h);
+#pragma unroll
+                for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+                    for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = mma16<T::ELEM>(xb[ni], xa[mi], acc[mi][ni]);
+            }
+        } else {
+            const float wb = scale_b[(int64_t)s * scale_b_step];
+            const float *const ls = (const float *)(lb + T::B_BYTES) + wm * (T::BM / T::WM) + (lane & 15);
+            xt_i8 xb[T::NI];
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ++ni) {
+                const xt_u4 lo = fb.read(lb, ni, 0), hi = fb.read(lb, ni, 1);
+                xb[ni] = xt_i8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+            }
+#pragma unroll
+            for (int mi = 0; mi < T::MI; ++mi) {
+                const xt_u4 lo = fa.read(la, mi, 0), hi = fa.read(la, mi, 1);
+                const xt_i8 xa = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+                const float w = ls[mi * 16] * wb;
+#pragma unroll
+                for (int ni = 0; ni < T::NI; ++ni) {
+                    const xt_f4 zero = {0, 0, 0, 0};
+                    const xt_f4 x = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(xb[ni], xa, zero, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[mi][ni][v] = __builtin_fmaf(w, x[v], acc[mi][ni][v]);
+                }
+            }
+        }
+    }
+    if constexpr (T::WK > 1) {
+        // the k groups' sums, added up by the first in order (fp32, so the result does not depend on who came first)
+        __syncthreads();
+        constexpr int PER = T::MI * T::NI * 4 * 64;   // floats of a wave
+        float *const img = (float *)xt_smem;
+        if (kg > 0) {
+            float *const to = img + ((kg - 1) * T::NW + wave) * PER;
+#pragma unroll
+            for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+                for (int ni = 0; ni < T::NI; ++ni) *(xt_f4 *)(to + ((mi * T::NI + ni) * 64 + lane) * 4) = acc[mi][ni];
+        }
+        __syncthreads();
+        if (kg > 0) return false;
+#pragma unroll
+        for (int g = 1; g < T::WK; ++g)
+#pragma unroll
+            for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+                for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] += *(const xt_f4 *)(img + (((g - 1) * T::NW + wave) * PER) + ((mi * T::NI + ni) * 64 + lane) * 4);
+    }
+    return true;
+}
+
+// Element v of acc[mi][ni] of a lane: row mi * 16 + lane % 16 of the wave's rows, column col_of(ni, lane) + v of its columns.
+template <class T>
+__device__ __forceinline__ int col_of(int ni, int lane)
+{
+    return T::PERM ? (ni >> 1) * 32 + 8 * (lane >> 4) + 4 * (ni & 1) : ni * 16 + 4 * (lane >> 4);
+}
+
+template <class T>
+__global__ void __launch_bounds__(T::NT) experts_rows_kernel(const ExpertsArgs a)
+{
+    static_assert(!T::AKS, "by rows: k lies along A's rows");
+    static_assert(T::LDS <= 160 * 1024 && (T::WK - 1) * T::NW * T::MI * T::NI * 1024 <= T::LDS, "LDS");
+    const int lane = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), kg = w / T::NW, wave = w % T::NW;
+    const int tiles_n = (a.N + T::BN - 1) / T::BN;
+    RowTile t;
+    if (!find_row_tile<T::BM>(a, tiles_n, blockIdx.x, t)) return;
+    const int row0 = t.row0 + t.tm * T::BM, col0 = t.tn * T::BN;
+    const int wm = wave / T::WN, wn = wave % T::WN;
+
+    xt_f4 acc[T::MI][T::NI];
+    auto a_row = [&](int i) {   // storage row of row i of R; one that is not there reads row 0 and is zeros in the end
+        if (!a.rows) return i;
+        const int r = a.rows[i];
+        return (unsigned)r < (unsigned)a.a_rows ? r : 0;
+    };
+    const int K = t.group < 0 ? 0 : a.K;
+    Staged<T::BM, T::ES, T::AKS, false, T::NW> sa = {};
+    Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW> sb = {};
+    const char *const B = (const char *)a.B + (int64_t)(t.group < 0 ? 0 : t.group) * a.group_b * T::ES;
+    if (K > 0) {
+        sa.start_kc((const char *)a.A, a.lda * T::ES, row0, t.row1, K, kg * T::BK, wave, lane, a_row);
+        if constexpr (T::BKS) sb.start_ks(B, a.ldb * T::ES, nullptr, 0, col0, a.N, K, kg * T::BK, wave, lane);
+        else sb.start_kc(B, a.ldb * T::ES, col0, a.N, K, kg * T::BK, wave, lane, [](int i) { return i; });
+    }
+    const char *scale_at = nullptr;
+    const float *scale_b = nullptr;
+    int64_t scale_b_step = 0;
+    if constexpr (T::ELEM == EXPERTS_FP8) {
+        const int i = row0 + (wave * 64 + lane) % (T::BM < 64 ? 64 : T::BM);
+        if (K > 0) scale_at = (const char *)(a.scale_a + a_row(i < t.row1 ? i : t.row1 - 1));
+        const int block = (col0 + wn * (T::BN / T::WN)) / 128, blocks = (a.N + 127) / 128;
+        const int64_t at = block < blocks ? block : blocks - 1;
+        scale_b = a.scale_b + (int64_t)(t.group < 0 ? 0 : t.group) * a.group_sb + (T::BKS ? at : at * a.ld_sb);
+        scale_b_step = T::BKS ? a.ld_sb : 1;
+    }
+    if (!tile_sums<T>(a, sa, sb, 0, K, wave, kg, lane, a_row, scale_at, a.ld_sa * 4, scale_b, scale_b_step, acc)) return;
+
+#pragma unroll
+    for (int mi = 0; mi < T::MI; ++mi) {
+        const int i = row0 + wm * (T::BM / T::WM) + mi * 16 + (lane & 15);
+        if (i >= t.row1) continue;
+        const bool there = !a.rows || (unsigned)a.rows[i] < (unsigned)a.a_rows;
+        const int64_t at = (int64_t)i * a.ldr;
+#pragma unroll
+        for (int ni = 0; ni < T::NI; ni += T::PERM ? 2 : 1) {
+            constexpr int V = T::PERM ? 8 : 4;
+            float x[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = there ? acc[mi][ni + v / 4][v % 4] : 0.0f;
+            const int c = col0 + wn * (T::BN / T::WN) + col_of<T>(ni, lane);
+            if (c < a.N) store_out<V>(a.R, a.out, at, c, a.N, x);
+        }
+    }
+}
+
+// The weights' gradients: k runs over a group's rows, lines of A are columns of its storage, lines of B of D's.  grid: parts x tiles x groups.
+// With several parts of a group's rows each writes its fp32 sums to the workspace, and experts_join_kernel adds them up in order.
+template <class T>
+__global__ void __launch_bounds__(T::NT) experts_sums_kernel(const ExpertsArgs a)
+{
+    static_assert(T::AKS && T::BKS && !T::PERM, "by sums: k runs across both storages");
+    static_assert(T::LDS <= 160 * 1024 && (T::WK - 1) * T::NW * T::MI * T::NI * 1024 <= T::LDS, "LDS");
+    const int lane = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), kg = w / T::NW, wave = w % T::NW;
+    const int tiles_m = (a.M + T::BM - 1) / T::BM, tiles_n = (a.N + T::BN - 1) / T::BN;
+    const int64_t tiles = (int64_t)tiles_m * tiles_n, all = tiles * a.G * a.parts;
+    // an eighth of the work to each XCD; within a group and part: panels of 8 row tiles, column by column
+    const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+    const int64_t begin = all * xcd / 8, end = all * (xcd + 1) / 8;
+    if (slot >= end - begin) return;
+    const int64_t at = begin + slot, piece = at / tiles;
+    const int g = (int)(piece / a.parts), part = (int)(piece % a.parts);
+    const int in = (int)(at - piece * tiles);
+    const int panel = in / (8 * tiles_n), high = tiles_m - panel * 8 < 8 ? tiles_m - panel * 8 : 8, rem = in - panel * 8 * tiles_n;
+    const int tm = panel * 8 + rem % high, tn = rem / high;
+    const int m0 = tm * T::BM, n0 = tn * T::BN;
+
+    const int lo = clamp_row(a.offsets[g], a.k_rows), hi = clamp_row(a.offsets[g + 1], a.k_rows);
+    const int k_all = hi > lo ? hi - lo : 0;
+    // whole stages to a part
+    const int chunk = ((k_all + a.parts - 1) / a.parts + T::BK - 1) / T::BK * T::BK;
+    const int64_t k0 = (int64_t)part * chunk;
+    const int from = k0 < k_all ? (int)k0 : k_all, to = k0 + chunk < k_all ? (int)(k0 + chunk) : k_all;
+
+    Staged<T::BM, T::ES, T::AKS, false, T::NW> sa;
+    Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW> sb;
+    const char *const A = (const char *)a.A, *const B = (const char *)a.B;
+    const int32_t *const ia = a.rows_of_b ? nullptr : a.rows, *const ib = a.rows_of_b ? a.rows : nullptr;
+    sa.start_ks(ia ? A : A + (int64_t)lo * a.lda * T::ES, a.lda * T::ES, ia ? ia + lo : nullptr, a.a_rows, m0, a.M, to, from + kg * T::BK, wave, lane);
+    sb.start_ks(ib ? B : B + (int64_t)lo * a.ldb * T::ES, a.ldb * T::ES, ib ? ib + lo : nullptr, a.a_rows, n0, a.N, to, from + kg * T::BK, wave, lane);
+    xt_f4 acc[T::MI][T::NI];
+    if (!tile_sums<T>(a, sa, sb, from, to, wave, kg, lane, [](int i) { return i; }, nullptr, 0, nullptr, 0, acc)) return;
+
+    const int wm = wave / T::WN, wn = wave % T::WN;
+    if (a.parts > 1) {
+        float *const ws = a.workspace + ((int64_t)(g * tiles + (int64_t)tm * tiles_n + tn) * a.parts + part) * (T::BM * T::BN);
+#pragma unroll
+        for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ++ni) {
+                const int i = wm * (T::BM / T::WM) + mi * 16 + (lane & 15), c = wn * (T::BN / T::WN) + col_of<T>(ni, lane);
+                *(xt_f4 *)(ws + i * T::BN + c) = acc[mi][ni];
+            }
+        return;
+    }
+#pragma unroll
+    for (int mi = 0; mi < T::MI; ++mi) {
+        const int i = m0 + wm * (T::BM / T::WM) + mi * 16 + (lane & 15);
+        if (i >= a.M) continue;
+        const int64_t row_at = (int64_t)g * a.group_r + (int64_t)i * a.ldr;
+#pragma unroll
+        for (int ni = 0; ni < T::NI; ++ni) {
+            float x[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) x[v] = acc[mi][ni][v];
+            const int c = n0 + wn * (T::BN / T::WN) + col_of<T>(ni, lane);
+            if (c < a.N) store_out<4>(a.R, a.out, row_at, c, a.N, x);
+        }
+    }
+}
+
+// (the kernel is a template argument: what it was granted is kept once for each)
+template <class T, void (*kernel)(const ExpertsArgs)>
+inline hipError_t launch_experts(const ExpertsArgs &a, int64_t blocks, hipStream_t s)
+{
+    if (blocks <= 0) return hipSuccess;
+    if (forced_launch_failure()) return hipErrorLaunchFailure;
+    static const hipError_t granted = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
+    if (granted != hipSuccess) { (void)hipGetLastError(); return granted; }
+    kernel<<<dim3((unsigned)blocks), dim3(T::NT), T::LDS, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace amulet
+#endif

@@ -1,0 +1,378 @@
+// The router of a mixture-of-experts layer: for every token the k experts with the highest logits and their weights, and
+// the rows of all (token, expert) pairs in order of expert, then of token; and its gradient.
+//
+// Forward: one kernel chooses (a token to L lanes, each with the logits of experts lane + L j in registers; k rounds of a
+// maximum over keys that hold the logit's order and, below it, the complement of the expert's index, so that ties go to the
+// lowest one) and counts its 64 tokens' experts in LDS; a second one finds where each expert's rows of its tokens begin,
+// from all counts, and ranks its pairs among equals by ballots, 64 at a time.  Up to 64 tokens one workgroup does both: one
+// launch.  Everything that decides an order is an integer and every sum of weights is one lane group's, so results do not
+// depend on timing.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "experts_internal.h"
+
+namespace amulet {
+
+constexpr int RT_TOKENS = 64;          // tokens that a workgroup chooses for at a time
+constexpr int RT_MOST_BLOCKS = 256;    // ... workgroups: more tokens make longer blocks
+constexpr int RT_MOST_EXPERTS = 1024;
+
+static int64_t tokens_of_a_block(int64_t T)
+{
+    const int64_t passes = (T + (int64_t)RT_TOKENS * RT_MOST_BLOCKS - 1) / ((int64_t)RT_TOKENS * RT_MOST_BLOCKS);
+    return RT_TOKENS * (passes < 1 ? 1 : passes);
+}
+int64_t route_blocks(int64_t T) { return (T + tokens_of_a_block(T) - 1) / tokens_of_a_block(T); }
+
+template <int TYPE>
+__device__ __forceinline__ float load_logit(const void *p, int64_t at)
+{
+    if constexpr (TYPE == EXPERTS_FP32) return ((const float *)p)[at];
+    else if constexpr (TYPE == EXPERTS_BF16) return __builtin_bit_cast(float, (uint32_t)((const uint16_t *)p)[at] << 16);
+    else return (float)((const _Float16 *)p)[at];
+}
+
+// another lane's word, by the crossbars that a group of 16 lanes has (after steps 1 and 2 the four lanes of a quad agree,
+// so mirrors do for the distances 4 and 8)
+template <int STEP>
+__device__ __forceinline__ uint32_t of_partner(uint32_t x)
+{
+    if constexpr (STEP == 1) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, true);       // quad_perm 1 0 3 2
+    else if constexpr (STEP == 2) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xf, 0xf, true);  // quad_perm 2 3 0 1
+    else if constexpr (STEP == 4) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, true); // row_half_mirror
+    else if constexpr (STEP == 8) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, true); // row_mirror
+    else return (uint32_t)__shfl_xor((int)x, STEP);
+}
+template <int STEP>
+__device__ __forceinline__ uint64_t larger_of_pair(uint64_t x)
+{
+    const uint64_t y = ((uint64_t)of_partner<STEP>((uint32_t)(x >> 32)) << 32) | of_partner<STEP>((uint32_t)x);
+    return x > y ? x : y;
+}
+template <int L>
+__device__ __forceinline__ uint64_t group_most(uint64_t x)
+{
+    x = larger_of_pair<1>(x);
+    x = larger_of_pair<2>(x);
+    x = larger_of_pair<4>(x);
+    x = larger_of_pair<8>(x);
+    if constexpr (L == 64) { x = larger_of_pair<16>(x); x = larger_of_pair<32>(x); }
+    return x;
+}
+template <int L>
+__device__ __forceinline__ float group_sum(float x)
+{
+    x += __builtin_bit_cast(float, of_partner<1>(__builtin_bit_cast(uint32_t, x)));
+    x += __builtin_bit_cast(float, of_partner<2>(__builtin_bit_cast(uint32_t, x)));
+    x += __builtin_bit_cast(float, of_partner<4>(__builtin_bit_cast(uint32_t, x)));
+    x += __builtin_bit_cast(float, of_partner<8>(__builtin_bit_cast(uint32_t, x)));
+    if constexpr (L == 64) { x += __shfl_xor(x, 16); x += __shfl_xor(x, 32); }
+    return x;
+}
+template <int L>
+__device__ __forceinline__ float group_max(float x)
+{
+    x = fmaxf(x, __builtin_bit_cast(float, of_partner<1>(__builtin_bit_cast(uint32_t, x))));
+    x = fmaxf(x, __builtin_bit_cast(float, of_partner<2>(__builtin_bit_cast(uint32_t, x))));
+    x = fmaxf(x, __builtin_bit_cast(float, of_partner<4>(__builtin_bit_cast(uint32_t, x))));
+    x = fmaxf(x, __builtin_bit_cast(float, of_partner<8>(__builtin_bit_cast(uint32_t, x))));
+    if constexpr (L == 64) { x = fmaxf(x, __shfl_xor(x, 16)); x = fmaxf(x, __shfl_xor(x, 32)); }
+    return x;
+}
+
+// a logit's share before it is divided by the sum: an infinite maximum shares among the infinite ones
+__device__ __forceinline__ float term_of(float x, float most)
+{
+    return most == INFINITY ? (x == INFINITY ? 1.0f : 0.0f) : expf(x - most);
+}
+
+// Keys: the order of a float as an unsigned number, above the complement of the index; 0: masked or taken.
+__device__ __forceinline__ uint64_t key_of(float x, int e)
+{
+    if (!(x > -INFINITY)) return 0;                        // (NaN too)
+    const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);   // (-0 is 0: a tie)
+    const uint32_t order = u & 0x80000000u ? ~u : u | 0x80000000u;
+    return ((uint64_t)order << 32) | (uint32_t)~e;
+}
+__device__ __forceinline__ float logit_of(uint64_t key)
+{
+    const uint32_t order = (uint32_t)(key >> 32);
+    return __builtin_bit_cast(float, order & 0x80000000u ? order & 0x7fffffffu : ~order);
+}
+
+// the counts before this block and all of them, for every expert -> first row of the block's pairs in base[], offsets
+// Returns the number of rows.  All threads of the workgroup.
+__device__ int place_bases(const RouteArgs &a, const int32_t *counts, int blocks, int block, int *base, int *total, int *rows)
+{
+    const int tid = threadIdx.x, nt = blockDim.x;
+    for (int e = tid; e < a.E; e += nt) { base[e] = 0; total[e] = 0; }
+    __syncthreads();
+    // the blocks' rows of counts, dealt out to as many sets of E threads as there are
+    const int sets = nt / a.E > 0 ? nt / a.E : 1, set = tid / a.E;
+    if (set < sets)
+        for (int e = sets > 1 ? tid % a.E : tid; e < a.E; e += sets > 1 ? a.E : nt) {
+            int before = 0, all = 0;
+#pragma unroll 8
+            for (int b = sets > 1 ? set : 0; b < blocks; b += sets > 1 ? sets : 1) {
+                const int n = counts[(int64_t)b * a.E + e];
+                all += n;
+                before += b < block ? n : 0;
+            }
+            atomicAdd(&base[e], before);
+            atomicAdd(&total[e], all);
+        }
+    __syncthreads();
+    if (tid < 64) {
+        int sum = 0;
+        for (int c = 0; c < a.E; c += 64) {
+            const int n = c + tid < a.E ? total[c + tid] : 0;
+            int upto = n;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int x = __shfl_up(upto, d);
+                if (tid >= d) upto += x;
+            }
+            if (c + tid < a.E) {
+                base[c + tid] += sum + upto - n;
+                if (block == 0) a.offsets[c + tid] = sum + upto - n;
+            }
+            sum += __shfl(upto, 63);
+        }
+        if (tid == 0) {
+            *rows = sum;
+            if (block == 0) a.offsets[a.E] = sum;
+        }
+    }
+    __syncthreads();
+    return *rows;
+}
+
+// Rows of a block's pairs, by one wave: pairs [first, last) of T x k in order; base[e] is the next row of expert e.
+__device__ void place_pairs(const RouteArgs &a, const int32_t *experts, int64_t first, int64_t last, int *base)
+{
+    const int lane = threadIdx.x & 63;
+    const int bits = 32 - __builtin_clz((unsigned)a.E);   // E itself stands for a dropped pair
+    for (int64_t p = first; p < last; p += 64) {
+        int e = -1;
+        if (p + lane < last) e = experts[p + lane - first];
+        const int key = e < 0 ? a.E : e;
+        uint64_t same = ~0ull;
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t set = __ballot((key >> b) & 1);
+            same &= (key >> b) & 1 ? set : ~set;
+        }
+        const int rank = __builtin_popcountll(same & ((1ull << lane) - 1)), n = __builtin_popcountll(same);
+        int row = -1;
+        if (e >= 0) row = base[e] + rank;
+        __builtin_amdgcn_wave_barrier();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (e >= 0 && rank == 0) base[e] = row + n;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (p + lane < last) {
+            a.place[p + lane] = row;
+            if (row >= 0) a.tokens[row] = (int32_t)((p + lane) / a.k);
+        }
+    }
+}
+
+// L lanes to a token; V logits to a lane.  alone: the workgroup has all tokens, and places their pairs too.
+template <int TYPE, int L, int V>
+__global__ void __launch_bounds__(1024) route_choose_kernel(const RouteArgs a, const int block_tokens, const int alone)
+{
+    extern __shared__ int route_lds[];   // E counts; alone: and E totals, the pairs' experts, the number of rows
+    int *const count = route_lds;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int in = tid % L, group = tid / L, groups = 1024 / L;
+    for (int e = tid; e < a.E; e += 1024) count[e] = 0;
+    __syncthreads();
+    int32_t *const chosen_lds = alone ? route_lds + 2 * a.E + 1 : nullptr;
+    const int64_t t0 = (int64_t)blockIdx.x * block_tokens;
+    for (int i = group; i < block_tokens; i += groups) {
+        const int64_t t = t0 + i;
+        if (t >= a.T) break;                              // (a whole group of lanes; the shuffles below stay within groups)
+        uint64_t key[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int e = in + L * j;
+            key[j] = e < a.E ? key_of(load_logit<TYPE>(a.logits, t * a.ldx + e), e) : 0;
+        }
+        float most = 0.0f, all = 0.0f, mine = 0.0f;
+        int expert = -1;
+        float sum = 0.0f;
+        for (int j = 0; j < a.k; ++j) {
+            uint64_t best = key[0];
+#pragma unroll
+            for (int v = 1; v < V; ++v) best = key[v] > best ? key[v] : best;
+            best = group_most<L>(best);
+            const float x = logit_of(best);
+            if (j == 0) {
+                most = x;
+                if (!a.norm && best) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) all += key[v] ? term_of(logit_of(key[v]), most) : 0.0f;
+                    all = group_sum<L>(all);
+                }
+            }
+            const float term = best ? term_of(x, most) : 0.0f;
+            sum += term;
+            if (in == j) { mine = term; expert = best ? (int)~(uint32_t)best : -1; }
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = key[v] == best ? 0 : key[v];
+        }
+        if (in < a.k) {
+            const int64_t at = t * a.k + in;
+            a.experts[at] = expert;
+            a.weights[at] = expert < 0 ? 0.0f : mine / (a.norm ? sum : all);
+            if (chosen_lds) chosen_lds[i * a.k + in] = expert;
+            if (expert >= 0) atomicAdd(&count[expert], 1);
+        }
+    }
+    __syncthreads();
+    if (!alone) {
+        for (int e = tid; e < a.E; e += 1024) a.counts[(int64_t)blockIdx.x * a.E + e] = count[e];
+        return;
+    }
+    // all tokens are here: the counts are the totals
+    int *const base = route_lds + a.E, *const rows = route_lds + 2 * a.E;
+    if (tid < 64) {
+        int sum = 0;
+        for (int c = 0; c < a.E; c += 64) {
+            const int n = c + lane < a.E ? count[c + lane] : 0;
+            int upto = n;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int x = __shfl_up(upto, d);
+                if (lane >= d) upto += x;
+            }
+            if (c + lane < a.E) {
+                base[c + lane] = sum + upto - n;
+                a.offsets[c + lane] = sum + upto - n;
+            }
+            sum += __shfl(upto, 63);
+        }
+        if (lane == 0) { *rows = sum; a.offsets[a.E] = sum; }
+    }
+    __syncthreads();
+    const int64_t pairs = (int64_t)a.T * a.k;
+    if (tid < 64) place_pairs(a, chosen_lds, 0, pairs, base);
+    else
+        for (int64_t r = *rows + tid - 64; r < pairs; r += 1024 - 64) a.tokens[r] = -1;
+}
+
+__global__ void __launch_bounds__(1024) route_place_kernel(const RouteArgs a, const int block_tokens)
+{
+    extern __shared__ int route_lds[];   // E bases, E totals, the number of rows
+    const int rows = place_bases(a, a.counts, gridDim.x, blockIdx.x, route_lds, route_lds + a.E, route_lds + 2 * a.E);
+    const int64_t pairs = (int64_t)a.T * a.k;
+    const int64_t first = (int64_t)blockIdx.x * block_tokens * a.k;
+    const int64_t last = first + (int64_t)block_tokens * a.k < pairs ? first + (int64_t)block_tokens * a.k : pairs;
+    if (threadIdx.x < 64) place_pairs(a, a.experts + first, first, last, route_lds);
+    else
+        // rows that no pair has
+        for (int64_t r = rows + (int64_t)blockIdx.x * (1024 - 64) + threadIdx.x - 64; r < pairs; r += (int64_t)gridDim.x * (1024 - 64)) a.tokens[r] = -1;
+}
+
+// dx = p (up - sum p up), up: the weights' gradients at the chosen experts; p: the weights (norm) or the softmax over all.
+// A token to L lanes, its row in LDS while the chosen experts' parts are added (each expert once: no two lanes meet).
+template <int TYPE, int L>
+__global__ void __launch_bounds__(256) route_grad_kernel(const RouteArgs a)
+{
+    extern __shared__ float grad_lds[];
+    const int in = threadIdx.x % L, group = threadIdx.x / L;
+    const int64_t t = (int64_t)blockIdx.x * (256 / L) + group;
+    if (t >= a.T) return;
+    float *const row = grad_lds + group * a.E;
+    float mean = 0.0f;
+    for (int j = in; j < a.k; j += L)
+        if (a.experts[t * a.k + j] >= 0) mean += a.weights[t * a.k + j] * a.dweights[t * a.k + j];
+    mean = group_sum<L>(mean);
+    if (a.norm) {
+        for (int e = in; e < a.E; e += L) row[e] = 0.0f;
+    } else {
+        float most = -INFINITY, all = 0.0f;
+        for (int e = in; e < a.E; e += L) {
+            const float x = load_logit<TYPE>(a.logits, t * a.ldx + e);
+            row[e] = x > -INFINITY ? x : -INFINITY;        // (NaN: masked)
+            most = fmaxf(most, row[e]);
+        }
+        most = group_max<L>(most);
+        for (int e = in; e < a.E; e += L) {
+            row[e] = row[e] > -INFINITY ? term_of(row[e], most) : 0.0f;
+            all += row[e];
+        }
+        all = group_sum<L>(all);
+        const float scale = all > 0.0f ? -mean / all : 0.0f;
+        for (int e = in; e < a.E; e += L) row[e] = row[e] * scale;
+    }
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    for (int j = in; j < a.k; j += L) {
+        const int e = a.experts[t * a.k + j];
+        if ((unsigned)e >= (unsigned)a.E) continue;
+        const float w = a.weights[t * a.k + j], up = a.dweights[t * a.k + j];
+        row[e] += a.norm ? w * (up - mean) : w * up;
+    }
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    for (int e = in; e < a.E; e += L) {
+        const int64_t at = t * a.lddx + e;
+        if constexpr (TYPE == EXPERTS_FP32) ((float *)a.dlogits)[at] = row[e];
+        else if constexpr (TYPE == EXPERTS_BF16) ((__bf16 *)a.dlogits)[at] = (__bf16)row[e];
+        else ((_Float16 *)a.dlogits)[at] = (_Float16)row[e];
+    }
+}
+
+template <int TYPE, int L, int V>
+static hipError_t launch_choose(const RouteArgs &a, hipStream_t s)
+{
+    const int64_t block_tokens = tokens_of_a_block(a.T), blocks = route_blocks(a.T);
+    const bool alone = blocks == 1 && block_tokens == RT_TOKENS;
+    const size_t lds = alone ? (2 * (size_t)a.E + 1 + RT_TOKENS * (size_t)a.k) * 4 : (size_t)a.E * 4;
+    if (forced_launch_failure()) return hipErrorLaunchFailure;
+    route_choose_kernel<TYPE, L, V><<<dim3((unsigned)blocks), dim3(1024), lds, s>>>(a, (int)block_tokens, alone ? 1 : 0);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || alone) return e;
+    if (forced_launch_failure()) return hipErrorLaunchFailure;
+    route_place_kernel<<<dim3((unsigned)blocks), dim3(1024), (2 * (size_t)a.E + 1) * 4, s>>>(a, (int)block_tokens);
+    return hipGetLastError();
+}
+template <int TYPE>
+static hipError_t launch_route_type(const RouteArgs &a, hipStream_t s)
+{
+    if (a.k <= 16) {
+        if (a.E <= 64) return launch_choose<TYPE, 16, 4>(a, s);
+        if (a.E <= 128) return launch_choose<TYPE, 16, 8>(a, s);
+        if (a.E <= 256) return launch_choose<TYPE, 16, 16>(a, s);
+    }
+    return launch_choose<TYPE, 64, 16>(a, s);
+}
+hipError_t launch_route(const RouteArgs &a, hipStream_t s)
+{
+    switch (a.type) {
+    case EXPERTS_FP32: return launch_route_type<EXPERTS_FP32>(a, s);
+    case EXPERTS_BF16: return launch_route_type<EXPERTS_BF16>(a, s);
+    default: return launch_route_type<EXPERTS_FP16>(a, s);
+    }
+}
+
+template <int TYPE>
+static hipError_t launch_grad_type(const RouteArgs &a, hipStream_t s)
+{
+    if (forced_launch_failure()) return hipErrorLaunchFailure;
+    // (a row of up to 1024 logits: 16 rows of them are 64 KB)
+    if (a.E <= 256) route_grad_kernel<TYPE, 16><<<dim3((unsigned)((a.T + 15) / 16)), dim3(256), 16 * (size_t)a.E * 4, s>>>(a);
+    else route_grad_kernel<TYPE, 64><<<dim3((unsigned)((a.T + 3) / 4)), dim3(256), 4 * (size_t)a.E * 4, s>>>(a);
+    return hipGetLastError();
+}
+hipError_t launch_route_grad(const RouteArgs &a, hipStream_t s)
+{
+    switch (a.type) {
+    case EXPERTS_FP32: return launch_grad_type<EXPERTS_FP32>(a, s);
+    case EXPERTS_BF16: return launch_grad_type<EXPERTS_BF16>(a, s);
+    default: return launch_grad_type<EXPERTS_FP16>(a, s);
+    }
+}
+
+}  // namespace amulet
