@@ -11,6 +11,9 @@ static const int64_t kMostRows = 2147483647LL - 65536LL;   // of a dimension, as
 static const int64_t kMostGroups = 1 << 20;
 static const int64_t kMostBlocks = 0xffffffffLL / 512;     // workgroups of a launch (a grid holds 2^32 - 1 work-items)
 
+// the longest pitch (bytes) of an operand whose tile's lines, or a stage's k, lie within 32 bits of each other: 256 of them
+static const int64_t kMostPitch = 0xffffffffLL / 256 - 65536;
+
 static bool known16(int type) { return type == AMULET_BF16 || type == AMULET_FP16; }
 static bool known(int type) { return type == AMULET_FP32 || known16(type); }
 
@@ -46,12 +49,17 @@ static int check_rows(int64_t M, int64_t N, int64_t K, int64_t G, int trans_b, c
     if (K == 0 || G == 0 || (rows && a_rows == 0)) return AMULET_OK;   // zeros: the operands are not read
     if (!A || !B) return AMULET_ERR_NULL;
     if (lda < K || ldb < (trans_b ? K : N) || (G > 1 && group_b < 0)) return AMULET_ERR_LD;
+    if (lda > kMostPitch / 2 || ldb > kMostPitch / 2) return AMULET_ERR_RANGE;
     return AMULET_OK;
 }
 
 static int run_rows(const char *const *names, int type, int trans_b, ExpertsArgs &a, int64_t M, int64_t N, int64_t G, void *stream)
 {
-    const int tile = rows_tile(M, N, G < 1 ? 1 : G);
+    int tile = rows_tile(M, N, G < 1 ? 1 : G);
+    // 8-bit operands whose results keep 32 bits have no 256 x 256 tile, and that tile's offsets have 32 bits
+    const int64_t es = type == EXPERTS_BF16 || type == EXPERTS_FP16 ? 2 : 1;
+    const bool near = (a.rows ? (int64_t)a.a_rows : 256) <= 0xffffffffLL / es / (a.lda > 0 ? a.lda : 1);
+    if (tile == EXPERTS_256x256 && (type == EXPERTS_FP8_EXACT || !near)) tile = EXPERTS_128x128;
     const int64_t blocks = rows_blocks(tile, M, N, G, a.offsets != nullptr);
     if (blocks > kMostBlocks) return AMULET_ERR_RANGE;
     note_kernel(names[tile], M);
@@ -59,6 +67,7 @@ static int run_rows(const char *const *names, int type, int trans_b, ExpertsArgs
     switch (type) {
     case EXPERTS_BF16: return launch_status(launch_experts_rows_bf16(tile, !trans_b, a, blocks, s));
     case EXPERTS_FP16: return launch_status(launch_experts_rows_fp16(tile, !trans_b, a, blocks, s));
+    case EXPERTS_FP8_EXACT: return launch_status(launch_experts_rows_fp8_exact(tile, !trans_b, a, blocks, s));
     default: return launch_status(launch_experts_rows_fp8(tile, !trans_b, a, blocks, s));
     }
 }
@@ -226,6 +235,7 @@ int amulet_grouped_mm_wgrad(int type, int out_type, int trans_r, int64_t M, int6
     const bool some = M > 0 && !(rows && a_rows == 0);   // else: zeros, and the operands are not read
     if (some && (!A || !D)) return AMULET_ERR_NULL;
     if (some && (lda < K || ldd < N)) return AMULET_ERR_LD;
+    if (some && (lda > kMostPitch / 2 || ldd > kMostPitch / 2)) return AMULET_ERR_RANGE;
     ExpertsArgs a = {};
     a.R = R; a.offsets = offsets; a.rows = rows; a.ldr = ldr; a.group_r = group_r;
     a.G = (int)G; a.a_rows = (int)a_rows; a.k_rows = some ? (int)M : 0; a.out = out_type;
@@ -298,7 +308,7 @@ static int run_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K, i
     a.lda = lda; a.ldb = ldb; a.ldr = ldr; a.group_b = group_b; a.ld_sa = lds_a; a.ld_sb = lds_b; a.group_sb = group_sb;
     a.M = (int)M; a.N = (int)N; a.K = some ? (int)K : 0; a.G = (int)G; a.a_rows = (int)a_rows;
     a.out = out_type;
-    return run_rows(kFp8Names, EXPERTS_FP8, trans_b, a, M, N, G, stream);
+    return run_rows(kFp8Names, out_type == AMULET_FP32 ? EXPERTS_FP8_EXACT : EXPERTS_FP8, trans_b, a, M, N, G, stream);
 }
 
 int amulet_grouped_mm_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K, int64_t G,

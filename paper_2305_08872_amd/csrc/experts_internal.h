@@ -11,7 +11,8 @@
 namespace amulet {
 
 // types of elements, as in the C ABI (amulet_type_t)
-enum { EXPERTS_FP32 = 0, EXPERTS_BF16 = 1, EXPERTS_FP16 = 2, EXPERTS_FP8 = 3 };
+enum { EXPERTS_FP32 = 0, EXPERTS_BF16 = 1, EXPERTS_FP16 = 2, EXPERTS_FP8 = 3,
+       EXPERTS_FP8_EXACT = 4 };   // 8-bit operands, their products summed as bf16 ones (experts_mm_fp8_exact.hip)
 
 // A product by groups of rows, checked on the host.  Pitches and strides in elements.
 struct ExpertsArgs {
@@ -39,6 +40,8 @@ constexpr int kExpertsTileCols[EXPERTS_TILES] = {256, 128, 128, 64, 64, 32};
 hipError_t launch_experts_rows_bf16(int tile, bool b_across, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
 hipError_t launch_experts_rows_fp16(int tile, bool b_across, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
 hipError_t launch_experts_rows_fp8(int tile, bool b_across, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
+// ... for results of 32 bits; no 256 x 256 tile
+hipError_t launch_experts_rows_fp8_exact(int tile, bool b_across, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
 // by sums: tile EXPERTS_256x256 or EXPERTS_128x128
 hipError_t launch_experts_sums(int type, int tile, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
 // R = the parts' sums, added up in order

@@ -43,19 +43,23 @@ extern __shared__ __attribute__((aligned(16))) char xt_smem[];
 
 template <int ELEM_, int BM_, int BN_, int WM_, int WN_, int WK_, int S_, bool AKS_, bool BKS_>
 struct ExpertTile {
-    static constexpr int ELEM = ELEM_;                       // EXPERTS_BF16, _FP16, _FP8
-    static constexpr int ES = ELEM == EXPERTS_FP8 ? 1 : 2;   // bytes of an element
+    static constexpr int ELEM = ELEM_;                       // EXPERTS_BF16, _FP16, _FP8, _FP8_EXACT
+    static constexpr bool FP8 = ELEM == EXPERTS_FP8 || ELEM == EXPERTS_FP8_EXACT;
+    static constexpr int ES = FP8 ? 1 : 2;                   // bytes of an element
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WK = WK_, S = S_;
     static constexpr bool AKS = AKS_, BKS = BKS_;
     static constexpr int BK = 128 / ES;                      // k of a stage
     static constexpr int NW = WM * WN, NT = 64 * NW * WK;    // waves of a k group; threads
     static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
     static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;
-    static constexpr int SA_BYTES = ELEM == EXPERTS_FP8 ? (BM < 64 ? 256 : BM * 4) : 0;   // scales of A's rows
+    static constexpr int SA_BYTES = FP8 ? (BM < 64 ? 256 : BM * 4) : 0;   // scales of A's rows
     static constexpr int STAGE = A_BYTES + B_BYTES + SA_BYTES;
     static constexpr int LDS = S * STAGE * WK;
     // neighbouring fragments of B interleave their columns, so that a lane's values of both are 8 in a row
     static constexpr bool PERM = !BKS && NI % 2 == 0;
+    // the largest tile has registers for 32-bit offsets of A's rows only (its caller sees to it that they fit)
+    static constexpr bool WIDE = BM < 256;
+    static_assert(WK == 1 || NW == 1, "k groups of one wave: they share no stage");
 };
 
 // Position of 16-byte unit `u` of LDS line `line` (RB bytes long); see the two storages above.  256 bytes hold 16 units,
@@ -85,9 +89,22 @@ __device__ __forceinline__ void dma16(const char *p, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
 }
-__device__ __forceinline__ void dma4(const char *p, uint32_t lds)
+// a pointer that is the same in all lanes, in scalar registers
+__device__ __forceinline__ const char *uniform(const char *p)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
+    const uint64_t x = (uint64_t)p;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)x), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32));
+    return (const char *)(((uint64_t)hi << 32) | lo);
+}
+__device__ __forceinline__ void dma16(const char *base, uint32_t off, uint32_t lds)
+{
+    base = uniform(base);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(const char *base, uint32_t off, uint32_t lds)
+{
+    base = uniform(base);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(off), "s"(base), "s"(lds) : "memory", "m0");
 }
 
 // what an index that names no row stands for
@@ -107,73 +124,96 @@ __device__ __forceinline__ xt_u4 load_some(const char *p, int n)
 }
 
 // One operand on its way into LDS: LINES lines (rows of A, columns of B), one stage at a time, by the NW waves of a k group.
-// The LDS units of a stage are loaded 64 by a wave instruction: instruction j of the stage, j = wave + NW q.
-template <int LINES, int ES, bool KS, bool PERM, int NW>
+// The LDS units of a stage are loaded 64 by a wave instruction: instruction j of the stage, j = wave + NW q.  An address is a
+// base in scalar registers that moves on by stages and 32 bits per lane that stay; WIDE: 64 bits per lane (rows given by an
+// index may lie further apart).  A KS operand with an index has its storage rows read a stage ahead.
+template <int LINES, int ES, bool KS, bool PERM, int NW, bool WIDE>
 struct Staged {
     static constexpr int BYTES = LINES * 128, LOADS = LINES / 8;             // instructions of a stage, all waves
     static constexpr int Q = (LOADS + NW - 1) / NW;                           // ... of one wave (the last waves may repeat others')
     static constexpr int RB = KS ? LINES * ES : 128, UR = RB / 16;            // bytes, units of an LDS line
     static constexpr int BK = 128 / ES, E = 16 / ES;
 
-    const char *base;        // storage at the group's first k (KS) or at line 0 (KC)
+    const char *first;       // storage at the group's first k (KS) or at line 0 (KC)
+    const char *base;        // ... at the next stage to load
     int64_t pitch;           // bytes between storage rows
     const int32_t *index;    // KS: storage row of a k, or null: the k itself
-    const char *p[Q];        // KC, and KS without an index: each lane's next unit
+    const char *p[WIDE && !KS ? Q : 1];
+    uint32_t off[WIDE && !KS ? 1 : Q];
+    int row[KS ? Q : 1];     // KS with an index: the next stage's
     int lines, line0;        // lines of the operand, the tile's first
     int k, storage_rows;     // k of the group; rows that an index may name
 
     static __device__ __forceinline__ int slot(int q, int wave, int lane) { return ((wave + NW * q) % LOADS) * 64 + lane; }
 
-    // KC: `row_of(line)` gives the storage row of a line that is inside
+    // `row_of(line)`: storage row of a line that is inside
     template <class RowOf>
-    __device__ __forceinline__ void start_kc(const char *b, int64_t pitch_bytes, int first, int n, int k_all, int k0, int wave, int lane, RowOf row_of)
+    __device__ __forceinline__ void start_kc(const char *b, int64_t pitch_bytes, int first_line, int n, int k_all, int k0, int wave, int lane, RowOf row_of, bool relative)
     {
-        base = b; pitch = pitch_bytes; lines = n; line0 = first; k = k_all; index = nullptr; storage_rows = 0;
+        first = b; pitch = pitch_bytes; lines = n; line0 = first_line; k = k_all; index = nullptr; storage_rows = 0;
+        // (relative: lines are storage rows, and the offsets count from the tile's first)
+        base = b + (relative && !WIDE ? (int64_t)first_line * pitch_bytes : 0) + (int64_t)k0 * ES;
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const int s = slot(q, wave, lane), line = s / 8, u = unit_of<128, false, PERM, ES>(line, s % 8);
-            const int in = first + line < n ? first + line : n - 1;
-            p[q] = b + (int64_t)row_of(in) * pitch_bytes + (int64_t)(k0 * ES + u * 16);
+            const int in = first_line + line < n ? first_line + line : n - 1;
+            if constexpr (WIDE) p[q] = base + (int64_t)row_of(in) * pitch_bytes + u * 16;
+            else off[q] = (uint32_t)(row_of(in) - (relative ? first_line : 0)) * (uint32_t)pitch_bytes + (uint32_t)(u * 16);
         }
     }
-    __device__ __forceinline__ void start_ks(const char *b, int64_t pitch_bytes, const int32_t *idx, int rows, int first, int n, int k_all, int k0, int wave, int lane)
+    __device__ __forceinline__ void start_ks(const char *b, int64_t pitch_bytes, const int32_t *idx, int rows, int first_line, int n, int k_all, int k0, int wave, int lane)
     {
-        base = b; pitch = pitch_bytes; lines = n; line0 = first; k = k_all; index = idx; storage_rows = rows;
-        if (idx) return;
+        first = b; pitch = pitch_bytes; lines = n; line0 = first_line; k = k_all; index = idx; storage_rows = rows;
+        base = b + (idx ? 0 : (int64_t)k0 * pitch_bytes);
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-            const int s = slot(q, wave, lane), row = s / UR;
-            p[q] = b + (int64_t)(k0 + row) * pitch_bytes + column_of(row, s % UR);
+            const int s = slot(q, wave, lane), r = s / UR;
+            off[q] = (uint32_t)column_of(r, s % UR) + (idx ? 0u : (uint32_t)r * (uint32_t)pitch_bytes);
+        }
+        if (idx) read_index(k0, wave, lane);
+    }
+    __device__ __forceinline__ void read_index(int k0, int wave, int lane)
+    {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const int at = k0 + slot(q, wave, lane) / UR;
+            row[KS ? q : 0] = at < k ? index[at] : -1;
         }
     }
-    // byte offset in a storage row of the unit at LDS place `place` of line `row` (past the edge: the last whole unit, whose values nobody stores)
-    __device__ __forceinline__ int64_t column_of(int row, int place) const
+    // byte offset in a storage row of the unit at LDS place `place` of line `r` (past the edge: the last whole unit, whose values nobody stores)
+    __device__ __forceinline__ int64_t column_of(int r, int place) const
     {
-        int c = line0 + unit_of<RB, KS, PERM, ES>(row, place) * E;
+        int c = line0 + unit_of<RB, KS, PERM, ES>(r, place) * E;
         c = c < lines ? c : (lines - 1) / E * E;
         return (int64_t)c * ES;
     }
     // whether some unit of the tile holds lines on both sides of the edge: read whole it ends outside its row
     __device__ __forceinline__ bool cut() const { return KS && line0 + LINES > lines && lines % E != 0; }
 
-    // the whole stage at k0 into `lds`; then on to the stage `ahead` k further
+    // the whole stage at k0 into `lds`; the next one is `ahead` k further
     __device__ __forceinline__ void load(uint32_t lds, int k0, int ahead, int wave, int lane)
     {
+        if (KS && index) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const int r = row[KS ? q : 0];
+                const char *const from = base + (int64_t)r * pitch + off[WIDE && !KS ? 0 : q];
+                dma16((unsigned)r < (unsigned)storage_rows ? from : (const char *)&xt_zeros, lds + (uint32_t)((wave + NW * q) % LOADS) * 1024u);
+            }
+            read_index(k0 + ahead, wave, lane);
+            return;
+        }
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const uint32_t to = lds + (uint32_t)((wave + NW * q) % LOADS) * 1024u;
-            if (KS && index) {
-                const int row = slot(q, wave, lane) / UR;
-                const int r = index[k0 + row];
-                const char *const from = base + (int64_t)r * pitch + column_of(row, slot(q, wave, lane) % UR);
-                dma16((unsigned)r < (unsigned)storage_rows ? from : (const char *)&xt_zeros, to);
-            } else {
+            if constexpr (WIDE && !KS) {
                 dma16(p[q], to);
-                p[q] += KS ? (int64_t)ahead * pitch : (int64_t)ahead * ES;
-            }
+                p[q] += ahead * ES;
+            } else dma16(base, off[q], to);
         }
+        base += KS ? (int64_t)ahead * pitch : (int64_t)ahead * ES;
     }
-    // the stage at k0, of which `left` k are there (any number, also none), through registers
+    // the stage at k0, of which any part may be there, through registers
     template <class RowOf>
     __device__ __forceinline__ void load_cut(char *lds, int k0, int wave, int lane, RowOf row_of)
     {
@@ -184,14 +224,14 @@ struct Staged {
             if constexpr (!KS) {
                 const int line = s / 8, at = k0 + unit_of<128, false, PERM, ES>(line, s % 8) * E;
                 const int in = line0 + line < lines ? line0 + line : lines - 1;
-                if (at < k) v = load_some<ES>(base + (int64_t)row_of(in) * pitch + (int64_t)at * ES, k - at);
+                if (at < k) v = load_some<ES>(first + (int64_t)row_of(in) * pitch + (int64_t)at * ES, k - at);
             } else {
-                const int row = s / UR, c = line0 + unit_of<RB, KS, PERM, ES>(row, s % UR) * E;
-                if (k0 + row < k && c < lines) {
-                    int r = k0 + row;
+                const int r0 = s / UR, c = line0 + unit_of<RB, KS, PERM, ES>(r0, s % UR) * E;
+                if (k0 + r0 < k && c < lines) {
+                    int r = k0 + r0;
                     bool there = true;
                     if (index) { r = index[r]; there = (unsigned)r < (unsigned)storage_rows; }
-                    if (there) v = load_some<ES>(base + (int64_t)r * pitch + (int64_t)c * ES, lines - c);
+                    if (there) v = load_some<ES>(first + (int64_t)r * pitch + (int64_t)c * ES, lines - c);
                 }
             }
             *(xt_u4 *)(lds + s * 16) = v;
@@ -266,6 +306,21 @@ __device__ __forceinline__ xt_f4 mma16(xt_u4 a, xt_u4 b, xt_f4 c)
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(xt_bf8, a), __builtin_bit_cast(xt_bf8, b), c, 0, 0, 0);
     else
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(xt_h8, a), __builtin_bit_cast(xt_h8, b), c, 0, 0, 0);
+}
+
+// eight e4m3 values of a unit (its first or second half) as bf16, exactly
+__device__ __forceinline__ xt_u4 bf16_of(xt_u4 x, int half)
+{
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    xt_u4 y;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t w = x[2 * half + i];
+        const bf2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+        y[2 * i] = __builtin_bit_cast(uint32_t, lo);
+        y[2 * i + 1] = __builtin_bit_cast(uint32_t, hi);
+    }
+    return y;
 }
 
 // `v` consecutive values of R from column c on, of which those below `cols` exist; rounded once, to the output's type.
@@ -382,29 +437,125 @@ __device__ __forceinline__ bool find_row_tile(const ExpertsArgs &a, int tiles_n,
     return true;
 }
 
+// A wave's products of one stage, in steps: 16 bits: halves of the stage's k times halves of the wave's rows; 8 bits: one or two row
+// blocks (an instruction has all 128 k).  While a step's matrix instructions run, the next one's fragments are read.
+template <class T>
+struct Steps {
+    static constexpr int MA = T::FP8 ? (T::MI > 1 && T::MI < 8 ? 2 : 1) : T::MI > 1 ? T::MI / 2 : 1;   // row blocks of a step
+    static constexpr int STEPS = T::FP8 ? T::MI / MA : T::MI > 1 ? 4 : 2;
+    typedef FragReader<T, T::BM, T::AKS, false> ReadA;
+    typedef FragReader<T, T::BN, T::BKS, T::PERM> ReadB;
+    static constexpr int U = T::FP8 ? 2 : 1;     // 16-byte halves of a fragment
+
+    xt_u4 a[2][MA][U];
+    xt_u4 b[T::FP8 ? 1 : 2][T::NI][U];
+    float w[2][MA];                              // fp8: the rows' scales
+
+    static __device__ __forceinline__ constexpr int first_row(int t) { return T::FP8 ? t * MA : (t % (STEPS / 2)) * MA; }
+    template <int t>
+    __device__ __forceinline__ void read_a(const ReadA &r, const char *la, const float *scales)
+    {
+#pragma unroll
+        for (int m = 0; m < MA; ++m) {
+            if constexpr (T::FP8) {
+                a[t & 1][m][0] = r.read(la, first_row(t) + m, 0);
+                a[t & 1][m][U - 1] = r.read(la, first_row(t) + m, 1);
+                w[t & 1][m] = scales[(first_row(t) + m) * 16];
+            } else a[t & 1][m][0] = r.read(la, first_row(t) + m, t / (STEPS / 2));
+        }
+    }
+    // the fragments of B that step t needs and the step before did not
+    template <int t>
+    __device__ __forceinline__ void read_b(const ReadB &r, const char *lb)
+    {
+        if constexpr (T::FP8) {
+            if constexpr (t == 0)
+#pragma unroll
+                for (int ni = 0; ni < T::NI; ++ni) {
+                    b[0][ni][0] = r.read(lb, ni, 0);
+                    b[0][ni][U - 1] = r.read(lb, ni, 1);
+                }
+        } else if constexpr (t % (STEPS / 2) == 0) {
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ++ni) b[t / (STEPS / 2)][ni][0] = r.read(lb, ni, t / (STEPS / 2));
+        }
+    }
+    template <int t>
+    __device__ __forceinline__ void mma(float wb, xt_f4 (&acc)[T::MI][T::NI])
+    {
+#pragma unroll
+        for (int m = 0; m < MA; ++m)
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ++ni) {
+                xt_f4 &c = acc[first_row(t) + m][ni];
+                if constexpr (!T::FP8) c = mma16<T::ELEM>(b[t / (STEPS / 2)][ni][0], a[t & 1][m][0], c);
+                else {
+                    const xt_f4 zero = {0, 0, 0, 0};
+                    xt_f4 x;
+                    if constexpr (T::ELEM == EXPERTS_FP8) {
+                        const xt_u4 *p = a[t & 1][m], *q = b[0][ni];
+                        const xt_i8 xa = {(int)p[0][0], (int)p[0][1], (int)p[0][2], (int)p[0][3], (int)p[U - 1][0], (int)p[U - 1][1], (int)p[U - 1][2], (int)p[U - 1][3]};
+                        const xt_i8 xb = {(int)q[0][0], (int)q[0][1], (int)q[0][2], (int)q[0][3], (int)q[U - 1][0], (int)q[U - 1][1], (int)q[U - 1][2], (int)q[U - 1][3]};
+                        x = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(xb, xa, zero, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+                    } else {
+                        x = zero;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            x = mma16<EXPERTS_BF16>(bf16_of(b[0][ni][u / 2], u % 2), bf16_of(a[t & 1][m][u / 2], u % 2), x);
+                    }
+                    const float f = w[t & 1][m] * wb;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) c[v] = __builtin_fmaf(f, x[v], c[v]);
+                }
+            }
+    }
+};
+
+// A constant wait: at most N of this wave's vector memory operations under way.
 template <int N>
 __device__ __forceinline__ void wait_vm()
 {
     asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
+template <int NW>
+__device__ __forceinline__ void meet()   // a group of one wave has nobody to wait for
+{
+    // (a bare s_barrier: a full fence would drain the loads under way)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Where a wave finds the scales of its tile (fp8).
+struct TileScales {
+    const char *a;       // of A, k block 0 (uniform)
+    uint32_t a_off;      // this lane's row, bytes
+    int64_t a_step;      // bytes from block to block
+    const float *b;
+    int64_t b_step;
+};
 
 // The sums of a tile: acc[mi][ni] of this wave, over the k of [k0, k1) of the group; k-group waves each their stages, joined
 // at the end.  True for the waves that hold the result.
+//
+// Stages that lie wholly inside go through the ring: S of them are requested at first, and the one barrier of a stage lies before its last
+// step, when every wave has read all of it: behind it the slot is refilled with the stage S further on, and the first fragments of the
+// next stage are read, which the same barrier certifies as landed.  What is left is loaded through registers, one stage at a time.
 template <class T, class ARow>
-__device__ __forceinline__ bool tile_sums(const ExpertsArgs &a, Staged<T::BM, T::ES, T::AKS, false, T::NW> &sa, Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW> &sb,
-                                          const int k0, const int k1, const int wave, const int kg, const int lane, ARow a_row, const char *scale_at, int64_t scale_step,
-                                          const float *scale_b, int64_t scale_b_step, xt_f4 (&acc)[T::MI][T::NI])
+__device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::AKS, false, T::NW, T::WIDE> &sa, Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW, false> &sb,
+                                          const int k0, const int k1, const int wave, const int kg, const int lane, ARow a_row, const TileScales &scales, xt_f4 (&acc)[T::MI][T::NI])
 {
-    constexpr int S = T::S, BK = T::BK;
-    constexpr int LOADS = Staged<T::BM, T::ES, T::AKS, false, T::NW>::Q + Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW>::Q + (T::ELEM == EXPERTS_FP8 ? 1 : 0);
+    constexpr int S = T::S, BK = T::BK, STEPS = Steps<T>::STEPS;
+    constexpr int LOADS = Staged<T::BM, T::ES, T::AKS, false, T::NW, T::WIDE>::Q + Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW, false>::Q + (T::FP8 ? 1 : 0);
     static_assert(LOADS * (S - 2) <= 63, "the wait count is a 6-bit field");
     const int wm = wave / T::WN, wn = wave % T::WN;
     char *const ring = xt_smem + kg * (S * T::STAGE);
     const uint32_t ring_at = (uint32_t)(uintptr_t)(xt_lds_void)ring;
-    FragReader<T, T::BM, T::AKS, false> fa;
-    FragReader<T, T::BN, T::BKS, T::PERM> fb;
-    fa.start(wm * (T::BM / T::WM), lane);
-    fb.start(wn * (T::BN / T::WN), lane);
+    Steps<T> f;
+    typename Steps<T>::ReadA ra;
+    typename Steps<T>::ReadB rb;
+    ra.start(wm * (T::BM / T::WM), lane);
+    rb.start(wn * (T::BN / T::WN), lane);
 #pragma unroll
     for (int mi = 0; mi < T::MI; ++mi)
 #pragma unroll
@@ -413,80 +564,91 @@ __device__ __forceinline__ bool tile_sums(const ExpertsArgs &a, Staged<T::BM, T:
     const int k = k1 - k0;
     const int stages = k > 0 ? (k + BK - 1) / BK : 0;
     // stages that lie wholly inside both operands
-    const bool a_cut = sa.cut(), b_cut = sb.cut();
     int whole = k > 0 ? k / BK : 0;
+    const bool a_cut = sa.cut(), b_cut = sb.cut();
     if (whole == stages && whole > 0 && (a_cut || b_cut)) --whole;
-    if ((T::AKS && a_cut && sa.index) || (T::BKS && b_cut && sb.index)) whole = 0;   // (any k may name the storage's last row)
-    const int rounds = (stages + T::WK - 1) / T::WK;
-    auto request = [&](int r) {
-        const int s = r * T::WK + kg, slot = r % S;
-        if (s < whole) {
-            const uint32_t to = ring_at + (uint32_t)(slot * T::STAGE);
-            sa.load(to, k0 + s * BK, BK * T::WK, wave, lane);
-            sb.load(to + T::A_BYTES, k0 + s * BK, BK * T::WK, wave, lane);
-        } else if (s < stages) {
-            char *const to = ring + slot * T::STAGE;
-            sa.load_cut(to, k0 + s * BK, wave, lane, a_row);
-            sb.load_cut(to + T::A_BYTES, k0 + s * BK, wave, lane, [](int r2) { return r2; });
+    if ((a_cut && sa.index) || (b_cut && sb.index)) whole = 0;   // (any k may name the storage's last row)
+    const int mine = whole > kg ? (whole - kg + T::WK - 1) / T::WK : 0;   // ... this group's
+    auto slot_of = [&](int r) { return r % S; };
+    auto request_scales = [&](int s, int slot) {
+        // (64 rows a wave; the last waves repeat others')
+        dma4(scales.a + (int64_t)s * scales.a_step, scales.a_off, ring_at + (uint32_t)(slot * T::STAGE + T::A_BYTES + T::B_BYTES + (wave * 64 % (T::BM < 64 ? 64 : T::BM)) * 4));
+    };
+    auto request = [&](int r, int slot) {
+        const int s = r * T::WK + kg;
+        const uint32_t to = ring_at + (uint32_t)(slot * T::STAGE);
+        sa.load(to, k0 + s * BK, BK * T::WK, wave, lane);
+        sb.load(to + T::A_BYTES, k0 + s * BK, BK * T::WK, wave, lane);
+        if constexpr (T::FP8) request_scales(s, slot);
+    };
+    auto scale_row = [&](const char *la) { return (const float *)(la + T::A_BYTES + T::B_BYTES) + wm * (T::BM / T::WM) + (lane & 15); };
+    auto scale_b = [&](int s) { return T::FP8 ? scales.b[(int64_t)s * scales.b_step] : 0.0f; };
+    // stage at `la`; `next`: what comes before its last step, and returns where the next one is (null: nowhere)
+    auto stage = [&](const char *la, float wb, auto next) {
+        const char *const lb = la + T::A_BYTES;
+        const char *after = nullptr;
+#define AMULET_STEP(t)                                                          \
+        if constexpr (t < STEPS) {                                              \
+            if constexpr (t + 1 < STEPS) {                                      \
+                f.template read_a<t + 1>(ra, la, scale_row(la));                \
+                f.template read_b<t + 1>(rb, lb);                               \
+            } else {                                                            \
+                after = next();                                                 \
+                if (STEPS > 1 && after) {                                       \
+                    f.template read_a<0>(ra, after, scale_row(after));          \
+                    if constexpr (!T::FP8) f.template read_b<0>(rb, after + T::A_BYTES); \
+                }                                                               \
+            }                                                                   \
+            f.template mma<t>(wb, acc);                                         \
         }
-        if constexpr (T::ELEM == EXPERTS_FP8) {
-            // (64 rows a wave; the last waves repeat others')
-            if (s < stages) dma4(scale_at + (int64_t)s * scale_step, ring_at + (uint32_t)(slot * T::STAGE + T::A_BYTES + T::B_BYTES + (wave * 64 % (T::BM < 64 ? 64 : T::BM)) * 4));
+        AMULET_STEP(0) AMULET_STEP(1) AMULET_STEP(2) AMULET_STEP(3) AMULET_STEP(4) AMULET_STEP(5) AMULET_STEP(6) AMULET_STEP(7)
+#undef AMULET_STEP
+        if (after) {
+            if constexpr (STEPS == 1) f.template read_a<0>(ra, after, scale_row(after));
+            if constexpr (T::FP8) f.template read_b<0>(rb, after + T::A_BYTES);
         }
     };
+
+    if (mine > 0) {
 #pragma unroll
-    for (int r = 0; r < S - 1; ++r)
-        if (r < rounds) request(r);
-    for (int r = 0; r < rounds; ++r) {
-        // stage r has landed: only the requests of the S - 2 rounds behind it may be under way
-        if (S > 2 && r + S - 2 < rounds && (r + S - 2) * T::WK + kg < whole) wait_vm<LOADS * (S - 2)>();
+        for (int r = 0; r < S; ++r)
+            if (r < mine) request(r, r);
+        if (mine >= S) wait_vm<LOADS * (S - 1)>();
         else wait_vm<0>();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (r + S - 1 < rounds) request(r + S - 1);   // into the slot that round r - 1 has left
-        const int s = r * T::WK + kg;
-        if (s >= stages) continue;
-        const char *const la = ring + (r % S) * T::STAGE, *const lb = la + T::A_BYTES;
-        if constexpr (T::ELEM != EXPERTS_FP8) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                xt_u4 xa[T::MI], xb[T::NI];
-#pragma unroll
-                for (int ni = 0; ni < T::NI; ++ni) xb[ni] = fb.read(lb, ni, h);
-#pragma unroll
-                for (int mi = 0; mi < T::MI; ++mi) xa[mi] = fa.read(la, mi, h);
-#pragma unroll
-                for (int mi = 0; mi < T::MI; ++mi)
-#pragma unroll
-                    for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = mma16<T::ELEM>(xb[ni], xa[mi], acc[mi][ni]);
-            }
-        } else {
-            const float wb = scale_b[(int64_t)s * scale_b_step];
-            const float *const ls = (const float *)(lb + T::B_BYTES) + wm * (T::BM / T::WM) + (lane & 15);
-            xt_i8 xb[T::NI];
-#pragma unroll
-            for (int ni = 0; ni < T::NI; ++ni) {
-                const xt_u4 lo = fb.read(lb, ni, 0), hi = fb.read(lb, ni, 1);
-                xb[ni] = xt_i8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-            }
-#pragma unroll
-            for (int mi = 0; mi < T::MI; ++mi) {
-                const xt_u4 lo = fa.read(la, mi, 0), hi = fa.read(la, mi, 1);
-                const xt_i8 xa = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-                const float w = ls[mi * 16] * wb;
-#pragma unroll
-                for (int ni = 0; ni < T::NI; ++ni) {
-                    const xt_f4 zero = {0, 0, 0, 0};
-                    const xt_f4 x = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(xb[ni], xa, zero, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[mi][ni][v] = __builtin_fmaf(w, x[v], acc[mi][ni][v]);
-                }
-            }
+        meet<T::NW>();
+        f.template read_a<0>(ra, ring, scale_row(ring));
+        f.template read_b<0>(rb, ring + T::A_BYTES);
+        int slot = 0;
+        float wb = scale_b(kg);
+        for (int r = 0; r < mine; ++r) {
+            const int here = slot;
+            slot = slot + 1 == S ? 0 : slot + 1;
+            const float wb_next = r + 1 < mine ? scale_b((r + 1) * T::WK + kg) : 0.0f;
+            stage(ring + here * T::STAGE, wb, [&]() -> const char * {
+                if (r + 1 >= mine) return nullptr;
+                // stage r + 1 has landed: only the S - 2 behind it may be under way
+                if (S > 2 && r + S - 1 < mine) wait_vm<LOADS * (S - 2)>();
+                else wait_vm<0>();
+                meet<T::NW>();
+                if (r + S < mine) request(r + S, here);
+                return ring + slot * T::STAGE;
+            });
+            wb = wb_next;
         }
     }
+    for (int s = whole; s < stages; ++s) {
+        if (T::WK > 1 && s % T::WK != kg) continue;
+        meet<T::NW>();                 // slot 0 is no longer read
+        sa.load_cut(ring, k0 + s * BK, wave, lane, a_row);
+        sb.load_cut(ring + T::A_BYTES, k0 + s * BK, wave, lane, [](int i) { return i; });
+        if constexpr (T::FP8) { request_scales(s, 0); wait_vm<0>(); }
+        meet<T::NW>();
+        f.template read_a<0>(ra, ring, scale_row(ring));
+        f.template read_b<0>(rb, ring + T::A_BYTES);
+        stage(ring, scale_b(s), []() -> const char * { return nullptr; });
+    }
     if constexpr (T::WK > 1) {
-        // the k groups' sums, added up by the first in order (fp32, so the result does not depend on who came first)
+        // the k groups' sums, added up by the first in order (so the result does not depend on who came first)
         __syncthreads();
         constexpr int PER = T::MI * T::NI * 4 * 64;   // floats of a wave
         float *const img = (float *)xt_smem;
@@ -536,26 +698,26 @@ __global__ void __launch_bounds__(T::NT) experts_rows_kernel(const ExpertsArgs a
         return (unsigned)r < (unsigned)a.a_rows ? r : 0;
     };
     const int K = t.group < 0 ? 0 : a.K;
-    Staged<T::BM, T::ES, T::AKS, false, T::NW> sa = {};
-    Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW> sb = {};
+    Staged<T::BM, T::ES, T::AKS, false, T::NW, T::WIDE> sa = {};
+    Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW, false> sb = {};
     const char *const B = (const char *)a.B + (int64_t)(t.group < 0 ? 0 : t.group) * a.group_b * T::ES;
     if (K > 0) {
-        sa.start_kc((const char *)a.A, a.lda * T::ES, row0, t.row1, K, kg * T::BK, wave, lane, a_row);
+        sa.start_kc((const char *)a.A, a.lda * T::ES, row0, t.row1, K, kg * T::BK, wave, lane, a_row, !a.rows);
         if constexpr (T::BKS) sb.start_ks(B, a.ldb * T::ES, nullptr, 0, col0, a.N, K, kg * T::BK, wave, lane);
-        else sb.start_kc(B, a.ldb * T::ES, col0, a.N, K, kg * T::BK, wave, lane, [](int i) { return i; });
+        else sb.start_kc(B, a.ldb * T::ES, col0, a.N, K, kg * T::BK, wave, lane, [](int i) { return i; }, true);
     }
-    const char *scale_at = nullptr;
-    const float *scale_b = nullptr;
-    int64_t scale_b_step = 0;
-    if constexpr (T::ELEM == EXPERTS_FP8) {
+    TileScales scales = {};
+    if constexpr (T::FP8) {
         const int i = row0 + (wave * 64 + lane) % (T::BM < 64 ? 64 : T::BM);
-        if (K > 0) scale_at = (const char *)(a.scale_a + a_row(i < t.row1 ? i : t.row1 - 1));
+        scales.a = (const char *)a.scale_a;
+        scales.a_step = a.ld_sa * 4;
+        if (K > 0) scales.a_off = (uint32_t)a_row(i < t.row1 ? i : t.row1 - 1) * 4u;
         const int block = (col0 + wn * (T::BN / T::WN)) / 128, blocks = (a.N + 127) / 128;
         const int64_t at = block < blocks ? block : blocks - 1;
-        scale_b = a.scale_b + (int64_t)(t.group < 0 ? 0 : t.group) * a.group_sb + (T::BKS ? at : at * a.ld_sb);
-        scale_b_step = T::BKS ? a.ld_sb : 1;
+        scales.b = a.scale_b + (int64_t)(t.group < 0 ? 0 : t.group) * a.group_sb + (T::BKS ? at : at * a.ld_sb);
+        scales.b_step = T::BKS ? a.ld_sb : 1;
     }
-    if (!tile_sums<T>(a, sa, sb, 0, K, wave, kg, lane, a_row, scale_at, a.ld_sa * 4, scale_b, scale_b_step, acc)) return;
+    if (!tile_sums<T>(sa, sb, 0, K, wave, kg, lane, a_row, scales, acc)) return;
 
 #pragma unroll
     for (int mi = 0; mi < T::MI; ++mi) {
@@ -604,14 +766,14 @@ __global__ void __launch_bounds__(T::NT) experts_sums_kernel(const ExpertsArgs a
     const int64_t k0 = (int64_t)part * chunk;
     const int from = k0 < k_all ? (int)k0 : k_all, to = k0 + chunk < k_all ? (int)(k0 + chunk) : k_all;
 
-    Staged<T::BM, T::ES, T::AKS, false, T::NW> sa;
-    Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW> sb;
+    Staged<T::BM, T::ES, T::AKS, false, T::NW, T::WIDE> sa;
+    Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW, false> sb;
     const char *const A = (const char *)a.A, *const B = (const char *)a.B;
     const int32_t *const ia = a.rows_of_b ? nullptr : a.rows, *const ib = a.rows_of_b ? a.rows : nullptr;
     sa.start_ks(ia ? A : A + (int64_t)lo * a.lda * T::ES, a.lda * T::ES, ia ? ia + lo : nullptr, a.a_rows, m0, a.M, to, from + kg * T::BK, wave, lane);
     sb.start_ks(ib ? B : B + (int64_t)lo * a.ldb * T::ES, a.ldb * T::ES, ib ? ib + lo : nullptr, a.a_rows, n0, a.N, to, from + kg * T::BK, wave, lane);
     xt_f4 acc[T::MI][T::NI];
-    if (!tile_sums<T>(a, sa, sb, from, to, wave, kg, lane, [](int i) { return i; }, nullptr, 0, nullptr, 0, acc)) return;
+    if (!tile_sums<T>(sa, sb, from, to, wave, kg, lane, [](int i) { return i; }, TileScales(), acc)) return;
 
     const int wm = wave / T::WN, wn = wave % T::WN;
     if (a.parts > 1) {
