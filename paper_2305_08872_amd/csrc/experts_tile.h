@@ -20,6 +20,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "experts_internal.h"
 
 // the LDS-DMA asm below sets M0 itself and says so in its clobber list
@@ -87,6 +89,7 @@ __device__ __forceinline__ int unit_of(int line, int u)
 
 __device__ __forceinline__ void dma16(const char *p, uint32_t lds)
 {
+    lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
 }
 // a pointer that is the same in all lanes, in scalar registers
@@ -99,11 +102,13 @@ __device__ __forceinline__ const char *uniform(const char *p)
 __device__ __forceinline__ void dma16(const char *base, uint32_t off, uint32_t lds)
 {
     base = uniform(base);
+    lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(lds) : "memory", "m0");
 }
 __device__ __forceinline__ void dma4(const char *base, uint32_t off, uint32_t lds)
 {
     base = uniform(base);
+    lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(off), "s"(base), "s"(lds) : "memory", "m0");
 }
 
@@ -569,7 +574,6 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::AKS, false, T:
     if (whole == stages && whole > 0 && (a_cut || b_cut)) --whole;
     if ((a_cut && sa.index) || (b_cut && sb.index)) whole = 0;   // (any k may name the storage's last row)
     const int mine = whole > kg ? (whole - kg + T::WK - 1) / T::WK : 0;   // ... this group's
-    auto slot_of = [&](int r) { return r % S; };
     auto request_scales = [&](int s, int slot) {
         // (64 rows a wave; the last waves repeat others')
         dma4(scales.a + (int64_t)s * scales.a_step, scales.a_off, ring_at + (uint32_t)(slot * T::STAGE + T::A_BYTES + T::B_BYTES + (wave * 64 % (T::BM < 64 ? 64 : T::BM)) * 4));
@@ -583,33 +587,35 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::AKS, false, T:
     };
     auto scale_row = [&](const char *la) { return (const float *)(la + T::A_BYTES + T::B_BYTES) + wm * (T::BM / T::WM) + (lane & 15); };
     auto scale_b = [&](int s) { return T::FP8 ? scales.b[(int64_t)s * scales.b_step] : 0.0f; };
-    // stage at `la`; `next`: what comes before its last step, and returns where the next one is (null: nowhere)
-    auto stage = [&](const char *la, float wb, auto next) {
+    // One stage at `la`, its first fragments read.  AFTER (another stage's address or null, known when compiled: a branch between
+    // the steps would have the compiler gather the matrix instructions behind it): read its first fragments before the last
+    // step, once `next` has seen to it that they are there.
+    auto stage = [&](const char *la, float wb, const char *after, auto there, auto next) {
+        constexpr bool AFTER = decltype(there)::value;
         const char *const lb = la + T::A_BYTES;
-        const char *after = nullptr;
 #define AMULET_STEP(t)                                                          \
         if constexpr (t < STEPS) {                                              \
             if constexpr (t + 1 < STEPS) {                                      \
                 f.template read_a<t + 1>(ra, la, scale_row(la));                \
                 f.template read_b<t + 1>(rb, lb);                               \
-            } else {                                                            \
-                after = next();                                                 \
-                if (STEPS > 1 && after) {                                       \
-                    f.template read_a<0>(ra, after, scale_row(after));          \
-                    if constexpr (!T::FP8) f.template read_b<0>(rb, after + T::A_BYTES); \
-                }                                                               \
+            } else if constexpr (AFTER) {                                       \
+                next();                                                         \
+                if constexpr (STEPS > 1) f.template read_a<0>(ra, after, scale_row(after)); \
+                if constexpr (!T::FP8) f.template read_b<0>(rb, after + T::A_BYTES); \
             }                                                                   \
             f.template mma<t>(wb, acc);                                         \
+            if constexpr (T::FP8) __builtin_amdgcn_sched_barrier(0);            \
         }
         AMULET_STEP(0) AMULET_STEP(1) AMULET_STEP(2) AMULET_STEP(3) AMULET_STEP(4) AMULET_STEP(5) AMULET_STEP(6) AMULET_STEP(7)
 #undef AMULET_STEP
-        if (after) {
+        if constexpr (AFTER) {
             if constexpr (STEPS == 1) f.template read_a<0>(ra, after, scale_row(after));
             if constexpr (T::FP8) f.template read_b<0>(rb, after + T::A_BYTES);
         }
     };
 
     if (mine > 0) {
+        int slot = 0;
 #pragma unroll
         for (int r = 0; r < S; ++r)
             if (r < mine) request(r, r);
@@ -618,24 +624,32 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::AKS, false, T:
         meet<T::NW>();
         f.template read_a<0>(ra, ring, scale_row(ring));
         f.template read_b<0>(rb, ring + T::A_BYTES);
-        int slot = 0;
         float wb = scale_b(kg);
-        for (int r = 0; r < mine; ++r) {
+        int r = 0;
+        for (; r + S < mine; ++r) {
             const int here = slot;
             slot = slot + 1 == S ? 0 : slot + 1;
-            const float wb_next = r + 1 < mine ? scale_b((r + 1) * T::WK + kg) : 0.0f;
-            stage(ring + here * T::STAGE, wb, [&]() -> const char * {
-                if (r + 1 >= mine) return nullptr;
-                // stage r + 1 has landed: only the S - 2 behind it may be under way
-                if (S > 2 && r + S - 1 < mine) wait_vm<LOADS * (S - 2)>();
-                else wait_vm<0>();
+            const float now = wb;
+            wb = scale_b((r + 1) * T::WK + kg);
+            stage(ring + here * T::STAGE, now, ring + slot * T::STAGE, std::true_type(), [&]() {
+                wait_vm<LOADS * (S - 2)>();   // stage r + 1 has landed: only the S - 2 behind it may be under way
                 meet<T::NW>();
-                if (r + S < mine) request(r + S, here);
-                return ring + slot * T::STAGE;
+                request(r + S, here);
             });
-            wb = wb_next;
         }
+        for (; r + 1 < mine; ++r) {
+            const int here = slot;
+            slot = slot + 1 == S ? 0 : slot + 1;
+            const float now = wb;
+            wb = scale_b((r + 1) * T::WK + kg);
+            stage(ring + here * T::STAGE, now, ring + slot * T::STAGE, std::true_type(), [&]() {
+                wait_vm<0>();
+                meet<T::NW>();
+            });
+        }
+        stage(ring + slot * T::STAGE, wb, nullptr, std::false_type(), []() {});
     }
+    // stages that are not whole
     for (int s = whole; s < stages; ++s) {
         if (T::WK > 1 && s % T::WK != kg) continue;
         meet<T::NW>();                 // slot 0 is no longer read
@@ -645,7 +659,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::AKS, false, T:
         meet<T::NW>();
         f.template read_a<0>(ra, ring, scale_row(ring));
         f.template read_b<0>(rb, ring + T::A_BYTES);
-        stage(ring, scale_b(s), []() -> const char * { return nullptr; });
+        stage(ring, scale_b(s), nullptr, std::false_type(), []() {});
     }
     if constexpr (T::WK > 1) {
         // the k groups' sums, added up by the first in order (so the result does not depend on who came first)
