@@ -3,9 +3,9 @@
 //     R[g]    = sum over the rows i of g of A[row(i)]^T D[i]  by sums (the gradients of the experts' weights)
 // One kernel body for both; the translation units experts_mm_*.hip hold its instances.
 //
-// A stage of an operand is 128 bytes of k per line (64 k of 16 bits, 128 of 8), streamed global -> LDS by
+// A stage of an operand is 128 bytes of k per line (64 k of 16 bits, 128 of 8) or 64, streamed global -> LDS by
 // global_load_lds_dwordx4 (64 lanes x 16 bytes, any byte alignment) through a ring of S stages.  Two storages:
-//   k along the rows (KC): LDS keeps [line][8 units of 16 bytes]; a lane's fragment is one ds_read_b128.
+//   k along the rows (KC): LDS keeps [line][units of 16 bytes]; a lane's fragment is one ds_read_b128.
 //   k across them   (KS): LDS keeps [k][line], and ds_read_b64_tr_b16 / _b8 hand a lane the k of its line.
 // Both are XOR-swizzled by unit so that the lanes of an LDS clock fall on distinct banks (unit_of below).  A stage that
 // does not lie wholly inside its operand (the last k, lines past the edge that end inside a unit) goes through registers
@@ -43,36 +43,41 @@ typedef __attribute__((address_space(3))) void *xt_lds_void;
 
 extern __shared__ __attribute__((aligned(16))) char xt_smem[];
 
-template <int ELEM_, int BM_, int BN_, int WM_, int WN_, int WK_, int S_, bool AKS_, bool BKS_>
+template <int ELEM_, int BM_, int BN_, int WM_, int WN_, int WK_, int S_, int KB_, bool AKS_, bool BKS_>
 struct ExpertTile {
     static constexpr int ELEM = ELEM_;                       // EXPERTS_BF16, _FP16, _FP8, _FP8_EXACT
     static constexpr bool FP8 = ELEM == EXPERTS_FP8 || ELEM == EXPERTS_FP8_EXACT;
     static constexpr int ES = FP8 ? 1 : 2;                   // bytes of an element
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WK = WK_, S = S_;
     static constexpr bool AKS = AKS_, BKS = BKS_;
-    static constexpr int BK = 128 / ES;                      // k of a stage
+    static constexpr int KB = KB_, BK = KB / ES;             // bytes and k of a stage's line
+    static_assert(KB == 128 || (KB == 64 && !FP8), "a stage is one or two instructions' k");
     static constexpr int NW = WM * WN, NT = 64 * NW * WK;    // waves of a k group; threads
     static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
-    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;
+    static constexpr int A_BYTES = BM * KB, B_BYTES = BN * KB;
     static constexpr int SA_BYTES = FP8 ? (BM < 64 ? 256 : BM * 4) : 0;   // scales of A's rows
     static constexpr int STAGE = A_BYTES + B_BYTES + SA_BYTES;
-    static constexpr int LDS = S * STAGE * WK;
+    static constexpr int SPREAD = BM >= 256 && !FP8 ? 2 : 0;   // matrix instructions between those of a request
+    static constexpr int PREFETCH = BM >= 256 && AKS ? 2 : 0;      // stages further on whose lines are asked for ahead, see tile_sums
+    static constexpr int LDS = S * STAGE * WK + (PREFETCH ? 256 : 0);
     // neighbouring fragments of B interleave their columns, so that a lane's values of both are 8 in a row
     static constexpr bool PERM = !BKS && NI % 2 == 0;
     // the largest tile has registers for 32-bit offsets of A's rows only (its caller sees to it that they fit)
     static constexpr bool WIDE = BM < 256;
+    static constexpr bool ALWAYS = BM >= 256;   // requests past the end, see tile_sums
     static_assert(WK == 1 || NW == 1, "k groups of one wave: they share no stage");
 };
 
 // Position of 16-byte unit `u` of LDS line `line` (RB bytes long); see the two storages above.  256 bytes hold 16 units,
 // the banks of one clock:
-//   KC, natural fragments (lines 0..15 at one u): 2 lines per 256 bytes, so bits 1..3 of the line;
-//   KC, interleaved (lines 8 a + c, a, c = 0..3, or + 4): bits 1 and 3, 4;
+//   KC, natural fragments (lines 0..15 at one u): 2 lines per 256 bytes, so bits 1..3 of the line (64 bytes: 4 lines, bits 2, 3);
+//   KC, interleaved (lines 8 a + c, a, c = 0..3, or + 4): bits 1 and 3, 4 (64 bytes: bits 3, 4);
 //   KS: 16-bit reads take 32 bytes of rows {0..3, 8..11} at a time, 8-bit reads 16 of rows {0..7, 16..23}.
 template <int RB, bool KS, bool PERM, int ES>
 __device__ __forceinline__ int unit_of(int line, int u)
 {
-    if constexpr (!KS) return u ^ (PERM ? ((line >> 2) & 6) | ((line >> 1) & 1) : (line >> 1) & 7);
+    if constexpr (!KS && RB == 64) return u ^ (PERM ? (line >> 3) & 3 : (line >> 2) & 3);
+    else if constexpr (!KS) return u ^ (PERM ? ((line >> 2) & 6) | ((line >> 1) & 1) : (line >> 1) & 7);
     else if constexpr (ES == 2) {
         if constexpr (RB >= 256) return u ^ (((line & 3) | ((line >> 1) & 4)) << 1);
         else if constexpr (RB == 128) return u ^ ((((line >> 1) & 1) | ((line >> 2) & 2)) << 1);
@@ -132,12 +137,12 @@ __device__ __forceinline__ xt_u4 load_some(const char *p, int n)
 // The LDS units of a stage are loaded 64 by a wave instruction: instruction j of the stage, j = wave + NW q.  An address is a
 // base in scalar registers that moves on by stages and 32 bits per lane that stay; WIDE: 64 bits per lane (rows given by an
 // index may lie further apart).  A KS operand with an index has its storage rows read a stage ahead.
-template <int LINES, int ES, bool KS, bool PERM, int NW, bool WIDE>
+template <int LINES, int ES, int KB, bool KS, bool PERM, int NW, bool WIDE>
 struct Staged {
-    static constexpr int BYTES = LINES * 128, LOADS = LINES / 8;             // instructions of a stage, all waves
+    static constexpr int LOADS = LINES * KB / 1024;                           // instructions of a stage, all waves
     static constexpr int Q = (LOADS + NW - 1) / NW;                           // ... of one wave (the last waves may repeat others')
-    static constexpr int RB = KS ? LINES * ES : 128, UR = RB / 16;            // bytes, units of an LDS line
-    static constexpr int BK = 128 / ES, E = 16 / ES;
+    static constexpr int RB = KS ? LINES * ES : KB, UR = RB / 16;             // bytes, units of an LDS line
+    static constexpr int E = 16 / ES;
 
     const char *first;       // storage at the group's first k (KS) or at line 0 (KC)
     const char *base;        // ... at the next stage to load
@@ -160,7 +165,7 @@ struct Staged {
         base = b + (relative && !WIDE ? (int64_t)first_line * pitch_bytes : 0) + (int64_t)k0 * ES;
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-            const int s = slot(q, wave, lane), line = s / 8, u = unit_of<128, false, PERM, ES>(line, s % 8);
+            const int s = slot(q, wave, lane), line = s / UR, u = unit_of<RB, false, PERM, ES>(line, s % UR);
             const int in = first_line + line < n ? first_line + line : n - 1;
             if constexpr (WIDE) p[q] = base + (int64_t)row_of(in) * pitch_bytes + u * 16;
             else off[q] = (uint32_t)(row_of(in) - (relative ? first_line : 0)) * (uint32_t)pitch_bytes + (uint32_t)(u * 16);
@@ -195,28 +200,44 @@ struct Staged {
     // whether some unit of the tile holds lines on both sides of the edge: read whole it ends outside its row
     __device__ __forceinline__ bool cut() const { return KS && line0 + LINES > lines && lines % E != 0; }
 
-    // the whole stage at k0 into `lds`; the next one is `ahead` k further
-    __device__ __forceinline__ void load(uint32_t lds, int k0, int ahead, int wave, int lane)
+    // instruction q of the whole stage that is next, into `lds`
+    template <int q>
+    __device__ __forceinline__ void load(uint32_t lds, int wave)
     {
-        if (KS && index) {
-#pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                const int r = row[KS ? q : 0];
-                const char *const from = base + (int64_t)r * pitch + off[WIDE && !KS ? 0 : q];
-                dma16((unsigned)r < (unsigned)storage_rows ? from : (const char *)&xt_zeros, lds + (uint32_t)((wave + NW * q) % LOADS) * 1024u);
+        const uint32_t to = lds + (uint32_t)((wave + NW * q) % LOADS) * 1024u;
+        if constexpr (KS) {
+            if (index) {
+                const int r = row[q];
+                const char *const from = base + (int64_t)r * pitch + off[q];
+                dma16((unsigned)r < (unsigned)storage_rows ? from : (const char *)&xt_zeros, to);
+                return;
             }
-            read_index(k0 + ahead, wave, lane);
-            return;
         }
+        if constexpr (WIDE && !KS) dma16(p[q], to);
+        else dma16(base, off[q], to);
+    }
+    // on to the stage at k0
+    __device__ __forceinline__ void advance(int k0, int ahead, int wave, int lane)
+    {
+        if (KS && index) { read_index(k0, wave, lane); return; }
+        if constexpr (WIDE && !KS)
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const uint32_t to = lds + (uint32_t)((wave + NW * q) % LOADS) * 1024u;
-            if constexpr (WIDE && !KS) {
-                dma16(p[q], to);
-                p[q] += ahead * ES;
-            } else dma16(base, off[q], to);
+            for (int q = 0; q < Q; ++q) p[q] += ahead * ES;
+        else base += KS ? (int64_t)ahead * pitch : (int64_t)ahead * ES;
+    }
+    // lane `at` of LINES: offset of one of the 128-byte lines that a stage is read from
+    template <class RowOf>
+    __device__ __forceinline__ uint32_t line_of(int at, RowOf row_of, bool relative) const
+    {
+        if constexpr (!KS) {
+            const int in = line0 + at < lines ? line0 + at : lines - 1;
+            return (uint32_t)(row_of(in) - (relative ? line0 : 0)) * (uint32_t)pitch;
+        } else {
+            constexpr int PER = RB / 128 > 0 ? RB / 128 : 1;
+            int c = line0 * ES + at % PER * 128;
+            c = c < lines * ES ? c : 0;
+            return (uint32_t)(at / PER) * (uint32_t)pitch + (uint32_t)c;
         }
-        base += KS ? (int64_t)ahead * pitch : (int64_t)ahead * ES;
     }
     // the stage at k0, of which any part may be there, through registers
     template <class RowOf>
@@ -227,7 +248,7 @@ struct Staged {
             const int s = slot(q, wave, lane);
             xt_u4 v = {0, 0, 0, 0};
             if constexpr (!KS) {
-                const int line = s / 8, at = k0 + unit_of<128, false, PERM, ES>(line, s % 8) * E;
+                const int line = s / UR, at = k0 + unit_of<RB, false, PERM, ES>(line, s % UR) * E;
                 const int in = line0 + line < lines ? line0 + line : lines - 1;
                 if (at < k) v = load_some<ES>(first + (int64_t)row_of(in) * pitch + (int64_t)at * ES, k - at);
             } else {
@@ -250,8 +271,8 @@ __device__ __forceinline__ xt_u4 read_kc(const char *at) { return *(const xt_u4 
 
 template <class T, int LINES, bool KS, bool PERM>
 struct FragReader {
-    static constexpr int ES = T::ES, RB = KS ? LINES * ES : 128, UR = RB / 16;
-    int at;          // KC: byte offset at half 0
+    static constexpr int ES = T::ES, RB = KS ? LINES * ES : T::KB;
+    int at[2];       // KC: byte offset of this lane's unit, of each half (units b and b + 4: the swizzle does not change bit 2)
     int row, part;   // KS: this lane's first row; half unit (16 bits: 8 bytes of four)
     int wave0;       // the wave's first line
     // i: fragment line of the lane, b: k block of the lane
@@ -261,7 +282,8 @@ struct FragReader {
         wave0 = first_line;
         if constexpr (!KS) {
             const int line = first_line + (PERM ? 8 * (i >> 2) + (i & 3) : i);
-            at = line * 128 + unit_of<128, false, PERM, ES>(line, b) * 16;
+            at[0] = line * RB + unit_of<RB, false, PERM, ES>(line, b) * 16;
+            at[1] = at[0] ^ 64;
         } else if constexpr (ES == 2) {
             row = 8 * b + (i >> 2);
             part = i & 3;
@@ -274,9 +296,9 @@ struct FragReader {
     __device__ __forceinline__ xt_u4 read(const char *lds, int f, int h) const
     {
         if constexpr (!KS) {
-            // (units b and b + 4: the swizzle changes neither with the fragment nor in bit 2 with the half)
+            // (nor does it change with the fragment: its lines are a constant further on)
             const int line = PERM ? (f >> 1) * 32 + (f & 1) * 4 : f * 16;
-            return *(const xt_u4 *)(lds + ((at + line * 128) ^ (h * 64)));
+            return *(const xt_u4 *)(lds + at[h] + line * RB);
         } else if constexpr (ES == 2) {
             xt_u4 v;
 #pragma unroll
@@ -442,80 +464,94 @@ __device__ __forceinline__ bool find_row_tile(const ExpertsArgs &a, int tiles_n,
     return true;
 }
 
-// A wave's products of one stage, in steps: 16 bits: halves of the stage's k times halves of the wave's rows; 8 bits: one or two row
-// blocks (an instruction has all 128 k).  While a step's matrix instructions run, the next one's fragments are read.
+// A wave's products of one stage, in steps: 16 bits: each instruction's k times halves of the wave's rows; 8 bits: one or two row
+// blocks (an instruction has all 128 k).  While a step's matrix instructions run, the next one's fragments are read, into
+// the other of two sets of registers.  PAIRS: B's sets change places from stage to stage (P: the stage's parity).
 template <class T>
 struct Steps {
+    static constexpr int KSTEPS = T::FP8 ? 1 : T::KB / 64;
     static constexpr int MA = T::FP8 ? (T::MI > 1 && T::MI < 8 ? 2 : 1) : T::MI > 1 ? T::MI / 2 : 1;   // row blocks of a step
-    static constexpr int STEPS = T::FP8 ? T::MI / MA : T::MI > 1 ? 4 : 2;
+    static constexpr int MSTEPS = T::MI / MA, STEPS = KSTEPS * MSTEPS;
+    static constexpr bool A2 = STEPS % 2 == 0;   // (one step of 8 bits: read when the stage before is done with)
+    static constexpr bool B2 = !T::FP8;          // (8 bits: one set, two would not leave room for the accumulators)
+    static constexpr bool PAIRS = B2 && KSTEPS % 2 != 0;
+    static_assert(A2 || !PAIRS, "a stage of a pair has an even number of steps");
     typedef FragReader<T, T::BM, T::AKS, false> ReadA;
     typedef FragReader<T, T::BN, T::BKS, T::PERM> ReadB;
     static constexpr int U = T::FP8 ? 2 : 1;     // 16-byte halves of a fragment
 
     xt_u4 a[2][MA][U];
-    xt_u4 b[T::FP8 ? 1 : 2][T::NI][U];
+    xt_u4 b[B2 ? 2 : 1][T::NI][U];
     float w[2][MA];                              // fp8: the rows' scales
 
-    static __device__ __forceinline__ constexpr int first_row(int t) { return T::FP8 ? t * MA : (t % (STEPS / 2)) * MA; }
     template <int t>
     __device__ __forceinline__ void read_a(const ReadA &r, const char *la, const float *scales)
     {
+        constexpr int set = t & 1, m0 = t % MSTEPS * MA;
 #pragma unroll
         for (int m = 0; m < MA; ++m) {
+            a[set][m][0] = r.read(la, m0 + m, T::FP8 ? 0 : t / MSTEPS);
             if constexpr (T::FP8) {
-                a[t & 1][m][0] = r.read(la, first_row(t) + m, 0);
-                a[t & 1][m][U - 1] = r.read(la, first_row(t) + m, 1);
-                w[t & 1][m] = scales[(first_row(t) + m) * 16];
-            } else a[t & 1][m][0] = r.read(la, first_row(t) + m, t / (STEPS / 2));
+                a[set][m][U - 1] = r.read(la, m0 + m, 1);
+                w[set][m] = scales[(m0 + m) * 16];
+            }
         }
     }
     // the fragments of B that step t needs and the step before did not
-    template <int t>
+    template <int P, int t>
     __device__ __forceinline__ void read_b(const ReadB &r, const char *lb)
     {
-        if constexpr (T::FP8) {
-            if constexpr (t == 0)
+        constexpr int set = B2 ? (P * KSTEPS + t / MSTEPS) & 1 : 0;
+        if constexpr (t % MSTEPS == 0) {
 #pragma unroll
-                for (int ni = 0; ni < T::NI; ++ni) {
-                    b[0][ni][0] = r.read(lb, ni, 0);
-                    b[0][ni][U - 1] = r.read(lb, ni, 1);
-                }
-        } else if constexpr (t % (STEPS / 2) == 0) {
-#pragma unroll
-            for (int ni = 0; ni < T::NI; ++ni) b[t / (STEPS / 2)][ni][0] = r.read(lb, ni, t / (STEPS / 2));
+            for (int ni = 0; ni < T::NI; ++ni) {
+                b[set][ni][0] = r.read(lb, ni, T::FP8 ? 0 : t / MSTEPS);
+                if constexpr (T::FP8) b[set][ni][U - 1] = r.read(lb, ni, 1);
+            }
         }
     }
-    template <int t>
-    __device__ __forceinline__ void mma(float wb, xt_f4 (&acc)[T::MI][T::NI])
+    // `hook` is called after every instruction
+    template <int P, int t, class Hook>
+    __device__ __forceinline__ void mma(float wb, xt_f4 (&acc)[T::MI][T::NI], Hook hook)
     {
+        constexpr int sa = t & 1, sb = B2 ? (P * KSTEPS + t / MSTEPS) & 1 : 0;
 #pragma unroll
         for (int m = 0; m < MA; ++m)
 #pragma unroll
             for (int ni = 0; ni < T::NI; ++ni) {
-                xt_f4 &c = acc[first_row(t) + m][ni];
-                if constexpr (!T::FP8) c = mma16<T::ELEM>(b[t / (STEPS / 2)][ni][0], a[t & 1][m][0], c);
+                xt_f4 &c = acc[t % MSTEPS * MA + m][ni];
+                const xt_u4 *p = a[sa][m], *q = b[sb][ni];
+                if constexpr (!T::FP8) c = mma16<T::ELEM>(q[0], p[0], c);
                 else {
                     const xt_f4 zero = {0, 0, 0, 0};
                     xt_f4 x;
                     if constexpr (T::ELEM == EXPERTS_FP8) {
-                        const xt_u4 *p = a[t & 1][m], *q = b[0][ni];
                         const xt_i8 xa = {(int)p[0][0], (int)p[0][1], (int)p[0][2], (int)p[0][3], (int)p[U - 1][0], (int)p[U - 1][1], (int)p[U - 1][2], (int)p[U - 1][3]};
                         const xt_i8 xb = {(int)q[0][0], (int)q[0][1], (int)q[0][2], (int)q[0][3], (int)q[U - 1][0], (int)q[U - 1][1], (int)q[U - 1][2], (int)q[U - 1][3]};
                         x = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(xb, xa, zero, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
                     } else {
                         x = zero;
 #pragma unroll
-                        for (int u = 0; u < 4; ++u)
-                            x = mma16<EXPERTS_BF16>(bf16_of(b[0][ni][u / 2], u % 2), bf16_of(a[t & 1][m][u / 2], u % 2), x);
+                        for (int u = 0; u < 4; ++u) x = mma16<EXPERTS_BF16>(bf16_of(q[u / 2], u % 2), bf16_of(p[u / 2], u % 2), x);
                     }
-                    const float f = w[t & 1][m] * wb;
+                    const float f = w[sa][m] * wb;
 #pragma unroll
                     for (int v = 0; v < 4; ++v) c[v] = __builtin_fmaf(f, x[v], c[v]);
                 }
+                hook(m * T::NI + ni);
             }
     }
 };
 
+// f(0), f(1), ... f(N - 1), the numbers known when compiled
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void for_each(F f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        for_each<N, I + 1>(f);
+    }
+}
 // A constant wait: at most N of this wave's vector memory operations under way.
 template <int N>
 __device__ __forceinline__ void wait_vm()
@@ -547,12 +583,12 @@ struct TileScales {
 // step, when every wave has read all of it: behind it the slot is refilled with the stage S further on, and the first fragments of the
 // next stage are read, which the same barrier certifies as landed.  What is left is loaded through registers, one stage at a time.
 template <class T, class ARow>
-__device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::AKS, false, T::NW, T::WIDE> &sa, Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW, false> &sb,
-                                          const int k0, const int k1, const int wave, const int kg, const int lane, ARow a_row, const TileScales &scales, xt_f4 (&acc)[T::MI][T::NI])
+__device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, false, T::NW, T::WIDE> &sa, Staged<T::BN, T::ES, T::KB, T::BKS, T::PERM, T::NW, false> &sb,
+                                          const int k0, const int k1, const int wave, const int kg, const int lane, ARow a_row, bool rel, const TileScales &scales, xt_f4 (&acc)[T::MI][T::NI])
 {
     constexpr int S = T::S, BK = T::BK, STEPS = Steps<T>::STEPS;
-    constexpr int LOADS = Staged<T::BM, T::ES, T::AKS, false, T::NW, T::WIDE>::Q + Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW, false>::Q + (T::FP8 ? 1 : 0);
-    static_assert(LOADS * (S - 2) <= 63, "the wait count is a 6-bit field");
+    constexpr int LOADS = Staged<T::BM, T::ES, T::KB, T::AKS, false, T::NW, T::WIDE>::Q + Staged<T::BN, T::ES, T::KB, T::BKS, T::PERM, T::NW, false>::Q + (T::FP8 ? 1 : 0) + (T::PREFETCH ? 1 : 0);
+    static_assert(S <= 5 && LOADS * (S - 1) <= 63, "the wait count is a 6-bit field");
     const int wm = wave / T::WN, wn = wave % T::WN;
     char *const ring = xt_smem + kg * (S * T::STAGE);
     const uint32_t ring_at = (uint32_t)(uintptr_t)(xt_lds_void)ring;
@@ -573,82 +609,127 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::AKS, false, T:
     const bool a_cut = sa.cut(), b_cut = sb.cut();
     if (whole == stages && whole > 0 && (a_cut || b_cut)) --whole;
     if ((a_cut && sa.index) || (b_cut && sb.index)) whole = 0;   // (any k may name the storage's last row)
+    if (Steps<T>::PAIRS) whole &= ~1;
     const int mine = whole > kg ? (whole - kg + T::WK - 1) / T::WK : 0;   // ... this group's
     auto request_scales = [&](int s, int slot) {
         // (64 rows a wave; the last waves repeat others')
         dma4(scales.a + (int64_t)s * scales.a_step, scales.a_off, ring_at + (uint32_t)(slot * T::STAGE + T::A_BYTES + T::B_BYTES + (wave * 64 % (T::BM < 64 ? 64 : T::BM)) * 4));
     };
-    auto request = [&](int r, int slot) {
-        const int s = r * T::WK + kg;
+    uint32_t pre = 0;
+    if (T::PREFETCH > 0 && mine > 0) {   // (a region without a group has no operands)
+        const int at = (wave % (T::NW / 2)) * 64 + lane;
+        pre = wave < T::NW / 2 ? (sa.index ? 0 : sa.line_of(at, a_row, rel)) : (sb.index ? 0 : sb.line_of(at, [](int i) { return i; }, true));
+    }
+    typedef Staged<T::BM, T::ES, T::KB, T::AKS, false, T::NW, T::WIDE> StagedA;
+    typedef Staged<T::BN, T::ES, T::KB, T::BKS, T::PERM, T::NW, false> StagedB;
+    // instruction q of the request for this group's stage r
+    auto request_one = [&](auto which, int r, int slot) {
+        constexpr int q = decltype(which)::value;
         const uint32_t to = ring_at + (uint32_t)(slot * T::STAGE);
-        sa.load(to, k0 + s * BK, BK * T::WK, wave, lane);
-        sb.load(to + T::A_BYTES, k0 + s * BK, BK * T::WK, wave, lane);
-        if constexpr (T::FP8) request_scales(s, slot);
+        if constexpr (q < StagedA::Q) sa.template load<q>(to, wave);
+        else if constexpr (q < StagedA::Q + StagedB::Q) sb.template load<q - StagedA::Q>(to + T::A_BYTES, wave);
+        if constexpr (q == StagedA::Q + StagedB::Q - 1) {
+            const int s = r * T::WK + kg;
+            const int ahead = !T::ALWAYS || s + 1 < whole ? BK * T::WK : 0;
+            sa.advance(k0 + s * BK + ahead, ahead, wave, lane);
+            sb.advance(k0 + s * BK + ahead, ahead, wave, lane);
+            if constexpr (T::FP8) request_scales(!T::ALWAYS || s < whole ? s : whole - 1, slot);
+            if constexpr (T::PREFETCH > 0) {
+                const int on = s + T::PREFETCH < whole ? T::PREFETCH * BK - ahead : 0;
+                const bool b = wave >= T::NW / 2;
+                // (rows named by an index are not known yet: the storage's first row stands for them)
+                const char *const from = b ? sb.base + (sb.index ? 0 : T::BKS ? on * sb.pitch : (int64_t)on * T::ES)
+                                           : sa.base + (sa.index ? 0 : T::AKS ? on * sa.pitch : (int64_t)on * T::ES);
+                dma4(from, pre, ring_at + S * T::STAGE);
+            }
+        }
     };
+    auto request = [&](int r, int slot) { for_each<StagedA::Q + StagedB::Q>([&](auto q) { request_one(q, r, slot); }); };
     auto scale_row = [&](const char *la) { return (const float *)(la + T::A_BYTES + T::B_BYTES) + wm * (T::BM / T::WM) + (lane & 15); };
     auto scale_b = [&](int s) { return T::FP8 ? scales.b[(int64_t)s * scales.b_step] : 0.0f; };
-    // One stage at `la`, its first fragments read.  AFTER (another stage's address or null, known when compiled: a branch between
-    // the steps would have the compiler gather the matrix instructions behind it): read its first fragments before the last
-    // step, once `next` has seen to it that they are there.
-    auto stage = [&](const char *la, float wb, const char *after, auto there, auto next) {
+    // One stage at `la`, its first fragments read.  AFTER: read those of the stage at `after` before the last step, once `next`
+    // has seen to it that they are there (known when compiled: a branch between the steps would have the compiler gather
+    // the matrix instructions behind it).
+    auto stage = [&](auto parity, const char *la, float wb, const char *after, auto there, auto next, auto hook) {
         constexpr bool AFTER = decltype(there)::value;
+        constexpr int P = decltype(parity)::value, P2 = Steps<T>::PAIRS ? 1 - P : 0;
         const char *const lb = la + T::A_BYTES;
 #define AMULET_STEP(t)                                                          \
         if constexpr (t < STEPS) {                                              \
             if constexpr (t + 1 < STEPS) {                                      \
                 f.template read_a<t + 1>(ra, la, scale_row(la));                \
-                f.template read_b<t + 1>(rb, lb);                               \
+                f.template read_b<P, t + 1>(rb, lb);                            \
             } else if constexpr (AFTER) {                                       \
                 next();                                                         \
-                if constexpr (STEPS > 1) f.template read_a<0>(ra, after, scale_row(after)); \
-                if constexpr (!T::FP8) f.template read_b<0>(rb, after + T::A_BYTES); \
+                if constexpr (Steps<T>::A2) f.template read_a<0>(ra, after, scale_row(after)); \
+                if constexpr (Steps<T>::B2) f.template read_b<P2, 0>(rb, after + T::A_BYTES); \
             }                                                                   \
-            f.template mma<t>(wb, acc);                                         \
+            f.template mma<P, t>(wb, acc, [&](int i) { hook(std::integral_constant<int, t>(), i); }); \
             if constexpr (T::FP8) __builtin_amdgcn_sched_barrier(0);            \
         }
         AMULET_STEP(0) AMULET_STEP(1) AMULET_STEP(2) AMULET_STEP(3) AMULET_STEP(4) AMULET_STEP(5) AMULET_STEP(6) AMULET_STEP(7)
 #undef AMULET_STEP
-        if constexpr (AFTER) {
-            if constexpr (STEPS == 1) f.template read_a<0>(ra, after, scale_row(after));
-            if constexpr (T::FP8) f.template read_b<0>(rb, after + T::A_BYTES);
-        }
+        if constexpr (AFTER && !Steps<T>::A2) f.template read_a<0>(ra, after, scale_row(after));
+        if constexpr (AFTER && !Steps<T>::B2) f.template read_b<P2, 0>(rb, after + T::A_BYTES);
     };
+    constexpr std::integral_constant<int, 0> even;
+    constexpr std::integral_constant<int, Steps<T>::PAIRS ? 1 : 0> odd;
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    constexpr auto none = [](auto, int) {};
 
     if (mine > 0) {
-        int slot = 0;
-#pragma unroll
-        for (int r = 0; r < S; ++r)
-            if (r < mine) request(r, r);
-        if (mine >= S) wait_vm<LOADS * (S - 1)>();
-        else wait_vm<0>();
-        meet<T::NW>();
-        f.template read_a<0>(ra, ring, scale_row(ring));
-        f.template read_b<0>(rb, ring + T::A_BYTES);
+        int slot = 0, r = 0;
         float wb = scale_b(kg);
-        int r = 0;
-        for (; r + S < mine; ++r) {
+        auto first = [&]() {
+            meet<T::NW>();
+            f.template read_a<0>(ra, ring, scale_row(ring));
+            f.template read_b<0, 0>(rb, ring + T::A_BYTES);
+        };
+        // stage r; `wait`: until stage r + 1 has landed; more: request the one S further on into this one's slot
+        auto go = [&](auto parity, auto more, auto wait) {
             const int here = slot;
             slot = slot + 1 == S ? 0 : slot + 1;
             const float now = wb;
             wb = scale_b((r + 1) * T::WK + kg);
-            stage(ring + here * T::STAGE, now, ring + slot * T::STAGE, std::true_type(), [&]() {
-                wait_vm<LOADS * (S - 2)>();   // stage r + 1 has landed: only the S - 2 behind it may be under way
+            stage(parity, ring + here * T::STAGE, now, ring + slot * T::STAGE, yes, [&]() {
+                wait();
                 meet<T::NW>();
-                request(r + S, here);
+                if constexpr (decltype(more)::value && T::SPREAD == 0) request(r + S, here);
+            }, [&](auto t, int i) {
+                if constexpr (decltype(more)::value && T::SPREAD > 0 && decltype(t)::value == STEPS - 1)
+                    for_each<StagedA::Q + StagedB::Q>([&](auto q) { if (i == decltype(q)::value * T::SPREAD) request_one(q, r + S, here); });
             });
+            ++r;
+        };
+        auto all_but = []() { wait_vm<LOADS * (S - 2) + (T::PREFETCH ? 1 : 0)>(); };   // only the S - 2 stages behind the next may be under way
+        if constexpr (T::ALWAYS) {
+            // There is always a request, past the end for the last stage once more (nobody reads it there): every wait is the
+            // same, and one loop does for all stages but the last (of pairs: two).
+            for (int q = 0; q < S; ++q) request(q, q);
+            wait_vm<LOADS * (S - 1)>();
+            first();
+            if constexpr (Steps<T>::PAIRS) {
+                while (r + 2 < mine) { go(even, yes, all_but); go(odd, yes, all_but); }
+                go(even, no, all_but);
+                stage(odd, ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
+            } else {
+                while (r + 1 < mine) go(even, yes, all_but);
+                stage(even, ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < S; ++q)
+                if (q < mine) request(q, q);
+            if (mine >= S) wait_vm<LOADS * (S - 1)>();
+            else wait_vm<0>();
+            first();
+            while (r + S < mine) go(even, yes, all_but);
+            while (r + 1 < mine) go(even, no, []() { wait_vm<0>(); });
+            stage(even, ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
         }
-        for (; r + 1 < mine; ++r) {
-            const int here = slot;
-            slot = slot + 1 == S ? 0 : slot + 1;
-            const float now = wb;
-            wb = scale_b((r + 1) * T::WK + kg);
-            stage(ring + here * T::STAGE, now, ring + slot * T::STAGE, std::true_type(), [&]() {
-                wait_vm<0>();
-                meet<T::NW>();
-            });
-        }
-        stage(ring + slot * T::STAGE, wb, nullptr, std::false_type(), []() {});
     }
+    if constexpr (T::ALWAYS) wait_vm<0>();   // (the requests past the end: nothing is under way when the workgroup ends)
     // stages that are not whole
     for (int s = whole; s < stages; ++s) {
         if (T::WK > 1 && s % T::WK != kg) continue;
@@ -658,8 +739,8 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::AKS, false, T:
         if constexpr (T::FP8) { request_scales(s, 0); wait_vm<0>(); }
         meet<T::NW>();
         f.template read_a<0>(ra, ring, scale_row(ring));
-        f.template read_b<0>(rb, ring + T::A_BYTES);
-        stage(ring, scale_b(s), nullptr, std::false_type(), []() {});
+        f.template read_b<0, 0>(rb, ring + T::A_BYTES);
+        stage(even, ring, scale_b(s), nullptr, no, []() {}, none);
     }
     if constexpr (T::WK > 1) {
         // the k groups' sums, added up by the first in order (so the result does not depend on who came first)
@@ -712,8 +793,8 @@ __global__ void __launch_bounds__(T::NT) experts_rows_kernel(const ExpertsArgs a
         return (unsigned)r < (unsigned)a.a_rows ? r : 0;
     };
     const int K = t.group < 0 ? 0 : a.K;
-    Staged<T::BM, T::ES, T::AKS, false, T::NW, T::WIDE> sa = {};
-    Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW, false> sb = {};
+    Staged<T::BM, T::ES, T::KB, T::AKS, false, T::NW, T::WIDE> sa = {};
+    Staged<T::BN, T::ES, T::KB, T::BKS, T::PERM, T::NW, false> sb = {};
     const char *const B = (const char *)a.B + (int64_t)(t.group < 0 ? 0 : t.group) * a.group_b * T::ES;
     if (K > 0) {
         sa.start_kc((const char *)a.A, a.lda * T::ES, row0, t.row1, K, kg * T::BK, wave, lane, a_row, !a.rows);
@@ -731,7 +812,7 @@ __global__ void __launch_bounds__(T::NT) experts_rows_kernel(const ExpertsArgs a
         scales.b = a.scale_b + (int64_t)(t.group < 0 ? 0 : t.group) * a.group_sb + (T::BKS ? at : at * a.ld_sb);
         scales.b_step = T::BKS ? a.ld_sb : 1;
     }
-    if (!tile_sums<T>(sa, sb, 0, K, wave, kg, lane, a_row, scales, acc)) return;
+    if (!tile_sums<T>(sa, sb, 0, K, wave, kg, lane, a_row, !a.rows, scales, acc)) return;
 
 #pragma unroll
     for (int mi = 0; mi < T::MI; ++mi) {
@@ -780,14 +861,14 @@ __global__ void __launch_bounds__(T::NT) experts_sums_kernel(const ExpertsArgs a
     const int64_t k0 = (int64_t)part * chunk;
     const int from = k0 < k_all ? (int)k0 : k_all, to = k0 + chunk < k_all ? (int)(k0 + chunk) : k_all;
 
-    Staged<T::BM, T::ES, T::AKS, false, T::NW, T::WIDE> sa;
-    Staged<T::BN, T::ES, T::BKS, T::PERM, T::NW, false> sb;
+    Staged<T::BM, T::ES, T::KB, T::AKS, false, T::NW, T::WIDE> sa;
+    Staged<T::BN, T::ES, T::KB, T::BKS, T::PERM, T::NW, false> sb;
     const char *const A = (const char *)a.A, *const B = (const char *)a.B;
     const int32_t *const ia = a.rows_of_b ? nullptr : a.rows, *const ib = a.rows_of_b ? a.rows : nullptr;
     sa.start_ks(ia ? A : A + (int64_t)lo * a.lda * T::ES, a.lda * T::ES, ia ? ia + lo : nullptr, a.a_rows, m0, a.M, to, from + kg * T::BK, wave, lane);
     sb.start_ks(ib ? B : B + (int64_t)lo * a.ldb * T::ES, a.ldb * T::ES, ib ? ib + lo : nullptr, a.a_rows, n0, a.N, to, from + kg * T::BK, wave, lane);
     xt_f4 acc[T::MI][T::NI];
-    if (!tile_sums<T>(sa, sb, from, to, wave, kg, lane, [](int i) { return i; }, TileScales(), acc)) return;
+    if (!tile_sums<T>(sa, sb, from, to, wave, kg, lane, [](int i) { return i; }, true, TileScales(), acc)) return;
 
     const int wm = wave / T::WN, wn = wave % T::WN;
     if (a.parts > 1) {
