@@ -702,6 +702,11 @@ def amulet_route(logits, experts, weights, place, tokens, offsets, workspace=Non
     """The k experts with the highest logits of every token, their weights, and the rows of all (token, expert) pairs
     in order of expert.  logits: T x E (fp32, bf16, fp16; -inf masks).  Written: experts, place (T x k int32), weights
     (T x k fp32: over the chosen with norm, else over all), tokens (T * k int32), offsets (E + 1 int32)."""
+    if _marshal is not None:
+        rc = _marshal.route(logits, experts, weights, place, tokens, offsets, workspace, norm, stream)
+        if rc is not None:
+            _check(rc, "amulet_route")
+            return
     lib = load_library()
     kind, px, T, E, ldx = _typed(logits, "logits")
     if experts.dim() != 2 or experts.shape[0] != T:
@@ -717,6 +722,11 @@ def amulet_route(logits, experts, weights, place, tokens, offsets, workspace=Non
 def amulet_route_grad(logits, experts, weights, dweights, dlogits, *, norm: bool = True, stream=None):
     """dlogits (T x E, written) from the weights' gradients; experts and weights as amulet_route wrote them.  logits is
     read without norm only (None will do with it)."""
+    if _marshal is not None:
+        rc = _marshal.route_grad(logits, experts, weights, dweights, dlogits, norm, stream)
+        if rc is not None:
+            _check(rc, "amulet_route_grad")
+            return
     lib = load_library()
     kind, pd, T, E, ldd = _typed(dlogits, "dlogits")
     if experts.dim() != 2 or experts.shape[0] != T:
@@ -734,6 +744,11 @@ def amulet_route_grad(logits, experts, weights, dweights, dlogits, *, norm: bool
 
 def amulet_combine(Y, weights, place, R, *, stream=None):
     """R[t] = sum_j weights[t, j] Y[place[t, j]]; a place outside Y adds nothing; weights None: ones."""
+    if _marshal is not None:
+        rc = _marshal.combine(Y, weights, place, R, stream)
+        if rc is not None:
+            _check(rc, "amulet_combine")
+            return
     lib = load_library()
     kind, pr, T, H, ldr = _typed(R, "R")
     py, rows, H2, ldy = _mat(Y, R.dtype, "Y")
@@ -748,6 +763,11 @@ def amulet_combine(Y, weights, place, R, *, stream=None):
 def amulet_combine_grad(Y, weights, place, dR, dY, dweights=None, *, stream=None):
     """dY[place[t, j]] = weights[t, j] dR[t] (rows of dY that no pair names stay as they are), and dweights[t, j] =
     <dR[t], Y[place[t, j]]> where dweights is given (else Y may be None)."""
+    if _marshal is not None:
+        rc = _marshal.combine_grad(Y, weights, place, dR, dY, dweights, stream)
+        if rc is not None:
+            _check(rc, "amulet_combine_grad")
+            return
     lib = load_library()
     kind, pd, T, H, ldd = _typed(dR, "dR")
     pdy, rows, H2, lddy = _mat(dY, dR.dtype, "dY")
@@ -772,6 +792,11 @@ def _rows_of(rows, M):
 def amulet_grouped_mm(A, B, offsets, R, *, rows=None, trans_b: bool = False, stream=None):
     """R[i] = A[i] B[g] for the rows i of group g, offsets[g] <= i < offsets[g + 1] (A[rows[i]] where rows is given); rows of
     no group are 0.  A bf16 or fp16; B G x K x N, or G x N x K with trans_b; R of A's type or fp32."""
+    if _marshal is not None:
+        rc = _marshal.grouped_mm(A, B, offsets, R, rows, trans_b, stream)
+        if rc is not None:
+            _check(rc, "amulet_grouped_mm")
+            return
     lib = load_library()
     kind, pa, Ra, K, lda = _typed(A, "A")
     pb, G, b0, b1, ldb, gb = _groups(B, A.dtype, "B")
@@ -790,6 +815,11 @@ def amulet_grouped_mm_wgrad_workspace_bytes(M: int, N: int, K: int, G: int) -> i
 def amulet_grouped_mm_wgrad(A, D, offsets, R, workspace=None, *, rows=None, trans_r: bool = False, stream=None):
     """R[g] = sum over the rows i of group g of A[i]^T D[i] (A[rows[i]] where rows is given): G x K x N, or G x N x K with
     trans_r; 0 for a group without rows.  A, D bf16 or fp16; R of their type or fp32."""
+    if _marshal is not None:
+        rc = _marshal.grouped_mm_wgrad(A, D, offsets, R, workspace, rows, trans_r, stream)
+        if rc is not None:
+            _check(rc, "amulet_grouped_mm_wgrad")
+            return
     lib = load_library()
     kind, pa, Ra, K, lda = _typed(A, "A")
     pd, M, N, ldd = _mat(D, A.dtype, "D")
@@ -806,6 +836,11 @@ def amulet_grouped_mm_wgrad(A, D, offsets, R, workspace=None, *, rows=None, tran
 
 def amulet_quantize_fp8(X, Q, scales, *, stream=None):
     """e4m3 values Q of X (M x K; fp32, bf16, fp16), one scale to 128 values of a row: scales[k // 128, i], ceil(K / 128) x M."""
+    if _marshal is not None:
+        rc = _marshal.quantize_fp8(X, Q, scales, stream)
+        if rc is not None:
+            _check(rc, "amulet_quantize_fp8")
+            return
     lib = load_library()
     kind, px, M, K, ldx = _typed(X, "X")
     pq, M2, K2, ldq = _mat(Q, _torch.float8_e4m3fn, "Q")
@@ -817,6 +852,11 @@ def amulet_quantize_fp8(X, Q, scales, *, stream=None):
 
 def amulet_quantize_fp8_blocks(X, Q, scales, *, stream=None):
     """e4m3 values Q of X (G x M x K; fp32, bf16, fp16), one scale to 128 x 128: scales[g, i // 128, k // 128]."""
+    if _marshal is not None:
+        rc = _marshal.quantize_fp8_blocks(X, Q, scales, stream)
+        if rc is not None:
+            _check(rc, "amulet_quantize_fp8_blocks")
+            return
     lib = load_library()
     if X.dtype not in _types:
         raise ValueError("X must be fp32, bf16 or fp16")
@@ -832,6 +872,11 @@ def amulet_quantize_fp8_blocks(X, Q, scales, *, stream=None):
 def amulet_grouped_mm_fp8(A, scales_a, B, scales_b, offsets, R, *, rows=None, trans_b: bool = False, stream=None):
     """amulet_grouped_mm of e4m3 operands: scales_a ceil(K / 128) x rows of A (amulet_quantize_fp8), scales_b one to 128 x 128
     of B as it is stored (amulet_quantize_fp8_blocks).  R fp32, bf16 or fp16."""
+    if _marshal is not None:
+        rc = _marshal.grouped_mm_fp8(A, scales_a, B, scales_b, offsets, R, rows, trans_b, stream)
+        if rc is not None:
+            _check(rc, "amulet_grouped_mm_fp8")
+            return
     lib = load_library()
     f8 = _torch.float8_e4m3fn
     pa, Ra, K, lda = _mat(A, f8, "A")
@@ -843,13 +888,18 @@ def amulet_grouped_mm_fp8(A, scales_a, B, scales_b, offsets, R, *, rows=None, tr
         raise ValueError("shape mismatch between A, B and R")
     if (KB, Rs) != ((K + 127) // 128, Ra) or (G2, s0, s1) != (G, (b0 + 127) // 128, (b1 + 127) // 128):
         raise ValueError("shape mismatch between operands and scales")
-    _check(lib.amulet_grouped_mm_fp8(out, int(trans_b), M, N, K, G, pa, lda, psa, lsa if KB > 1 else Ra, _rows_of(rows, M), Ra,
+    _check(lib.amulet_grouped_mm_fp8(out, int(trans_b), M, N, K, G, pa, lda, psa, lsa, _rows_of(rows, M), Ra,
                                      pb, ldb, gb, psb, lsb, gsb, _vec(offsets, _torch.int32, G + 1, "offsets"), pr, ldr,
                                      _stream_ptr(stream)), "amulet_grouped_mm_fp8")
 
 
 def amulet_mm_fp8(A, scales_a, B, scales_b, R, *, trans_b: bool = False, stream=None):
     """amulet_grouped_mm_fp8 with one matrix B (K x N, or N x K with trans_b) for all rows."""
+    if _marshal is not None:
+        rc = _marshal.mm_fp8(A, scales_a, B, scales_b, R, trans_b, stream)
+        if rc is not None:
+            _check(rc, "amulet_mm_fp8")
+            return
     lib = load_library()
     f8, f32 = _torch.float8_e4m3fn, _torch.float32
     pa, M, K, lda = _mat(A, f8, "A")

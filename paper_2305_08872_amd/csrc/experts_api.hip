@@ -17,16 +17,47 @@ static const int64_t kMostPitch = 0xffffffffLL / 256 - 65536;
 static bool known16(int type) { return type == AMULET_BF16 || type == AMULET_FP16; }
 static bool known(int type) { return type == AMULET_FP32 || known16(type); }
 
-// Tiles by rows.  A tile's rows follow the average group's: rows past a group's end are work for nothing, and a tile
-// of fewer rows reads the group's matrix more often.
-static int rows_tile(int64_t M, int64_t N, int64_t G)
+// Tiles by rows: the one with the lowest estimate.  A workgroup that has its unit alone takes `stage` us for a stage of its k
+// (64 of 16 bits, 128 of 8), of which larger tiles have less per product, and `start` for finding its tile, filling its ring and
+// storing; all workgroups together take no more from the L2s than some 64 KB a us and unit, of which smaller tiles
+// need more; under both lies what memory takes for the operands.  The numbers are fitted to 230 drawn sizes (4 ... 32768 rows, widths
+// of 64 to 4096, 1 ... 128 groups, 16 and 8 bits, both layouts): 1.6 % behind the fastest on average, 25 % at most.  us,
+// 256 x 256 / 128 x 128 / 64 x 128 / 64 x 64 / 64 x 64 with two k groups / 16 x 32, bf16, B stored N x K: 256 x 4096 x 4096
+// 85 / 46 / 28 / 22 / 18 / 38, 64 x 512 x 4096 58 / 42 / 25 / 19 / 14 / 8, 1024 x 4096 x 1024 over 8 groups 26 / 19 / 18 / 19 / 29 / 60, 8192 x 1024 x 1024
+// over 8 32 / 26 / 28 / 37 / - / 121; 4096 x 4096 x 1024 over 4 of 8 bits 30 / 33 / 40 / 46 / 83 / 216.
+// (Tiles of 16 x 64 and 32 x 64 that were tried gained 0.1 % on average and are not built.)
+struct TileCost {
+    double stage16, stage8, start;   // us
+    int resident;                    // workgroups that a unit's LDS holds
+};
+static const TileCost kTileCosts[EXPERTS_TILES] = {{1.22, 1.21, 7.9, 1}, {0.67, 0.75, 2.6, 2}, {0.37, 0.86, 2.6, 2}, {0.30, 0.50, 1.8, 3}, {0.25, 0.39, 3.8, 1}, {0.10, 0.14, 3.7, 2}};
+static double tile_us(int tile, int64_t M, int64_t N, int64_t K, int64_t G, int es, bool b_across)
 {
-    const int64_t per = (M + G - 1) / G;
-    if (per <= 16) return N >= 8192 ? EXPERTS_16x64 : EXPERTS_16x32;
-    if (per <= 32) return EXPERTS_32x64;
-    if (per <= 64) return EXPERTS_64x128;
-    const int64_t tiles = (M / 256 + G) * ((N + 255) / 256);
-    return per >= 192 && tiles >= compute_units() ? EXPERTS_256x256 : EXPERTS_128x128;
+    const double units = compute_units(), bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
+    const double busy = (double)(G < M ? G : M), per = (double)M / busy;
+    // row tiles: a group's last one is half full on average
+    const double rows = per <= bm ? busy : G > 1 ? (double)M / bm + 0.5 * busy : (double)((M + (int64_t)bm - 1) / (int64_t)bm);
+    const double groups = rows * (double)((N + (int64_t)bn - 1) / (int64_t)bn), stages = (double)((K * es + 127) / 128);
+    const TileCost &c = kTileCosts[tile];
+    const double round = units * c.resident;
+    const double rounds = groups <= round ? 1.0 : groups / round;   // (units take their next tile as they finish)
+    const double alone = rounds * (stages * (es == 1 ? c.stage8 : c.stage16) + c.start);
+    // (a line of 64 bytes of B across k: two requests for what one brings)
+    const double bytes = bm + bn * (b_across && bn * es < 128 ? 2.1 : 1.0);
+    const double supply = groups / units * stages * bytes * 0.128 / 64.0;
+    const double memory = (busy * (double)N * (double)K + (double)M * (double)K) * es / 4.3e6;
+    const double most = alone > supply ? alone : supply;
+    return (most > memory ? most : memory) + 0.03 * (alone + supply);
+}
+static int rows_tile(int64_t M, int64_t N, int64_t K, int64_t G, int es, bool b_across, bool largest)
+{
+    int best = EXPERTS_TILES - 1;
+    double least = tile_us(best, M, N, K, G, es, b_across);
+    for (int tile = EXPERTS_TILES - 2; tile >= (largest ? 0 : 1); --tile) {
+        const double us = tile_us(tile, M, N, K, G, es, b_across);
+        if (us < least) { least = us; best = tile; }
+    }
+    return best;
 }
 // Workgroups that are enough for any offsets: a group's last tile may hold one row only, and the rows outside the groups
 // are two regions more.
@@ -55,11 +86,10 @@ static int check_rows(int64_t M, int64_t N, int64_t K, int64_t G, int trans_b, c
 
 static int run_rows(const char *const *names, int type, int trans_b, ExpertsArgs &a, int64_t M, int64_t N, int64_t G, void *stream)
 {
-    int tile = rows_tile(M, N, G < 1 ? 1 : G);
-    // 8-bit operands whose results keep 32 bits have no 256 x 256 tile, and that tile's offsets have 32 bits
-    const int64_t es = type == EXPERTS_BF16 || type == EXPERTS_FP16 ? 2 : 1;
+    // 8-bit operands whose results keep 32 bits have no 256 x 256 tile, and that tile's offsets of A's rows have 32 bits
+    const int es = type == EXPERTS_BF16 || type == EXPERTS_FP16 ? 2 : 1;
     const bool near = (a.rows ? (int64_t)a.a_rows : 256) <= 0xffffffffLL / es / (a.lda > 0 ? a.lda : 1);
-    if (tile == EXPERTS_256x256 && (type == EXPERTS_FP8_EXACT || !near)) tile = EXPERTS_128x128;
+    const int tile = rows_tile(M, N, a.K, G < 1 ? 1 : G, es, !trans_b, type != EXPERTS_FP8_EXACT && near);
     const int64_t blocks = rows_blocks(tile, M, N, G, a.offsets != nullptr);
     if (blocks > kMostBlocks) return AMULET_ERR_RANGE;
     note_kernel(names[tile], M);
@@ -72,8 +102,10 @@ static int run_rows(const char *const *names, int type, int trans_b, ExpertsArgs
     }
 }
 
-static const char *const kRowsNames[EXPERTS_TILES] = {"grouped_mm_256x256", "grouped_mm_128x128", "grouped_mm_64x128", "grouped_mm_32x64", "grouped_mm_16x64", "grouped_mm_16x32"};
-static const char *const kFp8Names[EXPERTS_TILES] = {"mm_fp8_256x256", "mm_fp8_128x128", "mm_fp8_64x128", "mm_fp8_32x64", "mm_fp8_16x64", "mm_fp8_16x32"};
+static const char *const kRowsNames[EXPERTS_TILES] = {"grouped_mm_256x256", "grouped_mm_128x128", "grouped_mm_64x128", "grouped_mm_64x64",
+                                                      "grouped_mm_64x64_k2", "grouped_mm_16x32"};
+static const char *const kFp8Names[EXPERTS_TILES] = {"mm_fp8_256x256", "mm_fp8_128x128", "mm_fp8_64x128", "mm_fp8_64x64",
+                                                     "mm_fp8_64x64_k2", "mm_fp8_16x32"};
 
 // The weights' gradients: tiles, and the parts that a group's rows are summed in.  A part is a workgroup of its own that
 // writes its fp32 sums to the workspace, so there are only as many as bring the workgroups to two per compute unit, of at

@@ -31,9 +31,9 @@ struct ExpertsArgs {
     int out;                         // type of R
 };
 
-// tiles of R by rows (experts_mm_*.hip): rows x columns
-enum { EXPERTS_256x256 = 0, EXPERTS_128x128 = 1, EXPERTS_64x128 = 2, EXPERTS_32x64 = 3, EXPERTS_16x64 = 4, EXPERTS_16x32 = 5, EXPERTS_TILES = 6 };
-constexpr int kExpertsTileRows[EXPERTS_TILES] = {256, 128, 64, 32, 16, 16};
+// tiles of R by rows (experts_mm_*.hip): rows x columns; _K2: two groups of waves share a tile's k
+enum { EXPERTS_256x256 = 0, EXPERTS_128x128 = 1, EXPERTS_64x128 = 2, EXPERTS_64x64 = 3, EXPERTS_64x64_K2 = 4, EXPERTS_16x32 = 5, EXPERTS_TILES = 6 };
+constexpr int kExpertsTileRows[EXPERTS_TILES] = {256, 128, 64, 64, 64, 16};
 constexpr int kExpertsTileCols[EXPERTS_TILES] = {256, 128, 128, 64, 64, 32};
 
 // `blocks` workgroups of tile shape `tile`; b_across: B's storage has k across its rows (K x N), else N x K

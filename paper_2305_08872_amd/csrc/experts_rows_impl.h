@@ -21,8 +21,8 @@ inline hipError_t launch_experts_layout(int tile, const ExpertsArgs &a, int64_t 
         else return launch_experts_tile<ExpertTile<ELEM, 256, 256, 2, 4, 1, 2, 128, false, BKS>>(a, blocks, s);
     case EXPERTS_128x128: return launch_experts_tile<ExpertTile<ELEM, 128, 128, 2, 2, 1, 2, 128, false, BKS>>(a, blocks, s);
     case EXPERTS_64x128: return launch_experts_tile<ExpertTile<ELEM, 64, 128, 2, 2, 1, 3, 128, false, BKS>>(a, blocks, s);
-    case EXPERTS_32x64: return launch_experts_tile<ExpertTile<ELEM, 32, 64, 1, 1, 4, 2, 128, false, BKS>>(a, blocks, s);
-    case EXPERTS_16x64: return launch_experts_tile<ExpertTile<ELEM, 16, 64, 1, 1, 4, 2, 128, false, BKS>>(a, blocks, s);
+    case EXPERTS_64x64: return launch_experts_tile<ExpertTile<ELEM, 64, 64, 2, 2, 1, 3, 128, false, BKS>>(a, blocks, s);
+    case EXPERTS_64x64_K2: return launch_experts_tile<ExpertTile<ELEM, 64, 64, 2, 2, 2, 3, 128, false, BKS>>(a, blocks, s);
     default: return launch_experts_tile<ExpertTile<ELEM, 16, 32, 1, 1, 4, 3, 128, false, BKS>>(a, blocks, s);
     }
 }

@@ -65,7 +65,7 @@ struct ExpertTile {
     // the largest tile has registers for 32-bit offsets of A's rows only (its caller sees to it that they fit)
     static constexpr bool WIDE = BM < 256;
     static constexpr bool ALWAYS = BM >= 256;   // requests past the end, see tile_sums
-    static_assert(WK == 1 || NW == 1, "k groups of one wave: they share no stage");
+    static_assert(WK == 1 || BM < 256, "the largest tile has no room for k groups");
 };
 
 // Position of 16-byte unit `u` of LDS line `line` (RB bytes long); see the two storages above.  256 bytes hold 16 units,
@@ -120,15 +120,26 @@ __device__ __forceinline__ void dma4(const char *base, uint32_t off, uint32_t ld
 // what an index that names no row stands for
 __device__ const xt_u4 xt_zeros = {0, 0, 0, 0};
 
-// `n` (1..) elements from p, zeros behind them
+// 16 bytes of a storage row of `end` bytes (at least one of them) from byte `at` on, zeros past its end.  Where they cross it the row's
+// last 16 are read and moved down: one load, nothing outside the row.
 template <int ES>
-__device__ __forceinline__ xt_u4 load_some(const char *p, int n)
+__device__ __forceinline__ xt_u4 load_unit(const char *row, int at, int end)
 {
+    typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(1)));
     xt_u4 v = {0, 0, 0, 0};
+    if (end >= 16) {
+        const int from = at + 16 <= end ? at : end - 16, down = at - from;   // bytes
+        const u4 x = *(const u4 *)(row + from);
+        unsigned __int128 w = ((unsigned __int128)(((uint64_t)x[3] << 32) | x[2]) << 64) | (((uint64_t)x[1] << 32) | x[0]);
+        w = down < 16 ? w >> (8 * down) : 0;
+        v = xt_u4{(uint32_t)w, (uint32_t)(w >> 32), (uint32_t)(w >> 64), (uint32_t)(w >> 96)};
+    } else {
 #pragma unroll
-    for (int i = 0; i < 16 / ES; ++i) {
-        const uint32_t x = i >= n ? 0u : ES == 2 ? (uint32_t) * (const uint16_t *)(p + 2 * i) : (uint32_t) * (const uint8_t *)(p + i);
-        v[i * ES / 4] |= x << (8 * ((i * ES) % 4));
+        for (int i = 0; i < 16 / ES; ++i) {
+            const int b = at + i * ES;
+            const uint32_t x = b >= end ? 0u : ES == 2 ? (uint32_t) * (const uint16_t *)(row + b) : (uint32_t) * (const uint8_t *)(row + b);
+            v[i * ES / 4] |= x << (8 * ((i * ES) % 4));
+        }
     }
     return v;
 }
@@ -243,24 +254,32 @@ struct Staged {
     template <class RowOf>
     __device__ __forceinline__ void load_cut(char *lds, int k0, int wave, int lane, RowOf row_of)
     {
+        // (two units of a lane at a time: more would not fit beside the largest tile's accumulators)
+        constexpr int AT = Q > 1 ? 2 : 1;
+        static_assert(Q % AT == 0, "units in pairs");
 #pragma unroll 1
-        for (int q = 0; q < Q; ++q) {
-            const int s = slot(q, wave, lane);
-            xt_u4 v = {0, 0, 0, 0};
-            if constexpr (!KS) {
-                const int line = s / UR, at = k0 + unit_of<RB, false, PERM, ES>(line, s % UR) * E;
-                const int in = line0 + line < lines ? line0 + line : lines - 1;
-                if (at < k) v = load_some<ES>(first + (int64_t)row_of(in) * pitch + (int64_t)at * ES, k - at);
-            } else {
-                const int r0 = s / UR, c = line0 + unit_of<RB, KS, PERM, ES>(r0, s % UR) * E;
-                if (k0 + r0 < k && c < lines) {
-                    int r = k0 + r0;
-                    bool there = true;
-                    if (index) { r = index[r]; there = (unsigned)r < (unsigned)storage_rows; }
-                    if (there) v = load_some<ES>(first + (int64_t)r * pitch + (int64_t)c * ES, lines - c);
+        for (int q0 = 0; q0 < Q; q0 += AT) {
+            xt_u4 v[AT];
+#pragma unroll
+            for (int i = 0; i < AT; ++i) {
+                const int s = slot(q0 + i, wave, lane);
+                v[i] = xt_u4{0, 0, 0, 0};
+                if constexpr (!KS) {
+                    const int line = s / UR, at = k0 + unit_of<RB, false, PERM, ES>(line, s % UR) * E;
+                    const int in = line0 + line < lines ? line0 + line : lines - 1;
+                    if (at < k) v[i] = load_unit<ES>(first + (int64_t)row_of(in) * pitch, at * ES, k * ES);
+                } else {
+                    const int r0 = s / UR, c = line0 + unit_of<RB, KS, PERM, ES>(r0, s % UR) * E;
+                    if (k0 + r0 < k && c < lines) {
+                        int r = k0 + r0;
+                        bool there = true;
+                        if (index) { r = index[r]; there = (unsigned)r < (unsigned)storage_rows; }
+                        if (there) v[i] = load_unit<ES>(first + (int64_t)r * pitch, c * ES, lines * ES);
+                    }
                 }
             }
-            *(xt_u4 *)(lds + s * 16) = v;
+#pragma unroll
+            for (int i = 0; i < AT; ++i) *(xt_u4 *)(lds + slot(q0 + i, wave, lane) * 16) = v[i];
         }
     }
 };
@@ -558,8 +577,9 @@ __device__ __forceinline__ void wait_vm()
 {
     asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
+// A barrier of the workgroup; a k group of one wave needs none (and several groups of more waves meet as often as each other).
 template <int NW>
-__device__ __forceinline__ void meet()   // a group of one wave has nobody to wait for
+__device__ __forceinline__ void meet()
 {
     // (a bare s_barrier: a full fence would drain the loads under way)
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -584,7 +604,7 @@ struct TileScales {
 // next stage are read, which the same barrier certifies as landed.  What is left is loaded through registers, one stage at a time.
 template <class T, class ARow>
 __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, false, T::NW, T::WIDE> &sa, Staged<T::BN, T::ES, T::KB, T::BKS, T::PERM, T::NW, false> &sb,
-                                          const int k0, const int k1, const int wave, const int kg, const int lane, ARow a_row, bool rel, const TileScales &scales, xt_f4 (&acc)[T::MI][T::NI])
+                                          const int k0, const int k1, const int wave, const int kg, const int lane, ARow a_row, bool rel, const TileScales &scales, const bool idle, xt_f4 (&acc)[T::MI][T::NI])
 {
     constexpr int S = T::S, BK = T::BK, STEPS = Steps<T>::STEPS;
     constexpr int LOADS = Staged<T::BM, T::ES, T::KB, T::AKS, false, T::NW, T::WIDE>::Q + Staged<T::BN, T::ES, T::KB, T::BKS, T::PERM, T::NW, false>::Q + (T::FP8 ? 1 : 0) + (T::PREFETCH ? 1 : 0);
@@ -678,18 +698,31 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
     constexpr std::false_type no;
     constexpr auto none = [](auto, int) {};
 
+    // `busy`: a wave whose rows all lie past the group's end requests its part of the stages and meets the others, no more: its
+    // SIMD's other wave then has the matrix cores alone
+    auto run = [&](auto busy) {
+    constexpr bool BUSY = decltype(busy)::value;
     if (mine > 0) {
         int slot = 0, r = 0;
         float wb = scale_b(kg);
         auto first = [&]() {
             meet<T::NW>();
-            f.template read_a<0>(ra, ring, scale_row(ring));
-            f.template read_b<0, 0>(rb, ring + T::A_BYTES);
+            if constexpr (BUSY) {
+                f.template read_a<0>(ra, ring, scale_row(ring));
+                f.template read_b<0, 0>(rb, ring + T::A_BYTES);
+            }
         };
         // stage r; `wait`: until stage r + 1 has landed; more: request the one S further on into this one's slot
         auto go = [&](auto parity, auto more, auto wait) {
             const int here = slot;
             slot = slot + 1 == S ? 0 : slot + 1;
+            if constexpr (!BUSY) {
+                wait();
+                meet<T::NW>();
+                if constexpr (decltype(more)::value) request(r + S, here);
+                ++r;
+                return;
+            }
             const float now = wb;
             wb = scale_b((r + 1) * T::WK + kg);
             stage(parity, ring + here * T::STAGE, now, ring + slot * T::STAGE, yes, [&]() {
@@ -712,10 +745,10 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
             if constexpr (Steps<T>::PAIRS) {
                 while (r + 2 < mine) { go(even, yes, all_but); go(odd, yes, all_but); }
                 go(even, no, all_but);
-                stage(odd, ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
+                if constexpr (BUSY) stage(odd, ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
             } else {
                 while (r + 1 < mine) go(even, yes, all_but);
-                stage(even, ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
+                if constexpr (BUSY) stage(even, ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
             }
         } else {
 #pragma unroll
@@ -726,22 +759,32 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
             first();
             while (r + S < mine) go(even, yes, all_but);
             while (r + 1 < mine) go(even, no, []() { wait_vm<0>(); });
-            stage(even, ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
+            if constexpr (BUSY) stage(even, ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
         }
     }
     if constexpr (T::ALWAYS) wait_vm<0>();   // (the requests past the end: nothing is under way when the workgroup ends)
+    if constexpr (T::WK > 1 && T::NW > 1)
+        for (int r = mine; r < (whole + T::WK - 1) / T::WK; ++r) meet<T::NW>();   // (the groups that have one stage more)
     // stages that are not whole
     for (int s = whole; s < stages; ++s) {
-        if (T::WK > 1 && s % T::WK != kg) continue;
+        if (T::WK > 1 && s % T::WK != kg) {
+            if constexpr (T::NW > 1) { meet<T::NW>(); meet<T::NW>(); }
+            continue;
+        }
         meet<T::NW>();                 // slot 0 is no longer read
         sa.load_cut(ring, k0 + s * BK, wave, lane, a_row);
         sb.load_cut(ring + T::A_BYTES, k0 + s * BK, wave, lane, [](int i) { return i; });
         if constexpr (T::FP8) { request_scales(s, 0); wait_vm<0>(); }
         meet<T::NW>();
-        f.template read_a<0>(ra, ring, scale_row(ring));
-        f.template read_b<0, 0>(rb, ring + T::A_BYTES);
-        stage(even, ring, scale_b(s), nullptr, no, []() {}, none);
+        if constexpr (BUSY) {
+            f.template read_a<0>(ra, ring, scale_row(ring));
+            f.template read_b<0, 0>(rb, ring + T::A_BYTES);
+            stage(even, ring, scale_b(s), nullptr, no, []() {}, none);
+        }
     }
+    };
+    if (T::NW > 1 && idle) run(no);
+    else run(yes);
     if constexpr (T::WK > 1) {
         // the k groups' sums, added up by the first in order (so the result does not depend on who came first)
         __syncthreads();
@@ -812,7 +855,7 @@ __global__ void __launch_bounds__(T::NT) experts_rows_kernel(const ExpertsArgs a
         scales.b = a.scale_b + (int64_t)(t.group < 0 ? 0 : t.group) * a.group_sb + (T::BKS ? at : at * a.ld_sb);
         scales.b_step = T::BKS ? a.ld_sb : 1;
     }
-    if (!tile_sums<T>(sa, sb, 0, K, wave, kg, lane, a_row, !a.rows, scales, acc)) return;
+    if (!tile_sums<T>(sa, sb, 0, K, wave, kg, lane, a_row, !a.rows, scales, row0 + wm * (T::BM / T::WM) >= t.row1, acc)) return;
 
 #pragma unroll
     for (int mi = 0; mi < T::MI; ++mi) {
@@ -868,7 +911,7 @@ __global__ void __launch_bounds__(T::NT) experts_sums_kernel(const ExpertsArgs a
     sa.start_ks(ia ? A : A + (int64_t)lo * a.lda * T::ES, a.lda * T::ES, ia ? ia + lo : nullptr, a.a_rows, m0, a.M, to, from + kg * T::BK, wave, lane);
     sb.start_ks(ib ? B : B + (int64_t)lo * a.ldb * T::ES, a.ldb * T::ES, ib ? ib + lo : nullptr, a.a_rows, n0, a.N, to, from + kg * T::BK, wave, lane);
     xt_f4 acc[T::MI][T::NI];
-    if (!tile_sums<T>(sa, sb, from, to, wave, kg, lane, [](int i) { return i; }, true, TileScales(), acc)) return;
+    if (!tile_sums<T>(sa, sb, from, to, wave, kg, lane, [](int i) { return i; }, true, TileScales(), false, acc)) return;
 
     const int wm = wave / T::WN, wn = wave % T::WN;
     if (a.parts > 1) {

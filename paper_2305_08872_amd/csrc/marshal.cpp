@@ -230,9 +230,247 @@ PyObject *count_i8_general(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- operators of a mixture-of-experts layer
+
+const at::Tensor *tensor(PyObject *o) { return THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr; }
+
+// the type's code and torch's type of an fp32, bf16 or fp16 tensor
+bool known_type(PyObject *o, int &code, at::ScalarType &type)
+{
+    const at::Tensor *t = tensor(o);
+    if (!t || !t->defined()) return false;
+    type = t->scalar_type();
+    code = type == at::kFloat ? AMULET_FP32 : type == at::kBFloat16 ? AMULET_BF16 : type == at::kHalf ? AMULET_FP16 : -1;
+    return code >= 0;
+}
+
+struct Groups {
+    void *p;
+    int64_t n, rows, cols, ld, apart;
+};
+bool groups(PyObject *o, at::ScalarType type, Groups &g)
+{
+    const at::Tensor *t = device_tensor(o, type);
+    if (!t || t->dim() != 3) return false;
+    g.n = t->size(0);
+    g.rows = t->size(1);
+    g.cols = t->size(2);
+    if (g.cols > 1 && t->stride(2) != 1) return false;
+    g.ld = g.rows <= 1 ? g.cols : t->stride(1);
+    if (g.ld <= 0) g.ld = 1;
+    g.apart = g.n > 1 ? t->stride(0) : g.rows * g.ld;
+    g.p = t->data_ptr();
+    return true;
+}
+
+// None, or n contiguous values
+bool values_or_none(PyObject *o, at::ScalarType type, int64_t n, void *&p)
+{
+    p = nullptr;
+    return o == Py_None || values(o, type, n, p);
+}
+bool bytes_or_none(PyObject *o, void *&p, size_t &n)
+{
+    p = nullptr;
+    n = 0;
+    if (o == Py_None) return true;
+    const at::Tensor *t = tensor(o);
+    if (!t || !t->defined() || !t->is_cuda() || t->layout() != at::kStrided || !t->has_storage() || !t->is_contiguous()) return false;
+    p = t->data_ptr();
+    n = t->nbytes();
+    return true;
+}
+// rows and columns of a 2-D tensor, whatever else it is
+bool shape2(PyObject *o, int64_t &rows, int64_t &cols)
+{
+    const at::Tensor *t = tensor(o);
+    if (!t || !t->defined() || t->dim() != 2) return false;
+    rows = t->size(0);
+    cols = t->size(1);
+    return true;
+}
+int64_t blocks128(int64_t n) { return (n + 127) / 128; }
+
+// (logits, experts, weights, place, tokens, offsets, workspace, norm, stream)
+PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Mat X;
+    int type, norm;
+    at::ScalarType t;
+    int64_t T, k;
+    void *e, *w, *p, *tok, *off, *ws, *s;
+    size_t bytes;
+    if (n != 9 || !known_type(a[0], type, t) || !matrix(a[0], t, X) || !shape2(a[1], T, k) || T != X.rows || !values(a[1], at::kInt, T * k, e) ||
+        !values(a[2], at::kFloat, T * k, w) || !values(a[3], at::kInt, T * k, p) || !values(a[4], at::kInt, T * k, tok) ||
+        !values(a[5], at::kInt, X.cols + 1, off) || !bytes_or_none(a[6], ws, bytes) || !integer(a[7], norm) || !stream_handle(a[8], s))
+        return not_here();
+    return status([&] {
+        return amulet_route(type, T, X.cols, k, X.p, X.ld, norm, (int32_t *)e, (float *)w, (int32_t *)p, (int32_t *)tok, (int32_t *)off, ws, bytes, s);
+    });
+}
+
+// (logits, experts, weights, dweights, dlogits, norm, stream)
+PyObject *route_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Mat X, D;
+    int type, norm;
+    at::ScalarType t;
+    int64_t T, k;
+    void *e, *w, *dw, *s;
+    if (n != 7 || !known_type(a[4], type, t) || !matrix(a[4], t, D) || !integer(a[5], norm) || !shape2(a[1], T, k) || T != D.rows ||
+        !values(a[1], at::kInt, T * k, e) || !values(a[2], at::kFloat, T * k, w) || !values(a[3], at::kFloat, T * k, dw))
+        return not_here();
+    X.p = nullptr;
+    X.ld = D.cols;
+    if (!norm && a[0] != Py_None && (!matrix(a[0], t, X) || X.rows != D.rows || X.cols != D.cols)) return not_here();
+    if (!stream_handle(a[6], s)) return not_here();
+    return status([&] {
+        return amulet_route_grad(type, T, D.cols, k, X.p, X.ld, norm, (const int32_t *)e, (const float *)w, (const float *)dw, D.p, D.ld, s);
+    });
+}
+
+// (Y, weights, place, R, stream)
+PyObject *combine(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Mat Y, R;
+    int type;
+    at::ScalarType t;
+    int64_t T, k;
+    void *w, *p, *s;
+    if (n != 5 || !known_type(a[3], type, t) || !matrix(a[3], t, R) || !matrix(a[0], t, Y) || Y.cols != R.cols || !shape2(a[2], T, k) || T != R.rows ||
+        !values_or_none(a[1], at::kFloat, T * k, w) || !values(a[2], at::kInt, T * k, p) || !stream_handle(a[4], s))
+        return not_here();
+    return status([&] { return amulet_combine(type, T, k, R.cols, Y.rows, Y.p, Y.ld, (const float *)w, (const int32_t *)p, R.p, R.ld, s); });
+}
+
+// (Y, weights, place, dR, dY, dweights, stream)
+PyObject *combine_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Mat Y, D, dY;
+    int type;
+    at::ScalarType t;
+    int64_t T, k;
+    void *w, *p, *dw, *s;
+    if (n != 7 || !known_type(a[3], type, t) || !matrix(a[3], t, D) || !matrix(a[4], t, dY) || dY.cols != D.cols || !shape2(a[2], T, k) || T != D.rows ||
+        !values_or_none(a[1], at::kFloat, T * k, w) || !values(a[2], at::kInt, T * k, p) || !values_or_none(a[5], at::kFloat, T * k, dw))
+        return not_here();
+    Y.p = nullptr;
+    Y.ld = D.cols;
+    if (dw && (!matrix(a[0], t, Y) || Y.rows != dY.rows || Y.cols != dY.cols)) return not_here();
+    if (a[5] != Py_None && !dw) return not_here();
+    if (!stream_handle(a[6], s)) return not_here();
+    return status([&] {
+        return amulet_combine_grad(type, T, k, D.cols, dY.rows, Y.p, Y.ld, (const float *)w, (const int32_t *)p, D.p, D.ld, dY.p, dY.ld, (float *)dw, s);
+    });
+}
+
+// (A, B, offsets, R, rows, trans_b, stream)
+PyObject *grouped_mm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Mat A, R;
+    Groups B;
+    int type, out, tb;
+    at::ScalarType t, tr;
+    void *off, *rows, *s;
+    if (n != 7 || !known_type(a[0], type, t) || !matrix(a[0], t, A) || !groups(a[1], t, B) || !known_type(a[3], out, tr) || !matrix(a[3], tr, R) ||
+        !integer(a[5], tb) || (tb ? B.cols : B.rows) != A.cols || (tb ? B.rows : B.cols) != R.cols || !values_or_none(a[4], at::kInt, R.rows, rows) ||
+        (a[4] == Py_None && A.rows != R.rows) || (a[4] != Py_None && !rows) || !values(a[2], at::kInt, B.n + 1, off) || !stream_handle(a[6], s))
+        return not_here();
+    return status([&] {
+        return amulet_grouped_mm(type, out, tb, R.rows, R.cols, A.cols, B.n, A.p, A.ld, (const int32_t *)rows, A.rows, B.p, B.ld, B.apart,
+                                 (const int32_t *)off, R.p, R.ld, s);
+    });
+}
+
+// (A, D, offsets, R, workspace, rows, trans_r, stream)
+PyObject *grouped_mm_wgrad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Mat A, D;
+    Groups R;
+    int type, out, tr;
+    at::ScalarType t, to;
+    void *off, *rows, *ws, *s;
+    size_t bytes;
+    if (n != 8 || !known_type(a[0], type, t) || !matrix(a[0], t, A) || !matrix(a[1], t, D) || !known_type(a[3], out, to) || !groups(a[3], to, R) ||
+        !bytes_or_none(a[4], ws, bytes) || !integer(a[6], tr) || (tr ? R.cols : R.rows) != A.cols || (tr ? R.rows : R.cols) != D.cols ||
+        !values_or_none(a[5], at::kInt, D.rows, rows) || (a[5] == Py_None && A.rows != D.rows) || (a[5] != Py_None && !rows) ||
+        !values(a[2], at::kInt, R.n + 1, off) || !stream_handle(a[7], s))
+        return not_here();
+    return status([&] {
+        return amulet_grouped_mm_wgrad(type, out, tr, D.rows, D.cols, A.cols, R.n, A.p, A.ld, (const int32_t *)rows, A.rows, D.p, D.ld,
+                                       (const int32_t *)off, R.p, R.ld, R.apart, ws, bytes, s);
+    });
+}
+
+// (X, Q, scales, stream)
+PyObject *quantize_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Mat X, Q, S;
+    int type;
+    at::ScalarType t;
+    void *s;
+    if (n != 4 || !known_type(a[0], type, t) || !matrix(a[0], t, X) || !matrix(a[1], at::kFloat8_e4m3fn, Q) || !matrix(a[2], at::kFloat, S) ||
+        Q.rows != X.rows || Q.cols != X.cols || S.rows != blocks128(X.cols) || S.cols != X.rows || !stream_handle(a[3], s))
+        return not_here();
+    return status([&] { return amulet_quantize_fp8(type, X.rows, X.cols, X.p, X.ld, Q.p, Q.ld, (float *)S.p, S.ld, s); });
+}
+
+// (X, Q, scales, stream)
+PyObject *quantize_fp8_blocks(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Groups X, Q, S;
+    int type;
+    at::ScalarType t;
+    void *s;
+    if (n != 4 || !known_type(a[0], type, t) || !groups(a[0], t, X) || !groups(a[1], at::kFloat8_e4m3fn, Q) || !groups(a[2], at::kFloat, S) ||
+        Q.n != X.n || Q.rows != X.rows || Q.cols != X.cols || S.n != X.n || S.rows != blocks128(X.rows) || S.cols != blocks128(X.cols) || !stream_handle(a[3], s))
+        return not_here();
+    return status([&] {
+        return amulet_quantize_fp8_blocks(type, X.n, X.rows, X.cols, X.p, X.ld, X.apart, Q.p, Q.ld, Q.apart, (float *)S.p, S.ld, S.apart, s);
+    });
+}
+
+// (A, scales_a, B, scales_b, offsets, R, rows, trans_b, stream)
+PyObject *grouped_mm_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Mat A, SA, R;
+    Groups B, SB;
+    int out, tb;
+    at::ScalarType tr;
+    void *off, *rows, *s;
+    if (n != 9 || !matrix(a[0], at::kFloat8_e4m3fn, A) || !matrix(a[1], at::kFloat, SA) || !groups(a[2], at::kFloat8_e4m3fn, B) || !groups(a[3], at::kFloat, SB) ||
+        !known_type(a[5], out, tr) || !matrix(a[5], tr, R) || !integer(a[7], tb) || (tb ? B.cols : B.rows) != A.cols || (tb ? B.rows : B.cols) != R.cols ||
+        SA.rows != blocks128(A.cols) || SA.cols != A.rows || SB.n != B.n || SB.rows != blocks128(B.rows) || SB.cols != blocks128(B.cols) ||
+        !values_or_none(a[6], at::kInt, R.rows, rows) || (a[6] == Py_None && A.rows != R.rows) || (a[6] != Py_None && !rows) ||
+        !values(a[4], at::kInt, B.n + 1, off) || !stream_handle(a[8], s))
+        return not_here();
+    return status([&] {
+        return amulet_grouped_mm_fp8(out, tb, R.rows, R.cols, A.cols, B.n, A.p, A.ld, (const float *)SA.p, SA.ld, (const int32_t *)rows, A.rows,
+                                     B.p, B.ld, B.apart, (const float *)SB.p, SB.ld, SB.apart, (const int32_t *)off, R.p, R.ld, s);
+    });
+}
+
+// (A, scales_a, B, scales_b, R, trans_b, stream)
+PyObject *mm_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Mat A, SA, B, SB, R;
+    int out, tb;
+    at::ScalarType tr;
+    void *s;
+    if (n != 7 || !matrix(a[0], at::kFloat8_e4m3fn, A) || !matrix(a[1], at::kFloat, SA) || !matrix(a[2], at::kFloat8_e4m3fn, B) || !matrix(a[3], at::kFloat, SB) ||
+        !known_type(a[4], out, tr) || !matrix(a[4], tr, R) || !integer(a[5], tb) || (tb ? B.cols : B.rows) != A.cols || (tb ? B.rows : B.cols) != R.cols ||
+        R.rows != A.rows || SA.rows != blocks128(A.cols) || SA.cols != A.rows || SB.rows != blocks128(B.rows) || SB.cols != blocks128(B.cols) || !stream_handle(a[6], s))
+        return not_here();
+    return status([&] {
+        return amulet_mm_fp8(out, tb, R.rows, R.cols, A.cols, A.p, A.ld, (const float *)SA.p, SA.ld, B.p, B.ld, (const float *)SB.p, SB.ld, R.p, R.ld, s);
+    });
+}
+
 #define MARSHAL(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MARSHAL(mmlike_f32),      MARSHAL(mmlike_f32_general), MARSHAL(mmlike_f64), MARSHAL(count_i8),
-                         MARSHAL(count_i8_assign), MARSHAL(count_i8_general),   {nullptr, nullptr, 0, nullptr}};
+                         MARSHAL(count_i8_assign), MARSHAL(count_i8_general),   MARSHAL(route),      MARSHAL(route_grad),
+                         MARSHAL(combine),         MARSHAL(combine_grad),       MARSHAL(grouped_mm), MARSHAL(grouped_mm_wgrad),
+                         MARSHAL(quantize_fp8),    MARSHAL(quantize_fp8_blocks), MARSHAL(grouped_mm_fp8), MARSHAL(mm_fp8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -85,7 +85,8 @@ SHAPES = [
     ([1], 1, 1), ([0, 1, 0], 8, 8), ([3, 0, 2], 17, 33), ([5, 9, 1, 0, 2], 64, 64), ([16, 16], 32, 128), ([7], 130, 200),
     ([20, 31, 0, 25], 96, 127), ([30, 30], 129, 65), ([61, 40, 70], 200, 192), ([64], 100, 71), ([50, 64], 128, 640),
     ([100, 130, 90], 260, 136), ([300, 1, 200], 129, 321), ([128, 256], 256, 64), ([700], 72, 1000),
-    ([2100, 1996], 4000, 72), ([2300, 0, 1800], 4099, 130), ([4096], 4096, 193),
+    ([2100, 1996], 4000, 72), ([2300, 0, 1800], 4099, 130), ([4096], 4096, 193), ([1500, 1700], 1000, 520), ([256], 4096, 4096),
+    ([4096], 8192, 1030), ([2500, 0, 1700], 8200, 1000), ([4100], 8195, 1024),
 ]
 
 
@@ -107,19 +108,19 @@ def test_products_by_rows(am, sizes, N, K, dtype, out, trans_b):
 
 def test_the_shapes_above_run_every_kernel(am):
     seen = set()
-    for sizes, N, K in SHAPES + [([3, 2], 8200, 40)]:
+    for sizes, N, K in SHAPES:
         M = sum(sizes)
         A, B = torch.zeros(M, K, dtype=BF16, device="cuda"), torch.zeros(len(sizes), K, N, dtype=BF16, device="cuda")
         R = torch.ones(M, N, dtype=BF16, device="cuda")
         am.amulet_grouped_mm(A, B, torch.tensor(offsets_of(sizes), dtype=torch.int32, device="cuda"), R)
         seen.add(am.amulet_recent_kernel().split()[0])
         assert not R.any()
-    assert seen == {"grouped_mm_" + t for t in ("256x256", "128x128", "64x128", "32x64", "16x64", "16x32")}
+    assert seen == {"grouped_mm_" + t for t in ("256x256", "128x128", "64x128", "64x64", "64x64_k2", "16x32")}
 
 
 @pytest.mark.parametrize("trans_b", [False, True])
 @pytest.mark.parametrize("pad,shift", [(0, 1), (1, 0), (3, 5), (8, 8)])
-@pytest.mark.parametrize("sizes,N,K", [([3, 2], 37, 75), ([40, 0, 30], 136, 130), ([150, 150], 265, 200), ([4100], 4104, 200)])
+@pytest.mark.parametrize("sizes,N,K", [([3, 2], 37, 75), ([40, 0, 30], 136, 130), ([150, 150], 265, 200), ([4100], 4104, 200), ([4100], 8199, 1003)])
 def test_products_by_rows_of_views(am, sizes, N, K, pad, shift, trans_b):
     """Rows apart, at odd addresses, the groups' matrices apart, R a view too; nothing beside the operands is used or written."""
     print("views", sizes, N, K, pad, shift, trans_b, flush=True)
@@ -138,7 +139,7 @@ def test_products_by_rows_of_views(am, sizes, N, K, pad, shift, trans_b):
 
 @pytest.mark.parametrize("trans_b", [False, True])
 @pytest.mark.parametrize("first,sizes,rest,N,K,tokens", [(0, [3, 0, 5], 0, 40, 64, 4), (2, [20, 40], 9, 70, 96, 31), (0, [0, 0], 12, 16, 8, 3), (5, [200, 330, 120], 40, 200, 260, 100),
-                                                         (300, [2000, 2100], 290, 4000, 136, 777)])
+                                                         (300, [2000, 2100], 290, 4000, 136, 777), (300, [2000, 2100], 290, 8200, 1000, 777)])
 def test_gathered_rows_and_rows_of_no_group(am, first, sizes, rest, N, K, tokens, trans_b):
     """Row indexes that name no row stand for zeros; rows before the first group and behind the last are zeros."""
     print("gather", first, sizes, rest, N, K, tokens, trans_b, flush=True)
@@ -194,7 +195,7 @@ def test_nothing_to_sum_and_nothing_to_write(am):
 def test_infinities_and_nan_reach_their_own_outputs_only(am):
     """A NaN in a row, a column or a matrix, and in the k next to a ragged end: no other output has one."""
     g = gen(9)
-    for K, N, sizes in [(70, 50, [5, 6]), (200, 300, [150, 140]), (65, 4000, [2100, 2100])]:
+    for K, N, sizes in [(70, 50, [5, 6]), (200, 300, [150, 140]), (65, 4000, [2100, 2100]), (1001, 8200, [2100, 2100])]:
         M = sum(sizes)
         A, B = normal(g, M, K, dtype=BF16), normal(g, 2, K, N, dtype=BF16)
         A[2, K - 1] = math.nan
@@ -510,7 +511,7 @@ def check_fp8(R, A, sa, B, sb, at, rows, trans_b):
 @pytest.mark.parametrize("trans_b", [False, True])
 @pytest.mark.parametrize("out", [F32, BF16, FP16])
 @pytest.mark.parametrize("sizes,N,K,tokens", [([1], 1, 1, 0), ([3, 0, 2], 17, 33, 0), ([5, 9, 1], 64, 128, 7), ([16], 8200, 256, 0), ([20, 31, 0], 96, 127, 0), ([61, 40], 200, 500, 33),
-                                              ([100, 130, 90], 260, 136, 0), ([300, 1, 200], 129, 1321, 400), ([2100, 1996], 4000, 200, 0), ([4096], 4100, 384, 1000)])
+                                              ([100, 130, 90], 260, 136, 0), ([300, 1, 200], 129, 1321, 400), ([2100, 1996], 4000, 200, 0), ([4096], 4100, 384, 1000), ([2100, 1996], 8200, 1001, 0), ([4096], 8195, 1408, 1000), ([256], 4096, 4096, 0)])
 def test_fp8_products(am, sizes, N, K, tokens, out, trans_b):
     print("fp8", sizes, N, K, tokens, out, trans_b, flush=True)
     g = gen(N + K)
