@@ -20,17 +20,21 @@ static bool known(int type) { return type == AMULET_FP32 || known16(type); }
 // Tiles by rows: the one with the lowest estimate.  A workgroup that has its unit alone takes `stage` us for a stage of its k
 // (64 of 16 bits, 128 of 8), of which larger tiles have less per product, and `start` for finding its tile, filling its ring and
 // storing; all workgroups together take no more from the L2s than some 64 KB a us and unit, of which smaller tiles
-// need more; under both lies what memory takes for the operands.  The numbers are fitted to 230 drawn sizes (4 ... 32768 rows, widths
-// of 64 to 4096, 1 ... 128 groups, 16 and 8 bits, both layouts): 1.6 % behind the fastest on average, 25 % at most.  us,
+// need more; under both lies what memory takes for the operands, TB/s as a tile's requests draw it (of 16 bits along k,
+// across it, of 8 bits).  The numbers were measured, and fitted to 369 sizes (1 ... 32768 rows, widths of 64 to 4096, 1 ... 128 groups, 16
+// and 8 bits, both layouts, operands in the caches and out of them): 3 % behind the fastest on average.  us,
 // 256 x 256 / 128 x 128 / 64 x 128 / 64 x 64 / 64 x 64 with two k groups / 16 x 32, bf16, B stored N x K: 256 x 4096 x 4096
 // 85 / 46 / 28 / 22 / 18 / 38, 64 x 512 x 4096 58 / 42 / 25 / 19 / 14 / 8, 1024 x 4096 x 1024 over 8 groups 26 / 19 / 18 / 19 / 29 / 60, 8192 x 1024 x 1024
-// over 8 32 / 26 / 28 / 37 / - / 121; 4096 x 4096 x 1024 over 4 of 8 bits 30 / 33 / 40 / 46 / 83 / 216.
+// over 8 32 / 26 / 28 / 37 / - / 121, 48 x 2048 x 2048 over 64 (out of memory) 67 / 63 / 59 / 59 / 62 / 51; 4096 x 4096 x 1024 over 4 of 8 bits 30 / 33 / 40 / 46 / 83 / 216.
 // (Tiles of 16 x 64 and 32 x 64 that were tried gained 0.1 % on average and are not built.)
 struct TileCost {
-    double stage16, stage8, start;   // us
-    int resident;                    // workgroups that a unit's LDS holds
+    double stage16, stage8, start;       // us
+    double along16, across16, memory8;   // TB/s
+    int resident;                        // workgroups that a unit's LDS holds
 };
-static const TileCost kTileCosts[EXPERTS_TILES] = {{1.22, 1.21, 7.9, 1}, {0.67, 0.75, 2.6, 2}, {0.37, 0.86, 2.6, 2}, {0.30, 0.50, 1.8, 3}, {0.25, 0.39, 3.8, 1}, {0.10, 0.14, 3.7, 2}};
+static const TileCost kTileCosts[EXPERTS_TILES] = {
+    {1.22, 1.21, 7.9, 4.0, 4.6, 4.0, 1}, {0.67, 0.75, 2.6, 4.5, 5.3, 4.3, 2}, {0.37, 0.86, 2.6, 4.6, 5.1, 4.8, 2},
+    {0.30, 0.50, 1.8, 5.1, 4.8, 4.0, 3}, {0.25, 0.39, 3.8, 4.8, 4.7, 3.4, 1}, {0.10, 0.14, 3.7, 5.7, 4.7, 3.5, 2}};
 static double tile_us(int tile, int64_t M, int64_t N, int64_t K, int64_t G, int es, bool b_across)
 {
     const double units = compute_units(), bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
@@ -45,7 +49,7 @@ static double tile_us(int tile, int64_t M, int64_t N, int64_t K, int64_t G, int 
     // (a line of 64 bytes of B across k: two requests for what one brings)
     const double bytes = bm + bn * (b_across && bn * es < 128 ? 2.1 : 1.0);
     const double supply = groups / units * stages * bytes * 0.128 / 64.0;
-    const double memory = (busy * (double)N * (double)K + (double)M * (double)K) * es / 4.3e6;
+    const double memory = (busy * (double)N * (double)K + (double)M * (double)K) * es / (1e6 * (es == 1 ? c.memory8 : b_across ? c.across16 : c.along16));
     const double most = alone > supply ? alone : supply;
     return (most > memory ? most : memory) + 0.03 * (alone + supply);
 }

@@ -2,10 +2,9 @@
 // the rows of all (token, expert) pairs in order of expert, then of token; and its gradient.
 //
 // Forward: one kernel chooses (a token to L lanes, each with the logits of experts lane + L j in registers; k rounds of a
-// maximum over keys that hold the logit's order and, below it, the complement of the expert's index, so that ties go to the
-// lowest one) and counts its 64 tokens' experts in LDS; a second one finds where each expert's rows of its tokens begin,
-// from all counts, and ranks its pairs among equals by ballots, 64 at a time.  Up to 64 tokens one workgroup does both: one
-// launch.  Everything that decides an order is an integer and every sum of weights is one lane group's, so results do not
+// maximum over the logits and a minimum over the indexes that have it, so that ties go to the lowest one) and counts its 64
+// tokens' experts in LDS; a second one finds where each expert's rows of its tokens begin, from all counts, and ranks its
+// pairs among equals by ballots, 64 to a wave.  Up to 64 tokens one workgroup does both: one launch.  Everything that decides an order is an integer and every sum of weights is one lane group's, so results do not
 // depend on timing.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -45,20 +44,14 @@ __device__ __forceinline__ uint32_t of_partner(uint32_t x)
     else if constexpr (STEP == 8) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, true); // row_mirror
     else return (uint32_t)__shfl_xor((int)x, STEP);
 }
-template <int STEP>
-__device__ __forceinline__ uint64_t larger_of_pair(uint64_t x)
-{
-    const uint64_t y = ((uint64_t)of_partner<STEP>((uint32_t)(x >> 32)) << 32) | of_partner<STEP>((uint32_t)x);
-    return x > y ? x : y;
-}
 template <int L>
-__device__ __forceinline__ uint64_t group_most(uint64_t x)
+__device__ __forceinline__ uint32_t group_min(uint32_t x)
 {
-    x = larger_of_pair<1>(x);
-    x = larger_of_pair<2>(x);
-    x = larger_of_pair<4>(x);
-    x = larger_of_pair<8>(x);
-    if constexpr (L == 64) { x = larger_of_pair<16>(x); x = larger_of_pair<32>(x); }
+    x = min(x, of_partner<1>(x));
+    x = min(x, of_partner<2>(x));
+    x = min(x, of_partner<4>(x));
+    x = min(x, of_partner<8>(x));
+    if constexpr (L == 64) { x = min(x, of_partner<16>(x)); x = min(x, of_partner<32>(x)); }
     return x;
 }
 template <int L>
@@ -88,20 +81,6 @@ __device__ __forceinline__ float term_of(float x, float most)
     return most == INFINITY ? (x == INFINITY ? 1.0f : 0.0f) : expf(x - most);
 }
 
-// Keys: the order of a float as an unsigned number, above the complement of the index; 0: masked or taken.
-__device__ __forceinline__ uint64_t key_of(float x, int e)
-{
-    if (!(x > -INFINITY)) return 0;                        // (NaN too)
-    const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);   // (-0 is 0: a tie)
-    const uint32_t order = u & 0x80000000u ? ~u : u | 0x80000000u;
-    return ((uint64_t)order << 32) | (uint32_t)~e;
-}
-__device__ __forceinline__ float logit_of(uint64_t key)
-{
-    const uint32_t order = (uint32_t)(key >> 32);
-    return __builtin_bit_cast(float, order & 0x80000000u ? order & 0x7fffffffu : ~order);
-}
-
 // the counts before this block and all of them, for every expert -> first row of the block's pairs in base[], offsets
 // Returns the number of rows.  All threads of the workgroup.
 __device__ int place_bases(const RouteArgs &a, const int32_t *counts, int blocks, int block, int *base, int *total, int *rows)
@@ -114,7 +93,7 @@ __device__ int place_bases(const RouteArgs &a, const int32_t *counts, int blocks
     if (set < sets)
         for (int e = sets > 1 ? tid % a.E : tid; e < a.E; e += sets > 1 ? a.E : nt) {
             int before = 0, all = 0;
-#pragma unroll 8
+#pragma unroll 16
             for (int b = sets > 1 ? set : 0; b < blocks; b += sets > 1 ? sets : 1) {
                 const int n = counts[(int64_t)b * a.E + e];
                 all += n;
@@ -149,31 +128,43 @@ __device__ int place_bases(const RouteArgs &a, const int32_t *counts, int blocks
     return *rows;
 }
 
-// Rows of a block's pairs, by one wave: pairs [first, last) of T x k in order; base[e] is the next row of expert e.
-__device__ void place_pairs(const RouteArgs &a, const int32_t *experts, int64_t first, int64_t last, int *base)
+// Rows of a block's pairs [first, last) of T x k in order, by all waves of the workgroup: 64 pairs to a wave, as many waves at a time
+// as `seen` has counts of every expert for (RT_SEEN).  base[e] is the next row of expert e.
+constexpr int RT_SEEN = 8192;
+__device__ void place_pairs(const RouteArgs &a, const int32_t *experts, int64_t first, int64_t last, int *base, int *seen)
 {
-    const int lane = threadIdx.x & 63;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int bits = 32 - __builtin_clz((unsigned)a.E);   // E itself stands for a dropped pair
-    for (int64_t p = first; p < last; p += 64) {
+    const int waves = RT_SEEN / a.E < 16 ? RT_SEEN / a.E : 16;
+    for (int64_t p0 = first; p0 < last; p0 += 64 * waves) {
+        const int64_t p = p0 + 64 * wave + lane;
+        for (int i = tid; i < waves * a.E; i += 1024) seen[i] = 0;
         int e = -1;
-        if (p + lane < last) e = experts[p + lane - first];
+        if (wave < waves && p < last) e = experts[p - first];
         const int key = e < 0 ? a.E : e;
         uint64_t same = ~0ull;
         for (int b = 0; b < bits; ++b) {
             const uint64_t set = __ballot((key >> b) & 1);
             same &= (key >> b) & 1 ? set : ~set;
         }
-        const int rank = __builtin_popcountll(same & ((1ull << lane) - 1)), n = __builtin_popcountll(same);
+        const int rank = __builtin_popcountll(same & ((1ull << lane) - 1));
+        __syncthreads();
+        if (e >= 0 && rank == 0) seen[wave * a.E + e] = __builtin_popcountll(same);
+        __syncthreads();
         int row = -1;
-        if (e >= 0) row = base[e] + rank;
-        __builtin_amdgcn_wave_barrier();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (e >= 0 && rank == 0) base[e] = row + n;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (p + lane < last) {
-            a.place[p + lane] = row;
-            if (row >= 0) a.tokens[row] = (int32_t)((p + lane) / a.k);
+        if (e >= 0) {
+            row = base[e] + rank;
+            for (int w = 0; w < wave; ++w) row += seen[w * a.E + e];
         }
+        if (wave < waves && p < last) {
+            a.place[p] = row;
+            if (row >= 0) a.tokens[row] = (int32_t)(p / a.k);
+        }
+        if (p0 + 64 * waves >= last) break;
+        __syncthreads();
+        for (int x = tid; x < a.E; x += 1024)
+            for (int w = 0; w < waves; ++w) base[x] += seen[w * a.E + x];
+        __syncthreads();
     }
 }
 
@@ -181,7 +172,7 @@ __device__ void place_pairs(const RouteArgs &a, const int32_t *experts, int64_t 
 template <int TYPE, int L, int V>
 __global__ void __launch_bounds__(1024) route_choose_kernel(const RouteArgs a, const int block_tokens, const int alone)
 {
-    extern __shared__ int route_lds[];   // E counts; alone: and E totals, the pairs' experts, the number of rows
+    extern __shared__ int route_lds[];   // E counts; alone: and E bases, the number of rows, the pairs' experts, what place_pairs needs
     int *const count = route_lds;
     const int tid = threadIdx.x, lane = tid & 63;
     const int in = tid % L, group = tid / L, groups = 1024 / L;
@@ -192,34 +183,41 @@ __global__ void __launch_bounds__(1024) route_choose_kernel(const RouteArgs a, c
     for (int i = group; i < block_tokens; i += groups) {
         const int64_t t = t0 + i;
         if (t >= a.T) break;                              // (a whole group of lanes; the shuffles below stay within groups)
-        uint64_t key[V];
+        float x[V];                                       // -inf: masked, taken or past the last expert
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int e = in + L * j;
-            key[j] = e < a.E ? key_of(load_logit<TYPE>(a.logits, t * a.ldx + e), e) : 0;
+            x[j] = -INFINITY;
+            if (e < a.E) {
+                const float v = load_logit<TYPE>(a.logits, t * a.ldx + e);
+                x[j] = v > -INFINITY ? v : -INFINITY;     // (NaN too)
+            }
         }
-        float most = 0.0f, all = 0.0f, mine = 0.0f;
+        float most = 0.0f, all = 0.0f, mine = 0.0f, sum = 0.0f;
         int expert = -1;
-        float sum = 0.0f;
         for (int j = 0; j < a.k; ++j) {
-            uint64_t best = key[0];
+            float best = x[0];
 #pragma unroll
-            for (int v = 1; v < V; ++v) best = key[v] > best ? key[v] : best;
-            best = group_most<L>(best);
-            const float x = logit_of(best);
+            for (int v = 1; v < V; ++v) best = fmaxf(best, x[v]);
+            best = group_max<L>(best);
+            const bool found = best > -INFINITY;
+            uint32_t e = 0xffffffffu;
+#pragma unroll
+            for (int v = V - 1; v >= 0; --v) e = x[v] == best ? (uint32_t)(in + L * v) : e;   // (0 and -0 are equal)
+            e = group_min<L>(e);
             if (j == 0) {
-                most = x;
-                if (!a.norm && best) {
+                most = best;
+                if (!a.norm && found) {
 #pragma unroll
-                    for (int v = 0; v < V; ++v) all += key[v] ? term_of(logit_of(key[v]), most) : 0.0f;
+                    for (int v = 0; v < V; ++v) all += x[v] > -INFINITY ? term_of(x[v], most) : 0.0f;
                     all = group_sum<L>(all);
                 }
             }
-            const float term = best ? term_of(x, most) : 0.0f;
+            const float term = found ? term_of(best, most) : 0.0f;
             sum += term;
-            if (in == j) { mine = term; expert = best ? (int)~(uint32_t)best : -1; }
+            if (in == j) { mine = term; expert = found ? (int)e : -1; }
 #pragma unroll
-            for (int v = 0; v < V; ++v) key[v] = key[v] == best ? 0 : key[v];
+            for (int v = 0; v < V; ++v) x[v] = e == (uint32_t)(in + L * v) ? -INFINITY : x[v];
         }
         if (in < a.k) {
             const int64_t at = t * a.k + in;
@@ -256,22 +254,20 @@ __global__ void __launch_bounds__(1024) route_choose_kernel(const RouteArgs a, c
     }
     __syncthreads();
     const int64_t pairs = (int64_t)a.T * a.k;
-    if (tid < 64) place_pairs(a, chosen_lds, 0, pairs, base);
-    else
-        for (int64_t r = *rows + tid - 64; r < pairs; r += 1024 - 64) a.tokens[r] = -1;
+    place_pairs(a, chosen_lds, 0, pairs, base, chosen_lds + RT_TOKENS * a.k);
+    for (int64_t r = *rows + tid; r < pairs; r += 1024) a.tokens[r] = -1;
 }
 
 __global__ void __launch_bounds__(1024) route_place_kernel(const RouteArgs a, const int block_tokens)
 {
-    extern __shared__ int route_lds[];   // E bases, E totals, the number of rows
+    extern __shared__ int route_lds[];   // E bases, E totals, the number of rows, what place_pairs needs
     const int rows = place_bases(a, a.counts, gridDim.x, blockIdx.x, route_lds, route_lds + a.E, route_lds + 2 * a.E);
     const int64_t pairs = (int64_t)a.T * a.k;
     const int64_t first = (int64_t)blockIdx.x * block_tokens * a.k;
     const int64_t last = first + (int64_t)block_tokens * a.k < pairs ? first + (int64_t)block_tokens * a.k : pairs;
-    if (threadIdx.x < 64) place_pairs(a, a.experts + first, first, last, route_lds);
-    else
-        // rows that no pair has
-        for (int64_t r = rows + (int64_t)blockIdx.x * (1024 - 64) + threadIdx.x - 64; r < pairs; r += (int64_t)gridDim.x * (1024 - 64)) a.tokens[r] = -1;
+    place_pairs(a, a.experts + first, first, last, route_lds, route_lds + 2 * a.E + 1);
+    // rows that no pair has
+    for (int64_t r = rows + (int64_t)blockIdx.x * 1024 + threadIdx.x; r < pairs; r += (int64_t)gridDim.x * 1024) a.tokens[r] = -1;
 }
 
 // dx = p (up - sum p up), up: the weights' gradients at the chosen experts; p: the weights (norm) or the softmax over all.
@@ -329,13 +325,14 @@ static hipError_t launch_choose(const RouteArgs &a, hipStream_t s)
 {
     const int64_t block_tokens = tokens_of_a_block(a.T), blocks = route_blocks(a.T);
     const bool alone = blocks == 1 && block_tokens == RT_TOKENS;
-    const size_t lds = alone ? (2 * (size_t)a.E + 1 + RT_TOKENS * (size_t)a.k) * 4 : (size_t)a.E * 4;
+    const size_t seen = (RT_SEEN / a.E < 16 ? RT_SEEN / a.E : 16) * (size_t)a.E;
+    const size_t lds = alone ? (2 * (size_t)a.E + 1 + RT_TOKENS * (size_t)a.k + seen) * 4 : (size_t)a.E * 4;
     if (forced_launch_failure()) return hipErrorLaunchFailure;
     route_choose_kernel<TYPE, L, V><<<dim3((unsigned)blocks), dim3(1024), lds, s>>>(a, (int)block_tokens, alone ? 1 : 0);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || alone) return e;
     if (forced_launch_failure()) return hipErrorLaunchFailure;
-    route_place_kernel<<<dim3((unsigned)blocks), dim3(1024), (2 * (size_t)a.E + 1) * 4, s>>>(a, (int)block_tokens);
+    route_place_kernel<<<dim3((unsigned)blocks), dim3(1024), (2 * (size_t)a.E + 1 + seen) * 4, s>>>(a, (int)block_tokens);
     return hipGetLastError();
 }
 template <int TYPE>
