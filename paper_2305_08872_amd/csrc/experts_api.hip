@@ -112,22 +112,35 @@ static const char *const kFp8Names[EXPERTS_TILES] = {"mm_fp8_256x256", "mm_fp8_1
                                                      "mm_fp8_64x64_k2", "mm_fp8_16x32"};
 
 // The weights' gradients: tiles, and the parts that a group's rows are summed in.  A part is a workgroup of its own that
-// writes its fp32 sums to the workspace, so there are only as many as bring the workgroups to two per compute unit, of at
-// least 512 rows of an average group each, and as the workspace holds.
-static int sums_tile(int64_t rows_r, int64_t cols_r, int64_t G)
+// writes its fp32 sums to the workspace, which a second kernel adds up: worth it where few outputs have many rows.  The estimate is
+// of the same kind as tile_us: a workgroup's stages of 64 rows and its start (stores among it), what the L2s
+// supply, what memory takes.
+struct SumsPlan {
+    int tile, parts;
+};
+static SumsPlan sums_plan(int64_t rows_r, int64_t cols_r, int64_t G, int64_t M, int out_bytes, size_t bytes)
 {
-    const int64_t tiles = ((rows_r + 255) / 256) * ((cols_r + 255) / 256) * G;
-    return tiles >= compute_units() ? EXPERTS_256x256 : EXPERTS_128x128;
-}
-static int64_t sums_parts(int tile, int64_t rows_r, int64_t cols_r, int64_t G, int64_t M, size_t bytes)
-{
-    const int64_t bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
-    const int64_t tiles = ((rows_r + bm - 1) / bm) * ((cols_r + bn - 1) / bn) * G;
-    int64_t parts = 2 * (int64_t)compute_units() / tiles;
-    const int64_t most = M / (512 * G), room = (int64_t)(bytes / 4 / (size_t)(bm * bn)) / tiles;
-    if (parts > most) parts = most;
-    if (parts > room) parts = room;
-    return parts < 1 ? 1 : parts;
+    static const struct { int tile; double stage, start; int resident; } kinds[3] = {{EXPERTS_256x256, 1.5, 14.0, 1}, {EXPERTS_128x128, 0.75, 4.5, 2}, {EXPERTS_64x64, 0.36, 2.2, 3}};
+    const double units = compute_units();
+    SumsPlan best = {EXPERTS_128x128, 1};
+    double least = -1.0;
+    for (const auto &k : kinds) {
+        const int64_t bm = kExpertsTileRows[k.tile], bn = kExpertsTileCols[k.tile];
+        const int64_t tiles = ((rows_r + bm - 1) / bm) * ((cols_r + bn - 1) / bn) * G;
+        const int64_t room = (int64_t)(bytes / 4 / (size_t)(bm * bn)) / tiles, most = M / (256 * G) < room ? M / (256 * G) : room;
+        for (int64_t parts = 1; parts == 1 || (parts <= most && parts <= 64 && tiles * parts <= 4 * k.resident * (int64_t)units); parts += parts < 8 ? 1 : 4) {
+            const double groups = (double)tiles * parts, stages = (double)((M + G * parts * 64 - 1) / (G * parts * 64));
+            const double rounds = groups <= units * k.resident ? 1.0 : groups / (units * k.resident);
+            const double alone = rounds * (stages * k.stage + k.start);
+            const double supply = groups / units * stages * (double)(bm + bn) * 0.128 / 64.0;
+            const double memory = ((double)M * (rows_r + cols_r) * 2.0 + (double)G * rows_r * cols_r * out_bytes) / 4.5e6;
+            double us = alone > supply ? alone : supply;
+            us = (us > memory ? us : memory) + 0.03 * (alone + supply);
+            if (parts > 1) us += 4.0 + (double)tiles * bm * bn * 4.0 * parts / 4.5e6;
+            if (least < 0 || us < least) { least = us; best = {k.tile, (int)parts}; }
+        }
+    }
+    return best;
 }
 
 }  // namespace amulet
@@ -250,10 +263,10 @@ int amulet_grouped_mm(int type, int out_type, int trans_b, int64_t M, int64_t N,
 size_t amulet_grouped_mm_wgrad_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t G)
 {
     if (M <= 0 || N <= 0 || K <= 0 || G <= 0 || M > kMostRows || N > kMostRows || K > kMostRows || G > kMostGroups) return 0;
-    const int tile = sums_tile(K, N, G);
-    const int64_t bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
-    const int64_t tiles = ((K + bm - 1) / bm) * ((N + bn - 1) / bn) * G, parts = sums_parts(tile, K, N, G, M, ~(size_t)0 >> 1);
-    return parts < 2 ? 0 : (size_t)(tiles * parts * bm * bn * 4);
+    SumsPlan plan = sums_plan(K, N, G, M, 2, ~(size_t)0 >> 1);
+    const int64_t bm = kExpertsTileRows[plan.tile], bn = kExpertsTileCols[plan.tile];
+    const int64_t tiles = ((K + bm - 1) / bm) * ((N + bn - 1) / bn) * G;
+    return plan.parts < 2 ? 0 : (size_t)(tiles * plan.parts * bm * bn * 4);
 }
 
 int amulet_grouped_mm_wgrad(int type, int out_type, int trans_r, int64_t M, int64_t N, int64_t K, int64_t G,
@@ -278,14 +291,15 @@ int amulet_grouped_mm_wgrad(int type, int out_type, int trans_r, int64_t M, int6
     // lines of the first operand are R's rows
     if (trans_r) { a.A = D; a.lda = ldd; a.B = A; a.ldb = lda; a.M = (int)N; a.N = (int)K; a.rows_of_b = 1; }
     else { a.A = A; a.lda = lda; a.B = D; a.ldb = ldd; a.M = (int)K; a.N = (int)N; }
-    const int tile = sums_tile(a.M, a.N, G);
     if (((uintptr_t)workspace & 15) != 0) return AMULET_ERR_WORKSPACE;
     a.workspace = (float *)workspace;
-    a.parts = (int)sums_parts(tile, a.M, a.N, G, M, workspace ? workspace_bytes : 0);
+    const SumsPlan plan = sums_plan(a.M, a.N, G, M, out_type == AMULET_FP32 ? 4 : 2, workspace ? workspace_bytes : 0);
+    const int tile = plan.tile;
+    a.parts = plan.parts;
     const int64_t bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
     const int64_t tiles = ((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn) * G;
     if (tiles * a.parts > kMostBlocks || tiles * (bm * bn / 1024) > kMostBlocks) return AMULET_ERR_RANGE;
-    note_kernel(tile == EXPERTS_256x256 ? "grouped_mm_wgrad_256x256" : "grouped_mm_wgrad_128x128", M);
+    note_kernel(tile == EXPERTS_256x256 ? "grouped_mm_wgrad_256x256" : tile == EXPERTS_128x128 ? "grouped_mm_wgrad_128x128" : "grouped_mm_wgrad_64x64", M);
     hipStream_t s = (hipStream_t)stream;
     const int rc = launch_status(launch_experts_sums(type, tile, a, (tiles * a.parts + 7) / 8 * 8, s));
     if (rc != AMULET_OK || a.parts == 1) return rc;

@@ -42,7 +42,7 @@ hipError_t launch_experts_rows_fp16(int tile, bool b_across, const ExpertsArgs &
 hipError_t launch_experts_rows_fp8(int tile, bool b_across, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
 // ... for results of 32 bits; no 256 x 256 tile
 hipError_t launch_experts_rows_fp8_exact(int tile, bool b_across, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
-// by sums: tile EXPERTS_256x256 or EXPERTS_128x128
+// by sums: tile EXPERTS_256x256, EXPERTS_128x128 or EXPERTS_64x64
 hipError_t launch_experts_sums(int type, int tile, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
 // R = the parts' sums, added up in order
 hipError_t launch_experts_join(int tile, const ExpertsArgs &a, hipStream_t s);

@@ -8,8 +8,10 @@ template <int ELEM>
 static hipError_t launch_sums(int tile, const ExpertsArgs &a, int64_t blocks, hipStream_t s)
 {
     typedef ExpertTile<ELEM, 256, 256, 2, 4, 1, 2, 128, true, true> Large;
-    typedef ExpertTile<ELEM, 128, 128, 2, 2, 1, 2, 128, true, true> Small;
+    typedef ExpertTile<ELEM, 128, 128, 2, 2, 1, 2, 128, true, true> Middle;
+    typedef ExpertTile<ELEM, 64, 64, 2, 2, 1, 3, 128, true, true> Small;
     if (tile == EXPERTS_256x256) return launch_experts<Large, experts_sums_kernel<Large>>(a, blocks, s);
+    if (tile == EXPERTS_128x128) return launch_experts<Middle, experts_sums_kernel<Middle>>(a, blocks, s);
     return launch_experts<Small, experts_sums_kernel<Small>>(a, blocks, s);
 }
 
@@ -26,13 +28,15 @@ __global__ void __launch_bounds__(256) experts_join_kernel(const ExpertsArgs a, 
     const int at = (int)(blockIdx.x % per) * 1024 + (int)threadIdx.x * 4;
     const int64_t tiles = (int64_t)tiles_m * tiles_n;
     const int g = (int)(tile / tiles), in = (int)(tile % tiles);
-    const int i = in / tiles_n * bm + at / bn, c = in % tiles_n * bn + at % bn;
-    if (i >= a.M || c >= a.N) return;
+    // (tiles at the edge are moved back: experts_sums_kernel)
+    const int from_m = in / tiles_n * bm, from_n = in % tiles_n * bn;
+    const int i = inside(from_m, bm, a.M) + at / bn, c = inside(from_n, bn, a.N) + at % bn;
+    if (i < from_m || i >= a.M) return;
     const float *ws = a.workspace + tile * a.parts * (int64_t)(bm * bn) + at;
     xt_f4 sum = *(const xt_f4 *)ws;
     for (int p = 1; p < a.parts; ++p) sum += *(const xt_f4 *)(ws + (int64_t)p * bm * bn);
     const float x[4] = {sum[0], sum[1], sum[2], sum[3]};
-    store_out<4>(a.R, a.out, (int64_t)g * a.group_r + (int64_t)i * a.ldr, c, a.N, x);
+    store_out<4>(a.R, a.out, (int64_t)g * a.group_r + (int64_t)i * a.ldr, c, from_n, a.N, x);
 }
 
 hipError_t launch_experts_join(int tile, const ExpertsArgs &a, hipStream_t s)

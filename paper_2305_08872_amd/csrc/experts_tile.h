@@ -369,19 +369,25 @@ __device__ __forceinline__ xt_u4 bf16_of(xt_u4 x, int half)
     return y;
 }
 
-// `v` consecutive values of R from column c on, of which those below `cols` exist; rounded once, to the output's type.
+// V consecutive values of R from column c on, those of columns `from` to `cols` - 1; rounded once, to the output's type.
+// (Vector stores whatever the address: 5 x 2341 x 457 over 33 groups, rows at odd multiples of two bytes.)
 template <int V>
-__device__ __forceinline__ void store_out(void *R, int out, int64_t row_at, int c, int cols, const float *x)
+__device__ __forceinline__ void store_out(void *R, int out, int64_t row_at, int c, int from, int cols, const float *x)
 {
+    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+    typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+    typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
+    if (c >= cols || c + V <= from) return;
+    const bool whole = c >= from && c + V <= cols;
     if (out == EXPERTS_FP32) {
         float *p = (float *)R + row_at + c;
-        if (c + V <= cols && ((uintptr_t)p & 15) == 0) {
+        if (whole) {
 #pragma unroll
-            for (int i = 0; i < V; i += 4) *(xt_f4 *)(p + i) = xt_f4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+            for (int i = 0; i < V; i += 4) *(f4 *)(p + i) = f4{x[i], x[i + 1], x[i + 2], x[i + 3]};
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (c + i < cols) p[i] = x[i];
+                if (c + i >= from && c + i < cols) p[i] = x[i];
         }
         return;
     }
@@ -399,13 +405,13 @@ __device__ __forceinline__ void store_out(void *R, int out, int64_t row_at, int 
         w[i / 2] = lo | ((uint32_t)hi << 16);
     }
     uint16_t *p = (uint16_t *)R + row_at + c;
-    if (c + V <= cols && ((uintptr_t)p & (2 * V - 1)) == 0) {
-        if constexpr (V == 8) *(xt_u4 *)p = xt_u4{w[0], w[1], w[2], w[3]};
-        else *(xt_u2 *)p = xt_u2{w[0], w[1]};
+    if (whole) {
+        if constexpr (V == 8) *(u4 *)p = u4{w[0], w[1], w[2], w[3]};
+        else *(u2 *)p = u2{w[0], w[1]};
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (c + i < cols) p[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+            if (c + i >= from && c + i < cols) p[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
     }
 }
 
@@ -815,6 +821,49 @@ __device__ __forceinline__ int col_of(int ni, int lane)
 {
     return T::PERM ? (ni >> 1) * 32 + 8 * (lane >> 4) + 4 * (ni & 1) : ni * 16 + 4 * (lane >> 4);
 }
+// Row blocks mi of a wave's sums into R: row i of R at element row_at(mi), columns col0 + ..., those from `from` to N - 1.  Two
+// fragments at a time: a lane's columns of both are 8 in a row, as they lie (PERM) or after the odd groups of 16 lanes have
+// exchanged their first fragment's for their neighbours' second's.
+template <class T, class RowAt>
+__device__ __forceinline__ void store_sums(const xt_f4 (&acc)[T::MI][T::NI], void *R, int out, int lane, int col0, int from, int N, RowAt row_at)
+{
+#pragma unroll
+    for (int mi = 0; mi < T::MI; ++mi) {
+        const int64_t at = row_at(mi);
+        if constexpr (T::NI % 2 == 0) {
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ni += 2) {
+                float x[8];
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    x[v] = acc[mi][ni][v];
+                    x[4 + v] = acc[mi][ni + 1][v];
+                    if constexpr (!T::PERM) {
+                        const auto y = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x[v]), __builtin_bit_cast(uint32_t, x[4 + v]), false, false);
+                        const uint32_t lo = y[0], hi = y[1];
+                        x[v] = __builtin_bit_cast(float, lo);
+                        x[4 + v] = __builtin_bit_cast(float, hi);
+                    }
+                }
+                const int c = col0 + (T::PERM ? col_of<T>(ni, lane) : ni * 16 + 16 * ((lane >> 4) & 1) + 8 * (lane >> 5));
+                if (at >= 0) store_out<8>(R, out, at, c, from, N, x);
+            }
+        } else {
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ++ni) {
+                const float x[4] = {acc[mi][ni][0], acc[mi][ni][1], acc[mi][ni][2], acc[mi][ni][3]};
+                if (at >= 0) store_out<4>(R, out, at, col0 + col_of<T>(ni, lane), from, N, x);
+            }
+        }
+    }
+}
+
+// First line of a tile of n lines from `first` on, moved back so that it ends at the last one of an operand that is at least
+// as long: lines stored across k then never end inside a unit.  (8-bit products do not: their blocks' scales are a wave's.)
+__device__ __forceinline__ int inside(int first, int n, int lines)
+{
+    return first + n <= lines || lines < n ? first : lines - n;
+}
 
 template <class T>
 __global__ void __launch_bounds__(T::NT) experts_rows_kernel(const ExpertsArgs a)
@@ -826,7 +875,8 @@ __global__ void __launch_bounds__(T::NT) experts_rows_kernel(const ExpertsArgs a
     const int tiles_n = (a.N + T::BN - 1) / T::BN;
     RowTile t;
     if (!find_row_tile<T::BM>(a, tiles_n, blockIdx.x, t)) return;
-    const int row0 = t.row0 + t.tm * T::BM, col0 = t.tn * T::BN;
+    const int row0 = t.row0 + t.tm * T::BM, from = t.tn * T::BN;   // (columns from `from` on are this tile's)
+    const int col0 = T::BKS && !T::FP8 ? inside(from, T::BN, a.N) : from;
     const int wm = wave / T::WN, wn = wave % T::WN;
 
     xt_f4 acc[T::MI][T::NI];
@@ -857,22 +907,19 @@ __global__ void __launch_bounds__(T::NT) experts_rows_kernel(const ExpertsArgs a
     }
     if (!tile_sums<T>(sa, sb, 0, K, wave, kg, lane, a_row, !a.rows, scales, row0 + wm * (T::BM / T::WM) >= t.row1, acc)) return;
 
+    if (a.rows)
 #pragma unroll
-    for (int mi = 0; mi < T::MI; ++mi) {
-        const int i = row0 + wm * (T::BM / T::WM) + mi * 16 + (lane & 15);
-        if (i >= t.row1) continue;
-        const bool there = !a.rows || (unsigned)a.rows[i] < (unsigned)a.a_rows;
-        const int64_t at = (int64_t)i * a.ldr;
+        for (int mi = 0; mi < T::MI; ++mi) {
+            const int i = row0 + wm * (T::BM / T::WM) + mi * 16 + (lane & 15);
+            if (i < t.row1 && (unsigned)a.rows[i] >= (unsigned)a.a_rows) {
 #pragma unroll
-        for (int ni = 0; ni < T::NI; ni += T::PERM ? 2 : 1) {
-            constexpr int V = T::PERM ? 8 : 4;
-            float x[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) x[v] = there ? acc[mi][ni + v / 4][v % 4] : 0.0f;
-            const int c = col0 + wn * (T::BN / T::WN) + col_of<T>(ni, lane);
-            if (c < a.N) store_out<V>(a.R, a.out, at, c, a.N, x);
+                for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = xt_f4{0, 0, 0, 0};
+            }
         }
-    }
+    store_sums<T>(acc, a.R, a.out, lane, col0 + wn * (T::BN / T::WN), from, a.N, [&](int mi) -> int64_t {
+        const int i = row0 + wm * (T::BM / T::WM) + mi * 16 + (lane & 15);
+        return i < t.row1 ? (int64_t)i * a.ldr : -1;
+    });
 }
 
 // The weights' gradients: k runs over a group's rows, lines of A are columns of its storage, lines of B of D's.  grid: parts x tiles x groups.
@@ -895,7 +942,8 @@ __global__ void __launch_bounds__(T::NT) experts_sums_kernel(const ExpertsArgs a
     const int in = (int)(at - piece * tiles);
     const int panel = in / (8 * tiles_n), high = tiles_m - panel * 8 < 8 ? tiles_m - panel * 8 : 8, rem = in - panel * 8 * tiles_n;
     const int tm = panel * 8 + rem % high, tn = rem / high;
-    const int m0 = tm * T::BM, n0 = tn * T::BN;
+    const int from_m = tm * T::BM, from_n = tn * T::BN;   // (rows and columns from here on are this tile's)
+    const int m0 = inside(from_m, T::BM, a.M), n0 = inside(from_n, T::BN, a.N);
 
     const int lo = clamp_row(a.offsets[g], a.k_rows), hi = clamp_row(a.offsets[g + 1], a.k_rows);
     const int k_all = hi > lo ? hi - lo : 0;
@@ -916,29 +964,15 @@ __global__ void __launch_bounds__(T::NT) experts_sums_kernel(const ExpertsArgs a
     const int wm = wave / T::WN, wn = wave % T::WN;
     if (a.parts > 1) {
         float *const ws = a.workspace + ((int64_t)(g * tiles + (int64_t)tm * tiles_n + tn) * a.parts + part) * (T::BM * T::BN);
-#pragma unroll
-        for (int mi = 0; mi < T::MI; ++mi)
-#pragma unroll
-            for (int ni = 0; ni < T::NI; ++ni) {
-                const int i = wm * (T::BM / T::WM) + mi * 16 + (lane & 15), c = wn * (T::BN / T::WN) + col_of<T>(ni, lane);
-                *(xt_f4 *)(ws + i * T::BN + c) = acc[mi][ni];
-            }
+        store_sums<T>(acc, ws, EXPERTS_FP32, lane, wn * (T::BN / T::WN), 0, T::BN, [&](int mi) -> int64_t {
+            return (int64_t)(wm * (T::BM / T::WM) + mi * 16 + (lane & 15)) * T::BN;
+        });
         return;
     }
-#pragma unroll
-    for (int mi = 0; mi < T::MI; ++mi) {
+    store_sums<T>(acc, a.R, a.out, lane, n0 + wn * (T::BN / T::WN), from_n, a.N, [&](int mi) -> int64_t {
         const int i = m0 + wm * (T::BM / T::WM) + mi * 16 + (lane & 15);
-        if (i >= a.M) continue;
-        const int64_t row_at = (int64_t)g * a.group_r + (int64_t)i * a.ldr;
-#pragma unroll
-        for (int ni = 0; ni < T::NI; ++ni) {
-            float x[4];
-#pragma unroll
-            for (int v = 0; v < 4; ++v) x[v] = acc[mi][ni][v];
-            const int c = n0 + wn * (T::BN / T::WN) + col_of<T>(ni, lane);
-            if (c < a.N) store_out<4>(a.R, a.out, row_at, c, a.N, x);
-        }
-    }
+        return i >= from_m && i < a.M ? (int64_t)g * a.group_r + (int64_t)i * a.ldr : -1;
+    });
 }
 
 // (the kernel is a template argument: what it was granted is kept once for each)
