@@ -298,10 +298,10 @@ int amulet_grouped_mm_wgrad(int type, int out_type, int trans_r, int64_t M, int6
     a.parts = plan.parts;
     const int64_t bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
     const int64_t tiles = ((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn) * G;
-    if (tiles * a.parts > kMostBlocks || tiles * (bm * bn / 1024) > kMostBlocks) return AMULET_ERR_RANGE;
+    if (sums_blocks(tiles / G, G * a.parts) > kMostBlocks || tiles * (bm * bn / 1024) > kMostBlocks) return AMULET_ERR_RANGE;
     note_kernel(tile == EXPERTS_256x256 ? "grouped_mm_wgrad_256x256" : tile == EXPERTS_128x128 ? "grouped_mm_wgrad_128x128" : "grouped_mm_wgrad_64x64", M);
     hipStream_t s = (hipStream_t)stream;
-    const int rc = launch_status(launch_experts_sums(type, tile, a, (tiles * a.parts + 7) / 8 * 8, s));
+    const int rc = launch_status(launch_experts_sums(type, tile, a, sums_blocks(tiles / G, G * a.parts), s));
     if (rc != AMULET_OK || a.parts == 1) return rc;
     return launch_status(launch_experts_join(tile, a, s));
 }

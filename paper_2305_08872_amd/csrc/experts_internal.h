@@ -44,6 +44,12 @@ hipError_t launch_experts_rows_fp8(int tile, bool b_across, const ExpertsArgs &a
 hipError_t launch_experts_rows_fp8_exact(int tile, bool b_across, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
 // by sums: tile EXPERTS_256x256, EXPERTS_128x128 or EXPERTS_64x64
 hipError_t launch_experts_sums(int type, int tile, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
+// how its workgroups share the tiles of a group out over the XCDs, and how many there are of them
+__host__ __device__ inline bool sums_by_group(int64_t tiles_of_a_group) { return tiles_of_a_group >= 32; }
+inline int64_t sums_blocks(int64_t tiles_of_a_group, int64_t pieces)
+{
+    return 8 * (sums_by_group(tiles_of_a_group) ? (tiles_of_a_group + 7) / 8 * pieces : (tiles_of_a_group * pieces + 7) / 8);
+}
 // R = the parts' sums, added up in order
 hipError_t launch_experts_join(int tile, const ExpertsArgs &a, hipStream_t s);
 

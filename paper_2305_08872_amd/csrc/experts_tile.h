@@ -421,14 +421,34 @@ struct RowTile {
     int group, row0, row1, tm, tn;
 };
 __device__ __forceinline__ int clamp_row(int x, int M) { return x < 0 ? 0 : x > M ? M : x; }
-template <int BM>
-__device__ __forceinline__ bool find_row_tile(const ExpertsArgs &a, int tiles_n, int block, RowTile &t)
+// Tile `in` of a region of `high_all` row tiles: panels of 8 row tiles, column by column.  (Unsigned 32-bit divisions: a grid
+// has fewer than 2^23 workgroups.)
+__device__ __forceinline__ void tile_in_region(uint32_t in, uint32_t high_all, uint32_t tiles_n, int &tm, int &tn)
 {
+    const uint32_t panel = in / (8 * tiles_n), rem = in - panel * 8 * tiles_n;
+    const uint32_t high = high_all - panel * 8 < 8 ? high_all - panel * 8 : 8, col = rem / high;
+    tm = (int)(panel * 8 + rem - col * high);
+    tn = (int)col;
+}
+template <int BM>
+__device__ __forceinline__ bool find_row_tile(const ExpertsArgs &a, int tiles_n, uint32_t block, RowTile &t)
+{
+    // XCD x (workgroup b runs on XCD b % 8) takes an eighth of the tiles, neighbours in the order of regions
+    const uint32_t xcd = block & 7, slot = block >> 3;
+    if (!a.offsets) {
+        const uint32_t high = (uint32_t)(a.M + BM - 1) / BM, tiles = high * (uint32_t)tiles_n;
+        const uint32_t begin = (uint32_t)((uint64_t)tiles * xcd >> 3), end = (uint32_t)((uint64_t)tiles * (xcd + 1) >> 3);
+        if (slot >= end - begin) return false;
+        t.group = 0;
+        t.row0 = 0;
+        t.row1 = a.M;
+        tile_in_region(begin + slot, high, (uint32_t)tiles_n, t.tm, t.tn);
+        return true;
+    }
     const int lane = threadIdx.x & 63;
-    const int regions = a.offsets ? a.G + 2 : 1;
+    const int regions = a.G + 2;
     auto region = [&](int g, int &lo, int &hi) {
-        if (!a.offsets) { lo = 0; hi = g == 0 ? a.M : 0; }
-        else if (g < a.G) { lo = clamp_row(a.offsets[g], a.M); hi = clamp_row(a.offsets[g + 1], a.M); }
+        if (g < a.G) { lo = clamp_row(a.offsets[g], a.M); hi = clamp_row(a.offsets[g + 1], a.M); }
         else if (g == a.G) { lo = 0; hi = clamp_row(a.offsets[0], a.M); }
         else if (g == a.G + 1) { lo = clamp_row(a.offsets[a.G], a.M); hi = a.M; }
         else lo = hi = 0;
@@ -444,49 +464,36 @@ __device__ __forceinline__ bool find_row_tile(const ExpertsArgs &a, int tiles_n,
         }
         return sum;
     };
-    int lo, hi, n, total = 0;
+    int lo, hi, n;
     int first = scan(0, lo, hi, n);
-    total = __shfl(first, 63);
+    uint32_t total = (uint32_t)__builtin_amdgcn_readlane(first, 63);
     for (int c = 64; c < regions; c += 64) {
         int l2, h2, n2;
-        total += __shfl(scan(c, l2, h2, n2), 63);
+        total += (uint32_t)__builtin_amdgcn_readlane(scan(c, l2, h2, n2), 63);
     }
-    // XCD x (workgroup b runs on XCD b % 8) takes an eighth of the tiles, neighbours in the order below
-    const int64_t tiles = (int64_t)total * tiles_n;
-    const int xcd = block & 7, slot = block >> 3;
-    const int64_t begin = tiles * xcd / 8, end = tiles * (xcd + 1) / 8;
+    const uint64_t tiles = (uint64_t)total * (uint32_t)tiles_n;
+    const uint32_t begin = (uint32_t)(tiles * xcd >> 3), end = (uint32_t)(tiles * (xcd + 1) >> 3);
     if (slot >= end - begin) return false;
-    const int64_t at = begin + slot;
+    const uint32_t at = begin + slot;
     // the region that holds tile `at`
-    int before = 0, c = 0;
+    uint32_t before = 0;
+    int c = 0;
     for (;;) {
-        const uint64_t past = __ballot((int64_t)(before + first) * tiles_n > at);
+        const uint64_t past = __ballot((uint64_t)(before + (uint32_t)first) * (uint32_t)tiles_n > at);
         if (past) {
             const int l = __builtin_ctzll(past);
-            const int nl = __shfl(n, l), upto = __shfl(first, l);
-            t.group = c + l;
-            t.row0 = __shfl(lo, l);
-            t.row1 = __shfl(hi, l);
-            // within a region: panels of 8 row tiles, column by column
-            const int64_t in = at - (int64_t)(before + upto - nl) * tiles_n;
-            const int panel = (int)(in / (8 * (int64_t)tiles_n));
-            const int high = nl - panel * 8 < 8 ? nl - panel * 8 : 8;
-            const int rem = (int)(in - (int64_t)panel * 8 * tiles_n);
-            t.tm = panel * 8 + rem % high;
-            t.tn = rem / high;
-            break;
+            const uint32_t nl = (uint32_t)__builtin_amdgcn_readlane(n, l), upto = (uint32_t)__builtin_amdgcn_readlane(first, l);
+            t.group = c + l < a.G ? c + l : -1;
+            t.row0 = __builtin_amdgcn_readlane(lo, l);
+            t.row1 = __builtin_amdgcn_readlane(hi, l);
+            tile_in_region(at - (before + upto - nl) * (uint32_t)tiles_n, nl, (uint32_t)tiles_n, t.tm, t.tn);
+            return true;
         }
-        before += __shfl(first, 63);
+        before += (uint32_t)__builtin_amdgcn_readlane(first, 63);
         c += 64;
+        if (c >= regions) return false;   // (never: the tiles counted above are there)
         first = scan(c, lo, hi, n);
     }
-    t.group = __builtin_amdgcn_readfirstlane(t.group);
-    t.row0 = __builtin_amdgcn_readfirstlane(t.row0);
-    t.row1 = __builtin_amdgcn_readfirstlane(t.row1);
-    t.tm = __builtin_amdgcn_readfirstlane(t.tm);
-    t.tn = __builtin_amdgcn_readfirstlane(t.tn);
-    if (t.group >= a.G) t.group = -1;
-    return true;
 }
 
 // A wave's products of one stage, in steps: 16 bits: each instruction's k times halves of the wave's rows; 8 bits: one or two row
@@ -932,16 +939,28 @@ __global__ void __launch_bounds__(T::NT) experts_sums_kernel(const ExpertsArgs a
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), kg = w / T::NW, wave = w % T::NW;
     const int tiles_m = (a.M + T::BM - 1) / T::BM, tiles_n = (a.N + T::BN - 1) / T::BN;
-    const int64_t tiles = (int64_t)tiles_m * tiles_n, all = tiles * a.G * a.parts;
-    // an eighth of the work to each XCD; within a group and part: panels of 8 row tiles, column by column
-    const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
-    const int64_t begin = all * xcd / 8, end = all * (xcd + 1) / 8;
-    if (slot >= end - begin) return;
-    const int64_t at = begin + slot, piece = at / tiles;
-    const int g = (int)(piece / a.parts), part = (int)(piece % a.parts);
-    const int in = (int)(at - piece * tiles);
-    const int panel = in / (8 * tiles_n), high = tiles_m - panel * 8 < 8 ? tiles_m - panel * 8 : 8, rem = in - panel * 8 * tiles_n;
-    const int tm = panel * 8 + rem % high, tn = rem / high;
+    const uint32_t tiles = (uint32_t)tiles_m * (uint32_t)tiles_n;
+    // Within a group and part: panels of 8 row tiles, column by column.  An eighth of every group's tiles to each XCD where a
+    // group has many (groups have unequal rows: 16384 rows over 16 groups of 2048 x 4096 450 us with an eighth of the groups to each, 396
+    // so), an eighth of all tiles where it has few.
+    const uint32_t xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, pieces = (uint32_t)a.G * (uint32_t)a.parts;
+    uint32_t piece, in;
+    if (sums_by_group(tiles)) {
+        const uint32_t per = (tiles + 7) / 8;
+        piece = slot / per;
+        const uint32_t off = slot - piece * per, x = (xcd + piece) & 7, first = tiles * x / 8, last = tiles * (x + 1) / 8;
+        if (piece >= pieces || off >= last - first) return;
+        in = first + off;
+    } else {
+        const uint64_t all = (uint64_t)tiles * pieces;
+        const uint32_t begin = (uint32_t)(all * xcd >> 3), end = (uint32_t)(all * (xcd + 1) >> 3);
+        if (slot >= end - begin) return;
+        piece = (begin + slot) / tiles;
+        in = begin + slot - piece * tiles;
+    }
+    const int g = (int)(piece / (uint32_t)a.parts), part = (int)(piece - (uint32_t)g * (uint32_t)a.parts);
+    int tm, tn;
+    tile_in_region(in, (uint32_t)tiles_m, (uint32_t)tiles_n, tm, tn);
     const int from_m = tm * T::BM, from_n = tn * T::BN;   // (rows and columns from here on are this tile's)
     const int m0 = inside(from_m, T::BM, a.M), n0 = inside(from_n, T::BN, a.N);
 
