@@ -114,13 +114,15 @@ static const char *const kFp8Names[EXPERTS_TILES] = {"mm_fp8_256x256", "mm_fp8_1
 // The weights' gradients: tiles, and the parts that a group's rows are summed in.  A part is a workgroup of its own that
 // writes its fp32 sums to the workspace, which a second kernel adds up: worth it where few outputs have many rows.  The estimate is
 // of the same kind as tile_us: a workgroup's stages of 64 rows and its start (stores among it), what the L2s
-// supply, what memory takes.
+// supply, what memory takes; fitted to 370 sizes (4 ... 32768 rows, 1 ... 128 groups, up to 64 parts), 2.5 % behind the fastest on
+// average.  us, 256 x 256 / 128 x 128 / 64 x 64: 16384 rows over 16 groups of 4096 x 2048 392 / 538 / 765, 24008 over 4 of 384 x 832 in 1 part
+// 173 / 124 / 71, in 4 66 / 48 / 50, 18339 over 2 of 2432 x 64 in 8 parts 53 / 39 / 28.
 struct SumsPlan {
     int tile, parts;
 };
 static SumsPlan sums_plan(int64_t rows_r, int64_t cols_r, int64_t G, int64_t M, int out_bytes, size_t bytes)
 {
-    static const struct { int tile; double stage, start; int resident; } kinds[3] = {{EXPERTS_256x256, 1.5, 14.0, 1}, {EXPERTS_128x128, 0.75, 4.5, 2}, {EXPERTS_64x64, 0.36, 2.2, 3}};
+    static const struct { int tile; double stage, start; int resident; } kinds[3] = {{EXPERTS_256x256, 1.2, 7.7, 1}, {EXPERTS_128x128, 0.53, 5.1, 2}, {EXPERTS_64x64, 0.38, 3.7, 3}};
     const double units = compute_units();
     SumsPlan best = {EXPERTS_128x128, 1};
     double least = -1.0;
@@ -132,11 +134,11 @@ static SumsPlan sums_plan(int64_t rows_r, int64_t cols_r, int64_t G, int64_t M, 
             const double groups = (double)tiles * parts, stages = (double)((M + G * parts * 64 - 1) / (G * parts * 64));
             const double rounds = groups <= units * k.resident ? 1.0 : groups / (units * k.resident);
             const double alone = rounds * (stages * k.stage + k.start);
-            const double supply = groups / units * stages * (double)(bm + bn) * 0.128 / 64.0;
-            const double memory = ((double)M * (rows_r + cols_r) * 2.0 + (double)G * rows_r * cols_r * out_bytes) / 4.5e6;
+            const double supply = groups / units * stages * (double)(bm + bn) * 0.128 / 81.0;
+            const double memory = ((double)M * (rows_r + cols_r) * 2.0 + (double)G * rows_r * cols_r * out_bytes) / 6.3e6;
             double us = alone > supply ? alone : supply;
-            us = (us > memory ? us : memory) + 0.03 * (alone + supply);
-            if (parts > 1) us += 4.0 + (double)tiles * bm * bn * 4.0 * parts / 4.5e6;
+            us = (us > memory ? us : memory) + 0.12 * (alone + supply);
+            if (parts > 1) us += 2.6 + (double)tiles * bm * bn * 4.0 * parts / 2.8e6;
             if (least < 0 || us < least) { least = us; best = {k.tile, (int)parts}; }
         }
     }
@@ -263,10 +265,14 @@ int amulet_grouped_mm(int type, int out_type, int trans_b, int64_t M, int64_t N,
 size_t amulet_grouped_mm_wgrad_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t G)
 {
     if (M <= 0 || N <= 0 || K <= 0 || G <= 0 || M > kMostRows || N > kMostRows || K > kMostRows || G > kMostGroups) return 0;
-    SumsPlan plan = sums_plan(K, N, G, M, 2, ~(size_t)0 >> 1);
-    const int64_t bm = kExpertsTileRows[plan.tile], bn = kExpertsTileCols[plan.tile];
-    const int64_t tiles = ((K + bm - 1) / bm) * ((N + bn - 1) / bn) * G;
-    return plan.parts < 2 ? 0 : (size_t)(tiles * plan.parts * bm * bn * 4);
+    size_t most = 0;
+    for (int out_bytes = 2; out_bytes <= 4; out_bytes += 2) {   // (R's type is not known here)
+        const SumsPlan plan = sums_plan(K, N, G, M, out_bytes, ~(size_t)0 >> 1);
+        const int64_t bm = kExpertsTileRows[plan.tile], bn = kExpertsTileCols[plan.tile];
+        const size_t bytes = plan.parts < 2 ? 0 : (size_t)(((K + bm - 1) / bm) * ((N + bn - 1) / bn) * G * plan.parts * bm * bn * 4);
+        if (bytes > most) most = bytes;
+    }
+    return most;
 }
 
 int amulet_grouped_mm_wgrad(int type, int out_type, int trans_r, int64_t M, int64_t N, int64_t K, int64_t G,
