@@ -528,7 +528,10 @@ int amulet_selected_shape(int task, int64_t M, int64_t N, int64_t K);
  * " critical_rows <rows of its tile>" (the rows past its own are a launch of their
  * own, of the tile kernels; of a count with a threshold per row, the columns); and
  * for the fp64 identity task " k_groups <2 or 4>" where so many groups of waves
- * share a tile's K.  The adaptive
+ * share a tile's K.  An operator of a mixture-of-experts layer: its name and
+ * tile (grouped_mm_256x256, ..., _k2: two groups of waves share a tile's k;
+ * grouped_mm_wgrad_..., mm_fp8_..., route, combine_grad, ...) and " rows
+ * <rows or tokens>".  The adaptive
  * calls make one launch per trial and one for the rest.  Static storage of the
  * calling thread, until its next call of this function.
  */
