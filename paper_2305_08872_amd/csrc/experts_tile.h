@@ -512,9 +512,44 @@ struct Steps {
     typedef FragReader<T, T::BN, T::BKS, T::PERM> ReadB;
     static constexpr int U = T::FP8 ? 2 : 1;     // 16-byte halves of a fragment
 
+    // 8 bits, the largest tile: the rows' first half step by step, the second half column by column (stage_split)
+    static constexpr bool SPLIT = T::FP8 && T::MI == 8;
+
     xt_u4 a[2][MA][U];
     xt_u4 b[B2 ? 2 : 1][T::NI][U];
     float w[2][MA];                              // fp8: the rows' scales
+    xt_u4 rest[SPLIT ? T::MI / 2 : 1][U];        // (SPLIT: the second half's fragments and scales)
+    float rest_w[SPLIT ? T::MI / 2 : 1];
+
+    template <int j>
+    __device__ __forceinline__ void read_rest(const ReadA &r, const char *la, const float *scales)
+    {
+        rest[j][0] = r.read(la, T::MI / 2 + j, 0);
+        rest[j][U - 1] = r.read(la, T::MI / 2 + j, 1);
+        rest_w[j] = scales[(T::MI / 2 + j) * 16];
+    }
+    __device__ __forceinline__ void read_b_one(const ReadB &r, const char *lb, int ni)
+    {
+        b[0][ni][0] = r.read(lb, ni, 0);
+        b[0][ni][U - 1] = r.read(lb, ni, 1);
+    }
+    // one instruction of 128 k, added up times f
+    __device__ __forceinline__ void mma_scaled(const xt_u4 *p, const xt_u4 *q, float f, xt_f4 &c)
+    {
+        const xt_f4 zero = {0, 0, 0, 0};
+        xt_f4 x;
+        if constexpr (T::ELEM == EXPERTS_FP8) {
+            const xt_i8 xa = {(int)p[0][0], (int)p[0][1], (int)p[0][2], (int)p[0][3], (int)p[U - 1][0], (int)p[U - 1][1], (int)p[U - 1][2], (int)p[U - 1][3]};
+            const xt_i8 xb = {(int)q[0][0], (int)q[0][1], (int)q[0][2], (int)q[0][3], (int)q[U - 1][0], (int)q[U - 1][1], (int)q[U - 1][2], (int)q[U - 1][3]};
+            x = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(xb, xa, zero, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+        } else {
+            x = zero;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x = mma16<EXPERTS_BF16>(bf16_of(q[u / 2], u % 2), bf16_of(p[u / 2], u % 2), x);
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) c[v] = __builtin_fmaf(f, x[v], c[v]);
+    }
 
     template <int t>
     __device__ __forceinline__ void read_a(const ReadA &r, const char *la, const float *scales)
@@ -554,22 +589,7 @@ struct Steps {
                 xt_f4 &c = acc[t % MSTEPS * MA + m][ni];
                 const xt_u4 *p = a[sa][m], *q = b[sb][ni];
                 if constexpr (!T::FP8) c = mma16<T::ELEM>(q[0], p[0], c);
-                else {
-                    const xt_f4 zero = {0, 0, 0, 0};
-                    xt_f4 x;
-                    if constexpr (T::ELEM == EXPERTS_FP8) {
-                        const xt_i8 xa = {(int)p[0][0], (int)p[0][1], (int)p[0][2], (int)p[0][3], (int)p[U - 1][0], (int)p[U - 1][1], (int)p[U - 1][2], (int)p[U - 1][3]};
-                        const xt_i8 xb = {(int)q[0][0], (int)q[0][1], (int)q[0][2], (int)q[0][3], (int)q[U - 1][0], (int)q[U - 1][1], (int)q[U - 1][2], (int)q[U - 1][3]};
-                        x = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(xb, xa, zero, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
-                    } else {
-                        x = zero;
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) x = mma16<EXPERTS_BF16>(bf16_of(q[u / 2], u % 2), bf16_of(p[u / 2], u % 2), x);
-                    }
-                    const float f = w[sa][m] * wb;
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) c[v] = __builtin_fmaf(f, x[v], c[v]);
-                }
+                else mma_scaled(p, q, w[sa][m] * wb, c);
                 hook(m * T::NI + ni);
             }
     }
@@ -687,6 +707,30 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
         constexpr bool AFTER = decltype(there)::value;
         constexpr int P = decltype(parity)::value, P2 = Steps<T>::PAIRS ? 1 - P : 0;
         const char *const lb = la + T::A_BYTES;
+        if constexpr (Steps<T>::SPLIT) {
+            // The first half of the rows a fragment at a time, the second half's being read meanwhile; then every wave has read
+            // all of the stage, and the second half runs column block by column block: each of B's fragments, of which there is
+            // room for one set, is done with after a quarter of it and read anew.
+            constexpr int H = T::MI / 2;
+            for_each<H>([&](auto t) {
+                constexpr int i = decltype(t)::value;
+                if constexpr (i + 1 < H) f.template read_a<i + 1>(ra, la, scale_row(la));
+                f.template read_rest<i>(ra, la, scale_row(la));
+                f.template mma<0, i>(wb, acc, [](int) {});
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            if constexpr (AFTER) next();
+            for_each<T::NI>([&](auto n) {
+                constexpr int ni = decltype(n)::value;
+                for_each<H>([&](auto t) { f.mma_scaled(f.rest[decltype(t)::value], f.b[0][ni], f.rest_w[decltype(t)::value] * wb, acc[H + decltype(t)::value][ni]); });
+                if constexpr (AFTER) {
+                    f.read_b_one(rb, after + T::A_BYTES, ni);
+                    if constexpr (ni == T::NI - 2) f.template read_a<0>(ra, after, scale_row(after));
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            return;
+        }
 #define AMULET_STEP(t)                                                          \
         if constexpr (t < STEPS) {                                              \
             if constexpr (t + 1 < STEPS) {                                      \
