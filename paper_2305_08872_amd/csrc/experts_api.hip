@@ -8,7 +8,7 @@
 namespace amulet {
 
 static const int64_t kMostRows = 2147483647LL - 65536LL;   // of a dimension, as in the other calls
-static const int64_t kMostGroups = 1 << 20;
+static const int64_t kMostGroups = 1 << 16;              // (every workgroup looks through the offsets)
 static const int64_t kMostBlocks = 0xffffffffLL / 512;     // workgroups of a launch (a grid holds 2^32 - 1 work-items)
 
 // the longest pitch (bytes) of an operand whose tile's lines, or a stage's k, lie within 32 bits of each other: 256 of them
@@ -357,6 +357,7 @@ static int run_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K, i
     const int rc = check_rows(M, N, K, G, trans_b, A, lda, rows, a_rows, B, ldb, group_b, offsets, grouped, R, ldr);
     if (rc != AMULET_OK) return rc > 0 ? AMULET_OK : rc;
     const bool some = K > 0 && G > 0 && !(rows && a_rows == 0);
+    if (some && (rows ? a_rows : M) > (1 << 30)) return AMULET_ERR_RANGE;   // (32-bit byte offsets of a block's scales)
     if (some && (!scales_a || !scales_b)) return AMULET_ERR_NULL;
     if (some && (lds_a < (rows ? a_rows : M) || lds_b < ((trans_b ? K : N) + 127) / 128 || (G > 1 && group_sb < 0))) return AMULET_ERR_LD;
     ExpertsArgs a = {};

@@ -57,6 +57,7 @@ struct ExpertTile {
     static constexpr int A_BYTES = BM * KB, B_BYTES = BN * KB;
     static constexpr int SA_BYTES = FP8 ? (BM < 64 ? 256 : BM * 4) : 0;   // scales of A's rows
     static constexpr int STAGE = A_BYTES + B_BYTES + SA_BYTES;
+    static constexpr bool TURN = BM >= 256 && !AKS && !FP8;   // where the k begin, see tile_sums
     static constexpr int SPREAD = BM >= 256 && !FP8 ? 2 : 0;   // matrix instructions between those of a request
     static constexpr int PREFETCH = BM >= 256 && AKS ? 2 : 0;      // stages further on whose lines are asked for ahead, see tile_sums
     static constexpr int LDS = S * STAGE * WK + (PREFETCH ? 256 : 0);
@@ -427,8 +428,8 @@ __device__ __forceinline__ void tile_in_region(uint32_t in, uint32_t high_all, u
 {
     const uint32_t panel = in / (8 * tiles_n), rem = in - panel * 8 * tiles_n;
     const uint32_t high = high_all - panel * 8 < 8 ? high_all - panel * 8 : 8, col = rem / high;
-    tm = (int)(panel * 8 + rem - col * high);
-    tn = (int)col;
+    tm = (int)min(panel * 8 + rem - col * high, high_all - 1);   // (inside in any case: offsets that do not ascend may count more tiles than 32 bits)
+    tn = (int)min(col, tiles_n - 1);
 }
 template <int BM>
 __device__ __forceinline__ bool find_row_tile(const ExpertsArgs &a, int tiles_n, uint32_t block, RowTile &t)
@@ -483,6 +484,7 @@ __device__ __forceinline__ bool find_row_tile(const ExpertsArgs &a, int tiles_n,
         if (past) {
             const int l = __builtin_ctzll(past);
             const uint32_t nl = (uint32_t)__builtin_amdgcn_readlane(n, l), upto = (uint32_t)__builtin_amdgcn_readlane(first, l);
+            if (nl == 0) return false;
             t.group = c + l < a.G ? c + l : -1;
             t.row0 = __builtin_amdgcn_readlane(lo, l);
             t.row1 = __builtin_amdgcn_readlane(hi, l);
@@ -663,6 +665,15 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
     if (whole == stages && whole > 0 && (a_cut || b_cut)) --whole;
     if ((a_cut && sa.index) || (b_cut && sb.index)) whole = 0;   // (any k may name the storage's last row)
     if (Steps<T>::PAIRS) whole &= ~1;
+    // TURN: an XCD's workgroups begin with a stage of their own and go round: rows that lie a multiple of 4 KB apart
+    // have the same stage in the same memory channels, which all XCDs would ask for at once (bf16, 32768 x 4096 x 4096 over 32
+    // groups as before, 16384 x 4096 x 2048 backward 691 / 672 us.  8 bits: no registers left for it; rows 4096 + 256 bytes apart, 310 / 272)
+    const int turn = T::TURN ? (int)((uint32_t)whole * (blockIdx.x & 7) / 8) : 0;
+    auto stage_at = [&](int s) { return T::TURN ? (s + turn < whole ? s + turn : s + turn - whole) : s; };
+    if constexpr (T::TURN) {
+        sa.base += (int64_t)turn * BK * T::ES;
+        sb.base += T::BKS ? (int64_t)turn * BK * sb.pitch : (int64_t)turn * BK * T::ES;
+    }
     const int mine = whole > kg ? (whole - kg + T::WK - 1) / T::WK : 0;   // ... this group's
     auto request_scales = [&](int s, int slot) {
         // (64 rows a wave; the last waves repeat others')
@@ -683,10 +694,12 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
         else if constexpr (q < StagedA::Q + StagedB::Q) sb.template load<q - StagedA::Q>(to + T::A_BYTES, wave);
         if constexpr (q == StagedA::Q + StagedB::Q - 1) {
             const int s = r * T::WK + kg;
-            const int ahead = !T::ALWAYS || s + 1 < whole ? BK * T::WK : 0;
+            const int at = stage_at(!T::ALWAYS || s < whole ? s : whole - 1);
+            // (past the end: the last one again)
+            const int ahead = !T::ALWAYS || s + 1 < whole ? (T::TURN && at + 1 == whole ? -at * BK : BK * T::WK) : 0;
             sa.advance(k0 + s * BK + ahead, ahead, wave, lane);
             sb.advance(k0 + s * BK + ahead, ahead, wave, lane);
-            if constexpr (T::FP8) request_scales(!T::ALWAYS || s < whole ? s : whole - 1, slot);
+            if constexpr (T::FP8) request_scales(at, slot);
             if constexpr (T::PREFETCH > 0) {
                 const int on = s + T::PREFETCH < whole ? T::PREFETCH * BK - ahead : 0;
                 const bool b = wave >= T::NW / 2;
@@ -761,7 +774,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
     constexpr bool BUSY = decltype(busy)::value;
     if (mine > 0) {
         int slot = 0, r = 0;
-        float wb = scale_b(kg);
+        float wb = scale_b(stage_at(kg));
         auto first = [&]() {
             meet<T::NW>();
             if constexpr (BUSY) {
@@ -781,7 +794,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
                 return;
             }
             const float now = wb;
-            wb = scale_b((r + 1) * T::WK + kg);
+            wb = scale_b(stage_at((r + 1) * T::WK + kg));
             stage(parity, ring + here * T::STAGE, now, ring + slot * T::STAGE, yes, [&]() {
                 wait();
                 meet<T::NW>();

@@ -29,7 +29,7 @@ def test_refusals_of_the_products(lib):
     assert grouped(lib, type=F32, out=F32) == -9 and grouped(lib, type=7) == -9 and grouped(lib, out=FP16) == -9
     for name in ("M", "N", "K", "G", "a_rows"):
         assert grouped(lib, **{name: -1}) == -2
-    assert grouped(lib, M=2 ** 31) == -7 and grouped(lib, G=2 ** 21) == -7
+    assert grouped(lib, M=2 ** 31) == -7 and grouped(lib, G=2 ** 17) == -7
     for name in ("A", "B", "off", "R"):
         assert grouped(lib, **{name: None}) == -3
     assert grouped(lib, lda=5) == -4 and grouped(lib, ldb=4) == -4 and grouped(lib, ldr=4) == -4 and grouped(lib, tb=1, ldb=5) == -4 and grouped(lib, gb=-1) == -4
