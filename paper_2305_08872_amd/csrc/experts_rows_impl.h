@@ -18,12 +18,12 @@ inline hipError_t launch_experts_layout(int tile, const ExpertsArgs &a, int64_t 
     case EXPERTS_256x256:
         // (its fragments as bf16 have no room beside the accumulators)
         if constexpr (ELEM == EXPERTS_FP8_EXACT) return hipErrorInvalidValue;
-        else return launch_experts_tile<ExpertTile<ELEM, 256, 256, 2, 4, 1, 2, 128, false, BKS>>(a, blocks, s);
-    case EXPERTS_128x128: return launch_experts_tile<ExpertTile<ELEM, 128, 128, 2, 2, 1, 2, 128, false, BKS>>(a, blocks, s);
-    case EXPERTS_64x128: return launch_experts_tile<ExpertTile<ELEM, 64, 128, 2, 2, 1, 3, 128, false, BKS>>(a, blocks, s);
-    case EXPERTS_64x64: return launch_experts_tile<ExpertTile<ELEM, 64, 64, 2, 2, 1, 3, 128, false, BKS>>(a, blocks, s);
-    case EXPERTS_64x64_K2: return launch_experts_tile<ExpertTile<ELEM, 64, 64, 2, 2, 2, 3, 128, false, BKS>>(a, blocks, s);
-    default: return launch_experts_tile<ExpertTile<ELEM, 16, 32, 1, 1, 4, 3, 128, false, BKS>>(a, blocks, s);
+        else return launch_experts_tile<ExpertTile<ELEM, 256, 256, 2, 4, 1, 2, false, BKS>>(a, blocks, s);
+    case EXPERTS_128x128: return launch_experts_tile<ExpertTile<ELEM, 128, 128, 2, 2, 1, 2, false, BKS>>(a, blocks, s);
+    case EXPERTS_64x128: return launch_experts_tile<ExpertTile<ELEM, 64, 128, 2, 2, 1, 3, false, BKS>>(a, blocks, s);
+    case EXPERTS_64x64: return launch_experts_tile<ExpertTile<ELEM, 64, 64, 2, 2, 1, 3, false, BKS>>(a, blocks, s);
+    case EXPERTS_64x64_K2: return launch_experts_tile<ExpertTile<ELEM, 64, 64, 2, 2, 2, 3, false, BKS>>(a, blocks, s);
+    default: return launch_experts_tile<ExpertTile<ELEM, 16, 32, 1, 1, 4, 3, false, BKS>>(a, blocks, s);
     }
 }
 

@@ -7,9 +7,9 @@ namespace amulet {
 template <int ELEM>
 static hipError_t launch_sums(int tile, const ExpertsArgs &a, int64_t blocks, hipStream_t s)
 {
-    typedef ExpertTile<ELEM, 256, 256, 2, 4, 1, 2, 128, true, true> Large;
-    typedef ExpertTile<ELEM, 128, 128, 2, 2, 1, 2, 128, true, true> Middle;
-    typedef ExpertTile<ELEM, 64, 64, 2, 2, 1, 3, 128, true, true> Small;
+    typedef ExpertTile<ELEM, 256, 256, 2, 4, 1, 2, true, true> Large;
+    typedef ExpertTile<ELEM, 128, 128, 2, 2, 1, 2, true, true> Middle;
+    typedef ExpertTile<ELEM, 64, 64, 2, 2, 1, 3, true, true> Small;
     if (tile == EXPERTS_256x256) return launch_experts<Large, experts_sums_kernel<Large>>(a, blocks, s);
     if (tile == EXPERTS_128x128) return launch_experts<Middle, experts_sums_kernel<Middle>>(a, blocks, s);
     return launch_experts<Small, experts_sums_kernel<Small>>(a, blocks, s);

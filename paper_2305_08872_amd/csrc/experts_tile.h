@@ -3,7 +3,7 @@
 //     R[g]    = sum over the rows i of g of A[row(i)]^T D[i]  by sums (the gradients of the experts' weights)
 // One kernel body for both; the translation units experts_mm_*.hip hold its instances.
 //
-// A stage of an operand is 128 bytes of k per line (64 k of 16 bits, 128 of 8) or 64, streamed global -> LDS by
+// A stage of an operand is 128 bytes of k per line (64 k of 16 bits, 128 of 8), streamed global -> LDS by
 // global_load_lds_dwordx4 (64 lanes x 16 bytes, any byte alignment) through a ring of S stages.  Two storages:
 //   k along the rows (KC): LDS keeps [line][units of 16 bytes]; a lane's fragment is one ds_read_b128.
 //   k across them   (KS): LDS keeps [k][line], and ds_read_b64_tr_b16 / _b8 hand a lane the k of its line.
@@ -43,15 +43,14 @@ typedef __attribute__((address_space(3))) void *xt_lds_void;
 
 extern __shared__ __attribute__((aligned(16))) char xt_smem[];
 
-template <int ELEM_, int BM_, int BN_, int WM_, int WN_, int WK_, int S_, int KB_, bool AKS_, bool BKS_>
+template <int ELEM_, int BM_, int BN_, int WM_, int WN_, int WK_, int S_, bool AKS_, bool BKS_>
 struct ExpertTile {
     static constexpr int ELEM = ELEM_;                       // EXPERTS_BF16, _FP16, _FP8, _FP8_EXACT
     static constexpr bool FP8 = ELEM == EXPERTS_FP8 || ELEM == EXPERTS_FP8_EXACT;
     static constexpr int ES = FP8 ? 1 : 2;                   // bytes of an element
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WK = WK_, S = S_;
     static constexpr bool AKS = AKS_, BKS = BKS_;
-    static constexpr int KB = KB_, BK = KB / ES;             // bytes and k of a stage's line
-    static_assert(KB == 128 || (KB == 64 && !FP8), "a stage is one or two instructions' k");
+    static constexpr int KB = 128, BK = KB / ES;             // bytes and k of a stage's line
     static constexpr int NW = WM * WN, NT = 64 * NW * WK;    // waves of a k group; threads
     static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
     static constexpr int A_BYTES = BM * KB, B_BYTES = BN * KB;
@@ -71,14 +70,13 @@ struct ExpertTile {
 
 // Position of 16-byte unit `u` of LDS line `line` (RB bytes long); see the two storages above.  256 bytes hold 16 units,
 // the banks of one clock:
-//   KC, natural fragments (lines 0..15 at one u): 2 lines per 256 bytes, so bits 1..3 of the line (64 bytes: 4 lines, bits 2, 3);
-//   KC, interleaved (lines 8 a + c, a, c = 0..3, or + 4): bits 1 and 3, 4 (64 bytes: bits 3, 4);
+//   KC, natural fragments (lines 0..15 at one u): 2 lines per 256 bytes, so bits 1..3 of the line;
+//   KC, interleaved (lines 8 a + c, a, c = 0..3, or + 4): bits 1 and 3, 4;
 //   KS: 16-bit reads take 32 bytes of rows {0..3, 8..11} at a time, 8-bit reads 16 of rows {0..7, 16..23}.
 template <int RB, bool KS, bool PERM, int ES>
 __device__ __forceinline__ int unit_of(int line, int u)
 {
-    if constexpr (!KS && RB == 64) return u ^ (PERM ? (line >> 3) & 3 : (line >> 2) & 3);
-    else if constexpr (!KS) return u ^ (PERM ? ((line >> 2) & 6) | ((line >> 1) & 1) : (line >> 1) & 7);
+    if constexpr (!KS) return u ^ (PERM ? ((line >> 2) & 6) | ((line >> 1) & 1) : (line >> 1) & 7);
     else if constexpr (ES == 2) {
         if constexpr (RB >= 256) return u ^ (((line & 3) | ((line >> 1) & 4)) << 1);
         else if constexpr (RB == 128) return u ^ ((((line >> 1) & 1) | ((line >> 2) & 2)) << 1);
@@ -286,9 +284,6 @@ struct Staged {
 };
 
 // Fragments: a lane's 16 bytes of half `h` of a stage, of the fragment that starts at line f (KC) or at its columns (KS).
-template <int ES>
-__device__ __forceinline__ xt_u4 read_kc(const char *at) { return *(const xt_u4 *)at; }
-
 template <class T, int LINES, bool KS, bool PERM>
 struct FragReader {
     static constexpr int ES = T::ES, RB = KS ? LINES * ES : T::KB;
@@ -500,7 +495,7 @@ __device__ __forceinline__ bool find_row_tile(const ExpertsArgs &a, int tiles_n,
 
 // A wave's products of one stage, in steps: 16 bits: each instruction's k times halves of the wave's rows; 8 bits: one or two row
 // blocks (an instruction has all 128 k).  While a step's matrix instructions run, the next one's fragments are read, into
-// the other of two sets of registers.  PAIRS: B's sets change places from stage to stage (P: the stage's parity).
+// the other of two sets of registers.
 template <class T>
 struct Steps {
     static constexpr int KSTEPS = T::FP8 ? 1 : T::KB / 64;
@@ -508,8 +503,7 @@ struct Steps {
     static constexpr int MSTEPS = T::MI / MA, STEPS = KSTEPS * MSTEPS;
     static constexpr bool A2 = STEPS % 2 == 0;   // (one step of 8 bits: read when the stage before is done with)
     static constexpr bool B2 = !T::FP8;          // (8 bits: one set, two would not leave room for the accumulators)
-    static constexpr bool PAIRS = B2 && KSTEPS % 2 != 0;
-    static_assert(A2 || !PAIRS, "a stage of a pair has an even number of steps");
+    static_assert(!B2 || KSTEPS == 2, "a stage begins with the first set");
     typedef FragReader<T, T::BM, T::AKS, false> ReadA;
     typedef FragReader<T, T::BN, T::BKS, T::PERM> ReadB;
     static constexpr int U = T::FP8 ? 2 : 1;     // 16-byte halves of a fragment
@@ -567,10 +561,10 @@ struct Steps {
         }
     }
     // the fragments of B that step t needs and the step before did not
-    template <int P, int t>
+    template <int t>
     __device__ __forceinline__ void read_b(const ReadB &r, const char *lb)
     {
-        constexpr int set = B2 ? (P * KSTEPS + t / MSTEPS) & 1 : 0;
+        constexpr int set = B2 ? (t / MSTEPS) & 1 : 0;
         if constexpr (t % MSTEPS == 0) {
 #pragma unroll
             for (int ni = 0; ni < T::NI; ++ni) {
@@ -580,10 +574,10 @@ struct Steps {
         }
     }
     // `hook` is called after every instruction
-    template <int P, int t, class Hook>
+    template <int t, class Hook>
     __device__ __forceinline__ void mma(float wb, xt_f4 (&acc)[T::MI][T::NI], Hook hook)
     {
-        constexpr int sa = t & 1, sb = B2 ? (P * KSTEPS + t / MSTEPS) & 1 : 0;
+        constexpr int sa = t & 1, sb = B2 ? (t / MSTEPS) & 1 : 0;
 #pragma unroll
         for (int m = 0; m < MA; ++m)
 #pragma unroll
@@ -664,7 +658,6 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
     const bool a_cut = sa.cut(), b_cut = sb.cut();
     if (whole == stages && whole > 0 && (a_cut || b_cut)) --whole;
     if ((a_cut && sa.index) || (b_cut && sb.index)) whole = 0;   // (any k may name the storage's last row)
-    if (Steps<T>::PAIRS) whole &= ~1;
     // TURN: an XCD's workgroups begin with a stage of their own and go round: rows that lie a multiple of 4 KB apart
     // have the same stage in the same memory channels, which all XCDs would ask for at once (bf16, 32768 x 4096 x 4096 over 32
     // groups as before, 16384 x 4096 x 2048 backward 691 / 672 us.  8 bits: no registers left for it; rows 4096 + 256 bytes apart, 310 / 272)
@@ -716,9 +709,8 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
     // One stage at `la`, its first fragments read.  AFTER: read those of the stage at `after` before the last step, once `next`
     // has seen to it that they are there (known when compiled: a branch between the steps would have the compiler gather
     // the matrix instructions behind it).
-    auto stage = [&](auto parity, const char *la, float wb, const char *after, auto there, auto next, auto hook) {
+    auto stage = [&](const char *la, float wb, const char *after, auto there, auto next, auto hook) {
         constexpr bool AFTER = decltype(there)::value;
-        constexpr int P = decltype(parity)::value, P2 = Steps<T>::PAIRS ? 1 - P : 0;
         const char *const lb = la + T::A_BYTES;
         if constexpr (Steps<T>::SPLIT) {
             // The first half of the rows a fragment at a time, the second half's being read meanwhile; then every wave has read
@@ -729,7 +721,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
                 constexpr int i = decltype(t)::value;
                 if constexpr (i + 1 < H) f.template read_a<i + 1>(ra, la, scale_row(la));
                 f.template read_rest<i>(ra, la, scale_row(la));
-                f.template mma<0, i>(wb, acc, [](int) {});
+                f.template mma<i>(wb, acc, [](int) {});
                 __builtin_amdgcn_sched_barrier(0);
             });
             if constexpr (AFTER) next();
@@ -744,26 +736,22 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
             });
             return;
         }
-#define AMULET_STEP(t)                                                          \
-        if constexpr (t < STEPS) {                                              \
-            if constexpr (t + 1 < STEPS) {                                      \
-                f.template read_a<t + 1>(ra, la, scale_row(la));                \
-                f.template read_b<P, t + 1>(rb, lb);                            \
-            } else if constexpr (AFTER) {                                       \
-                next();                                                         \
-                if constexpr (Steps<T>::A2) f.template read_a<0>(ra, after, scale_row(after)); \
-                if constexpr (Steps<T>::B2) f.template read_b<P2, 0>(rb, after + T::A_BYTES); \
-            }                                                                   \
-            f.template mma<P, t>(wb, acc, [&](int i) { hook(std::integral_constant<int, t>(), i); }); \
-            if constexpr (T::FP8) __builtin_amdgcn_sched_barrier(0);            \
-        }
-        AMULET_STEP(0) AMULET_STEP(1) AMULET_STEP(2) AMULET_STEP(3) AMULET_STEP(4) AMULET_STEP(5) AMULET_STEP(6) AMULET_STEP(7)
-#undef AMULET_STEP
+        for_each<STEPS>([&](auto step) {
+            constexpr int t = decltype(step)::value;
+            if constexpr (t + 1 < STEPS) {
+                f.template read_a<t + 1>(ra, la, scale_row(la));
+                f.template read_b<t + 1>(rb, lb);
+            } else if constexpr (AFTER) {
+                next();
+                if constexpr (Steps<T>::A2) f.template read_a<0>(ra, after, scale_row(after));
+                if constexpr (Steps<T>::B2) f.template read_b<0>(rb, after + T::A_BYTES);
+            }
+            f.template mma<t>(wb, acc, [&](int i) { hook(step, i); });
+            if constexpr (T::FP8) __builtin_amdgcn_sched_barrier(0);
+        });
         if constexpr (AFTER && !Steps<T>::A2) f.template read_a<0>(ra, after, scale_row(after));
-        if constexpr (AFTER && !Steps<T>::B2) f.template read_b<P2, 0>(rb, after + T::A_BYTES);
+        if constexpr (AFTER && !Steps<T>::B2) f.template read_b<0>(rb, after + T::A_BYTES);
     };
-    constexpr std::integral_constant<int, 0> even;
-    constexpr std::integral_constant<int, Steps<T>::PAIRS ? 1 : 0> odd;
     constexpr std::true_type yes;
     constexpr std::false_type no;
     constexpr auto none = [](auto, int) {};
@@ -779,11 +767,11 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
             meet<T::NW>();
             if constexpr (BUSY) {
                 f.template read_a<0>(ra, ring, scale_row(ring));
-                f.template read_b<0, 0>(rb, ring + T::A_BYTES);
+                f.template read_b<0>(rb, ring + T::A_BYTES);
             }
         };
         // stage r; `wait`: until stage r + 1 has landed; more: request the one S further on into this one's slot
-        auto go = [&](auto parity, auto more, auto wait) {
+        auto go = [&](auto more, auto wait) {
             const int here = slot;
             slot = slot + 1 == S ? 0 : slot + 1;
             if constexpr (!BUSY) {
@@ -795,7 +783,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
             }
             const float now = wb;
             wb = scale_b(stage_at((r + 1) * T::WK + kg));
-            stage(parity, ring + here * T::STAGE, now, ring + slot * T::STAGE, yes, [&]() {
+            stage(ring + here * T::STAGE, now, ring + slot * T::STAGE, yes, [&]() {
                 wait();
                 meet<T::NW>();
                 if constexpr (decltype(more)::value && T::SPREAD == 0) request(r + S, here);
@@ -808,18 +796,12 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
         auto all_but = []() { wait_vm<LOADS * (S - 2) + (T::PREFETCH ? 1 : 0)>(); };   // only the S - 2 stages behind the next may be under way
         if constexpr (T::ALWAYS) {
             // There is always a request, past the end for the last stage once more (nobody reads it there): every wait is the
-            // same, and one loop does for all stages but the last (of pairs: two).
+            // same, and one loop does for all stages but the last.
             for (int q = 0; q < S; ++q) request(q, q);
             wait_vm<LOADS * (S - 1)>();
             first();
-            if constexpr (Steps<T>::PAIRS) {
-                while (r + 2 < mine) { go(even, yes, all_but); go(odd, yes, all_but); }
-                go(even, no, all_but);
-                if constexpr (BUSY) stage(odd, ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
-            } else {
-                while (r + 1 < mine) go(even, yes, all_but);
-                if constexpr (BUSY) stage(even, ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
-            }
+            while (r + 1 < mine) go(yes, all_but);
+            if constexpr (BUSY) stage(ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
         } else {
 #pragma unroll
             for (int q = 0; q < S; ++q)
@@ -827,9 +809,9 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
             if (mine >= S) wait_vm<LOADS * (S - 1)>();
             else wait_vm<0>();
             first();
-            while (r + S < mine) go(even, yes, all_but);
-            while (r + 1 < mine) go(even, no, []() { wait_vm<0>(); });
-            if constexpr (BUSY) stage(even, ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
+            while (r + S < mine) go(yes, all_but);
+            while (r + 1 < mine) go(no, []() { wait_vm<0>(); });
+            if constexpr (BUSY) stage(ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
         }
     }
     if constexpr (T::ALWAYS) wait_vm<0>();   // (the requests past the end: nothing is under way when the workgroup ends)
@@ -848,8 +830,8 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
         meet<T::NW>();
         if constexpr (BUSY) {
             f.template read_a<0>(ra, ring, scale_row(ring));
-            f.template read_b<0, 0>(rb, ring + T::A_BYTES);
-            stage(even, ring, scale_b(s), nullptr, no, []() {}, none);
+            f.template read_b<0>(rb, ring + T::A_BYTES);
+            stage(ring, scale_b(s), nullptr, no, []() {}, none);
         }
     }
     };
