@@ -65,6 +65,7 @@ struct ExpertTile {
     // the largest tile has registers for 32-bit offsets of A's rows only (its caller sees to it that they fit)
     static constexpr bool WIDE = BM < 256;
     static constexpr bool ALWAYS = BM >= 256;   // requests past the end, see tile_sums
+    static constexpr bool BACK = BM < 256;      // the last k as a whole stage moved back, see tile_sums (the largest tile has no registers for its masks)
     static_assert(WK == 1 || BM < 256, "the largest tile has no room for k groups");
 };
 
@@ -573,6 +574,20 @@ struct Steps {
             }
         }
     }
+    // the fragments of step t without the k that another stage has had
+    template <int t>
+    __device__ __forceinline__ void mask(const xt_u4 (&keep)[2])
+    {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const xt_u4 &w = keep[T::FP8 ? u : t / MSTEPS];
+#pragma unroll
+            for (int m = 0; m < MA; ++m) a[t & 1][m][u] &= w;
+            if constexpr (t % MSTEPS == 0)
+#pragma unroll
+                for (int ni = 0; ni < T::NI; ++ni) b[B2 ? (t / MSTEPS) & 1 : 0][ni][u] &= w;
+        }
+    }
     // `hook` is called after every instruction
     template <int t, class Hook>
     __device__ __forceinline__ void mma(float wb, xt_f4 (&acc)[T::MI][T::NI], Hook hook)
@@ -658,6 +673,11 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
     const bool a_cut = sa.cut(), b_cut = sb.cut();
     if (whole == stages && whole > 0 && (a_cut || b_cut)) --whole;
     if ((a_cut && sa.index) || (b_cut && sb.index)) whole = 0;   // (any k may name the storage's last row)
+    // BACK: the k that are left are the end of one more stage, which begins before them; what it shares with the stage before is
+    // masked in both operands' fragments.  (Through registers / so: fp16, 3001 x 1501 x 1003 over 7 groups
+    // 35.4 / 32.4 us; 8 bits, 1777 x 1368 x 2504 over 5 36.0 / 34.5.)
+    const bool back = T::BACK && whole > 0 && whole < stages && !a_cut && !b_cut;
+    const int ringed = whole + (back ? 1 : 0);
     // TURN: an XCD's workgroups begin with a stage of their own and go round: rows that lie a multiple of 4 KB apart
     // have the same stage in the same memory channels, which all XCDs would ask for at once (bf16, 32768 x 4096 x 4096 over 32
     // groups as before, 16384 x 4096 x 2048 backward 691 / 672 us.  8 bits: no registers left for it; rows 4096 + 256 bytes apart, 310 / 272)
@@ -667,7 +687,12 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
         sa.base += (int64_t)turn * BK * T::ES;
         sb.base += T::BKS ? (int64_t)turn * BK * sb.pitch : (int64_t)turn * BK * T::ES;
     }
-    const int mine = whole > kg ? (whole - kg + T::WK - 1) / T::WK : 0;   // ... this group's
+    const int mine = ringed > kg ? (ringed - kg + T::WK - 1) / T::WK : 0;   // ... this group's
+    const int plain = whole > kg ? (whole - kg + T::WK - 1) / T::WK : 0;    // ... those not moved back
+    auto move_back = [&]() {   // (a branch of its own: as a part of what each request moves on by it cost the 8-bit 128 x 128 tile a third)
+        sa.advance(k0 + k - BK, k - BK - whole * BK, wave, lane);
+        sb.advance(k0 + k - BK, k - BK - whole * BK, wave, lane);
+    };
     auto request_scales = [&](int s, int slot) {
         // (64 rows a wave; the last waves repeat others')
         dma4(scales.a + (int64_t)s * scales.a_step, scales.a_off, ring_at + (uint32_t)(slot * T::STAGE + T::A_BYTES + T::B_BYTES + (wave * 64 % (T::BM < 64 ? 64 : T::BM)) * 4));
@@ -706,10 +731,13 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
     auto request = [&](int r, int slot) { for_each<StagedA::Q + StagedB::Q>([&](auto q) { request_one(q, r, slot); }); };
     auto scale_row = [&](const char *la) { return (const float *)(la + T::A_BYTES + T::B_BYTES) + wm * (T::BM / T::WM) + (lane & 15); };
     auto scale_b = [&](int s) { return T::FP8 ? scales.b[(int64_t)s * scales.b_step] : 0.0f; };
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    xt_u4 keep[2];   // BACK: what stays of a lane's units
     // One stage at `la`, its first fragments read.  AFTER: read those of the stage at `after` before the last step, once `next`
     // has seen to it that they are there (known when compiled: a branch between the steps would have the compiler gather
     // the matrix instructions behind it).
-    auto stage = [&](const char *la, float wb, const char *after, auto there, auto next, auto hook) {
+    auto stage = [&](const char *la, float wb, const char *after, auto there, auto masked, auto next, auto hook) {
         constexpr bool AFTER = decltype(there)::value;
         const char *const lb = la + T::A_BYTES;
         if constexpr (Steps<T>::SPLIT) {
@@ -746,14 +774,13 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
                 if constexpr (Steps<T>::A2) f.template read_a<0>(ra, after, scale_row(after));
                 if constexpr (Steps<T>::B2) f.template read_b<0>(rb, after + T::A_BYTES);
             }
+            if constexpr (decltype(masked)::value) f.template mask<t>(keep);
             f.template mma<t>(wb, acc, [&](int i) { hook(step, i); });
             if constexpr (T::FP8) __builtin_amdgcn_sched_barrier(0);
         });
         if constexpr (AFTER && !Steps<T>::A2) f.template read_a<0>(ra, after, scale_row(after));
         if constexpr (AFTER && !Steps<T>::B2) f.template read_b<0>(rb, after + T::A_BYTES);
     };
-    constexpr std::true_type yes;
-    constexpr std::false_type no;
     constexpr auto none = [](auto, int) {};
 
     // `busy`: a wave whose rows all lie past the group's end requests its part of the stages and meets the others, no more: its
@@ -783,7 +810,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
             }
             const float now = wb;
             wb = scale_b(stage_at((r + 1) * T::WK + kg));
-            stage(ring + here * T::STAGE, now, ring + slot * T::STAGE, yes, [&]() {
+            stage(ring + here * T::STAGE, now, ring + slot * T::STAGE, yes, no, [&]() {
                 wait();
                 meet<T::NW>();
                 if constexpr (decltype(more)::value && T::SPREAD == 0) request(r + S, here);
@@ -801,24 +828,42 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
             wait_vm<LOADS * (S - 1)>();
             first();
             while (r + 1 < mine) go(yes, all_but);
-            if constexpr (BUSY) stage(ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
+            if constexpr (BUSY) stage(ring + slot * T::STAGE, wb, nullptr, no, no, []() {}, none);
         } else {
 #pragma unroll
             for (int q = 0; q < S; ++q)
-                if (q < mine) request(q, q);
+                if (q < mine) {
+                    if (q == plain) move_back();
+                    request(q, q);
+                }
             if (mine >= S) wait_vm<LOADS * (S - 1)>();
             else wait_vm<0>();
             first();
-            while (r + S < mine) go(yes, all_but);
+            for (int upto = plain;; upto = mine) {
+                while (r + S < upto) go(yes, all_but);
+                if (r + S >= mine) break;
+                move_back();
+            }
             while (r + 1 < mine) go(no, []() { wait_vm<0>(); });
-            if constexpr (BUSY) stage(ring + slot * T::STAGE, wb, nullptr, no, []() {}, none);
+            if constexpr (BUSY) {
+                // bytes of a lane's units that the stage before has had
+                const int skip = back && (mine - 1) * T::WK + kg == whole ? (BK - (k - whole * BK)) * T::ES : 0;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int gone = skip - 64 * h - 16 * (lane >> 4) - 4 * i;
+                        keep[h][i] = gone <= 0 ? ~0u : gone >= 4 ? 0u : ~0u << (8 * gone);
+                    }
+                stage(ring + slot * T::STAGE, wb, nullptr, no, std::integral_constant<bool, T::BACK>(), []() {}, none);
+            }
         }
     }
     if constexpr (T::ALWAYS) wait_vm<0>();   // (the requests past the end: nothing is under way when the workgroup ends)
     if constexpr (T::WK > 1 && T::NW > 1)
-        for (int r = mine; r < (whole + T::WK - 1) / T::WK; ++r) meet<T::NW>();   // (the groups that have one stage more)
+        for (int r = mine; r < (ringed + T::WK - 1) / T::WK; ++r) meet<T::NW>();   // (the groups that have one stage more)
     // stages that are not whole
-    for (int s = whole; s < stages; ++s) {
+    for (int s = ringed; s < stages; ++s) {
         if (T::WK > 1 && s % T::WK != kg) {
             if constexpr (T::NW > 1) { meet<T::NW>(); meet<T::NW>(); }
             continue;
@@ -831,7 +876,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
         if constexpr (BUSY) {
             f.template read_a<0>(ra, ring, scale_row(ring));
             f.template read_b<0>(rb, ring + T::A_BYTES);
-            stage(ring, scale_b(s), nullptr, no, []() {}, none);
+            stage(ring, scale_b(s), nullptr, no, no, []() {}, none);
         }
     }
     };

@@ -210,6 +210,33 @@ def test_infinities_and_nan_reach_their_own_outputs_only(am):
             assert torch.equal(~torch.isfinite(R), bad)
 
 
+@pytest.mark.parametrize("sizes,N,K", [([1], 8, 65), ([7], 130, 200), ([64], 100, 71), ([50, 64], 128, 616), ([300, 1, 200], 129, 321), ([700], 72, 1000), ([2100, 1996], 4000, 72)])
+def test_an_infinity_near_a_ragged_end_stays_one(am, sizes, N, K):
+    """The k before a ragged end, each infinite in one operand and 2 in the other: every sum is infinite and none is NaN, whichever
+    stages have that k."""
+    M, G = sum(sizes), len(sizes)
+    off = torch.tensor(offsets_of(sizes), dtype=torch.int32, device="cuda")
+    for k in {K - 1, K - K % 64, K - K % 64 - 1, max(0, K - 64), max(0, K - 65)}:
+        A, B = torch.full((M, K), 2.0, dtype=BF16, device="cuda"), torch.ones(G, K, N, dtype=BF16, device="cuda")
+        A[::2, k] = math.inf
+        want = torch.full((M, N), 2.0 * K, device="cuda")
+        want[::2] = math.inf
+        for trans_b in (False, True):
+            b = B.transpose(1, 2).contiguous() if trans_b else B
+            R = torch.empty(M, N, dtype=F32, device="cuda")
+            am.amulet_grouped_mm(A, b, off, R, trans_b=trans_b)
+            assert torch.equal(R, want)
+        B[:, k, ::3] = -math.inf
+        A[:, k] = 2.0
+        want = torch.full((M, N), 2.0 * K, device="cuda")
+        want[:, ::3] = -math.inf
+        for trans_b in (False, True):
+            b = B.transpose(1, 2).contiguous() if trans_b else B
+            R = torch.empty(M, N, dtype=F32, device="cuda")
+            am.amulet_grouped_mm(A, b, off, R, trans_b=trans_b)
+            assert torch.equal(R, want)
+
+
 @pytest.mark.parametrize("trans_r", [False, True])
 @pytest.mark.parametrize("dtype,out,space", [(BF16, BF16, 0), (BF16, F32, 1 << 24), (FP16, FP16, 1 << 30)])
 @pytest.mark.parametrize("sizes,N,K,tokens", [([1], 1, 1, 0), ([3, 0, 2], 17, 33, 0), ([64, 0, 128], 64, 72, 0), ([65, 200, 1], 129, 130, 50), ([700, 3, 0, 90], 136, 264, 333),
