@@ -640,7 +640,7 @@ int amulet_probe_mfma_i8(int waves_per_simd, double *macs_per_second, void *stre
  *  - `offsets`: int32, G + 1 values in device memory, ascending; rows offsets[g] to
  *    offsets[g+1] - 1 belong to group g.  They are read on the device only.  Values
  *    outside 0..M count as the nearest of the two; where they do not ascend, results are
- *    unspecified (and nothing outside the operands is read or written).
+ *    unspecified (and nothing outside the operands is read or written).  At most 65536 groups.
  */
 typedef enum { AMULET_FP32 = 0, AMULET_BF16 = 1, AMULET_FP16 = 2 } amulet_type_t;
 

@@ -2,7 +2,8 @@
 // e4m3(x * (1 / scale)), to the nearest, ties to even.  448 is the type's largest value; the least scale keeps its reciprocal finite for
 // blocks of zeros.  The reciprocal is rounded once per block instead of dividing every value (a value may end up on the
 // other side of a tie, never further).  A NaN stays one and does not count for amax; an infinity makes its block's scale
-// infinite and its own values NaN.  Bound by memory: each value is read once.
+// infinite and its own values NaN.  Bound by memory: each value is read once (16384 x 4096 bf16 by rows: 41 us = 4.95 TB/s,
+// a large copy's rate).
 //
 // By rows (1 x 128, activations): 16 lanes have a block, 16 rows a workgroup; scales [block of columns][row], so that the
 // products read those of a stage side by side.  By blocks (128 x 128, weights): a workgroup has a block, its values in registers.
