@@ -77,7 +77,9 @@ struct ExpertTile {
     // the largest tile has registers for 32-bit offsets of A's rows only (its caller sees to it that they fit)
     static constexpr bool WIDE = BM < 256;
     static constexpr bool ALWAYS = BM >= 256;   // requests past the end, see tile_sums
-    static constexpr bool BACK = BM < 256;      // the last k as a whole stage moved back, see tile_sums (the largest tile has no registers for its masks)
+    // the last k as a whole stage moved back, see tile_sums.  (Not the largest tile by rows: 8 bits leave no registers for the masks, and with 16 the
+    // other stages took 0.8 % longer; by sums, where every group has such an end, 666 / 653 us for the two gradients of 16384 x 4096 x 2048.)
+    static constexpr bool BACK = BM < 256 || AKS;
     static_assert(WK == 1 || BM < 256, "the largest tile has no room for k groups");
 };
 
@@ -695,6 +697,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
     // groups as before, 16384 x 4096 x 2048 backward 691 / 672 us.  8 bits: no registers left for it; rows 4096 + 256 bytes apart, 310 / 272)
     const int turn = T::TURN ? (int)((uint32_t)whole * (blockIdx.x & 7) / 8) : 0;
     auto stage_at = [&](int s) { return T::TURN ? (s + turn < whole ? s + turn : s + turn - whole) : s; };
+    auto begin_of = [&](int s) { return back && s == whole ? k - BK : stage_at(s) * BK; };   // (s < ringed)
     if constexpr (T::TURN) {
         sa.base += (int64_t)turn * BK * T::ES;
         sb.base += T::BKS ? (int64_t)turn * BK * sb.pitch : (int64_t)turn * BK * T::ES;
@@ -724,11 +727,12 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
         else if constexpr (q < StagedA::Q + StagedB::Q) sb.template load<q - StagedA::Q>(to + T::A_BYTES, wave);
         if constexpr (q == StagedA::Q + StagedB::Q - 1) {
             const int s = r * T::WK + kg;
-            const int at = stage_at(!T::ALWAYS || s < whole ? s : whole - 1);
+            const int at = T::FP8 ? (!T::ALWAYS || s < whole ? s : whole - 1) : 0;
             // (past the end: the last one again)
-            const int ahead = !T::ALWAYS || s + 1 < whole ? (T::TURN && at + 1 == whole ? -at * BK : BK * T::WK) : 0;
-            sa.advance(k0 + s * BK + ahead, ahead, wave, lane);
-            sb.advance(k0 + s * BK + ahead, ahead, wave, lane);
+            const int ahead = !T::ALWAYS ? BK * T::WK : s + 1 < ringed ? begin_of(s + 1) - begin_of(s) : 0;
+            const int next = k0 + (T::ALWAYS ? begin_of(s + 1 < ringed ? s + 1 : ringed - 1) : (s + T::WK) * BK);
+            sa.advance(next, ahead, wave, lane);
+            sb.advance(next, ahead, wave, lane);
             if constexpr (T::FP8) request_scales(at, slot);
             if constexpr (T::PREFETCH > 0) {
                 const int on = s + T::PREFETCH < whole ? T::PREFETCH * BK - ahead : 0;
@@ -832,6 +836,18 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
             });
             ++r;
         };
+        auto last = [&]() {
+            // bytes of a lane's units that the stage before has had
+            const int skip = back && (mine - 1) * T::WK + kg == whole ? (BK - (k - whole * BK)) * T::ES : 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int gone = skip - 64 * h - 16 * (lane >> 4) - 4 * i;
+                    keep[h][i] = gone <= 0 ? ~0u : gone >= 4 ? 0u : ~0u << (8 * gone);
+                }
+            stage(ring + slot * T::STAGE, wb, nullptr, no, std::integral_constant<bool, T::BACK>(), []() {}, none);
+        };
         auto all_but = []() { wait_vm<LOADS * (S - 2) + (T::PREFETCH ? 1 : 0)>(); };   // only the S - 2 stages behind the next may be under way
         if constexpr (T::ALWAYS) {
             // There is always a request, past the end for the last stage once more (nobody reads it there): every wait is the
@@ -840,7 +856,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
             wait_vm<LOADS * (S - 1)>();
             first();
             while (r + 1 < mine) go(yes, all_but);
-            if constexpr (BUSY) stage(ring + slot * T::STAGE, wb, nullptr, no, no, []() {}, none);
+            if constexpr (BUSY) last();
         } else {
 #pragma unroll
             for (int q = 0; q < S; ++q)
@@ -857,18 +873,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
                 move_back();
             }
             while (r + 1 < mine) go(no, []() { wait_vm<0>(); });
-            if constexpr (BUSY) {
-                // bytes of a lane's units that the stage before has had
-                const int skip = back && (mine - 1) * T::WK + kg == whole ? (BK - (k - whole * BK)) * T::ES : 0;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int gone = skip - 64 * h - 16 * (lane >> 4) - 4 * i;
-                        keep[h][i] = gone <= 0 ? ~0u : gone >= 4 ? 0u : ~0u << (8 * gone);
-                    }
-                stage(ring + slot * T::STAGE, wb, nullptr, no, std::integral_constant<bool, T::BACK>(), []() {}, none);
-            }
+            if constexpr (BUSY) last();
         }
     }
     if constexpr (T::ALWAYS) wait_vm<0>();   // (the requests past the end: nothing is under way when the workgroup ends)
