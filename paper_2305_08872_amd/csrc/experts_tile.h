@@ -697,7 +697,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
     // groups as before, 16384 x 4096 x 2048 backward 691 / 672 us.  8 bits: no registers left for it; rows 4096 + 256 bytes apart, 310 / 272)
     const int turn = T::TURN ? (int)((uint32_t)whole * (blockIdx.x & 7) / 8) : 0;
     auto stage_at = [&](int s) { return T::TURN ? (s + turn < whole ? s + turn : s + turn - whole) : s; };
-    auto begin_of = [&](int s) { return back && s == whole ? k - BK : stage_at(s) * BK; };   // (s < ringed)
+    auto begin_of = [&](int s) { return s < whole ? s * BK : back ? k - BK : (whole - 1) * BK; };   // (ALWAYS and BACK; past the end: the last one's)
     if constexpr (T::TURN) {
         sa.base += (int64_t)turn * BK * T::ES;
         sb.base += T::BKS ? (int64_t)turn * BK * sb.pitch : (int64_t)turn * BK * T::ES;
@@ -727,10 +727,11 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
         else if constexpr (q < StagedA::Q + StagedB::Q) sb.template load<q - StagedA::Q>(to + T::A_BYTES, wave);
         if constexpr (q == StagedA::Q + StagedB::Q - 1) {
             const int s = r * T::WK + kg;
-            const int at = T::FP8 ? (!T::ALWAYS || s < whole ? s : whole - 1) : 0;
+            const int at = stage_at(!T::ALWAYS || s < whole ? s : whole - 1);
             // (past the end: the last one again)
-            const int ahead = !T::ALWAYS ? BK * T::WK : s + 1 < ringed ? begin_of(s + 1) - begin_of(s) : 0;
-            const int next = k0 + (T::ALWAYS ? begin_of(s + 1 < ringed ? s + 1 : ringed - 1) : (s + T::WK) * BK);
+            const int ahead = T::ALWAYS && T::BACK ? begin_of(s + 1) - begin_of(s)
+                              : !T::ALWAYS || s + 1 < whole ? (T::TURN && at + 1 == whole ? -at * BK : BK * T::WK) : 0;
+            const int next = k0 + (T::ALWAYS && T::BACK ? begin_of(s + 1) : s * BK + ahead);
             sa.advance(next, ahead, wave, lane);
             sb.advance(next, ahead, wave, lane);
             if constexpr (T::FP8) request_scales(at, slot);
