@@ -1,5 +1,6 @@
 // C ABI of a mixture-of-experts layer's operators: argument checks, the choice of tiles, launches.
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include "amulet.h"
@@ -88,6 +89,29 @@ static int check_rows(int64_t M, int64_t N, int64_t K, int64_t G, int trans_b, c
     return AMULET_OK;
 }
 
+// Workgroups of 128 x 128 tiles for the columns behind the cut of columns_of_largest(), which the kernels make by the rows of tiles that the offsets
+// give; 0: one launch for all columns, as the cut is unlikely.  The rows of tiles of random groups lie within some sqrt(G / 3) of what half
+// a tile for each group's last makes.
+static int64_t cut_blocks(ExpertsArgs &a, int64_t M, int64_t N, int64_t G, bool grouped, int es)
+{
+    if (G > 128) return 0;   // (last tiles' number too uncertain, and each possible one is looked at)
+    const int cols = (int)((N + 255) / 256);
+    const double round_us = (double)((a.K * es + 127) / 128) * 1.7 + 8.0;
+    a.units = compute_units();
+    a.gap = (int)(256.0 * 4.0 / round_us);
+    const int64_t least = (M + 255) / 256, regions = G + 2 < M ? G + 2 : M, most = grouped ? (M + regions * 255) / 256 : least;
+    const int64_t usual = grouped ? M / 256 + G / 2 : least, spread = grouped ? (int64_t)sqrt((double)G / 3.0) + 1 : 0;
+    int64_t blocks = 0;
+    int cuts = 0, tried = 0;
+    for (int64_t rows = least; rows <= most; ++rows) {
+        const int before = columns_of_largest(rows, cols, a.units, a.gap);
+        if (rows >= usual - spread && rows <= usual + spread) { ++tried; cuts += before < cols; }
+        const int64_t n = 2 * rows * ((N + 127) / 128 - 2 * before);   // (a row of 256 x 256 tiles is at most two of 128 x 128)
+        if (before < cols && n > blocks) blocks = n;
+    }
+    return 2 * cuts > tried ? (blocks + 7) / 8 * 8 : 0;
+}
+
 static int run_rows(const char *const *names, int type, int trans_b, ExpertsArgs &a, int64_t M, int64_t N, int64_t G, void *stream)
 {
     // 8-bit operands whose results keep 32 bits have no 256 x 256 tile, and that tile's offsets of A's rows have 32 bits
@@ -98,12 +122,21 @@ static int run_rows(const char *const *names, int type, int trans_b, ExpertsArgs
     if (blocks > kMostBlocks) return AMULET_ERR_RANGE;
     note_kernel(names[tile], M);
     hipStream_t s = (hipStream_t)stream;
-    switch (type) {
-    case EXPERTS_BF16: return launch_status(launch_experts_rows_bf16(tile, !trans_b, a, blocks, s));
-    case EXPERTS_FP16: return launch_status(launch_experts_rows_fp16(tile, !trans_b, a, blocks, s));
-    case EXPERTS_FP8_EXACT: return launch_status(launch_experts_rows_fp8_exact(tile, !trans_b, a, blocks, s));
-    default: return launch_status(launch_experts_rows_fp8(tile, !trans_b, a, blocks, s));
-    }
+    auto launch = [&](int shape, int64_t n) {
+        switch (type) {
+        case EXPERTS_BF16: return launch_status(launch_experts_rows_bf16(shape, !trans_b, a, n, s));
+        case EXPERTS_FP16: return launch_status(launch_experts_rows_fp16(shape, !trans_b, a, n, s));
+        case EXPERTS_FP8_EXACT: return launch_status(launch_experts_rows_fp8_exact(shape, !trans_b, a, n, s));
+        default: return launch_status(launch_experts_rows_fp8(shape, !trans_b, a, n, s));
+        }
+    };
+    const int64_t behind = tile == EXPERTS_256x256 ? cut_blocks(a, M, N, G, a.offsets != nullptr, es) : 0;
+    if (behind == 0) return launch(tile, blocks);
+    a.part_of = EXPERTS_BEFORE;
+    const int rc = launch(tile, blocks);
+    if (rc != AMULET_OK) return rc;
+    a.part_of = EXPERTS_BEHIND;
+    return launch(EXPERTS_128x128, behind);
 }
 
 static const char *const kRowsNames[EXPERTS_TILES] = {"grouped_mm_256x256", "grouped_mm_128x128", "grouped_mm_64x128", "grouped_mm_64x64",

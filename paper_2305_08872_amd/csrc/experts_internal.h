@@ -29,7 +29,27 @@ struct ExpertsArgs {
     int parts;                       // by sums: ranges of a group's rows, each a workgroup's
     int rows_of_b;                   // by sums: `rows` names D's rows
     int out;                         // type of R
+    int part_of, units, gap;         // by rows: EXPERTS_BEFORE or _BEHIND the cut of columns_of_largest(), or all of them (0); what it goes by
 };
+enum { EXPERTS_BEFORE = 1, EXPERTS_BEHIND = 2 };
+
+// Of `cols` columns of 256 x 256 tiles, `rows` high, those that the 256 x 256 tile takes; 128 x 128 tiles take the others.  All, unless a last
+// round of few tiles on `units` compute units would cost more than one round of small tiles for the columns that the full rounds
+// leave.  In 256ths of a round: the partly full one takes 0.65 of it, whatever its share (of up to a half; what stands still leaves
+// the others more power), the small tiles 0.45, or 0.3 where no unit has two, the second launch `gap`; two rounds of small tiles gain nothing.
+// Measured, one launch / two, us: bf16, 4096 x 4608 x 4096 188 / 150 (1.12 rounds), 7000 x 2816 x 2816 over 3 groups 141 / 120 (1.2), 5000 x 4096 x
+// 4096 over 4 180 / 166 (1.3), 16384 x 2048 x 4096 over 16 327 / 304 (2.28); with small tiles for more than half a round 6000 x 4096 x 2048 99 / 113 (1.5), after
+// short rounds 8192 x 4096 x 1024 over 8 87 / 90 (2.25).  Integers: host and device have to agree.
+__host__ __device__ inline int columns_of_largest(int64_t rows, int cols, int units, int gap)
+{
+    const int64_t tiles = rows * cols, full = tiles / units, rest = tiles - full * units;
+    if (full == 0 || rest == 0) return cols;
+    const int64_t before = full * units / rows, behind = rows * (cols - before);
+    if (before == 0) return cols;
+    if (2 * behind > units) return cols;
+    const int64_t one = 256 * full + 166, two = 256 * full + (8 * behind <= units ? 77 : 115) + gap;
+    return 20 * two < 19 * one ? (int)before : cols;
+}
 
 // tiles of R by rows (experts_mm_*.hip): rows x columns; _K2: two groups of waves share a tile's k
 enum { EXPERTS_256x256 = 0, EXPERTS_128x128 = 1, EXPERTS_64x128 = 2, EXPERTS_64x64 = 3, EXPERTS_64x64_K2 = 4, EXPERTS_16x32 = 5, EXPERTS_TILES = 6 };

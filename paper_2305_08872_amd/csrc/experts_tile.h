@@ -441,19 +441,32 @@ __device__ __forceinline__ void tile_in_region(uint32_t in, uint32_t high_all, u
     tm = (int)min(panel * 8 + rem - col * high, high_all - 1);   // (inside in any case: offsets that do not ascend may count more tiles than 32 bits)
     tn = (int)min(col, tiles_n - 1);
 }
+// A launch that has a part of the columns: `tiles_n` becomes its own, and how many tiles lie before them.  rows: of 256 x 256 tiles.
+template <int BM>
+__device__ __forceinline__ int own_columns(const ExpertsArgs &a, uint32_t rows, int &tiles_n)
+{
+    if (BM < 128 || !a.part_of) return 0;
+    const int before = columns_of_largest(rows, (a.N + 255) / 256, a.units, a.gap) * (256 / BM);   // (square tiles only)
+    if (a.part_of == EXPERTS_BEFORE) { tiles_n = tiles_n < before ? tiles_n : before; return 0; }
+    tiles_n = tiles_n > before ? tiles_n - before : 0;
+    return before;
+}
 template <int BM>
 __device__ __forceinline__ bool find_row_tile(const ExpertsArgs &a, int tiles_n, uint32_t block, RowTile &t)
 {
     // XCD x (workgroup b runs on XCD b % 8) takes an eighth of the tiles, neighbours in the order of regions
     const uint32_t xcd = block & 7, slot = block >> 3;
     if (!a.offsets) {
-        const uint32_t high = (uint32_t)(a.M + BM - 1) / BM, tiles = high * (uint32_t)tiles_n;
+        const uint32_t high = (uint32_t)(a.M + BM - 1) / BM;
+        const int skipped = own_columns<BM>(a, (uint32_t)(a.M + 255) / 256, tiles_n);
+        const uint32_t tiles = high * (uint32_t)tiles_n;
         const uint32_t begin = (uint32_t)((uint64_t)tiles * xcd >> 3), end = (uint32_t)((uint64_t)tiles * (xcd + 1) >> 3);
         if (slot >= end - begin) return false;
         t.group = 0;
         t.row0 = 0;
         t.row1 = a.M;
         tile_in_region(begin + slot, high, (uint32_t)tiles_n, t.tm, t.tn);
+        t.tn += skipped;
         return true;
     }
     const int lane = threadIdx.x & 63;
@@ -482,6 +495,19 @@ __device__ __forceinline__ bool find_row_tile(const ExpertsArgs &a, int tiles_n,
         int l2, h2, n2;
         total += (uint32_t)__builtin_amdgcn_readlane(scan(c, l2, h2, n2), 63);
     }
+    uint32_t largest = total;   // rows of 256 x 256 tiles
+    if (BM == 128 && a.part_of) {
+        int sum = 0;
+        for (int c = 0; c < regions; c += 64) {
+            int l2, h2;
+            region(c + lane, l2, h2);
+            sum += h2 > l2 ? (h2 - l2 + 255) / 256 : 0;
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+        largest = (uint32_t)__builtin_amdgcn_readfirstlane(sum);
+    }
+    const int skipped = own_columns<BM>(a, largest, tiles_n);
     const uint64_t tiles = (uint64_t)total * (uint32_t)tiles_n;
     const uint32_t begin = (uint32_t)(tiles * xcd >> 3), end = (uint32_t)(tiles * (xcd + 1) >> 3);
     if (slot >= end - begin) return false;
@@ -499,6 +525,7 @@ __device__ __forceinline__ bool find_row_tile(const ExpertsArgs &a, int tiles_n,
             t.row0 = __builtin_amdgcn_readlane(lo, l);
             t.row1 = __builtin_amdgcn_readlane(hi, l);
             tile_in_region(at - (before + upto - nl) * (uint32_t)tiles_n, nl, (uint32_t)tiles_n, t.tm, t.tn);
+            t.tn += skipped;
             return true;
         }
         before += (uint32_t)__builtin_amdgcn_readlane(first, 63);

@@ -157,6 +157,39 @@ def test_gathered_rows_and_rows_of_no_group(am, first, sizes, rest, N, K, tokens
     within(R, want, 2 * (K + 8) * 2.0 ** -24 * S, "R")
 
 
+# the largest tiles fill the chip once and a bit: their last columns go to smaller tiles in a second launch
+@pytest.mark.parametrize("trans_b", [False, True])
+@pytest.mark.parametrize("first,sizes,rest,N,K,tokens", [(0, [1300, 1250, 1200, 1250], 0, 4099, 1203, 0), (300, [1024, 1024, 1280, 1024], 10, 4096, 1280, 900), (0, [4096], 0, 4608, 1088, 0)])
+def test_one_round_of_tiles_and_a_bit(am, first, sizes, rest, N, K, tokens, trans_b):
+    print("a round and a bit", first, sizes, rest, N, K, tokens, trans_b, flush=True)
+    g = gen(N + K)
+    M = first + sum(sizes) + rest
+    A = normal(g, tokens or M, K, dtype=BF16)
+    B = normal(g, len(sizes), *((N, K) if trans_b else (K, N)), dtype=BF16)
+    rows = torch.randint(0, tokens, (M,), generator=g, device="cuda", dtype=torch.int32) if tokens else None
+    at = offsets_of(sizes, first)
+    off = torch.tensor(at, dtype=torch.int32, device="cuda")
+    R = torch.full((M, N), math.nan, dtype=BF16, device="cuda")
+    am.amulet_grouped_mm(A, B, off, R, rows=rows, trans_b=trans_b)
+    assert am.amulet_recent_kernel().split()[0] == "grouped_mm_256x256"
+    want, S = ref_rows(A, B, at, M, rows, trans_b)
+    within(R, want, 2 * (K + 8) * 2.0 ** -24 * S, "R")
+    again = torch.full_like(R, math.nan)
+    am.amulet_grouped_mm(A, B, off, again, rows=rows, trans_b=trans_b)
+    assert torch.equal(again, R)
+
+
+@pytest.mark.parametrize("trans_b", [False, True])
+def test_fp8_one_round_of_tiles_and_a_bit(am, trans_b):
+    g = gen(77)
+    M, N, K = 4096, 4608, 2100
+    A, sa, B, sb = fp8_operands(g, M, K, (1, N, K) if trans_b else (1, K, N))
+    R = torch.full((M, N), math.nan, dtype=BF16, device="cuda")
+    am.amulet_mm_fp8(A, sa, B[0], sb[0], R, trans_b=trans_b)
+    assert am.amulet_recent_kernel().split()[0] == "mm_fp8_256x256"
+    check_fp8(R, A, sa, B, sb, [0, M], None, trans_b)
+
+
 def test_many_groups_and_offsets_out_of_range(am):
     """More groups than a wave has lanes; offsets past either end count as the end."""
     g = gen(3)
