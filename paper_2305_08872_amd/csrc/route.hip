@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(1024) route_choose_kernel(const RouteArgs a, c
                 x[j] = v > -INFINITY ? v : -INFINITY;     // (NaN too)
             }
         }
-        float most = 0.0f, all = 0.0f, mine = 0.0f, sum = 0.0f;
+        float most = 0.0f, all = 0.0f, mine = -INFINITY;   // lane j: the j-th highest
         int expert = -1;
         for (int j = 0; j < a.k; ++j) {
             float best = x[0];
@@ -218,16 +218,16 @@ __global__ void __launch_bounds__(1024) route_choose_kernel(const RouteArgs a, c
                     all = group_sum<L>(all);
                 }
             }
-            const float term = found ? term_of(best, most) : 0.0f;
-            sum += term;
-            if (in == j) { mine = term; expert = found ? (int)e : -1; }
+            if (in == j) { mine = best; expert = found ? (int)e : -1; }
 #pragma unroll
             for (int v = 0; v < V; ++v) x[v] = e == (uint32_t)(in + L * v) ? -INFINITY : x[v];
         }
+        const float term = expert < 0 ? 0.0f : term_of(mine, most);
+        if (a.norm) all = group_sum<L>(term);
         if (in < a.k) {
             const int64_t at = t * a.k + in;
             a.experts[at] = expert;
-            a.weights[at] = expert < 0 ? 0.0f : mine / (a.norm ? sum : all);
+            a.weights[at] = expert < 0 ? 0.0f : term / all;
             if (chosen_lds) chosen_lds[i * a.k + in] = expert;
             if (expert >= 0) atomicAdd(&count[expert], 1);
         }
@@ -276,8 +276,9 @@ __global__ void __launch_bounds__(1024) route_place_kernel(const RouteArgs a, co
 }
 
 // dx = p (up - sum p up), up: the weights' gradients at the chosen experts; p: the weights (norm) or the softmax over all.
-// A token to L lanes, its row in LDS while the chosen experts' parts are added (each expert once: no two lanes meet).
-template <int TYPE, int L>
+// A token to L lanes, each with the logits of experts lane + L j and one of the chosen ones, all asked for at once; the row passes through LDS, where
+// the chosen experts' parts are added (each expert once: no two lanes meet).
+template <int TYPE, int L, int V>
 __global__ void __launch_bounds__(256) route_grad_kernel(const RouteArgs a)
 {
     extern __shared__ float grad_lds[];
@@ -285,43 +286,51 @@ __global__ void __launch_bounds__(256) route_grad_kernel(const RouteArgs a)
     const int64_t t = (int64_t)blockIdx.x * (256 / L) + group;
     if (t >= a.T) return;
     float *const row = grad_lds + group * a.E;
-    float mean = 0.0f;
-    for (int j = in; j < a.k; j += L)
-        if (a.experts[t * a.k + j] >= 0) mean += a.weights[t * a.k + j] * a.dweights[t * a.k + j];
-    mean = group_sum<L>(mean);
+    int e = -1;
+    float w = 0.0f, up = 0.0f;
+    if (in < a.k) {
+        e = a.experts[t * a.k + in];
+        w = a.weights[t * a.k + in];
+        up = a.dweights[t * a.k + in];
+    }
+    float x[V];
+    if (!a.norm) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = in + L * v < a.E ? load_logit<TYPE>(a.logits, t * a.ldx + in + L * v) : -INFINITY;
+    }
+    if ((unsigned)e >= (unsigned)a.E) { e = -1; w = 0.0f; up = 0.0f; }
+    const float mean = group_sum<L>(w * up);
     if (a.norm) {
-        for (int e = in; e < a.E; e += L) row[e] = 0.0f;
+        for (int i = in; i < a.E; i += L) row[i] = 0.0f;
     } else {
         float most = -INFINITY, all = 0.0f;
-        for (int e = in; e < a.E; e += L) {
-            const float x = load_logit<TYPE>(a.logits, t * a.ldx + e);
-            row[e] = x > -INFINITY ? x : -INFINITY;        // (NaN: masked)
-            most = fmaxf(most, row[e]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            x[v] = x[v] > -INFINITY ? x[v] : -INFINITY;    // (NaN: masked)
+            most = fmaxf(most, x[v]);
         }
         most = group_max<L>(most);
-        for (int e = in; e < a.E; e += L) {
-            row[e] = row[e] > -INFINITY ? term_of(row[e], most) : 0.0f;
-            all += row[e];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            x[v] = x[v] > -INFINITY ? term_of(x[v], most) : 0.0f;
+            all += x[v];
         }
         all = group_sum<L>(all);
         const float scale = all > 0.0f ? -mean / all : 0.0f;
-        for (int e = in; e < a.E; e += L) row[e] = row[e] * scale;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (in + L * v < a.E) row[in + L * v] = x[v] > 0.0f ? x[v] * scale : 0.0f;   // (masked: whatever the mean is)
     }
     __builtin_amdgcn_wave_barrier();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    for (int j = in; j < a.k; j += L) {
-        const int e = a.experts[t * a.k + j];
-        if ((unsigned)e >= (unsigned)a.E) continue;
-        const float w = a.weights[t * a.k + j], up = a.dweights[t * a.k + j];
-        row[e] += a.norm ? w * (up - mean) : w * up;
-    }
+    if (e >= 0) row[e] += a.norm ? w * (up - mean) : w * up;
     __builtin_amdgcn_wave_barrier();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    for (int e = in; e < a.E; e += L) {
-        const int64_t at = t * a.lddx + e;
-        if constexpr (TYPE == EXPERTS_FP32) ((float *)a.dlogits)[at] = row[e];
-        else if constexpr (TYPE == EXPERTS_BF16) ((__bf16 *)a.dlogits)[at] = (__bf16)row[e];
-        else ((_Float16 *)a.dlogits)[at] = (_Float16)row[e];
+    for (int i = in; i < a.E; i += L) {
+        const int64_t at = t * a.lddx + i;
+        if constexpr (TYPE == EXPERTS_FP32) ((float *)a.dlogits)[at] = row[i];
+        else if constexpr (TYPE == EXPERTS_BF16) ((__bf16 *)a.dlogits)[at] = (__bf16)row[i];
+        else ((_Float16 *)a.dlogits)[at] = (_Float16)row[i];
     }
 }
 
@@ -363,9 +372,13 @@ template <int TYPE>
 static hipError_t launch_grad_type(const RouteArgs &a, hipStream_t s)
 {
     if (forced_launch_failure()) return hipErrorLaunchFailure;
-    // (a row of up to 1024 logits: 16 rows of them are 64 KB)
-    if (a.E <= 256) route_grad_kernel<TYPE, 16><<<dim3((unsigned)((a.T + 15) / 16)), dim3(256), 16 * (size_t)a.E * 4, s>>>(a);
-    else route_grad_kernel<TYPE, 64><<<dim3((unsigned)((a.T + 3) / 4)), dim3(256), 4 * (size_t)a.E * 4, s>>>(a);
+    const dim3 small((unsigned)((a.T + 15) / 16)), large((unsigned)((a.T + 3) / 4));
+    const size_t row = (size_t)a.E * 4;
+    // (every lane has one of the chosen experts)
+    if (a.k > 16 || a.E > 256) route_grad_kernel<TYPE, 64, 16><<<large, dim3(256), 4 * row, s>>>(a);
+    else if (a.E <= 64) route_grad_kernel<TYPE, 16, 4><<<small, dim3(256), 16 * row, s>>>(a);
+    else if (a.E <= 128) route_grad_kernel<TYPE, 16, 8><<<small, dim3(256), 16 * row, s>>>(a);
+    else route_grad_kernel<TYPE, 16, 16><<<small, dim3(256), 16 * row, s>>>(a);
     return hipGetLastError();
 }
 hipError_t launch_route_grad(const RouteArgs &a, hipStream_t s)
