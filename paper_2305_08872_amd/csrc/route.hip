@@ -80,6 +80,25 @@ __device__ __forceinline__ float group_max(float x)
     return x;
 }
 
+// Logits in the order of integers, whose maxima take no canonical forms: -0 is 0, and what is never chosen (-inf, NaN) is the least.
+constexpr int RT_MASKED = (int)0x807fffff;   // -inf
+__device__ __forceinline__ int key_of(float x)
+{
+    const int bits = __builtin_bit_cast(int, x + 0.0f);
+    return x > -INFINITY ? bits ^ ((bits >> 31) & 0x7fffffff) : RT_MASKED;
+}
+__device__ __forceinline__ float logit_of(int key) { return __builtin_bit_cast(float, key ^ ((key >> 31) & 0x7fffffff)); }
+template <int L>
+__device__ __forceinline__ int group_max(int x)
+{
+    x = max(x, (int)of_partner<1>((uint32_t)x));
+    x = max(x, (int)of_partner<2>((uint32_t)x));
+    x = max(x, (int)of_partner<4>((uint32_t)x));
+    x = max(x, (int)of_partner<8>((uint32_t)x));
+    if constexpr (L == 64) { x = max(x, (int)of_partner<16>((uint32_t)x)); x = max(x, (int)of_partner<32>((uint32_t)x)); }
+    return x;
+}
+
 // a logit's share before it is divided by the sum: an infinite maximum shares among the infinite ones
 __device__ __forceinline__ float term_of(float x, float most)
 {
@@ -188,41 +207,36 @@ __global__ void __launch_bounds__(1024) route_choose_kernel(const RouteArgs a, c
     for (int i = group; i < block_tokens; i += groups) {
         const int64_t t = t0 + i;
         if (t >= a.T) break;                              // (a whole group of lanes; the shuffles below stay within groups)
-        float x[V];                                       // -inf: masked, taken or past the last expert
+        int x[V];                                         // RT_MASKED: masked, taken or past the last expert
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int e = in + L * j;
-            x[j] = -INFINITY;
-            if (e < a.E) {
-                const float v = load_logit<TYPE>(a.logits, t * a.ldx + e);
-                x[j] = v > -INFINITY ? v : -INFINITY;     // (NaN too)
-            }
+            x[j] = e < a.E ? key_of(load_logit<TYPE>(a.logits, t * a.ldx + e)) : RT_MASKED;
         }
-        float most = 0.0f, all = 0.0f, mine = -INFINITY;   // lane j: the j-th highest
-        int expert = -1;
+        float most = 0.0f, all = 0.0f;
+        int mine = RT_MASKED, expert = -1;                // lane j: the j-th highest
         for (int j = 0; j < a.k; ++j) {
-            float best = x[0];
+            int best = x[0];
 #pragma unroll
-            for (int v = 1; v < V; ++v) best = fmaxf(best, x[v]);
+            for (int v = 1; v < V; ++v) best = max(best, x[v]);
             best = group_max<L>(best);
-            const bool found = best > -INFINITY;
             uint32_t e = 0xffffffffu;
 #pragma unroll
-            for (int v = V - 1; v >= 0; --v) e = x[v] == best ? (uint32_t)(in + L * v) : e;   // (0 and -0 are equal)
+            for (int v = V - 1; v >= 0; --v) e = x[v] == best ? (uint32_t)(in + L * v) : e;
             e = group_min<L>(e);
             if (j == 0) {
-                most = best;
-                if (!a.norm && found) {
+                most = logit_of(best);
+                if (!a.norm && best > RT_MASKED) {
 #pragma unroll
-                    for (int v = 0; v < V; ++v) all += x[v] > -INFINITY ? term_of(x[v], most) : 0.0f;
+                    for (int v = 0; v < V; ++v) all += x[v] > RT_MASKED ? term_of(logit_of(x[v]), most) : 0.0f;
                     all = group_sum<L>(all);
                 }
             }
-            if (in == j) { mine = best; expert = found ? (int)e : -1; }
+            if (in == j) { mine = best; expert = best > RT_MASKED ? (int)e : -1; }
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[v] = e == (uint32_t)(in + L * v) ? -INFINITY : x[v];
+            for (int v = 0; v < V; ++v) x[v] = e == (uint32_t)(in + L * v) ? RT_MASKED : x[v];
         }
-        const float term = expert < 0 ? 0.0f : term_of(mine, most);
+        const float term = expert < 0 ? 0.0f : term_of(logit_of(mine), most);
         if (a.norm) all = group_sum<L>(term);
         if (in < a.k) {
             const int64_t at = t * a.k + in;
