@@ -3,7 +3,8 @@
 //
 // dB[g] = sum over g's rows of A^T D: both operands lie across k, so both are read by ds_read_b64_tr_b16.  Bound by the matrix cores
 // and, more than the products by rows, by each tile's start: a group's sum is short (16384 rows over 16 groups of 2048 x
-// 4096, some 16 stages of 64 rows to a tile: 355 us = 775 TFLOP/s).
+// 4096, some 16 stages of 64 rows to a tile: 345 us = 797 TFLOP/s; the same rows in 4 groups, 64 stages, 262 = 1050).  A round of tiles writes
+// what memory takes 7 us for, while no tile computes.
 // Few outputs and many rows: parts of a group's rows on more of the chip, their fp32 tiles added up in order.
 #include "experts_tile.h"
 

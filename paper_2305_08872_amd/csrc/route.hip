@@ -8,8 +8,9 @@
 // order is an integer and every sum of weights is one lane group's, so results do not depend on timing.
 //
 // Bounds: its bytes are few (16384 tokens x 128 experts, k = 8, fp32: 10.5 MB forward, 18 with the gradient, 2 and 4 us as a copy).  Choosing takes
-// k maxima that wait for each other, 10.8 us there; placing 7.6, of which most is finding the bases in 256 blocks' counts and
-// the launch; the gradient 9.0.  8 tokens x 64 experts, k = 6: 4.9 us, launch included, one workgroup's latencies.  16 lanes to a token up to 256 experts:
+// k maxima that wait for each other, 9.6 us there (10.8 by floating point maxima and an exponential in each round); placing 7.6, of
+// which most is finding the bases in 256 blocks' counts; the gradient 6.4 (9.0 when it read a token's weights, then its logits).
+// 8 tokens x 64 experts, k = 6: 4.5 us, one workgroup's latencies.  16 lanes to a token up to 256 experts:
 // their maxima stay inside a row of lanes, without the LDS; 64 lanes for more.
 #include <hip/hip_runtime.h>
 #include <math.h>
