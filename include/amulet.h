@@ -633,7 +633,8 @@ int amulet_probe_mfma_i8(int waves_per_simd, double *macs_per_second, void *stre
  *    nothing is 0 (K = 0, a group without rows, rows outside every group).  Only
  *    amulet_combine_grad leaves the rows of dY that no pair names as they are.
  *  - sums are fp32 whatever the operands' type and rounded once to the result's.  Their
- *    order is fixed by the sizes: two calls on the same inputs give the same bits.
+ *    order is fixed by the sizes and the offsets: two calls on the same inputs give
+ *    the same bits.
  *  - NaN and infinities spread through the products as in any sum of products, to the
  *    outputs that they belong to and no others.
  *  - any alignment of elements and any pitch that holds a row is accepted.
