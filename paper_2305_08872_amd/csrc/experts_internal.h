@@ -51,6 +51,15 @@ __host__ __device__ inline int columns_of_largest(int64_t rows, int cols, int un
     return 20 * two < 19 * one ? (int)before : cols;
 }
 
+// Of an operand stored across k whose rows of `row` bytes end inside a unit of 16: of its first `whole` stages of bk k, those that may be read by
+// whole units.  The last unit of a row reaches past it, into rows that have to be there: of `k`, `pitch` bytes apart, k - whole bk
+// lie behind the last one read (rows shorter than a unit may need several).
+__host__ __device__ inline int stages_of_whole_units(int whole, int bk, int k, int64_t row, int64_t pitch)
+{
+    // (one stage fewer is enough: its rows hold more than a unit)
+    return whole > 0 && (int64_t)(k - whole * bk) * pitch < 16 - row % 16 ? whole - 1 : whole;
+}
+
 // tiles of R by rows (experts_mm_*.hip): rows x columns; _K2: two groups of waves share a tile's k
 enum { EXPERTS_256x256 = 0, EXPERTS_128x128 = 1, EXPERTS_64x128 = 2, EXPERTS_64x64 = 3, EXPERTS_64x64_K2 = 4, EXPERTS_16x32 = 5, EXPERTS_TILES = 6 };
 constexpr int kExpertsTileRows[EXPERTS_TILES] = {256, 128, 64, 64, 64, 16};

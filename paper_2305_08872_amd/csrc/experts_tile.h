@@ -712,7 +712,8 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
     // stages that lie wholly inside both operands
     int whole = k > 0 ? k / BK : 0;
     const bool a_cut = sa.cut(), b_cut = sb.cut();
-    if (whole == stages && whole > 0 && (a_cut || b_cut)) --whole;
+    if (a_cut) whole = stages_of_whole_units(whole, BK, k, (int64_t)sa.lines * T::ES, sa.pitch);
+    if (b_cut) whole = stages_of_whole_units(whole, BK, k, (int64_t)sb.lines * T::ES, sb.pitch);
     if ((a_cut && sa.index) || (b_cut && sb.index)) whole = 0;   // (any k may name the storage's last row)
     // BACK: the k that are left are the end of one more stage, which begins before them; what it shares with the stage before is
     // masked in both operands' fragments.  (Through registers / so: fp16, 3001 x 1501 x 1003 over 7 groups

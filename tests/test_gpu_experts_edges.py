@@ -1,0 +1,62 @@
+"""A mixture-of-experts layer's operators at the edges of their ranges, against 64 bits: operands of a few columns, no tokens, results
+in views, offsets that do not ascend.  Bounds as in test_gpu_experts."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from test_gpu_experts import BF16, F32, FP16, check_fp8, fp8_operands, gen, normal, offsets_of, ref_rows, within  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def am():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2305_08872_amd as am
+    am.load_library()
+    return am
+
+
+def i32(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+# rows of a matrix shorter than the 16 bytes of a request, and a few k behind the last whole stage
+@pytest.mark.parametrize("K", [64, 65, 66, 129, 131, 263])
+@pytest.mark.parametrize("N", [1, 2, 3, 5, 7])
+def test_matrices_of_a_few_columns(am, N, K):
+    print("few columns", N, K, flush=True)
+    g = gen(N * 1000 + K)
+    for sizes in ([5], [3, 0, 70]):
+        M, at = sum(sizes), offsets_of(sizes)
+        off = i32(at)
+        A, B = normal(g, M, K, dtype=BF16), normal(g, len(sizes), K, N, dtype=BF16)
+        R = torch.full((M, N), math.nan, device="cuda")
+        am.amulet_grouped_mm(A, B, off, R)
+        want, S = ref_rows(A, B, at, M, None, False)
+        within(R, want, 2 * (K + 8) * 2.0 ** -24 * S, "R")
+        A8, sa, B8, sb = fp8_operands(g, M, K, (len(sizes), K, N))
+        R = torch.full((M, N), math.nan, dtype=BF16, device="cuda")
+        am.amulet_grouped_mm_fp8(A8, sa, B8, sb, off, R)
+        check_fp8(R, A8, sa, B8, sb, at, None, False)
+
+
+@pytest.mark.parametrize("M", [65, 66, 129, 700])
+@pytest.mark.parametrize("K,N", [(1, 1), (2, 40), (3, 3), (300, 1), (7, 2)])
+def test_gradients_of_matrices_of_a_few_columns(am, M, K, N):
+    print("gradients, few columns", M, K, N, flush=True)
+    g = gen(M + K + N)
+    A, D = normal(g, M, K, dtype=FP16), normal(g, M, N, dtype=FP16)
+    for sizes in ([M], [M - 64, 64], [M - 1, 0, 1]):
+        at = offsets_of(sizes)
+        ws = torch.full((1 << 20,), math.nan, device="cuda")
+        for trans_r in (False, True):
+            R = torch.full((len(sizes), N, K) if trans_r else (len(sizes), K, N), math.nan, device="cuda")
+            am.amulet_grouped_mm_wgrad(A, D, i32(at), R, ws, trans_r=trans_r)
+            for e, (i, j) in enumerate(zip(at, at[1:])):
+                a, d = A[i:j].double(), D[i:j].double()
+                w, s = a.t().contiguous() @ d, a.abs().t().contiguous() @ d.abs()
+                within(R[e], w.t() if trans_r else w, 2 * (M + 8) * 2.0 ** -24 * (s.t() if trans_r else s), "dB")
