@@ -656,7 +656,7 @@ typedef enum { AMULET_FP32 = 0, AMULET_BF16 = 1, AMULET_FP16 = 2 } amulet_type_t
  *   tokens[row]       the token of a row (T * k values; -1 past the last row)
  *   offsets[e]        first row of expert e (E + 1 values; the last is the number of rows)
  * The workspace (amulet_route_workspace_bytes, 0 up to 64 tokens) holds counts during the call.
- * One kernel up to 64 tokens, two for more.
+ * One kernel up to 64 tokens, two for more.  Without tokens (T = 0) the offsets are written, zeros; the other pointers may be NULL.
  */
 size_t amulet_route_workspace_bytes(int64_t T, int64_t E);
 int amulet_route(int type, int64_t T, int64_t E, int64_t k, const void *logits, int64_t ldx, int norm,

@@ -29,7 +29,8 @@ static int64_t tokens_of_a_block(int64_t T)
     const int64_t passes = (T + (int64_t)RT_TOKENS * RT_MOST_BLOCKS - 1) / ((int64_t)RT_TOKENS * RT_MOST_BLOCKS);
     return RT_TOKENS * (passes < 1 ? 1 : passes);
 }
-int64_t route_blocks(int64_t T) { return (T + tokens_of_a_block(T) - 1) / tokens_of_a_block(T); }
+// (one without tokens too, which writes the offsets)
+int64_t route_blocks(int64_t T) { return T > 0 ? (T + tokens_of_a_block(T) - 1) / tokens_of_a_block(T) : 1; }
 
 template <int TYPE>
 __device__ __forceinline__ float load_logit(const void *p, int64_t at)

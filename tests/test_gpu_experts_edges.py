@@ -60,3 +60,44 @@ def test_gradients_of_matrices_of_a_few_columns(am, M, K, N):
                 a, d = A[i:j].double(), D[i:j].double()
                 w, s = a.t().contiguous() @ d, a.abs().t().contiguous() @ d.abs()
                 within(R[e], w.t() if trans_r else w, 2 * (M + 8) * 2.0 ** -24 * (s.t() if trans_r else s), "dB")
+
+
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("E,k", [(1, 1), (8, 2), (200, 8), (1000, 64)])
+def test_no_tokens(am, E, k, norm):
+    """A batch without tokens: no expert has a row.  The offsets say so to the products, which write zeros."""
+    print("no tokens", E, k, norm, flush=True)
+    none = dict(dtype=torch.int32, device="cuda")
+    for dtype in (F32, BF16, FP16):
+        offsets = torch.full((E + 1,), 99, **none)
+        logits = torch.empty(0, E, dtype=dtype, device="cuda")
+        experts, weights = torch.empty(0, k, **none), torch.empty(0, k, device="cuda")
+        place, tokens = torch.empty(0, k, **none), torch.empty(0, **none)
+        am.amulet_route(logits, experts, weights, place, tokens, offsets, norm=norm)
+        assert not offsets.any()
+        am.amulet_route_grad(logits, experts, weights, torch.empty(0, k, device="cuda"), torch.empty_like(logits), norm=norm)
+    x, W = torch.empty(0, 16, dtype=BF16, device="cuda"), torch.ones(E, 16, 24, dtype=BF16, device="cuda")
+    y, R = torch.empty(0, 24, dtype=BF16, device="cuda"), torch.empty(0, 24, dtype=BF16, device="cuda")
+    am.amulet_grouped_mm(x, W, offsets, y, rows=tokens)
+    am.amulet_combine(y, weights, place, R)
+    am.amulet_combine_grad(y, weights, place, R, y, weights)
+    dW = torch.ones_like(W)
+    am.amulet_grouped_mm_wgrad(x, y, offsets, dW, rows=tokens)
+    assert not dW.any()
+    am.amulet_quantize_fp8(x, torch.empty(0, 16, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(1, 0, device="cuda"))
+
+
+def test_layer_without_tokens(am):
+    """The example layer on an empty batch: outputs without rows, gradients that are zeros."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import experts_layer
+    layer = experts_layer.Layer(32, 48, 4, 2)
+    x = torch.empty(0, 32, dtype=BF16, device="cuda")
+    out = layer.forward(x)
+    dx, drouter, dw1, dw2 = layer.backward(out)
+    assert out.shape == dx.shape == (0, 32)
+    assert not drouter.any() and not dw1.any() and not dw2.any()
+    layer.quantize()
+    assert layer.forward_8bit(x).shape == (0, 32)
