@@ -531,7 +531,10 @@ int amulet_selected_shape(int task, int64_t M, int64_t N, int64_t K);
  * share a tile's K.  An operator of a mixture-of-experts layer: its name and
  * tile (grouped_mm_256x256, ..., _k2: two groups of waves share a tile's k;
  * grouped_mm_wgrad_..., mm_fp8_..., route, combine_grad, ...) and " rows
- * <rows or tokens>".  The adaptive
+ * <rows or tokens>"; a call whose launches are a pair has one text: " last_columns
+ * <side of their tiles>" where a second launch runs the last columns of a product by
+ * rows (as many as the device finds, for unlucky offsets none), and " parts <ranges>" where
+ * grouped_mm_wgrad sums a group's rows in so many ranges and adds them up afterwards.  The adaptive
  * calls make one launch per trial and one for the rest.  Static storage of the
  * calling thread, until its next call of this function.
  */

@@ -172,7 +172,8 @@ struct KernelNote {
     int critical;                  // (rows of a tile of the kernel by critical values, which has no shape id either)
     int groups;                    // (fp64 identity: groups of waves that share a tile's K)
     CountRan ran;                  // (join count by a shape id)
-    const char *name;              // (an operator of a mixture-of-experts layer: the whole name)
+    const char *name;              // (an operator of a mixture-of-experts layer: the whole name, and
+    int last_columns;              // the side of the tiles that a second launch runs for the last columns, if it does)
 };
 constexpr unsigned KERNEL_NOTES = 16;
 static thread_local KernelNote g_notes[KERNEL_NOTES];
@@ -180,14 +181,20 @@ static thread_local unsigned g_notes_made = 0;
 static KernelNote &new_note(int task, int f64, int shape, int64_t rows)
 {
     KernelNote &n = g_notes[g_notes_made++ % KERNEL_NOTES];
-    n = KernelNote{task, f64, shape, 0, 1, 0, 0, 0, 0, 0, 0, rows, 0, 0, 1, CountRan(), nullptr};
+    n = KernelNote{task, f64, shape, 0, 1, 0, 0, 0, 0, 0, 0, rows, 0, 0, 1, CountRan(), nullptr, 0};
     return n;
 }
 
 // text of the last HIP error a launch reported (diagnostics for AMULET_ERR_LAUNCH)
 static thread_local hipError_t g_last_hip_error = hipSuccess;
 
-void note_kernel(const char *name, int64_t rows) { new_note(-1, 0, -1, rows).name = name; }
+void note_kernel(const char *name, int64_t rows, int last_columns, int parts)
+{
+    KernelNote &n = new_note(-1, 0, -1, rows);
+    n.name = name;
+    n.last_columns = last_columns;
+    n.parts = parts;
+}
 int launch_status(hipError_t e)
 {
     g_last_hip_error = e;
@@ -1778,7 +1785,9 @@ const char *amulet_recent_kernel(int back)
     const KernelNote &n = g_notes[(g_notes_made - 1 - (unsigned)back) % KERNEL_NOTES];
     const long long rows = (long long)n.rows;
     if (n.name) {
-        snprintf(text, sizeof(text), "%s rows %lld", n.name, rows);
+        if (n.last_columns) snprintf(text, sizeof(text), "%s rows %lld last_columns %d", n.name, rows, n.last_columns);
+        else if (n.parts > 1) snprintf(text, sizeof(text), "%s rows %lld parts %d", n.name, rows, n.parts);
+        else snprintf(text, sizeof(text), "%s rows %lld", n.name, rows);
     } else if (n.shape >= 0) {
         const char *name = !n.f64 ? amulet_shape_name(n.task, n.shape)
                            : n.task != TASK_IDENTITY ? amulet_f64_shape_name(n.shape)

@@ -120,7 +120,8 @@ static int run_rows(const char *const *names, int type, int trans_b, ExpertsArgs
     const int tile = rows_tile(M, N, a.K, G < 1 ? 1 : G, es, !trans_b, type != EXPERTS_FP8_EXACT && near);
     const int64_t blocks = rows_blocks(tile, M, N, G, a.offsets != nullptr);
     if (blocks > kMostBlocks) return AMULET_ERR_RANGE;
-    note_kernel(names[tile], M);
+    const int64_t behind = tile == EXPERTS_256x256 ? cut_blocks(a, M, N, G, a.offsets != nullptr, es) : 0;
+    note_kernel(names[tile], M, behind ? kExpertsTileCols[EXPERTS_128x128] : 0);
     hipStream_t s = (hipStream_t)stream;
     auto launch = [&](int shape, int64_t n) {
         switch (type) {
@@ -130,7 +131,6 @@ static int run_rows(const char *const *names, int type, int trans_b, ExpertsArgs
         default: return launch_status(launch_experts_rows_fp8(shape, !trans_b, a, n, s));
         }
     };
-    const int64_t behind = tile == EXPERTS_256x256 ? cut_blocks(a, M, N, G, a.offsets != nullptr, es) : 0;
     if (behind == 0) return launch(tile, blocks);
     a.part_of = EXPERTS_BEFORE;
     const int rc = launch(tile, blocks);
@@ -338,7 +338,7 @@ int amulet_grouped_mm_wgrad(int type, int out_type, int trans_r, int64_t M, int6
     const int64_t bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
     const int64_t tiles = ((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn) * G;
     if (sums_blocks(tiles / G, G * a.parts) > kMostBlocks || tiles * (bm * bn / 1024) > kMostBlocks) return AMULET_ERR_RANGE;
-    note_kernel(tile == EXPERTS_256x256 ? "grouped_mm_wgrad_256x256" : tile == EXPERTS_128x128 ? "grouped_mm_wgrad_128x128" : "grouped_mm_wgrad_64x64", M);
+    note_kernel(tile == EXPERTS_256x256 ? "grouped_mm_wgrad_256x256" : tile == EXPERTS_128x128 ? "grouped_mm_wgrad_128x128" : "grouped_mm_wgrad_64x64", M, 0, a.parts);
     hipStream_t s = (hipStream_t)stream;
     const int rc = launch_status(launch_experts_sums(type, tile, a, sums_blocks(tiles / G, G * a.parts), s));
     if (rc != AMULET_OK || a.parts == 1) return rc;

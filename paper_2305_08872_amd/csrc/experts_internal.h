@@ -118,8 +118,9 @@ struct QuantizeArgs {
 hipError_t launch_quantize_rows(const QuantizeArgs &a, hipStream_t s);
 hipError_t launch_quantize_blocks(const QuantizeArgs &a, hipStream_t s);
 
-// the calling thread's note of a launch (amulet_recent_kernel), and the status of a launch's error (amulet_last_launch_error)
-void note_kernel(const char *name, int64_t rows);
+// the calling thread's note of a call (amulet_recent_kernel): what its second launch is, if there is one; and the status of a
+// launch's error (amulet_last_launch_error)
+void note_kernel(const char *name, int64_t rows, int last_columns = 0, int parts = 1);
 int launch_status(hipError_t e);
 
 }  // namespace amulet

@@ -1,0 +1,51 @@
+"""The mixture-of-experts operators' host side at the edges of their ranges (CPU only): what a call with two launches tells of them."""
+import ctypes
+import os
+
+import pytest
+
+import paper_2305_08872_amd as am
+from paper_2305_08872_amd import build as hip_build
+
+P = ctypes.c_void_p(1 << 20)      # never read
+F32, BF16, FP16 = am.AMULET_FP32, am.AMULET_BF16, am.AMULET_FP16
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(am.library_path()):
+        hip_build.build()
+    yield am.load_library()
+    am.amulet_debug_fail_launches(0)
+
+
+def note(call, status=-5):
+    """amulet_recent_kernel after a call whose launch is refused, as (name, fields)."""
+    am.amulet_debug_fail_launches(1)
+    try:
+        assert call() == status
+    finally:
+        am.amulet_debug_fail_launches(0)
+    words = am.amulet_recent_kernel().split()
+    return words[0], dict(zip(words[1::2], map(int, words[2::2])))
+
+
+def test_a_call_tells_of_its_second_launch(lib):
+    def rows(M, N, K, G):
+        return note(lambda: lib.amulet_grouped_mm(BF16, BF16, 1, M, N, K, G, P, K, None, M, P, K, N * K, P, P, N, None))
+    assert rows(4096, 4500, 1203, 1) == ("grouped_mm_256x256", {"rows": 4096, "last_columns": 128})
+    assert rows(4096, 4096, 1203, 1) == ("grouped_mm_256x256", {"rows": 4096})        # whole rounds
+    assert rows(4114, 4501, 1211, 2) == ("grouped_mm_256x256", {"rows": 4114, "last_columns": 128})
+
+    def fp8(N):
+        return note(lambda: lib.amulet_mm_fp8(BF16, 1, 4096, N, 2111, P, 2111, P, 4096, P, 2111, P, 17, P, N, None))
+    assert fp8(4501) == ("mm_fp8_256x256", {"rows": 4096, "last_columns": 128})
+    assert fp8(4096) == ("mm_fp8_256x256", {"rows": 4096})
+
+    def sums(M, N, K, G, ws, n):
+        return note(lambda: lib.amulet_grouped_mm_wgrad(BF16, F32, 0, M, N, K, G, P, K, None, M, P, N, P, P, N, N * K, ws, n, None))
+    assert sums(20000, 64, 64, 1, None, 0) == ("grouped_mm_wgrad_64x64", {"rows": 20000})
+    name, told = sums(20000, 64, 64, 1, P, 1 << 26)
+    assert name == "grouped_mm_wgrad_64x64" and told["parts"] > 1
+    # a call of the products after it has none
+    assert rows(4096, 4096, 1203, 1)[1] == {"rows": 4096}

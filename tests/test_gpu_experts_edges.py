@@ -101,3 +101,35 @@ def test_layer_without_tokens(am):
     assert not drouter.any() and not dw1.any() and not dw2.any()
     layer.quantize()
     assert layer.forward_8bit(x).shape == (0, 32)
+
+
+# The largest tiles fill the chip once and a bit, and the columns end inside a tile, a unit and a stage: the second launch's too.
+@pytest.mark.parametrize("trans_b", [False, True])
+@pytest.mark.parametrize("first,sizes,rest,N,K,tokens", [(0, [4096], 0, 4500, 1203, 0), (0, [4096], 0, 4367, 1211, 0), (5, [2000, 2100], 9, 4501, 1211, 777)])
+def test_the_last_columns_of_ragged_products(am, first, sizes, rest, N, K, tokens, trans_b):
+    print("last columns", first, sizes, rest, N, K, tokens, trans_b, flush=True)
+    g = gen(N + K)
+    M = first + sum(sizes) + rest
+    A = normal(g, tokens or M, K, dtype=BF16)
+    B = normal(g, len(sizes), *((N, K) if trans_b else (K, N)), dtype=BF16)
+    rows = torch.randint(-1, tokens + 1, (M,), generator=g, device="cuda", dtype=torch.int32) if tokens else None
+    at = offsets_of(sizes, first)
+    R = torch.full((M, N), math.nan, dtype=BF16, device="cuda")
+    am.amulet_grouped_mm(A, B, i32(at), R, rows=rows, trans_b=trans_b)
+    assert am.amulet_recent_kernel() == "grouped_mm_256x256 rows %d last_columns 128" % M
+    want, S = ref_rows(A, B, at, M, rows, trans_b)
+    within(R, want, 2 * (K + 8) * 2.0 ** -24 * S, "R")
+    again = torch.full_like(R, math.nan)
+    am.amulet_grouped_mm(A, B, i32(at), again, rows=rows, trans_b=trans_b)
+    assert torch.equal(again, R)
+
+
+@pytest.mark.parametrize("trans_b", [False, True])
+def test_the_last_columns_of_a_ragged_8_bit_product(am, trans_b):
+    g = gen(78)
+    M, N, K = 4096, 4501, 2111
+    A, sa, B, sb = fp8_operands(g, M, K, (1, N, K) if trans_b else (1, K, N))
+    R = torch.full((M, N), math.nan, dtype=BF16, device="cuda")
+    am.amulet_mm_fp8(A, sa, B[0], sb[0], R, trans_b=trans_b)
+    assert am.amulet_recent_kernel() == "mm_fp8_256x256 rows %d last_columns 128" % M
+    check_fp8(R, A, sa, B, sb, [0, M], None, trans_b)
