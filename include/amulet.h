@@ -641,6 +641,8 @@ int amulet_probe_mfma_i8(int waves_per_simd, double *macs_per_second, void *stre
  *  - NaN and infinities spread through the products as in any sum of products, to the
  *    outputs that they belong to and no others.
  *  - any alignment of elements and any pitch that holds a row is accepted.
+ *    Matrices of a group that are read may overlap; those that are written lie one
+ *    behind the other or have their rows in turn, at any distance that keeps them apart.
  *  - `offsets`: int32, G + 1 values in device memory, ascending; rows offsets[g] to
  *    offsets[g+1] - 1 belong to group g.  They are read on the device only.  Values
  *    outside 0..M count as the nearest of the two; where they do not ascend, results are

@@ -18,6 +18,14 @@ static const int64_t kMostPitch = 0xffffffffLL / 256 - 65536;
 static bool known16(int type) { return type == AMULET_BF16 || type == AMULET_FP16; }
 static bool known(int type) { return type == AMULET_FP32 || known16(type); }
 
+// G matrices of rows x cols, rows ld apart and matrices `group`, that are written: no two share an element.  Either they lie one behind
+// the other, or the rows of all of them in turn.
+static bool groups_apart(int64_t G, int64_t rows, int64_t cols, int64_t ld, int64_t group)
+{
+    if (G <= 1) return true;
+    return group >= cols && ((group - cols) / ld >= rows - 1 || (ld - cols) / group >= G - 1);
+}
+
 // Tiles by rows: the one with the lowest estimate.  A workgroup that has its unit alone takes `stage` us for a stage of its k
 // (64 of 16 bits, 128 of 8), of which larger tiles have less per product, and `start` for finding its tile, filling its ring and
 // storing; all workgroups together take no more from the L2s than some 64 KB a us and unit, of which smaller tiles
@@ -319,7 +327,7 @@ int amulet_grouped_mm_wgrad(int type, int out_type, int trans_r, int64_t M, int6
     if (M > kMostRows || N > kMostRows || K > kMostRows || a_rows > kMostRows || G > kMostGroups) return AMULET_ERR_RANGE;
     if (G == 0 || N == 0 || K == 0) return AMULET_OK;
     if (!R || !offsets) return AMULET_ERR_NULL;
-    if (ldr < (trans_r ? K : N) || (G > 1 && group_r / ldr < (trans_r ? N : K))) return AMULET_ERR_LD;
+    if (ldr < (trans_r ? K : N) || !groups_apart(G, trans_r ? N : K, trans_r ? K : N, ldr, group_r)) return AMULET_ERR_LD;
     const bool some = M > 0 && !(rows && a_rows == 0);   // else: zeros, and the operands are not read
     if (some && (!A || !D)) return AMULET_ERR_NULL;
     if (some && (lda < K || ldd < N)) return AMULET_ERR_LD;
@@ -372,7 +380,8 @@ int amulet_quantize_fp8_blocks(int type, int64_t G, int64_t M, int64_t K, const 
     const int64_t MB = (M + 127) / 128, KB = (K + 127) / 128;
     if (MB * KB > kMostBlocks / G) return AMULET_ERR_RANGE;
     if (!X || !Q || !scales) return AMULET_ERR_NULL;
-    if (ldx < K || ldq < K || lds < KB || (G > 1 && (group_x < 0 || group_q / ldq < M || group_s / lds < MB))) return AMULET_ERR_LD;
+    if (ldx < K || ldq < K || lds < KB || (G > 1 && group_x < 0)) return AMULET_ERR_LD;
+    if (!groups_apart(G, M, K, ldq, group_q) || !groups_apart(G, MB, KB, lds, group_s)) return AMULET_ERR_LD;
     QuantizeArgs a = {};
     a.X = X; a.ldx = ldx; a.group_x = group_x; a.Q = (uint8_t *)Q; a.ldq = ldq; a.group_q = group_q;
     a.scales = scales; a.lds = lds; a.group_s = group_s;

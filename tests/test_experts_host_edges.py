@@ -49,3 +49,22 @@ def test_a_call_tells_of_its_second_launch(lib):
     assert name == "grouped_mm_wgrad_64x64" and told["parts"] > 1
     # a call of the products after it has none
     assert rows(4096, 4096, 1203, 1)[1] == {"rows": 4096}
+
+
+def test_written_matrices_at_any_distance_that_keeps_them_apart(lib):
+    def wgrad(K, N, G, ldr, gr, tr=0):
+        am.amulet_debug_fail_launches(1)
+        return lib.amulet_grouped_mm_wgrad(BF16, F32, tr, 4, N, K, G, P, K, None, 4, P, N, P, P, ldr, gr, None, 0, None)
+    assert wgrad(6, 5, 3, 8, 45) == -5 and wgrad(6, 5, 3, 8, 44) == -4             # the last row without its padding
+    assert wgrad(6, 5, 3, 15, 5) == -5 and wgrad(6, 5, 3, 14, 5) == -4 and wgrad(6, 5, 3, 15, 4) == -4   # rows in turn
+    assert wgrad(6, 5, 3, 6, 30, tr=1) == -5 and wgrad(6, 5, 3, 6, 29, tr=1) == -4
+    assert wgrad(1, 5, 3, 5, 5) == -5 and wgrad(1, 5, 3, 5, 0) == -4 and wgrad(6, 5, 3, 8, -45) == -4
+    assert wgrad(6, 5, 2, 2 ** 62, 5) == -5 and wgrad(6, 5, 2, 2 ** 62, 2 ** 62) == -4 and wgrad(6, 5, 1, 5, 0) == -5
+
+    def blocks(G, M, K, ldq, gq, lds, gs):
+        am.amulet_debug_fail_launches(1)
+        return lib.amulet_quantize_fp8_blocks(F32, G, M, K, P, K, M * K, P, ldq, gq, P, lds, gs, None)
+    assert blocks(2, 4, 200, 208, 824, 2, 2) == -5 and blocks(2, 4, 200, 208, 823, 2, 2) == -4
+    assert blocks(2, 4, 200, 400, 200, 2, 2) == -5 and blocks(2, 300, 200, 200, 60000, 3, 8) == -5 and blocks(2, 300, 200, 200, 60000, 3, 7) == -4
+    assert blocks(2, 300, 200, 200, 60000, 4, 2) == -5 and blocks(2, 300, 200, 200, 60000, 3, 2) == -4
+    am.amulet_debug_fail_launches(0)

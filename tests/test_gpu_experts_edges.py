@@ -133,3 +133,51 @@ def test_the_last_columns_of_a_ragged_8_bit_product(am, trans_b):
     am.amulet_mm_fp8(A, sa, B[0], sb[0], R, trans_b=trans_b)
     assert am.amulet_recent_kernel() == "mm_fp8_256x256 rows %d last_columns 128" % M
     check_fp8(R, A, sa, B, sb, [0, M], None, trans_b)
+
+
+def matrices(layout, G, rows, cols, dtype):
+    """(storage filled with sevens, G x rows x cols of it): with a pitch, without the last row's padding, the rows of all matrices in turn."""
+    if layout == "turn":
+        s = torch.full((rows, G, cols + 1), 7.0, device="cuda").to(dtype)
+        return s, s.permute(1, 0, 2)[:, :, :cols]
+    ld = cols + 3
+    apart = rows * ld + 5 if layout == "pitch" else (rows - 1) * ld + cols
+    s = torch.full((1 + (G - 1) * apart + rows * ld,), 7.0, device="cuda").to(dtype)
+    return s, s.as_strided((G, rows, cols), (apart, ld, 1), 1)
+
+
+@pytest.mark.parametrize("layout", ["pitch", "tight", "turn"])
+@pytest.mark.parametrize("sizes,K,N,space", [([40, 0, 33], 37, 21, 0), ([6000, 2000], 70, 45, 1 << 24), ([300, 200], 300, 260, 0)])
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_gradients_into_views(am, sizes, K, N, space, out, layout):
+    """The results' rows and matrices apart: sums over ranges of the rows too.  Nothing beside them is written."""
+    print("gradients into", layout, sizes, K, N, space, out, flush=True)
+    g = gen(K + N)
+    M, G, at = sum(sizes), len(sizes), offsets_of(sizes)
+    A, D = normal(g, M, K, dtype=BF16), normal(g, M, N, dtype=BF16)
+    ws = torch.full((space // 4,), math.nan, device="cuda") if space else None
+    for trans_r in (False, True):
+        store, R = matrices(layout, G, *((N, K) if trans_r else (K, N)), out)
+        am.amulet_grouped_mm_wgrad(A, D, i32(at), R, ws, trans_r=trans_r)
+        assert ("parts" in am.amulet_recent_kernel()) == (space > 0)
+        for e, (i, j) in enumerate(zip(at, at[1:])):
+            a, d = A[i:j].double(), D[i:j].double()
+            w, s = a.t().contiguous() @ d, a.abs().t().contiguous() @ d.abs()
+            within(R[e], w.t() if trans_r else w, 2 * (max(sizes) + 8) * 2.0 ** -24 * (s.t() if trans_r else s), "dB")
+        R.fill_(7.0)
+        assert (store == 7).all()
+
+
+@pytest.mark.parametrize("layout", ["pitch", "tight", "turn"])
+def test_quantised_matrices_into_views(am, layout):
+    G, M, K = 3, 200, 300
+    x = normal(gen(8), G, M, K, dtype=BF16)
+    q, s = torch.empty(G, M, K, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(G, 2, 3, device="cuda")
+    am.amulet_quantize_fp8_blocks(x, q, s)
+    (bytes_q, q2), (store, s2) = matrices(layout, G, M, K, torch.float8_e4m3fn), matrices(layout, G, 2, 3, F32)
+    am.amulet_quantize_fp8_blocks(x, q2, s2)
+    assert torch.equal(q2.float(), q.float()) and torch.equal(s2, s)
+    s2.fill_(7.0)
+    assert (store == 7).all()
+    q2.view(torch.uint8).copy_(torch.full(q2.shape, 7.0, device="cuda").to(torch.float8_e4m3fn).view(torch.uint8))
+    assert (bytes_q.float() == 7).all()
