@@ -640,7 +640,8 @@ int amulet_probe_mfma_i8(int waves_per_simd, double *macs_per_second, void *stre
  *    the same bits.
  *  - NaN and infinities spread through the products as in any sum of products, to the
  *    outputs that they belong to and no others.
- *  - any alignment of elements and any pitch that holds a row is accepted.
+ *  - any alignment of elements and any pitch that holds a row is accepted; of the
+ *    products' operands (A, B, D) up to 16711679 bytes, AMULET_ERR_RANGE above.
  *    Matrices of a group that are read may overlap; those that are written lie one
  *    behind the other or have their rows in turn, at any distance that keeps them apart.
  *  - `offsets`: int32, G + 1 values in device memory, ascending; rows offsets[g] to

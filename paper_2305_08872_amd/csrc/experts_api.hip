@@ -12,7 +12,7 @@ static const int64_t kMostRows = 2147483647LL - 65536LL;   // of a dimension, as
 static const int64_t kMostGroups = 1 << 16;              // (every workgroup looks through the offsets)
 static const int64_t kMostBlocks = 0xffffffffLL / 512;     // workgroups of a launch (a grid holds 2^32 - 1 work-items)
 
-// the longest pitch (bytes) of an operand whose tile's lines, or a stage's k, lie within 32 bits of each other: 256 of them
+// the longest pitch (bytes) of an operand whose tile's lines, or a stage's k, lie within 32 bits of each other: 256 of them, and a row
 static const int64_t kMostPitch = 0xffffffffLL / 256 - 65536;
 
 static bool known16(int type) { return type == AMULET_BF16 || type == AMULET_FP16; }
@@ -82,7 +82,7 @@ static int64_t rows_blocks(int tile, int64_t M, int64_t N, int64_t G, bool group
     return (tiles + 7) / 8 * 8;
 }
 
-static int check_rows(int64_t M, int64_t N, int64_t K, int64_t G, int trans_b, const void *A, int64_t lda, const int32_t *rows, int64_t a_rows,
+static int check_rows(int es, int64_t M, int64_t N, int64_t K, int64_t G, int trans_b, const void *A, int64_t lda, const int32_t *rows, int64_t a_rows,
                       const void *B, int64_t ldb, int64_t group_b, const int32_t *offsets, bool grouped, const void *R, int64_t ldr)
 {
     if (M < 0 || N < 0 || K < 0 || G < 0 || a_rows < 0) return AMULET_ERR_DIM;
@@ -93,7 +93,7 @@ static int check_rows(int64_t M, int64_t N, int64_t K, int64_t G, int trans_b, c
     if (K == 0 || G == 0 || (rows && a_rows == 0)) return AMULET_OK;   // zeros: the operands are not read
     if (!A || !B) return AMULET_ERR_NULL;
     if (lda < K || ldb < (trans_b ? K : N) || (G > 1 && group_b < 0)) return AMULET_ERR_LD;
-    if (lda > kMostPitch / 2 || ldb > kMostPitch / 2) return AMULET_ERR_RANGE;
+    if (lda > kMostPitch / es || ldb > kMostPitch / es) return AMULET_ERR_RANGE;
     return AMULET_OK;
 }
 
@@ -293,7 +293,7 @@ int amulet_grouped_mm(int type, int out_type, int trans_b, int64_t M, int64_t N,
                       void *R, int64_t ldr, void *stream)
 {
     if (!known16(type) || (out_type != AMULET_FP32 && out_type != type)) return AMULET_ERR_TYPE;
-    const int rc = check_rows(M, N, K, G, trans_b, A, lda, rows, a_rows, B, ldb, group_b, offsets, true, R, ldr);
+    const int rc = check_rows(2, M, N, K, G, trans_b, A, lda, rows, a_rows, B, ldb, group_b, offsets, true, R, ldr);
     if (rc != AMULET_OK) return rc > 0 ? AMULET_OK : rc;
     ExpertsArgs a = {};
     a.A = A; a.B = B; a.R = R; a.offsets = offsets; a.rows = rows;
@@ -396,7 +396,7 @@ static int run_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K, i
                    const int32_t *offsets, bool grouped, void *R, int64_t ldr, void *stream)
 {
     if (!known(out_type)) return AMULET_ERR_TYPE;
-    const int rc = check_rows(M, N, K, G, trans_b, A, lda, rows, a_rows, B, ldb, group_b, offsets, grouped, R, ldr);
+    const int rc = check_rows(1, M, N, K, G, trans_b, A, lda, rows, a_rows, B, ldb, group_b, offsets, grouped, R, ldr);
     if (rc != AMULET_OK) return rc > 0 ? AMULET_OK : rc;
     const bool some = K > 0 && G > 0 && !(rows && a_rows == 0);
     if (some && (rows ? a_rows : M) > (1 << 30)) return AMULET_ERR_RANGE;   // (32-bit byte offsets of a block's scales)

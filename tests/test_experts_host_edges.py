@@ -68,3 +68,18 @@ def test_written_matrices_at_any_distance_that_keeps_them_apart(lib):
     assert blocks(2, 4, 200, 400, 200, 2, 2) == -5 and blocks(2, 300, 200, 200, 60000, 3, 8) == -5 and blocks(2, 300, 200, 200, 60000, 3, 7) == -4
     assert blocks(2, 300, 200, 200, 60000, 4, 2) == -5 and blocks(2, 300, 200, 200, 60000, 3, 2) == -4
     am.amulet_debug_fail_launches(0)
+
+
+def test_the_longest_pitch_is_one_of_bytes(lib):
+    most = 16711679
+
+    def mm16(lda=64, ldb=64):
+        am.amulet_debug_fail_launches(1)
+        return lib.amulet_grouped_mm(BF16, F32, 1, 4, 5, 64, 1, P, lda, None, 4, P, ldb, 0, P, P, 5, None)
+
+    def mm8(lda=64, ldb=64):
+        am.amulet_debug_fail_launches(1)
+        return lib.amulet_mm_fp8(BF16, 1, 4, 5, 64, P, lda, P, 4, P, ldb, P, 1, P, 5, None)
+    assert mm8(lda=most) == mm8(ldb=most) == -5 and mm8(lda=most + 1) == mm8(ldb=most + 1) == -7
+    assert mm16(lda=most // 2) == mm16(ldb=most // 2) == -5 and mm16(lda=most // 2 + 1) == mm16(ldb=most // 2 + 1) == -7
+    am.amulet_debug_fail_launches(0)

@@ -181,3 +181,20 @@ def test_quantised_matrices_into_views(am, layout):
     assert (store == 7).all()
     q2.view(torch.uint8).copy_(torch.full(q2.shape, 7.0, device="cuda").to(torch.float8_e4m3fn).view(torch.uint8))
     assert (bytes_q.float() == 7).all()
+
+
+@pytest.mark.parametrize("trans_b", [False, True])
+def test_8_bit_rows_far_apart(am, trans_b):
+    """Rows of 8-bit operands at the longest pitch: the same as of rows side by side."""
+    M, N, K, pitch = 130, 200, 150, 16711679
+    g = gen(31)
+    A, sa, B, sb = fp8_operands(g, M, K, (1, N, K) if trans_b else (1, K, N))
+    R, far = torch.full((M, N), math.nan, device="cuda"), torch.full((M, N), math.nan, device="cuda")
+    am.amulet_mm_fp8(A, sa, B[0], sb[0], R, trans_b=trans_b)
+
+    def apart(x):
+        y = torch.empty((x.shape[0] - 1) * pitch + x.shape[1], dtype=torch.uint8, device="cuda").as_strided(x.shape, (pitch, 1))
+        y.copy_(x.view(torch.uint8))
+        return y.view(torch.float8_e4m3fn)
+    am.amulet_mm_fp8(apart(A), sa, apart(B[0]), sb[0], far, trans_b=trans_b)
+    assert torch.equal(far, R)
