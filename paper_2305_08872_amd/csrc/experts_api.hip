@@ -345,7 +345,8 @@ int amulet_grouped_mm_wgrad(int type, int out_type, int trans_r, int64_t M, int6
     a.parts = plan.parts;
     const int64_t bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
     const int64_t tiles = ((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn) * G;
-    if (sums_blocks(tiles / G, G * a.parts) > kMostBlocks || tiles * (bm * bn / 1024) > kMostBlocks) return AMULET_ERR_RANGE;
+    // (with several parts, which are not for many tiles, the second launch has a workgroup to 1024 outputs)
+    if (sums_blocks(tiles / G, G * a.parts) > kMostBlocks || (a.parts > 1 && tiles * (bm * bn / 1024) > kMostBlocks)) return AMULET_ERR_RANGE;
     note_kernel(tile == EXPERTS_256x256 ? "grouped_mm_wgrad_256x256" : tile == EXPERTS_128x128 ? "grouped_mm_wgrad_128x128" : "grouped_mm_wgrad_64x64", M, 0, a.parts);
     hipStream_t s = (hipStream_t)stream;
     const int rc = launch_status(launch_experts_sums(type, tile, a, sums_blocks(tiles / G, G * a.parts), s));

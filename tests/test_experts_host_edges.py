@@ -83,3 +83,11 @@ def test_the_longest_pitch_is_one_of_bytes(lib):
     assert mm8(lda=most) == mm8(ldb=most) == -5 and mm8(lda=most + 1) == mm8(ldb=most + 1) == -7
     assert mm16(lda=most // 2) == mm16(ldb=most // 2) == -5 and mm16(lda=most // 2 + 1) == mm16(ldb=most // 2 + 1) == -7
     am.amulet_debug_fail_launches(0)
+
+
+def test_large_results_of_the_gradients_are_taken(lib):
+    """128 matrices of 8192 x 8192 (17 GB of bf16): only a launch that adds up ranges has a limit on R's tiles of its own."""
+    assert note(lambda: lib.amulet_grouped_mm_wgrad(BF16, BF16, 0, 65536, 8192, 8192, 128, P, 8192, None, 65536, P, 8192, P, P, 8192, 8192 * 8192, None, 0, None)) \
+        == ("grouped_mm_wgrad_256x256", {"rows": 65536})
+    assert note(lambda: lib.amulet_grouped_mm_wgrad(BF16, BF16, 0, 300, 8192, 8192, 128, P, 8192, None, 300, P, 8192, P, P, 8192, 8192 * 8192, P, 1 << 34, None))[1] \
+        == {"rows": 300}

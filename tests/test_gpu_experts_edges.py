@@ -198,3 +198,15 @@ def test_8_bit_rows_far_apart(am, trans_b):
         return y.view(torch.float8_e4m3fn)
     am.amulet_mm_fp8(apart(A), sa, apart(B[0]), sb[0], far, trans_b=trans_b)
     assert torch.equal(far, R)
+
+
+def test_gradients_of_large_matrices(am):
+    """128 matrices of 8192 x 8192, 17 GB: one group has all the rows, the last; the others' are zeros."""
+    G, K, M = 128, 8192, 70
+    g = gen(6)
+    A, D = normal(g, M, K, dtype=BF16), normal(g, M, K, dtype=BF16)
+    R = torch.full((G, K, K), 7.0, dtype=BF16, device="cuda")
+    am.amulet_grouped_mm_wgrad(A, D, i32([0] * G + [M]), R)
+    assert not R[:-1].any()
+    a, d = A.double(), D.double()
+    within(R[-1], a.t().contiguous() @ d, 2 * (M + 8) * 2.0 ** -24 * (a.abs().t().contiguous() @ d.abs()), "dB")
