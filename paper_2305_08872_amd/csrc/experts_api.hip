@@ -11,6 +11,7 @@ namespace amulet {
 static const int64_t kMostRows = 2147483647LL - 65536LL;   // of a dimension, as in the other calls
 static const int64_t kMostGroups = 1 << 16;              // (every workgroup looks through the offsets)
 static const int64_t kMostBlocks = 0xffffffffLL / 512;     // workgroups of a launch (a grid holds 2^32 - 1 work-items)
+static const int64_t kMostBlocks256 = 0xffffffffLL / 256;  // ... of 256 threads
 
 // the longest pitch (bytes) of an operand whose tile's lines, or a stage's k, lie within 32 bits of each other: 256 of them, and a row
 static const int64_t kMostPitch = 0xffffffffLL / 256 - 65536;
@@ -233,6 +234,7 @@ int amulet_route_grad(int type, int64_t T, int64_t E, int64_t k, const void *log
     const int rc = check_route(type, T, E, k, norm ? E : ldx);
     if (rc != AMULET_OK) return rc;
     if (T == 0) return AMULET_OK;
+    if ((T - 1) / (route_grad_lanes(E, k) == 16 ? 16 : 4) >= kMostBlocks256) return AMULET_ERR_RANGE;
     if ((!norm && !logits) || !experts || !weights || !dweights || !dlogits) return AMULET_ERR_NULL;
     if (lddx < E) return AMULET_ERR_LD;
     RouteArgs a = {};
@@ -244,21 +246,21 @@ int amulet_route_grad(int type, int64_t T, int64_t E, int64_t k, const void *log
     return launch_status(launch_route_grad(a, (hipStream_t)stream));
 }
 
-static int check_combine(int type, int64_t T, int64_t k, int64_t H, int64_t rows)
+static int check_combine(int type, int64_t T, int64_t k, int64_t H, int64_t rows, bool grad)
 {
     if (!known(type)) return AMULET_ERR_TYPE;
     if (T < 0 || k < 0 || H < 0 || rows < 0) return AMULET_ERR_DIM;
     if (H > kMostRows || rows > kMostRows || k > kMostRows || T > kMostRows / (k > 0 ? k : 1)) return AMULET_ERR_RANGE;
     if (T == 0 || H == 0) return 1;
-    // (four waves to a workgroup of 256 threads)
-    const int64_t chunks = (H + 255) / 256, waves = T * (k > chunks ? k : chunks);
-    return (waves + 3) / 4 > kMostBlocks ? AMULET_ERR_RANGE : AMULET_OK;
+    // (four waves to a workgroup: each has 16 bytes to a lane of a token's columns, backward a pair)
+    const int64_t columns = type == AMULET_FP32 ? 256 : 512, waves = T * (grad ? k : (H + columns - 1) / columns);
+    return (waves + 3) / 4 > kMostBlocks256 ? AMULET_ERR_RANGE : AMULET_OK;
 }
 
 int amulet_combine(int type, int64_t T, int64_t k, int64_t H, int64_t rows, const void *Y, int64_t ldy,
                    const float *weights, const int32_t *place, void *R, int64_t ldr, void *stream)
 {
-    const int rc = check_combine(type, T, k, H, rows);
+    const int rc = check_combine(type, T, k, H, rows, false);
     if (rc != AMULET_OK) return rc > 0 ? AMULET_OK : rc;
     if (!R || (k > 0 && !place) || (k > 0 && rows > 0 && !Y)) return AMULET_ERR_NULL;
     if (ldr < H || (k > 0 && rows > 0 && ldy < H)) return AMULET_ERR_LD;
@@ -273,7 +275,7 @@ int amulet_combine_grad(int type, int64_t T, int64_t k, int64_t H, int64_t rows,
                         const float *weights, const int32_t *place, const void *dR, int64_t lddr,
                         void *dY, int64_t lddy, float *dweights, void *stream)
 {
-    const int rc = check_combine(type, T, k, H > 0 ? H : 1, rows);
+    const int rc = check_combine(type, T, k, H > 0 ? H : 1, rows, true);
     if (rc != AMULET_OK) return rc > 0 ? AMULET_OK : rc;
     if (H < 0) return AMULET_ERR_DIM;
     if (k == 0) return AMULET_OK;
@@ -359,7 +361,7 @@ int amulet_quantize_fp8(int type, int64_t M, int64_t K, const void *X, int64_t l
 {
     if (!known(type)) return AMULET_ERR_TYPE;
     if (M < 0 || K < 0) return AMULET_ERR_DIM;
-    if (M > kMostRows || K > kMostRows || (M + 15) / 16 * ((K + 127) / 128) > kMostBlocks) return AMULET_ERR_RANGE;
+    if (M > kMostRows || K > kMostRows || (M + 15) / 16 * ((K + 511) / 512) > kMostBlocks256) return AMULET_ERR_RANGE;
     if (M == 0 || K == 0) return AMULET_OK;
     if (!X || !Q || !scales) return AMULET_ERR_NULL;
     if (ldx < K || ldq < K || lds < M) return AMULET_ERR_LD;

@@ -93,6 +93,8 @@ struct RouteArgs {
 };
 hipError_t launch_route(const RouteArgs &a, hipStream_t s);
 hipError_t launch_route_grad(const RouteArgs &a, hipStream_t s);
+// the lanes of a token there: every one has one of the chosen experts; 256 threads to a workgroup
+inline int route_grad_lanes(int64_t E, int64_t k) { return k > 16 || E > 256 ? 64 : 16; }
 int64_t route_blocks(int64_t T);     // blocks of tokens whose experts are counted apart
 
 struct CombineArgs {

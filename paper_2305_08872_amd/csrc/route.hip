@@ -390,8 +390,7 @@ static hipError_t launch_grad_type(const RouteArgs &a, hipStream_t s)
     if (forced_launch_failure()) return hipErrorLaunchFailure;
     const dim3 small((unsigned)((a.T + 15) / 16)), large((unsigned)((a.T + 3) / 4));
     const size_t row = (size_t)a.E * 4;
-    // (every lane has one of the chosen experts)
-    if (a.k > 16 || a.E > 256) route_grad_kernel<TYPE, 64, 16><<<large, dim3(256), 4 * row, s>>>(a);
+    if (route_grad_lanes(a.E, a.k) == 64) route_grad_kernel<TYPE, 64, 16><<<large, dim3(256), 4 * row, s>>>(a);
     else if (a.E <= 64) route_grad_kernel<TYPE, 16, 4><<<small, dim3(256), 16 * row, s>>>(a);
     else if (a.E <= 128) route_grad_kernel<TYPE, 16, 8><<<small, dim3(256), 16 * row, s>>>(a);
     else route_grad_kernel<TYPE, 16, 16><<<small, dim3(256), 16 * row, s>>>(a);

@@ -91,3 +91,30 @@ def test_large_results_of_the_gradients_are_taken(lib):
         == ("grouped_mm_wgrad_256x256", {"rows": 65536})
     assert note(lambda: lib.amulet_grouped_mm_wgrad(BF16, BF16, 0, 300, 8192, 8192, 128, P, 8192, None, 300, P, 8192, P, P, 8192, 8192 * 8192, P, 1 << 34, None))[1] \
         == {"rows": 300}
+
+
+def test_limits_of_the_small_kernels_are_those_of_their_launches(lib):
+    """What a launch can hold is taken; what it cannot is refused by its size, not by the launch."""
+    def q(M, K):
+        am.amulet_debug_fail_launches(1)
+        return lib.amulet_quantize_fp8(BF16, M, K, P, K, P, K, P, M, None)
+    assert q(1 << 20, 1 << 14) == -5 and q(1 << 22, 1 << 14) == -5          # 16 rows x 512 columns to a workgroup of 256
+    assert q(1 << 23, 1 << 14) == -7
+
+    def combine(type, T, k, H):
+        am.amulet_debug_fail_launches(1)
+        return lib.amulet_combine(type, T, k, H, 100, P, H, None, P, P, H, None)
+
+    def combine_grad(T, k, H):
+        am.amulet_debug_fail_launches(1)
+        return lib.amulet_combine_grad(BF16, T, k, H, 100, P, H, None, P, P, H, P, H, None, None)
+    assert combine(BF16, (1 << 24) - 4, 4, 2048) == -5 and combine(BF16, 1 << 24, 4, 2049) == -7     # four waves of 512 columns
+    assert combine(F32, (1 << 24) - 4, 4, 1024) == -5 and combine(F32, 1 << 24, 4, 1025) == -7       # ... of 256
+    assert combine(BF16, (1 << 24) - 4, 100, 512) == -5 and combine_grad((1 << 26) - 4, 1, 9000) == -5 and combine_grad(1 << 24, 4, 64) == -7
+
+    def route_grad(T, E, k):
+        am.amulet_debug_fail_launches(1)
+        return lib.amulet_route_grad(F32, T, E, k, None, E, 1, P, P, P, P, E, None)
+    assert route_grad((1 << 28) - 16, 8, 2) == -5 and route_grad(1 << 28, 8, 2) == -7          # 16 tokens to a workgroup
+    assert route_grad((1 << 26) - 4, 300, 2) == -5 and route_grad(1 << 26, 300, 2) == -7       # ... 4
+    am.amulet_debug_fail_launches(0)

@@ -210,3 +210,16 @@ def test_gradients_of_large_matrices(am):
     assert not R[:-1].any()
     a, d = A.double(), D.double()
     within(R[-1], a.t().contiguous() @ d, 2 * (M + 8) * 2.0 ** -24 * (a.abs().t().contiguous() @ d.abs()), "dB")
+
+
+def test_a_large_quantisation(am):
+    """2^20 rows of 16384: 34 GB of values, 2^34 of them; the last rows as alone."""
+    M, K = 1 << 20, 1 << 14
+    x = torch.zeros(M, K, dtype=BF16, device="cuda")
+    x[-40:] = normal(gen(4), 40, K, dtype=BF16)
+    q, s = torch.empty(M, K, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn), torch.full((K // 128, M), math.nan, device="cuda")
+    am.amulet_quantize_fp8(x, q, s)
+    q2, s2 = torch.empty(40, K, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(K // 128, 40, device="cuda")
+    am.amulet_quantize_fp8(x[-40:].contiguous(), q2, s2)
+    assert torch.equal(q[-40:].float(), q2.float()) and torch.equal(s[:, -40:], s2)
+    assert (s[:, :-40] == 2.0 ** -126).all() and not q[:-40].view(torch.uint8).any()
