@@ -725,8 +725,10 @@ int amulet_quantize_fp8_blocks(int type, int64_t G, int64_t M, int64_t K, const 
 /*
  * As amulet_grouped_mm with 8-bit operands: scales_a as amulet_quantize_fp8 writes them for A's rows (lds_a apart per
  * block of K, read at r), scales_b as amulet_quantize_fp8_blocks for the matrices as they are stored (K x N, or N x K
- * with trans_b).  R: fp32, bf16 or fp16.  The products of 128 k are summed by the matrix instruction, whose
- * sum drops what is below some 2^-17 of its largest product, and added up in fp32 times both scales.
+ * with trans_b).  R: fp32, bf16 or fp16.  Products are summed by blocks of 128 k, each block's sum times both scales, and added up in fp32.
+ * For R of 32 bits a block's sum is one of fp32 too.  For R of 16 bits the 8-bit matrix instruction makes it, at twice the rate,
+ * which drops of a product what is below some 2^-17 of the block's largest: all 127 together are a hundredth of what the largest
+ * may be off by for its factors having 4 significant bits, but they may be all that is left where the large products of a block cancel.
  * amulet_mm_fp8: one matrix, all rows.
  */
 int amulet_grouped_mm_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K, int64_t G,

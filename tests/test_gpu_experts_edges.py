@@ -223,3 +223,36 @@ def test_a_large_quantisation(am):
     am.amulet_quantize_fp8(x[-40:].contiguous(), q2, s2)
     assert torch.equal(q[-40:].float(), q2.float()) and torch.equal(s[:, -40:], s2)
     assert (s[:, :-40] == 2.0 ** -126).all() and not q[:-40].view(torch.uint8).any()
+
+
+def cancelling(g, M, N, K):
+    """8-bit operands whose sums cancel: two products of 2^16 in every 128 k, one of each sign, and the others 2^-20 to 2^-18 of them.  In
+    any order a block's partial sums are multiples of 2^-4 and at most 2^16 + 32, and up to 11 blocks' sums multiples of 2^-6
+    and less than 2^11: fp32 holds them all."""
+    f8 = torch.float8_e4m3fn
+    a = torch.where(torch.empty(M, K, device="cuda").uniform_(generator=g) < 0.5, 0.25, 0.5)
+    b = torch.where(torch.empty(K, N, device="cuda").uniform_(generator=g) < 0.5, 0.25, 0.5)
+    for k in range(0, K - 1, 128):
+        a[:, k:k + 2], b[k], b[k + 1] = 256.0, 256.0, -256.0
+    sa = torch.exp2(torch.randint(-1, 2, ((K + 127) // 128, M), generator=g, device="cuda").float())
+    sb = torch.exp2(torch.randint(-1, 2, (1, (K + 127) // 128, (N + 127) // 128), generator=g, device="cuda").float())
+    return a.to(f8), sa, b[None].to(f8), sb
+
+
+@pytest.mark.parametrize("trans_b", [False, True])
+@pytest.mark.parametrize("M,N,K", [(1, 40, 128), (16, 8200, 256), (61, 200, 500), (300, 260, 136), (300, 129, 1321), (4096, 4000, 200), (256, 4096, 1024), (2048, 1024, 256)])
+def test_8_bit_products_with_results_of_32_bits_drop_nothing(am, M, N, K, trans_b):
+    """K products of two e4m3 values, each exact in 32 bits, and one scale of each 128: within what an fp32 sum of them may be off; and
+    exact where fp32 holds every partial sum, however small beside the largest product."""
+    print("8 bits, 32-bit results", M, N, K, trans_b, flush=True)
+    g = gen(N + K)
+    for random in (True, False):
+        A, sa, B, sb = fp8_operands(g, M, K, (1, K, N)) if random else cancelling(g, M, N, K)
+        av = A.double() * sa.t().double().repeat_interleave(128, 1)[:, :K]
+        bv = B.double() * sb.double().repeat_interleave(128, 1)[:, :K].repeat_interleave(128, 2)[:, :, :N]
+        want, S = ref_rows(av, bv, [0, M], M, None, False)
+        if trans_b:
+            B, sb = B.transpose(1, 2).contiguous(), sb.transpose(1, 2).contiguous()
+        R = torch.full((M, N), math.nan, device="cuda")
+        am.amulet_mm_fp8(A, sa, B[0], sb[0], R, trans_b=trans_b)
+        within(R, want, 2 * (K + sa.shape[0] + 8) * 2.0 ** -24 * S if random else torch.zeros_like(S), "R")
