@@ -256,3 +256,93 @@ def test_8_bit_products_with_results_of_32_bits_drop_nothing(am, M, N, K, trans_
         R = torch.full((M, N), math.nan, device="cuda")
         am.amulet_mm_fp8(A, sa, B[0], sb[0], R, trans_b=trans_b)
         within(R, want, 2 * (K + sa.shape[0] + 8) * 2.0 ** -24 * S if random else torch.zeros_like(S), "R")
+
+
+# sizes that the middle tile of the sums takes, with and without ranges of rows, and the largest one's ranges
+@pytest.mark.parametrize("trans_r", [False, True])
+@pytest.mark.parametrize("dtype,out", [(BF16, F32), (FP16, FP16)])
+@pytest.mark.parametrize("sizes,N,K,tokens,space,kernel", [
+    ([400, 0, 505, 700], 1289, 1283, 0, 0, "128x128"), ([400, 0, 505, 700], 1289, 1283, 300, 0, "128x128"), ([64, 128, 1100, 13], 1296, 1288, 0, 0, "128x128"),
+    ([5003, 3997], 1030, 1037, 0, 1 << 28, "128x128"), ([5003, 3997], 1030, 1037, 777, 1 << 28, "128x128"), ([12291], 5463, 672, 0, 1 << 28, "256x256"), ([12291], 5463, 672, 999, 1 << 28, "256x256")])
+def test_gradients_by_the_larger_tiles(am, sizes, N, K, tokens, space, kernel, dtype, out, trans_r):
+    print("gradients", kernel, sizes, N, K, tokens, space, dtype, out, trans_r, flush=True)
+    g = gen(N + 7 * K)
+    M, G = sum(sizes) + 5, len(sizes)
+    at = offsets_of(sizes, 3)
+    A, D = normal(g, tokens or M, K, dtype=dtype, pad=1), normal(g, M, N, dtype=dtype, shift=1)
+    rows = torch.randint(-1, tokens + 1, (M,), generator=g, device="cuda", dtype=torch.int32) if tokens else None
+    R = torch.full((G, N, K) if trans_r else (G, K, N), math.nan, dtype=out, device="cuda")
+    ws = torch.full((space // 4,), math.nan, device="cuda") if space else None
+    am.amulet_grouped_mm_wgrad(A, D, i32(at), R, ws, rows=rows, trans_r=trans_r)
+    ran = am.amulet_recent_kernel()
+    assert ran.split()[0] == "grouped_mm_wgrad_" + kernel and ("parts" in ran) == (space > 0)
+    for e, (i, j) in enumerate(zip(at, at[1:])):
+        a, d = A[i:j].double() if rows is None else A.double()[rows[i:j].clamp(0, tokens - 1).long()], D[i:j].double()
+        if rows is not None:
+            a[(rows[i:j] < 0) | (rows[i:j] >= tokens)] = 0
+        w, s = a.t().contiguous() @ d, a.abs().t().contiguous() @ d.abs()
+        within(R[e], w.t() if trans_r else w, 2 * (max(sizes) + 8) * 2.0 ** -24 * (s.t() if trans_r else s), "dB")
+    again = torch.empty_like(R)
+    am.amulet_grouped_mm_wgrad(A, D, i32(at), again, ws, rows=rows, trans_r=trans_r)
+    assert torch.equal(R, again)
+
+
+@pytest.mark.parametrize("trans_b", [False, True])
+@pytest.mark.parametrize("out", [F32, BF16])
+@pytest.mark.parametrize("tokens", [0, 500])
+def test_8_bit_products_of_many_matrices_with_some_rows_each(am, tokens, out, trans_b):
+    g = gen(tokens + 1)
+    sizes, N, K = [50, 64, 37, 0, 33, 64, 65, 49, 1, 63, 50, 60, 48, 51, 52, 70] * 2, 2003, 343
+    M, G, at = sum(sizes), len(sizes), offsets_of(sizes)
+    A, sa, B, sb = fp8_operands(g, tokens or M, K, (G, N, K) if trans_b else (G, K, N), pad=1)
+    rows = torch.randint(-1, tokens + 1, (M,), generator=g, device="cuda", dtype=torch.int32) if tokens else None
+    R = torch.full((M, N), math.nan, dtype=out, device="cuda")
+    am.amulet_grouped_mm_fp8(A, sa, B, sb, i32(at), R, rows=rows, trans_b=trans_b)
+    assert am.amulet_recent_kernel().split()[0] == "mm_fp8_64x128"
+    check_fp8(R, A, sa, B, sb, at, rows, trans_b)
+
+
+@pytest.mark.parametrize("trans_b", [False, True])
+@pytest.mark.parametrize("sizes,N,K", [([5, 0, 9], 40, 72), ([300, 200, 100], 264, 200), ([2100, 1000, 1000], 4000, 136)])
+def test_matrices_further_apart_and_shared(am, sizes, N, K, trans_b):
+    """Every other matrix of a tensor, one matrix for all groups, and matrices whose rows lie in turn."""
+    print("matrices apart", sizes, N, K, trans_b, flush=True)
+    g = gen(N + K)
+    M, G, at = sum(sizes), len(sizes), offsets_of(sizes)
+    A = normal(g, M, K, dtype=BF16)
+    shape = (N, K) if trans_b else (K, N)
+    many = normal(g, 2 * G, *shape, dtype=BF16)
+    turn = normal(g, shape[0], G, shape[1], dtype=BF16).permute(1, 0, 2)
+    for B in (many[::2], many[1:2].expand(G, *shape), turn):
+        R = torch.full((M, N), math.nan, dtype=BF16, device="cuda")
+        am.amulet_grouped_mm(A, B, i32(at), R, trans_b=trans_b)
+        want, S = ref_rows(A, B, at, M, None, trans_b)
+        within(R, want, 2 * (K + 8) * 2.0 ** -24 * S, "R")
+    A8, sa, B8, sb = fp8_operands(g, M, K, (2 * G,) + shape)
+    R, packed = torch.full((M, N), math.nan, device="cuda"), torch.full((M, N), math.nan, device="cuda")
+    am.amulet_grouped_mm_fp8(A8, sa, B8[::2], sb[::2], i32(at), R, trans_b=trans_b)
+    am.amulet_grouped_mm_fp8(A8, sa, B8.view(torch.uint8)[::2].contiguous().view(torch.float8_e4m3fn), sb[::2].contiguous(), i32(at), packed, trans_b=trans_b)
+    assert torch.equal(R, packed)
+    check_fp8(R, A8, sa, B8[::2], sb[::2], at, None, trans_b)
+
+
+@pytest.mark.parametrize("at", [[0, 70, 30, 90], [90, 60, 30, 0], [100, 0, 100, 0], [-7, 200, -9, 50], [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1, 5]])
+@pytest.mark.parametrize("N,K", [(40, 72), (300, 136)])
+def test_offsets_that_do_not_ascend_touch_nothing_else(am, N, K, at):
+    """What the results are is not said, but nothing beside them is written, and no value beside the operands reaches them."""
+    print("offsets", at, N, K, flush=True)
+    g = gen(N)
+    M, G = 100, len(at) - 1
+    A, B, D = normal(g, M, K, dtype=BF16, pad=2, shift=9), normal(g, G, K, N, dtype=BF16, pad=2, shift=9), normal(g, M, N, dtype=BF16, pad=2, shift=9)
+    R = torch.full((50 + M, N + 4), 7.0, dtype=BF16, device="cuda")
+    R[25:25 + M, 2:2 + N] = 0
+    am.amulet_grouped_mm(A, B, i32(at), R[25:25 + M, 2:2 + N])
+    assert torch.isfinite(R).all()
+    R[25:25 + M, 2:2 + N] = 7.0
+    assert (R == 7).all()
+    for space in (None, torch.empty(1 << 22, dtype=torch.uint8, device="cuda")):
+        W = torch.full((G + 2, K + 3, N + 4), 7.0, device="cuda")
+        am.amulet_grouped_mm_wgrad(A, D, i32(at), W[1:1 + G, 1:1 + K, 2:2 + N], space)
+        assert torch.isfinite(W).all()
+        W[1:1 + G, 1:1 + K, 2:2 + N] = 7.0
+        assert (W == 7).all()
