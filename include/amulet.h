@@ -67,7 +67,7 @@ typedef enum {
     AMULET_ERR_LAUNCH = -5, /* HIP reported an error at launch                */
     AMULET_ERR_SHAPE = -6,  /* unknown tile-shape id, or one the task lacks   */
     AMULET_ERR_RANGE = -7,  /* a dimension exceeds what the kernels index     */
-    AMULET_ERR_WORKSPACE = -8, /* the workspace lent to the call is too small  */
+    AMULET_ERR_WORKSPACE = -8, /* the workspace lent: missing, too small, not aligned */
     AMULET_ERR_TYPE = -9    /* an element type the operator does not take      */
 } amulet_status_t;
 
@@ -661,7 +661,7 @@ typedef enum { AMULET_FP32 = 0, AMULET_BF16 = 1, AMULET_FP16 = 2 } amulet_type_t
  *   place[t*k + j]    the pair's row: rows lie in order of expert, then of token; -1 where experts is -1
  *   tokens[row]       the token of a row (T * k values; -1 past the last row)
  *   offsets[e]        first row of expert e (E + 1 values; the last is the number of rows)
- * The workspace (amulet_route_workspace_bytes, 0 up to 64 tokens) holds counts during the call.
+ * The workspace (amulet_route_workspace_bytes, 0 up to 64 tokens; 4-byte aligned) holds counts during the call.
  * One kernel up to 64 tokens, two for more.  Without tokens (T = 0) the offsets are written, zeros; the other pointers may be NULL.
  */
 size_t amulet_route_workspace_bytes(int64_t T, int64_t E);
@@ -699,7 +699,7 @@ int amulet_grouped_mm(int type, int out_type, int trans_b, int64_t M, int64_t N,
 /*
  * The matrices' gradients: R[g] = sum over the rows i of g of A[r]^T D[i], K x N, or its transpose
  * (N x K) with trans_r; A: M (or a_rows, with `rows`) x K, D: M x N, R: G matrices, group_r elements apart.
- * The workspace (any size, also none) lets sums over many rows that few outputs have run
+ * The workspace (any size, also none; 16-byte aligned) lets sums over many rows that few outputs have run
  * as parts on more of the chip; amulet_grouped_mm_wgrad_workspace_bytes: all that it could use.
  */
 size_t amulet_grouped_mm_wgrad_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t G);

@@ -1849,7 +1849,7 @@ const char *amulet_strerror(int code)
     case AMULET_ERR_LAUNCH: return "HIP reported an error at launch";
     case AMULET_ERR_SHAPE: return "unknown tile shape";
     case AMULET_ERR_RANGE: return "dimension too large for the kernels' 32-bit indexing";
-    case AMULET_ERR_WORKSPACE: return "workspace too small for the packed copy";
+    case AMULET_ERR_WORKSPACE: return "workspace missing, too small or not aligned";
     case AMULET_ERR_TYPE: return "unknown element type, or one the operator does not take";
     default: return "unknown status code";
     }

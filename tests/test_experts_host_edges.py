@@ -118,3 +118,9 @@ def test_limits_of_the_small_kernels_are_those_of_their_launches(lib):
     assert route_grad((1 << 28) - 16, 8, 2) == -5 and route_grad(1 << 28, 8, 2) == -7          # 16 tokens to a workgroup
     assert route_grad((1 << 26) - 4, 300, 2) == -5 and route_grad(1 << 26, 300, 2) == -7       # ... 4
     am.amulet_debug_fail_launches(0)
+
+
+def test_a_refused_workspace_is_named_as_one(lib):
+    """The router's counts and the sums of ranges lie in a workspace too, not only packed copies."""
+    text = am.amulet_strerror(-8)
+    assert "workspace" in text and "packed" not in text and "aligned" in text
