@@ -170,7 +170,9 @@ static SumsPlan sums_plan(int64_t rows_r, int64_t cols_r, int64_t G, int64_t M, 
     double least = -1.0;
     for (const auto &k : kinds) {
         const int64_t bm = kExpertsTileRows[k.tile], bn = kExpertsTileCols[k.tile];
-        const int64_t tiles = ((rows_r + bm - 1) / bm) * ((cols_r + bn - 1) / bn) * G;
+        const int64_t of_group = ((rows_r + bm - 1) / bm) * ((cols_r + bn - 1) / bn);
+        if (of_group > kMostBlocks / G) continue;   // (no launch holds them, and 64 bits need not)
+        const int64_t tiles = of_group * G;
         const int64_t room = (int64_t)(bytes / 4 / (size_t)(bm * bn)) / tiles, most = M / (256 * G) < room ? M / (256 * G) : room;
         for (int64_t parts = 1; parts == 1 || (parts <= most && parts <= 64 && tiles * parts <= 4 * k.resident * (int64_t)units); parts += parts < 8 ? 1 : 4) {
             const double groups = (double)tiles * parts, stages = (double)((M + G * parts * 64 - 1) / (G * parts * 64));
@@ -346,12 +348,14 @@ int amulet_grouped_mm_wgrad(int type, int out_type, int trans_r, int64_t M, int6
     const int tile = plan.tile;
     a.parts = plan.parts;
     const int64_t bm = kExpertsTileRows[tile], bn = kExpertsTileCols[tile];
-    const int64_t tiles = ((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn) * G;
+    const int64_t of_group = ((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn);
+    if (of_group > kMostBlocks / G) return AMULET_ERR_RANGE;
+    const int64_t tiles = of_group * G;
     // (with several parts, which are not for many tiles, the second launch has a workgroup to 1024 outputs)
-    if (sums_blocks(tiles / G, G * a.parts) > kMostBlocks || (a.parts > 1 && tiles * (bm * bn / 1024) > kMostBlocks)) return AMULET_ERR_RANGE;
+    if (sums_blocks(of_group, G * a.parts) > kMostBlocks || (a.parts > 1 && tiles * (bm * bn / 1024) > kMostBlocks)) return AMULET_ERR_RANGE;
     note_kernel(tile == EXPERTS_256x256 ? "grouped_mm_wgrad_256x256" : tile == EXPERTS_128x128 ? "grouped_mm_wgrad_128x128" : "grouped_mm_wgrad_64x64", M, 0, a.parts);
     hipStream_t s = (hipStream_t)stream;
-    const int rc = launch_status(launch_experts_sums(type, tile, a, sums_blocks(tiles / G, G * a.parts), s));
+    const int rc = launch_status(launch_experts_sums(type, tile, a, sums_blocks(of_group, G * a.parts), s));
     if (rc != AMULET_OK || a.parts == 1) return rc;
     return launch_status(launch_experts_join(tile, a, s));
 }

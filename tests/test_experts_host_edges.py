@@ -124,3 +124,20 @@ def test_a_refused_workspace_is_named_as_one(lib):
     """The router's counts and the sums of ranges lie in a workspace too, not only packed copies."""
     text = am.amulet_strerror(-8)
     assert "workspace" in text and "packed" not in text and "aligned" in text
+
+
+def test_sizes_whose_tiles_pass_64_bits(lib):
+    """2^64 tiles of 64 x 64: refused or without a workspace, in a process of its own (the number was a divisor once)."""
+    code = """
+import ctypes, paper_2305_08872_amd as am
+lib, P = am.load_library(), ctypes.c_void_p(1 << 20)
+n = 1 << 30
+assert am.amulet_grouped_mm_wgrad_workspace_bytes(1, n, n, 65536) == 0
+assert am.amulet_grouped_mm_wgrad_workspace_bytes(1 << 30, n, n, 32768) == 0
+assert lib.amulet_grouped_mm_wgrad(1, 0, 0, 0, n, n, 65536, P, n, None, 0, P, n, P, P, n, n * n, P, 1 << 30, None) == -7
+assert lib.amulet_grouped_mm_wgrad(1, 0, 0, 0, 2147418111, 2147418111, 65536, P, n, None, 0, P, n, P, P, 2147418111, 2147418111 ** 2, None, 0, None) == -7
+"""
+    import subprocess
+    import sys
+    res = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, (res.returncode, res.stderr[-2000:])
