@@ -63,16 +63,6 @@ static double tile_us(int tile, int64_t M, int64_t N, int64_t K, int64_t G, int 
     const double most = alone > supply ? alone : supply;
     return (most > memory ? most : memory) + 0.03 * (alone + supply);
 }
-static int rows_tile(int64_t M, int64_t N, int64_t K, int64_t G, int es, bool b_across, bool largest)
-{
-    int best = EXPERTS_TILES - 1;
-    double least = tile_us(best, M, N, K, G, es, b_across);
-    for (int tile = EXPERTS_TILES - 2; tile >= (largest ? 0 : 1); --tile) {
-        const double us = tile_us(tile, M, N, K, G, es, b_across);
-        if (us < least) { least = us; best = tile; }
-    }
-    return best;
-}
 // Workgroups that are enough for any offsets: a group's last tile may hold one row only, and the rows outside the groups
 // are two regions more.
 static int64_t rows_blocks(int tile, int64_t M, int64_t N, int64_t G, bool grouped)
@@ -81,6 +71,19 @@ static int64_t rows_blocks(int tile, int64_t M, int64_t N, int64_t G, bool group
     const int64_t regions = !grouped ? 1 : G + 2 < M ? G + 2 : M;
     const int64_t tiles = (M + regions * (bm - 1)) / bm * ((N + bn - 1) / bn);
     return (tiles + 7) / 8 * 8;
+}
+
+// The tile with the lowest estimate of those whose workgroups one launch holds; -1: none
+static int rows_tile(int64_t M, int64_t N, int64_t K, int64_t G, int es, bool b_across, bool grouped, bool largest)
+{
+    int best = -1;
+    double least = 0.0;
+    for (int tile = EXPERTS_TILES - 1; tile >= (largest ? 0 : 1); --tile) {
+        if (rows_blocks(tile, M, N, G, grouped) > kMostBlocks) continue;
+        const double us = tile_us(tile, M, N, K, G < 1 ? 1 : G, es, b_across);
+        if (best < 0 || us < least) { least = us; best = tile; }
+    }
+    return best;
 }
 
 static int check_rows(int es, int64_t M, int64_t N, int64_t K, int64_t G, int trans_b, const void *A, int64_t lda, const int32_t *rows, int64_t a_rows,
@@ -126,9 +129,9 @@ static int run_rows(const char *const *names, int type, int trans_b, ExpertsArgs
     // 8-bit operands whose results keep 32 bits have no 256 x 256 tile, and that tile's offsets of A's rows have 32 bits
     const int es = type == EXPERTS_BF16 || type == EXPERTS_FP16 ? 2 : 1;
     const bool near = (a.rows ? (int64_t)a.a_rows : 256) <= 0xffffffffLL / es / (a.lda > 0 ? a.lda : 1);
-    const int tile = rows_tile(M, N, a.K, G < 1 ? 1 : G, es, !trans_b, type != EXPERTS_FP8_EXACT && near);
+    const int tile = rows_tile(M, N, a.K, G, es, !trans_b, a.offsets != nullptr, type != EXPERTS_FP8_EXACT && near);
+    if (tile < 0) return AMULET_ERR_RANGE;
     const int64_t blocks = rows_blocks(tile, M, N, G, a.offsets != nullptr);
-    if (blocks > kMostBlocks) return AMULET_ERR_RANGE;
     const int64_t behind = tile == EXPERTS_256x256 ? cut_blocks(a, M, N, G, a.offsets != nullptr, es) : 0;
     note_kernel(names[tile], M, behind ? kExpertsTileCols[EXPERTS_128x128] : 0);
     hipStream_t s = (hipStream_t)stream;

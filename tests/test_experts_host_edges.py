@@ -141,3 +141,18 @@ assert lib.amulet_grouped_mm_wgrad(1, 0, 0, 0, 2147418111, 2147418111, 65536, P,
     import sys
     res = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
     assert res.returncode == 0, (res.returncode, res.stderr[-2000:])
+
+
+def test_a_tile_that_the_launch_holds_is_taken(lib):
+    """Sizes whose fastest tile by the estimate would need more workgroups than a launch holds: the fastest of the others."""
+    def fp8(out, M, N, K, G):
+        blocks = (N + 127) // 128
+        return note(lambda: lib.amulet_grouped_mm_fp8(out, 0, M, N, K, G, P, K, P, M, None, M, P, N, N * K, P, blocks, blocks * ((K + 127) // 128), P, P, N, None))
+    for out in (F32, BF16):
+        assert fp8(out, 17018, 264383, 65, 1801)[0].startswith("mm_fp8_") and fp8(out, 565, 1038212, 71, 584)[1] == {"rows": 565}
+    assert note(lambda: lib.amulet_grouped_mm(BF16, BF16, 0, 17018, 264383, 65, 1801, P, 65, None, 17018, P, 264383, 264383 * 65, P, P, 264383, None))[1] == {"rows": 17018}
+    am.amulet_debug_fail_launches(1)
+    n = 1 << 30                                              # more than any tile's
+    assert lib.amulet_grouped_mm(BF16, BF16, 0, n, n, 1, 1, P, 1, None, n, P, 1, 0, P, P, n, None) in (-4, -7)
+    assert lib.amulet_grouped_mm(BF16, BF16, 1, n, n, 1, 1, P, 1, None, n, P, 1, 0, P, P, n, None) == -7
+    am.amulet_debug_fail_launches(0)
