@@ -250,19 +250,14 @@ struct Staged {
             for (int q = 0; q < Q; ++q) p[q] += ahead * ES;
         else base += KS ? (int64_t)ahead * pitch : (int64_t)ahead * ES;
     }
-    // lane `at` of LINES: offset of one of the 128-byte lines that a stage is read from
-    template <class RowOf>
-    __device__ __forceinline__ uint32_t line_of(int at, RowOf row_of, bool relative) const
+    // KS, lane `at` of LINES: offset of one of the 128-byte lines that a stage is read from
+    __device__ __forceinline__ uint32_t line_of(int at) const
     {
-        if constexpr (!KS) {
-            const int in = line0 + at < lines ? line0 + at : lines - 1;
-            return (uint32_t)(row_of(in) - (relative ? line0 : 0)) * (uint32_t)pitch;
-        } else {
-            constexpr int PER = RB / 128 > 0 ? RB / 128 : 1;
-            int c = line0 * ES + at % PER * 128;
-            c = c < lines * ES ? c : 0;
-            return (uint32_t)(at / PER) * (uint32_t)pitch + (uint32_t)c;
-        }
+        static_assert(KS, "lines of k across the storage");
+        constexpr int PER = RB / 128;
+        int c = line0 * ES + at % PER * 128;
+        c = c < lines * ES ? c : 0;
+        return (uint32_t)(at / PER) * (uint32_t)pitch + (uint32_t)c;
     }
     // the stage at k0, of which any part may be there, through registers
     template <class RowOf>
@@ -692,7 +687,7 @@ struct TileScales {
 // next stage are read, which the same barrier certifies as landed.  What is left is loaded through registers, one stage at a time.
 template <class T, class ARow>
 __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, false, T::NW, T::WIDE> &sa, Staged<T::BN, T::ES, T::KB, T::BKS, T::PERM, T::NW, false> &sb,
-                                          const int k0, const int k1, const int wave, const int kg, const int lane, ARow a_row, bool rel, const TileScales &scales, const bool idle, xt_f4 (&acc)[T::MI][T::NI])
+                                          const int k0, const int k1, const int wave, const int kg, const int lane, ARow a_row, const TileScales &scales, const bool idle, xt_f4 (&acc)[T::MI][T::NI])
 {
     constexpr int S = T::S, BK = T::BK, STEPS = Steps<T>::STEPS;
     constexpr int LOADS = Staged<T::BM, T::ES, T::KB, T::AKS, false, T::NW, T::WIDE>::Q + Staged<T::BN, T::ES, T::KB, T::BKS, T::PERM, T::NW, false>::Q + (T::FP8 ? 1 : 0) + (T::PREFETCH ? 1 : 0);
@@ -744,10 +739,11 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
         dma4(scales.a + (int64_t)s * scales.a_step, scales.a_off, ring_at + (uint32_t)(slot * T::STAGE + T::A_BYTES + T::B_BYTES + (wave * 64 % (T::BM < 64 ? 64 : T::BM)) * 4));
     };
     uint32_t pre = 0;
-    if (T::PREFETCH > 0 && mine > 0) {   // (a region without a group has no operands)
-        const int at = (wave % (T::NW / 2)) * 64 + lane;
-        pre = wave < T::NW / 2 ? (sa.index ? 0 : sa.line_of(at, a_row, rel)) : (sb.index ? 0 : sb.line_of(at, [](int i) { return i; }, true));
-    }
+    if constexpr (T::PREFETCH > 0)
+        if (mine > 0) {   // (a group without rows: no operand need be there)
+            const int at = (wave % (T::NW / 2)) * 64 + lane;
+            pre = wave < T::NW / 2 ? (sa.index ? 0 : sa.line_of(at)) : (sb.index ? 0 : sb.line_of(at));
+        }
     typedef Staged<T::BM, T::ES, T::KB, T::AKS, false, T::NW, T::WIDE> StagedA;
     typedef Staged<T::BN, T::ES, T::KB, T::BKS, T::PERM, T::NW, false> StagedB;
     // instruction q of the request for this group's stage r
@@ -770,8 +766,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
                 const int on = s + T::PREFETCH < whole ? T::PREFETCH * BK - ahead : 0;
                 const bool b = wave >= T::NW / 2;
                 // (rows named by an index are not known yet: the storage's first row stands for them)
-                const char *const from = b ? sb.base + (sb.index ? 0 : T::BKS ? on * sb.pitch : (int64_t)on * T::ES)
-                                           : sa.base + (sa.index ? 0 : T::AKS ? on * sa.pitch : (int64_t)on * T::ES);
+                const char *const from = b ? sb.base + (sb.index ? 0 : on * sb.pitch) : sa.base + (sa.index ? 0 : on * sa.pitch);
                 dma4(from, pre, ring_at + S * T::STAGE);
             }
         }
@@ -1045,7 +1040,7 @@ __global__ void __launch_bounds__(T::NT) experts_rows_kernel(const ExpertsArgs a
         scales.b = a.scale_b + (int64_t)(t.group < 0 ? 0 : t.group) * a.group_sb + (T::BKS ? at : at * a.ld_sb);
         scales.b_step = T::BKS ? a.ld_sb : 1;
     }
-    if (!tile_sums<T>(sa, sb, 0, K, wave, kg, lane, a_row, !a.rows, scales, row0 + wm * (T::BM / T::WM) >= t.row1, acc)) return;
+    if (!tile_sums<T>(sa, sb, 0, K, wave, kg, lane, a_row, scales, row0 + wm * (T::BM / T::WM) >= t.row1, acc)) return;
 
     if (a.rows)
 #pragma unroll
@@ -1111,7 +1106,7 @@ __global__ void __launch_bounds__(T::NT) experts_sums_kernel(const ExpertsArgs a
     sa.start_ks(ia ? A : A + (int64_t)lo * a.lda * T::ES, a.lda * T::ES, ia ? ia + lo : nullptr, a.a_rows, m0, a.M, to, from + kg * T::BK, wave, lane);
     sb.start_ks(ib ? B : B + (int64_t)lo * a.ldb * T::ES, a.ldb * T::ES, ib ? ib + lo : nullptr, a.a_rows, n0, a.N, to, from + kg * T::BK, wave, lane);
     xt_f4 acc[T::MI][T::NI];
-    if (!tile_sums<T>(sa, sb, from, to, wave, kg, lane, [](int i) { return i; }, true, TileScales(), false, acc)) return;
+    if (!tile_sums<T>(sa, sb, from, to, wave, kg, lane, [](int i) { return i; }, TileScales(), false, acc)) return;
 
     const int wm = wave / T::WN, wn = wave % T::WN;
     if (a.parts > 1) {
