@@ -635,8 +635,10 @@ int amulet_probe_mfma_i8(int waves_per_simd, double *macs_per_second, void *stre
  *  - results are WRITTEN, not accumulated, and every element of them is: a sum over
  *    nothing is 0 (K = 0, a group without rows, rows outside every group).  Only
  *    amulet_combine_grad leaves the rows of dY that no pair names as they are.
- *  - sums are fp32 whatever the operands' type and rounded once to the result's.  Their
- *    order is fixed by the sizes and the offsets: two calls on the same inputs give
+ *  - sums are fp32 whatever the operands' type and rounded once to the result's (8-bit
+ *    products with results of 16 bits: blocks of 128 in fewer, see there).  Their order is
+ *    fixed by the sizes, the offsets, the device's number of compute units and, for the
+ *    matrices' gradients, the size of the workspace lent: two calls on the same inputs give
  *    the same bits.
  *  - NaN and infinities spread through the products as in any sum of products, to the
  *    outputs that they belong to and no others.

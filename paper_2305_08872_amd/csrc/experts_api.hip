@@ -36,6 +36,9 @@ static bool groups_apart(int64_t G, int64_t rows, int64_t cols, int64_t ld, int6
 // 256 x 256 / 128 x 128 / 64 x 128 / 64 x 64 / 64 x 64 with two k groups / 16 x 32, bf16, B stored N x K: 256 x 4096 x 4096
 // 85 / 46 / 28 / 22 / 18 / 38, 64 x 512 x 4096 58 / 42 / 25 / 19 / 14 / 8, 1024 x 4096 x 1024 over 8 groups 26 / 19 / 18 / 19 / 29 / 60, 8192 x 1024 x 1024
 // over 8 32 / 26 / 28 / 37 / - / 121, 48 x 2048 x 2048 over 64 (out of memory) 67 / 63 / 59 / 59 / 62 / 51; 4096 x 4096 x 1024 over 4 of 8 bits 30 / 33 / 40 / 46 / 83 / 216.
+// It knows nothing of the address of rows and takes 8-bit operands with results of 32 bits, whose stage has four times the instructions, for
+// the others of 8 bits: 3001 x 1501 x 1003 over 7 groups, rows at odd addresses, fp16, 14 us where 31 are measured, 1777 x 1368 x 2504 over 5, 8 bits with
+// results of 32, 18 where 34 are.
 // (Tiles of 16 x 64 and 32 x 64 that were tried gained 0.1 % on average and are not built.)
 struct TileCost {
     double stage16, stage8, start;       // us

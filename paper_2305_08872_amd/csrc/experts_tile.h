@@ -9,7 +9,8 @@
 //   k across them   (KS): LDS keeps [k][line], and ds_read_b64_tr_b16 / _b8 hand a lane the k of its line.
 // Both are XOR-swizzled by unit so that the lanes of an LDS clock fall on distinct banks (unit_of below).  A stage that
 // does not lie wholly inside its operand (the last k, lines past the edge that end inside a unit) goes through registers
-// instead, element by element, with zeros past the end: nothing outside an operand is read.
+// instead, element by element, with zeros past the end: nothing outside an operand is read.  (Of a whole stage a unit that the edge
+// cuts is read whole; what it reads past its row lies in rows behind it, see stages_of_whole_units.)
 //
 // The matrix instruction takes B's lines as its rows and A's as its columns, so that a lane ends up with neighbouring
 // columns of one row of R.  Sums are fp32; fp8 operands have one scale per 128 k, so an instruction's 16 x 16 x 128 products
@@ -25,7 +26,7 @@
 // Why these tiles: of the LDS, 2 x 64 KB of stages for 256 x 256 (an operand byte is read from L2 once per 256 lines), the smaller ones two or
 // three workgroups to a unit so that one's start lies under another's products; 16 x 32 with four k groups for a
 // handful of rows, where more workgroups draw more of the memory (57 us for the 48 rows above; 128 x 128 63).
-// LDS bank conflicts: none counted in any of them.
+// LDS bank conflicts: none counted in any of them, by rows or by sums, bf16 and 8 bits, B in either storage.
 #ifndef AMULET_EXPERTS_TILE_H
 #define AMULET_EXPERTS_TILE_H
 

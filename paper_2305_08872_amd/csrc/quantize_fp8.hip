@@ -6,7 +6,8 @@
 // a large copy's rate).
 //
 // By rows (1 x 128, activations): 16 lanes have a block, 16 rows a workgroup; scales [block of columns][row], so that the
-// products read those of a stage side by side.  By blocks (128 x 128, weights): a workgroup has a block, its values in registers.
+// products read those of a stage side by side.  By blocks (128 x 128, weights): a workgroup has a block, its values in registers
+// (16 matrices of 4096 x 4096 bf16 147 us = 5.46 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
