@@ -742,6 +742,70 @@ int amulet_mm_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K,
                   const void *B, int64_t ldb, const float *scales_b, int64_t lds_b,
                   void *R, int64_t ldr, void *stream);
 
+/*
+ * ---- Low-rank adapters beside a shared projection ------------------------------
+ *
+ * The rows of a batch through one matrix, each with the adapter of its request or none:
+ *
+ *     T[i] = scales[a] X[i] A[a]         M x r, fp32
+ *     R[i] = X[i] W + T[i] B[a]          M x N
+ *
+ * Conventions of the operators above hold.  Which rows have which adapter is read on the device only: segment s is the rows
+ * offsets[s] to offsets[s+1] - 1 (S + 1 values, as the groups' above) and has adapter a = adapters[s] of G; several segments may have
+ * the same; a value outside 0..G-1: none.  adapters NULL: segment s has adapter s (S = G).  Rows without an adapter, those outside
+ * every segment among them, are X W, and their T is 0.
+ *   X  M x K, bf16 or fp16 (`type`)      W  K x N, or N x K with trans_w; NULL: no shared matrix, R = T B
+ *   A  G matrices, group_a elements apart, K x r, or r x K with trans_a      B  r x N, or N x r with trans_b
+ *   scales  G values, NULL: ones         T  M x r, fp32, written (the gradients below take it)      R  fp32 or X's type
+ * An adapter of a lower rank than r has zeros behind it.  r up to 65536, S and G up to 65536.
+ * T is not rounded between the two products: R's sums take it as two bf16 values (16 bits of it) where R has 16 bits, three (all 24) where
+ * it has 32, and X A, X W and T B are each summed in fp32.  (T B of fp16 operands too is made of bf16 products, B in two, exactly: T may
+ * lie outside fp16's range.)
+ *
+ * The rows' gradients are the same call: D for X, W read the other way, A and B exchanged and read the other way:
+ *     U[i] = scales[a] D[i] B[a]^T,  dX[i] = D[i] W^T + U[i] A[a]^T
+ * and the matrices' gradients (without the shared one's, which adapters leave as it is) are
+ *     dA[a] = sum of X[i]^T U[i],  dB[a] = sum of T[i]^T D[i]  over the rows i of a
+ */
+int amulet_adapters_mm(int type, int out_type, int trans_w, int trans_a, int trans_b, int64_t M, int64_t N, int64_t K, int64_t r, int64_t S, int64_t G,
+                       const void *X, int64_t ldx, const void *W, int64_t ldw,
+                       const void *A, int64_t lda, int64_t group_a, const void *B, int64_t ldb, int64_t group_b,
+                       const int32_t *offsets, const int32_t *adapters, const float *scales,
+                       float *T, int64_t ldt, void *R, int64_t ldr, void *stream);
+/*
+ * R[g] = sum over the rows i of adapter g of X[i]^T T[i]: N x r (ldr >= r), or r x N with trans_r (ldr >= N); 0 for an adapter without
+ * rows.  X: M x N, bf16 or fp16; T: M x r, fp32, taken as above; R: fp32 or X's type, G matrices, group_r elements apart.
+ * The workspace (any size, also none; 16-byte aligned) lets the sums of few and narrow matrices run as parts on more of the
+ * chip; amulet_adapters_wgrad_workspace_bytes: all that it could use.
+ */
+size_t amulet_adapters_wgrad_workspace_bytes(int64_t M, int64_t N, int64_t r, int64_t G);
+int amulet_adapters_wgrad(int type, int out_type, int trans_r, int64_t M, int64_t N, int64_t r, int64_t S, int64_t G,
+                          const void *X, int64_t ldx, const float *T, int64_t ldt,
+                          const int32_t *offsets, const int32_t *adapters, void *R, int64_t ldr, int64_t group_r,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * ---- The gradients' norm ---------------------------------------------------------
+ *
+ * n tensors together: types[i] (amulet_type_t), counts[i] values (none is fine) one behind the other from grads[i] on, at any
+ * alignment of elements.  The arrays lie in host memory and are read before the call returns; the tensors and `norm` (one fp32
+ * value) lie in device memory.
+ *   amulet_grad_norm       norm = sqrt(sum of the squares of all values), summed in fp64 in an order that the sizes fix
+ *   amulet_grad_clip       outs[i] = grads[i] times max_norm / norm where norm is above max_norm, else grads[i]; rounded once
+ *   amulet_grad_norm_clip  both (norm is written too)
+ * outs NULL: in place; outs[i] may be grads[i], and tensors overlap in no other way.  A norm that is infinite or no number changes nothing:
+ * the tensors stay as they are, or are copied, and `norm` tells.  max_norm >= 0, may be infinite (AMULET_ERR_RANGE for a
+ * negative one or a NaN).  Between the calls a program may join norms of its own: a step over several cards adds their squares up.
+ * The workspace (amulet_grad_norm_workspace_bytes; 8-byte aligned) holds sums during the call.
+ */
+size_t amulet_grad_norm_workspace_bytes(int64_t n);
+int amulet_grad_norm(int64_t n, const int32_t *types, const int64_t *counts, const void *const *grads, float *norm,
+                     void *workspace, size_t workspace_bytes, void *stream);
+int amulet_grad_clip(int64_t n, const int32_t *types, const int64_t *counts, const void *const *grads, void *const *outs, float max_norm,
+                     const float *norm, void *stream);
+int amulet_grad_norm_clip(int64_t n, const int32_t *types, const int64_t *counts, const void *const *grads, void *const *outs, float max_norm,
+                          float *norm, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Printable text for a status code (static storage). */
 const char *amulet_strerror(int code);
 

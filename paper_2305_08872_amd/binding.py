@@ -186,6 +186,21 @@ def load_library():
                                           vp, vp, i64, vp]
     lib.amulet_mm_fp8.restype = i32
     lib.amulet_mm_fp8.argtypes = [i32, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.amulet_adapters_mm.restype = i32
+    lib.amulet_adapters_mm.argtypes = [i32, i32, i32, i32, i32, i64, i64, i64, i64, i64, i64, vp, i64, vp, i64, vp, i64, i64, vp, i64, i64,
+                                       vp, vp, vp, vp, i64, vp, i64, vp]
+    lib.amulet_adapters_wgrad_workspace_bytes.restype = sz
+    lib.amulet_adapters_wgrad_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    lib.amulet_adapters_wgrad.restype = i32
+    lib.amulet_adapters_wgrad.argtypes = [i32, i32, i32, i64, i64, i64, i64, i64, vp, i64, vp, i64, vp, vp, vp, i64, i64, vp, sz, vp]
+    lib.amulet_grad_norm_workspace_bytes.restype = sz
+    lib.amulet_grad_norm_workspace_bytes.argtypes = [i64]
+    lib.amulet_grad_norm.restype = i32
+    lib.amulet_grad_norm.argtypes = [i64, vp, vp, vp, vp, vp, sz, vp]
+    lib.amulet_grad_clip.restype = i32
+    lib.amulet_grad_clip.argtypes = [i64, vp, vp, vp, vp, ctypes.c_float, vp, vp]
+    lib.amulet_grad_norm_clip.restype = i32
+    lib.amulet_grad_norm_clip.argtypes = [i64, vp, vp, vp, vp, ctypes.c_float, vp, vp, sz, vp]
     _types.update({torch.float32: AMULET_FP32, torch.bfloat16: AMULET_BF16, torch.float16: AMULET_FP16})
     _torch, _raw_stream = torch, getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _marshal = _compiled_marshalling()
@@ -913,6 +928,161 @@ def amulet_mm_fp8(A, scales_a, B, scales_b, R, *, trans_b: bool = False, stream=
         raise ValueError("shape mismatch between operands and scales")
     _check(lib.amulet_mm_fp8(out, int(trans_b), M, N, K, pa, lda, psa, lsa, pb, ldb, psb, lsb, pr, ldr, _stream_ptr(stream)),
            "amulet_mm_fp8")
+
+
+# ---- low-rank adapters, the gradients' norm ------------------------------------------------------------------------------
+
+def _on_this_device(**tensors):
+    here = _torch.cuda.current_device()
+    for what, t in tensors.items():
+        if t is not None and t.get_device() != here:
+            raise ValueError("%s must live on the current device" % what)
+
+
+def amulet_adapters_mm(X, W, A, B, offsets, T, R, *, adapters=None, scales=None, trans_w: bool = False, trans_a: bool = False,
+                       trans_b: bool = False, stream=None):
+    """T[i] = scales[a] X[i] A[a] and R[i] = X[i] W + T[i] B[a], both written, a the adapter of row i: that of its segment,
+    offsets[s] <= i < offsets[s + 1], adapters[s] (outside 0..G-1: none; adapters None: s).  Rows without one: T 0, R = X W.
+    X (M x K) bf16 or fp16; W K x N (N x K with trans_w; None: no shared matrix); A G x K x r (G x r x K with trans_a); B G x r x N
+    (G x N x r with trans_b); scales G fp32 (None: ones); T M x r fp32; R M x N, X's type or fp32.  The rows' gradients are the same
+    call: amulet_adapters_mm(dR, W, B, A, offsets, U, dX, trans_w=not trans_w, trans_a=not trans_b, trans_b=not trans_a, ...)."""
+    if _marshal is not None:
+        rc = _marshal.adapters_mm(X, W, A, B, offsets, T, R, adapters, scales, trans_w, trans_a, trans_b, stream)
+        if rc is not None:
+            _check(rc, "amulet_adapters_mm")
+            return
+    lib = load_library()
+    i32, f32 = _torch.int32, _torch.float32
+    kind, px, M, K, ldx = _typed(X, "X")
+    pa, G, a0, a1, lda, ga = _groups(A, X.dtype, "A")
+    pb, G2, b0, b1, ldb, gb = _groups(B, X.dtype, "B")
+    pt, M2, r, ldt = _mat(T, f32, "T")
+    out, pr, M3, N, ldr = _typed(R, "R")
+    pw, ldw = None, 1
+    if W is not None:
+        pw, w0, w1, ldw = _mat(W, X.dtype, "W")
+        if (w0, w1) != ((N, K) if trans_w else (K, N)):
+            raise ValueError("shape mismatch between X, W and R")
+    if (G2, M2, M3) != (G, M, M) or (a0, a1) != ((r, K) if trans_a else (K, r)) or (b0, b1) != ((N, r) if trans_b else (r, N)):
+        raise ValueError("shape mismatch between X, A, B, T and R")
+    S = G if adapters is None else adapters.numel()
+    pad = None if adapters is None else _vec(adapters, i32, S, "adapters")
+    psc = None if scales is None else _vec(scales, f32, G, "scales")
+    poff = _vec(offsets, i32, S + 1, "offsets")
+    _on_this_device(X=X, W=W, A=A, B=B, offsets=offsets, T=T, R=R, adapters=adapters, scales=scales)
+    _check(lib.amulet_adapters_mm(kind, out, int(trans_w), int(trans_a), int(trans_b), M, N, K, r, S, G, px, ldx, pw, ldw, pa, lda, ga,
+                                  pb, ldb, gb, poff, pad, psc, pt, ldt, pr, ldr, _stream_ptr(stream)), "amulet_adapters_mm")
+
+
+def amulet_adapters_wgrad_workspace_bytes(M: int, N: int, r: int, G: int) -> int:
+    """All the workspace that amulet_adapters_wgrad can use for these sizes (it runs with less, or none)."""
+    return int(load_library().amulet_adapters_wgrad_workspace_bytes(M, N, r, G))
+
+
+def amulet_adapters_wgrad(X, T, offsets, R, workspace=None, *, adapters=None, trans_r: bool = False, stream=None):
+    """R[g] = sum over the rows i of adapter g of X[i]^T T[i]: G x N x r, or G x r x N with trans_r; 0 for an adapter without rows.
+    X (M x N) bf16 or fp16, T (M x r) fp32, R of X's type or fp32; offsets and adapters as amulet_adapters_mm takes them.  With U
+    and T of the two amulet_adapters_mm calls: dA from (X, U), dB from (dR, T)."""
+    if _marshal is not None:
+        rc = _marshal.adapters_wgrad(X, T, offsets, R, workspace, adapters, trans_r, stream)
+        if rc is not None:
+            _check(rc, "amulet_adapters_wgrad")
+            return
+    lib = load_library()
+    kind, px, M, N, ldx = _typed(X, "X")
+    pt, M2, r, ldt = _mat(T, _torch.float32, "T")
+    if R.dtype not in _types:
+        raise ValueError("R must be fp32, bf16 or fp16")
+    pr, G, r0, r1, ldr, gr = _groups(R, R.dtype, "R")
+    if M2 != M or (r0, r1) != ((r, N) if trans_r else (N, r)):
+        raise ValueError("shape mismatch between X, T and R")
+    S = G if adapters is None else adapters.numel()
+    pad = None if adapters is None else _vec(adapters, _torch.int32, S, "adapters")
+    poff = _vec(offsets, _torch.int32, S + 1, "offsets")
+    ws, nw = _bytes(workspace, "workspace")
+    _on_this_device(X=X, T=T, offsets=offsets, R=R, workspace=workspace, adapters=adapters)
+    _check(lib.amulet_adapters_wgrad(kind, _types[R.dtype], int(trans_r), M, N, r, S, G, px, ldx, pt, ldt, poff, pad, pr, ldr, gr, ws, nw,
+                                     _stream_ptr(stream)), "amulet_adapters_wgrad")
+
+
+def _tensors(grads, outs):
+    """The arrays that the C calls take of a list of dense device tensors (and of those they are written to)."""
+    n = len(grads)
+    if outs is not None and len(outs) != n:
+        raise ValueError("outs must be as many as grads")
+    here = _torch.cuda.current_device() if n else 0
+    types, counts = (ctypes.c_int32 * max(n, 1))(), (ctypes.c_int64 * max(n, 1))()
+    ins, to = (ctypes.c_void_p * max(n, 1))(), (ctypes.c_void_p * max(n, 1))()
+
+    def dense(t, what):
+        if not t.is_cuda or t.dtype not in _types or t.layout != _torch.strided:
+            raise ValueError("%s must be fp32, bf16 or fp16 tensors on the GPU" % what)
+        if t.numel() and not _torch.ops.aten.is_non_overlapping_and_dense(t):
+            raise ValueError("%s must be dense: every value once, without gaps" % what)
+        if t.get_device() != here:
+            raise ValueError("%s must live on the current device" % what)
+
+    for i, t in enumerate(grads):
+        dense(t, "grads")
+        types[i], counts[i], ins[i] = _types[t.dtype], t.numel(), t.data_ptr()
+        if outs is not None:
+            o = outs[i]
+            dense(o, "outs")
+            if o.dtype is not t.dtype or o.shape != t.shape or (t.numel() and o.stride() != t.stride()):
+                raise ValueError("outs must have the types, shapes and strides of grads")
+            to[i] = o.data_ptr()
+    return n, types, counts, ins, (None if outs is None else to)
+
+
+def amulet_grad_norm_workspace_bytes(n: int) -> int:
+    """Bytes of workspace that amulet_grad_norm and amulet_grad_norm_clip need for n tensors."""
+    return int(load_library().amulet_grad_norm_workspace_bytes(n))
+
+
+def amulet_grad_norm(grads, norm, workspace, *, stream=None):
+    """norm (1 fp32 value on the device, written) = sqrt of the sum of the squares of all values of the tensors in `grads` (a list;
+    fp32, bf16, fp16, dense)."""
+    if _marshal is not None:
+        rc = _marshal.grad_norm(grads, norm, workspace, stream)
+        if rc is not None:
+            _check(rc, "amulet_grad_norm")
+            return
+    lib = load_library()
+    n, types, counts, ins, _ = _tensors(grads, None)
+    pn = _vec(norm, _torch.float32, 1, "norm")
+    ws, nw = _bytes(workspace, "workspace")
+    _on_this_device(norm=norm, workspace=workspace)
+    _check(lib.amulet_grad_norm(n, types, counts, ins, pn, ws, nw, _stream_ptr(stream)), "amulet_grad_norm")
+
+
+def amulet_grad_clip(grads, max_norm: float, norm, *, outs=None, stream=None):
+    """The tensors of `grads` times max_norm / norm where norm (as amulet_grad_norm writes it, or joined from several) is above
+    max_norm, into `outs` or in place.  A norm that is infinite or no number changes nothing."""
+    if _marshal is not None:
+        rc = _marshal.grad_clip(grads, max_norm, norm, outs, stream)
+        if rc is not None:
+            _check(rc, "amulet_grad_clip")
+            return
+    lib = load_library()
+    n, types, counts, ins, to = _tensors(grads, outs)
+    pn = _vec(norm, _torch.float32, 1, "norm")
+    _on_this_device(norm=norm)
+    _check(lib.amulet_grad_clip(n, types, counts, ins, to, float(max_norm), pn, _stream_ptr(stream)), "amulet_grad_clip")
+
+
+def amulet_grad_norm_clip(grads, max_norm: float, norm, workspace, *, outs=None, stream=None):
+    """amulet_grad_norm and amulet_grad_clip in one call: two launches for up to 120 tensors."""
+    if _marshal is not None:
+        rc = _marshal.grad_norm_clip(grads, max_norm, norm, workspace, outs, stream)
+        if rc is not None:
+            _check(rc, "amulet_grad_norm_clip")
+            return
+    lib = load_library()
+    n, types, counts, ins, to = _tensors(grads, outs)
+    pn = _vec(norm, _torch.float32, 1, "norm")
+    ws, nw = _bytes(workspace, "workspace")
+    _on_this_device(norm=norm, workspace=workspace)
+    _check(lib.amulet_grad_norm_clip(n, types, counts, ins, to, float(max_norm), pn, ws, nw, _stream_ptr(stream)), "amulet_grad_norm_clip")
 
 
 def amulet_strerror(code: int) -> str:

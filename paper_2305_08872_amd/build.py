@@ -36,7 +36,8 @@ SOURCES = ["amulet_api.hip", "mmlike_valu_identity_col.hip"] + [
     for elem in ("f64", "f32")
     for task in ("discount", "boost", "count_gt")
 ] + ["identity_mfma.hip", "identity_mfma_dma.hip", "identity_split.hip", "identity_split_waves.hip", "count_i8.hip", "count_i8_dma.hip", "count_i8_stream.hip", "count_i8_tile.hip", "valu_probe.hip", "mmlike_valu_f64.hip", "identity_mfma_f64.hip", "identity_mfma_f64_dma.hip", "pack.hip"] + [
-    "experts_api.hip", "experts_mm_bf16.hip", "experts_mm_fp16.hip", "experts_mm_fp8.hip", "experts_mm_fp8_exact.hip", "experts_sums.hip", "route.hip", "combine.hip", "quantize_fp8.hip"]
+    "experts_api.hip", "experts_mm_bf16.hip", "experts_mm_fp16.hip", "experts_mm_fp8.hip", "experts_mm_fp8_exact.hip", "experts_sums.hip", "route.hip", "combine.hip", "quantize_fp8.hip",
+    "adapters_api.hip", "adapters_down.hip", "adapters_up_bf16.hip", "adapters_up_fp16.hip", "adapters_outer.hip", "grad_norm.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

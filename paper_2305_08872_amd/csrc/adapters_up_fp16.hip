@@ -1,0 +1,11 @@
+// A shared product with low-rank adapters, fp16 operands: the instances of adapters_up_kernel (adapters_up_impl.h).
+#include "adapters_up_impl.h"
+
+namespace amulet {
+
+hipError_t launch_adapters_up_fp16(int tile, bool w_across, const UpArgs &a, int64_t blocks, hipStream_t s)
+{
+    return launch_adapters_up<EXPERTS_FP16>(tile, w_across, a, blocks, s);
+}
+
+}  // namespace amulet

@@ -127,15 +127,24 @@ static int64_t cut_blocks(ExpertsArgs &a, int64_t M, int64_t N, int64_t G, bool 
     return 2 * cuts > tried ? (blocks + 7) / 8 * 8 : 0;
 }
 
+RowsPlan rows_plan(int es, bool b_across, ExpertsArgs &a, int64_t M, int64_t N, int64_t G, bool largest)
+{
+    RowsPlan p = {rows_tile(M, N, a.K, G, es, b_across, a.offsets != nullptr, largest), 0, 0};
+    if (p.tile < 0) return p;
+    p.blocks = rows_blocks(p.tile, M, N, G, a.offsets != nullptr);
+    p.behind = p.tile == EXPERTS_256x256 ? cut_blocks(a, M, N, G, a.offsets != nullptr, es) : 0;
+    return p;
+}
+
 static int run_rows(const char *const *names, int type, int trans_b, ExpertsArgs &a, int64_t M, int64_t N, int64_t G, void *stream)
 {
     // 8-bit operands whose results keep 32 bits have no 256 x 256 tile, and that tile's offsets of A's rows have 32 bits
     const int es = type == EXPERTS_BF16 || type == EXPERTS_FP16 ? 2 : 1;
     const bool near = (a.rows ? (int64_t)a.a_rows : 256) <= 0xffffffffLL / es / (a.lda > 0 ? a.lda : 1);
-    const int tile = rows_tile(M, N, a.K, G, es, !trans_b, a.offsets != nullptr, type != EXPERTS_FP8_EXACT && near);
+    const RowsPlan plan = rows_plan(es, !trans_b, a, M, N, G, type != EXPERTS_FP8_EXACT && near);
+    const int tile = plan.tile;
     if (tile < 0) return AMULET_ERR_RANGE;
-    const int64_t blocks = rows_blocks(tile, M, N, G, a.offsets != nullptr);
-    const int64_t behind = tile == EXPERTS_256x256 ? cut_blocks(a, M, N, G, a.offsets != nullptr, es) : 0;
+    const int64_t blocks = plan.blocks, behind = plan.behind;
     note_kernel(names[tile], M, behind ? kExpertsTileCols[EXPERTS_128x128] : 0);
     hipStream_t s = (hipStream_t)stream;
     auto launch = [&](int shape, int64_t n) {

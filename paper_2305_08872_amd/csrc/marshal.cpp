@@ -8,6 +8,10 @@
 
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <exception>
+#include <initializer_list>
+#include <vector>
+
 #include "amulet.h"
 
 namespace {
@@ -466,11 +470,204 @@ PyObject *mm_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- low-rank adapters, the gradients' norm: tensors of the current device only
+
+bool current_device(int &d)
+{
+    PyObject *dev = PyObject_CallNoArgs(g_get_device);
+    if (!dev) {
+        PyErr_Clear();
+        return false;
+    }
+    const bool ok = integer(dev, d);
+    Py_DECREF(dev);
+    return ok;
+}
+bool on_device(int d, PyObject *const *a, std::initializer_list<int> which)
+{
+    for (int i : which) {
+        if (a[i] == Py_None) continue;
+        const at::Tensor *t = tensor(a[i]);
+        if (!t || t->get_device() != d) return false;
+    }
+    return true;
+}
+
+// (X, W, A, B, offsets, T, R, adapters, scales, trans_w, trans_a, trans_b, stream)
+PyObject *adapters_mm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Mat X, W, T, R;
+    Groups A, B;
+    int type, out, tw, ta, tb, d;
+    at::ScalarType t, to;
+    void *off, *ad, *sc, *s;
+    if (n != 13 || !known_type(a[0], type, t) || !matrix(a[0], t, X) || !groups(a[2], t, A) || !groups(a[3], t, B) || !matrix(a[5], at::kFloat, T) ||
+        !known_type(a[6], out, to) || !matrix(a[6], to, R) || !integer(a[9], tw) || !integer(a[10], ta) || !integer(a[11], tb))
+        return not_here();
+    W.p = nullptr;
+    W.ld = 1;
+    if (a[1] != Py_None && (!matrix(a[1], t, W) || (tw ? W.cols : W.rows) != X.cols || (tw ? W.rows : W.cols) != R.cols || !W.p)) return not_here();
+    const int64_t r = T.cols;
+    if (A.n != B.n || T.rows != X.rows || R.rows != X.rows || (ta ? A.cols : A.rows) != X.cols || (ta ? A.rows : A.cols) != r ||
+        (tb ? B.cols : B.rows) != r || (tb ? B.rows : B.cols) != R.cols)
+        return not_here();
+    int64_t S = A.n;
+    if (a[7] != Py_None) {
+        const at::Tensor *x = tensor(a[7]);
+        if (!x || !x->defined()) return not_here();
+        S = x->numel();
+    }
+    if (!values_or_none(a[7], at::kInt, S, ad) || (a[7] != Py_None && !ad) || !values_or_none(a[8], at::kFloat, A.n, sc) || !values(a[4], at::kInt, S + 1, off) ||
+        !current_device(d) || !on_device(d, a, {0, 1, 2, 3, 4, 5, 6, 7, 8}) || !stream_handle(a[12], s))
+        return not_here();
+    return status([&] {
+        return amulet_adapters_mm(type, out, tw, ta, tb, X.rows, R.cols, X.cols, r, S, A.n, X.p, X.ld, W.p, W.ld, A.p, A.ld, A.apart, B.p, B.ld, B.apart,
+                                  (const int32_t *)off, (const int32_t *)ad, (const float *)sc, (float *)T.p, T.ld, R.p, R.ld, s);
+    });
+}
+
+// (X, T, offsets, R, workspace, adapters, trans_r, stream)
+PyObject *adapters_wgrad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Mat X, T;
+    Groups R;
+    int type, out, tr, d;
+    at::ScalarType t, to;
+    void *off, *ad, *ws, *s;
+    size_t bytes;
+    if (n != 8 || !known_type(a[0], type, t) || !matrix(a[0], t, X) || !matrix(a[1], at::kFloat, T) || !known_type(a[3], out, to) || !groups(a[3], to, R) ||
+        !bytes_or_none(a[4], ws, bytes) || !integer(a[6], tr) || T.rows != X.rows || (tr ? R.cols : R.rows) != X.cols || (tr ? R.rows : R.cols) != T.cols)
+        return not_here();
+    int64_t S = R.n;
+    if (a[5] != Py_None) {
+        const at::Tensor *x = tensor(a[5]);
+        if (!x || !x->defined()) return not_here();
+        S = x->numel();
+    }
+    if (!values_or_none(a[5], at::kInt, S, ad) || (a[5] != Py_None && !ad) || !values(a[2], at::kInt, S + 1, off) || !current_device(d) ||
+        !on_device(d, a, {0, 1, 2, 3, 4, 5}) || !stream_handle(a[7], s))
+        return not_here();
+    return status([&] {
+        return amulet_adapters_wgrad(type, out, tr, X.rows, X.cols, T.cols, S, R.n, X.p, X.ld, (const float *)T.p, T.ld, (const int32_t *)off, (const int32_t *)ad,
+                                     R.p, R.ld, R.apart, ws, bytes, s);
+    });
+}
+
+// The arrays that the calls take of a list of tensors (and of those they are written to, Py_None: in place)
+struct Tensors {
+    std::vector<int32_t> types;
+    std::vector<int64_t> counts;
+    std::vector<void *> in, out;
+
+    bool read(PyObject *grads, PyObject *outs, int device)
+    {
+        if (!PyList_CheckExact(grads) || (outs != Py_None && !PyList_CheckExact(outs))) return false;
+        const Py_ssize_t n = PyList_GET_SIZE(grads);
+        if (outs != Py_None && PyList_GET_SIZE(outs) != n) return false;
+        // (one more: no null pointers for an empty list)
+        types.resize(n + 1);
+        counts.resize(n + 1);
+        in.resize(n + 1);
+        out.resize(n + 1);
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            const at::Tensor *t = dense(PyList_GET_ITEM(grads, i), device);
+            if (!t) return false;
+            const at::ScalarType type = t->scalar_type();
+            types[i] = type == at::kFloat ? AMULET_FP32 : type == at::kBFloat16 ? AMULET_BF16 : AMULET_FP16;
+            counts[i] = t->numel();
+            in[i] = t->data_ptr();
+            if (outs == Py_None) continue;
+            const at::Tensor *o = dense(PyList_GET_ITEM(outs, i), device);
+            if (!o || o->scalar_type() != type || o->sizes() != t->sizes() || (counts[i] > 0 && o->strides() != t->strides())) return false;
+            out[i] = o->data_ptr();
+        }
+        return true;
+    }
+    static const at::Tensor *dense(PyObject *o, int device)
+    {
+        const at::Tensor *t = tensor(o);
+        if (!t && PyObject_TypeCheck(o, (PyTypeObject *)THPVariableClass)) t = &THPVariable_Unpack(o);   // (parameters)
+        if (!t || !t->defined() || !t->is_cuda() || t->layout() != at::kStrided || !t->has_storage() || t->get_device() != device) return nullptr;
+        const at::ScalarType type = t->scalar_type();
+        if (type != at::kFloat && type != at::kBFloat16 && type != at::kHalf) return nullptr;
+        return t->numel() == 0 || t->is_non_overlapping_and_dense() ? t : nullptr;
+    }
+};
+bool number(PyObject *o, float &x)
+{
+    if (!PyFloat_CheckExact(o) && !PyLong_CheckExact(o)) return false;
+    const double v = PyFloat_AsDouble(o);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    x = (float)v;
+    return true;
+}
+
+// (grads, norm, workspace, stream)
+PyObject *grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    try {
+        Tensors t;
+        int d;
+        void *norm, *ws, *s;
+        size_t bytes;
+        if (n != 4 || !current_device(d) || !t.read(a[0], Py_None, d) || !values(a[1], at::kFloat, 1, norm) || !bytes_or_none(a[2], ws, bytes) ||
+            !on_device(d, a, {1, 2}) || !stream_handle(a[3], s))
+            return not_here();
+        return status([&] { return amulet_grad_norm((int64_t)t.types.size() - 1, t.types.data(), t.counts.data(), t.in.data(), (float *)norm, ws, bytes, s); });
+    } catch (const std::exception &) {
+        return not_here();
+    }
+}
+
+// (grads, max_norm, norm, outs, stream)
+PyObject *grad_clip(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    try {
+        Tensors t;
+        int d;
+        float most;
+        void *norm, *s;
+        if (n != 5 || !current_device(d) || !t.read(a[0], a[3], d) || !number(a[1], most) || !values(a[2], at::kFloat, 1, norm) || !on_device(d, a, {2}) ||
+            !stream_handle(a[4], s))
+            return not_here();
+        void *const *const out = a[3] == Py_None ? nullptr : t.out.data();
+        return status([&] { return amulet_grad_clip((int64_t)t.types.size() - 1, t.types.data(), t.counts.data(), t.in.data(), out, most, (const float *)norm, s); });
+    } catch (const std::exception &) {
+        return not_here();
+    }
+}
+
+// (grads, max_norm, norm, workspace, outs, stream)
+PyObject *grad_norm_clip(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    try {
+        Tensors t;
+        int d;
+        float most;
+        void *norm, *ws, *s;
+        size_t bytes;
+        if (n != 6 || !current_device(d) || !t.read(a[0], a[4], d) || !number(a[1], most) || !values(a[2], at::kFloat, 1, norm) || !bytes_or_none(a[3], ws, bytes) ||
+            !on_device(d, a, {2, 3}) || !stream_handle(a[5], s))
+            return not_here();
+        void *const *const out = a[4] == Py_None ? nullptr : t.out.data();
+        return status([&] {
+            return amulet_grad_norm_clip((int64_t)t.types.size() - 1, t.types.data(), t.counts.data(), t.in.data(), out, most, (float *)norm, ws, bytes, s);
+        });
+    } catch (const std::exception &) {
+        return not_here();
+    }
+}
+
 #define MARSHAL(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MARSHAL(mmlike_f32),      MARSHAL(mmlike_f32_general), MARSHAL(mmlike_f64), MARSHAL(count_i8),
                          MARSHAL(count_i8_assign), MARSHAL(count_i8_general),   MARSHAL(route),      MARSHAL(route_grad),
                          MARSHAL(combine),         MARSHAL(combine_grad),       MARSHAL(grouped_mm), MARSHAL(grouped_mm_wgrad),
-                         MARSHAL(quantize_fp8),    MARSHAL(quantize_fp8_blocks), MARSHAL(grouped_mm_fp8), MARSHAL(mm_fp8), {nullptr, nullptr, 0, nullptr}};
+                         MARSHAL(quantize_fp8),    MARSHAL(quantize_fp8_blocks), MARSHAL(grouped_mm_fp8), MARSHAL(mm_fp8),
+                         MARSHAL(adapters_mm),     MARSHAL(adapters_wgrad),     MARSHAL(grad_norm),  MARSHAL(grad_clip),
+                         MARSHAL(grad_norm_clip),  {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,504 @@
+"""Low-rank adapters beside a shared projection and their gradients against the definition in 64 bits.
+
+Bounds are of the arithmetic.  A product of two 16-bit values is exact in fp32; a sum of n of them, in any order, is within n 2^-24 of
+the sum of their magnitudes (twice that is allowed for the additions inside a matrix instruction), and a result is rounded once.
+T enters the sums of R, and of the matrices' gradients, as pieces of bf16: two for results of 16 bits (the first has the upper 8 bits, so that
+what is left is below 2^-7 of the value, and is rounded by 2^-8 of itself: 2^-15), three for 32 (all 24 bits; a piece of which nothing is
+left stands for 2^-30 of the one before)."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+F32, BF16, FP16 = torch.float32, torch.bfloat16, torch.float16
+HALF_ULP = {F32: 2.0 ** -24, BF16: 2.0 ** -8, FP16: 2.0 ** -11}
+LEAST = {F32: 2.0 ** -126, BF16: 2.0 ** -126, FP16: 2.0 ** -25}     # half the step of the smallest values
+PIECES = {F32: 2.0 ** -29, BF16: 2.0 ** -15, FP16: 2.0 ** -15}      # of a value taken in pieces, by the result's type
+
+
+@pytest.fixture(scope="module")
+def am():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2305_08872_amd as am
+    am.load_library()
+    return am
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def normal(g, *shape, dtype=F32, pad=0, shift=0, scale=1.0):
+    """Normal values; pad: elements between rows; shift: elements that the first value lies off its allocation; NaN around them."""
+    *lead, rows, cols = shape
+    n = math.prod(lead) * rows * (cols + pad)
+    x = torch.empty(shift + n, device="cuda").normal_(0, scale, generator=g).to(dtype)
+    x[:shift] = math.nan
+    v = x[shift:].view(*lead, rows, cols + pad)
+    v[..., cols:] = math.nan
+    return v[..., :cols]
+
+
+def room(*shape, dtype, pad=0, shift=0, fill=7.0):
+    """(a view to be written, a check that nothing beside it was)"""
+    *lead, rows, cols = shape
+    x = torch.full((shift + math.prod(lead) * rows * (cols + pad),), fill, dtype=dtype, device="cuda")
+    v = x[shift:].view(*lead, rows, cols + pad)
+
+    def untouched():
+        assert (x[:shift] == fill).all() and (v[..., cols:] == fill).all()
+    return v[..., :cols], untouched
+
+
+def within(got, want, slack, what):
+    """|got - want| <= slack + the rounding of the result, everywhere; nan where it is wanted."""
+    got64 = got.double()
+    assert torch.equal(torch.isnan(got64), torch.isnan(want)), what
+    limit = slack + HALF_ULP[got.dtype] * (want.abs() + slack) + LEAST[got.dtype]
+    off = (got64 - want).abs()
+    bad = (off > limit) & ~torch.isnan(want) & (got64 != want)
+    assert not bad.any(), "%s: %d off, worst %.3g over its limit" % (what, int(bad.sum()), float((off / limit)[bad].max()))
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def offsets_of(sizes, first=0):
+    at = [first]
+    for n in sizes:
+        at.append(at[-1] + n)
+    return at
+
+
+def spans(at, which, G):
+    return [(slice(i, j), a) for i, j, a in zip(at, at[1:], which) if j > i and 0 <= a < G]
+
+
+def reference(X, W, A, B, at, which, scales, out, trans_w, trans_a, trans_b, N):
+    """T and R in 64 bits, and what each may be off by before its last rounding."""
+    x = X.double()
+    (M, K), G = X.shape, A.shape[0]
+    a = A.double().transpose(1, 2) if trans_a else A.double()
+    b = B.double().transpose(1, 2) if trans_b else B.double()
+    r = a.shape[2]
+    R, S = torch.zeros(M, N, dtype=torch.float64, device="cuda"), torch.zeros(M, N, dtype=torch.float64, device="cuda")
+    if W is not None:
+        w = W.double().t() if trans_w else W.double()
+        R, S = x @ w, x.abs() @ w.abs()
+    T, dT, extra = torch.zeros(M, r, dtype=torch.float64, device="cuda"), torch.zeros(M, r, dtype=torch.float64, device="cuda"), torch.zeros_like(S)
+    for rows, g in spans(at, which, G):
+        f = 1.0 if scales is None else float(scales[g])
+        T[rows] = f * (x[rows] @ a[g])
+        dT[rows] = 2 * (K + 8) * 2.0 ** -24 * abs(f) * (x[rows].abs() @ a[g].abs()) + 2.0 ** -24 * T[rows].abs()
+        R[rows] += T[rows] @ b[g]
+        size = T[rows].abs() + dT[rows]
+        S[rows] += size @ b[g].abs()
+        extra[rows] = (dT[rows] + PIECES[out] * size) @ b[g].abs()
+    return T, dT, R, 2 * (K + 6 * r + 16) * 2.0 ** -24 * S + extra
+
+
+def problem(seed, sizes, which, G, N, K, r, dtype, trans, spare=0, pad=0, shift=0, first=0):
+    """Operands stored as `trans` (of W, A, B) says."""
+    g = gen(seed)
+    M = first + sum(sizes) + spare
+    X = normal(g, M, K, dtype=dtype, pad=pad, shift=shift)
+    W = normal(g, *((N, K) if trans[0] else (K, N)), dtype=dtype, pad=pad, shift=shift, scale=max(K, 1) ** -0.5)
+    A = normal(g, G, *((r, K) if trans[1] else (K, r)), dtype=dtype, pad=pad, shift=shift, scale=max(K, 1) ** -0.5)
+    B = normal(g, G, *((N, r) if trans[2] else (r, N)), dtype=dtype, pad=pad, shift=shift)
+    scales = torch.empty(G, device="cuda").uniform_(0.25, 4.0, generator=g)
+    at = offsets_of(sizes, first)
+    return X, W, A, B, scales, at, (list(range(G)) if which is None else which)
+
+
+# sizes of segments, their adapters (None: their own number), adapters, N, K, rank, rows behind the last segment
+CASES = [
+    ([1], None, 1, 1, 1, 1, 0), ([0, 1, 0], None, 3, 8, 8, 8, 1), ([3, 0, 2, 4], [1, 0, -1, 1], 2, 17, 33, 3, 2), ([1] * 8, None, 8, 64, 64, 16, 0),
+    ([1] * 70, [i % 9 - 1 for i in range(70)], 8, 96, 200, 12, 5), ([5, 9, 1, 0, 2], [2, 2, 7, 0, -5], 3, 130, 127, 33, 0), ([64], None, 1, 100, 71, 128, 0),
+    ([100, 28], None, 2, 256, 96, 64, 0), ([61, 40, 70], [0, 0, 0], 1, 200, 192, 17, 9), ([300, 1, 200], None, 3, 129, 321, 20, 0),
+    ([256], None, 1, 4096, 1024, 16, 0), ([130, 3, 120], [3, -1, 3], 4, 4096, 256, 40, 3), ([1] * 48, None, 48, 2048, 2048, 16, 0),
+    ([700, 10, 324], None, 3, 1024, 1024, 32, 0), ([4100], None, 1, 4104, 200, 8, 0), ([2100, 1900, 96], [1, 0, 1], 2, 4096, 520, 64, 0),
+    ([1500, 0, 2500, 300], None, 4, 4099, 131, 24, 50), ([1000, 2500], None, 2, 8200, 1030, 16, 600),
+    ([200, 1, 55], [1, 0, 1], 2, 4096, 4096, 16, 0), ([700, 324], None, 2, 4096, 1024, 20, 0),
+]
+
+
+@pytest.mark.parametrize("trans", [(True, True, True), (False, False, False), (True, False, True), (False, True, False)])
+@pytest.mark.parametrize("dtype,out", [(BF16, BF16), (BF16, F32), (FP16, FP16), (FP16, F32)])
+@pytest.mark.parametrize("sizes,which,G,N,K,r,spare", CASES)
+def test_adapters(am, sizes, which, G, N, K, r, spare, dtype, out, trans):
+    print("adapters", sizes[:8], G, N, K, r, spare, dtype, out, trans, flush=True)
+    X, W, A, B, scales, at, who = problem(N * 1000 + K + r, sizes, which, G, N, K, r, dtype, trans, spare)
+    M = X.shape[0]
+    T, R = torch.full((M, r), math.nan, device="cuda"), torch.full((M, N), math.nan, dtype=out, device="cuda")
+    am.amulet_adapters_mm(X, W, A, B, i32(at), T, R, adapters=None if which is None else i32(which), scales=scales,
+                          trans_w=trans[0], trans_a=trans[1], trans_b=trans[2])
+    wantT, dT, wantR, dR = reference(X, W, A, B, at, who, scales, out, *trans, N)
+    within(T, wantT, dT, "T")
+    within(R, wantR, dR, "R")
+
+
+def test_the_cases_above_run_every_kernel(am):
+    seen = set()
+    for sizes, which, G, N, K, r, spare in CASES:
+        M = sum(sizes) + spare
+        z = lambda *s: torch.zeros(*s, dtype=BF16, device="cuda")   # noqa: E731
+        R = torch.ones(M, N, dtype=BF16, device="cuda")
+        am.amulet_adapters_mm(z(M, K), z(K, N), z(G, K, r), z(G, r, N), i32(offsets_of(sizes)), torch.empty(M, r, device="cuda"), R,
+                              adapters=None if which is None else i32(which))
+        seen.add(am.amulet_recent_kernel().split()[0])
+        assert not R.any()
+    assert seen == {"adapters_" + t for t in ("256x256", "128x128", "64x128", "64x64", "64x64_k2", "16x32")}
+
+
+@pytest.mark.parametrize("trans", [(True, True, True), (False, False, False)])
+@pytest.mark.parametrize("pad,shift", [(0, 1), (1, 0), (3, 5), (8, 8)])
+@pytest.mark.parametrize("sizes,which,G,N,K,r,spare", [([1, 1, 1], None, 3, 37, 75, 9, 1), ([40, 0, 30], [1, 1, 0], 2, 136, 130, 16, 0),
+                                                       ([150, 150], None, 2, 265, 200, 31, 4), ([4100], None, 1, 4104, 200, 16, 0)])
+def test_adapters_of_views(am, sizes, which, G, N, K, r, spare, pad, shift, trans):
+    """Rows apart, at odd addresses, the first rows in no segment; nothing beside the operands is used or written."""
+    print("views", sizes, N, K, r, pad, shift, trans, flush=True)
+    X, W, A, B, scales, at, who = problem(pad + 10 * shift + K, sizes, which, G, N, K, r, BF16, trans, spare, pad, shift, first=5)
+    M = X.shape[0]
+    (T, t_ok), (R, r_ok) = room(M, r, dtype=F32, pad=pad, shift=shift), room(M, N, dtype=BF16, pad=pad, shift=shift)
+    am.amulet_adapters_mm(X, W, A, B, i32(at), T, R, adapters=None if which is None else i32(which), scales=scales,
+                          trans_w=trans[0], trans_a=trans[1], trans_b=trans[2])
+    wantT, dT, wantR, dR = reference(X, W, A, B, at, who, scales, BF16, *trans, N)
+    within(T, wantT, dT, "T")
+    within(R, wantR, dR, "R")
+    t_ok()
+    r_ok()
+
+
+def test_without_a_shared_matrix_without_scales_and_without_adapters(am):
+    sizes, G, N, K, r = [5, 20, 7], 3, 70, 90, 10
+    t3 = (True, True, True)
+    X, W, A, B, _, at, who = problem(3, sizes, None, G, N, K, r, BF16, t3, spare=3)
+    M = X.shape[0]
+    kw = dict(trans_w=True, trans_a=True, trans_b=True)
+    T, R = torch.empty(M, r, device="cuda"), torch.empty(M, N, device="cuda")
+    am.amulet_adapters_mm(X, None, A, B, i32(at), T, R, **kw)
+    wantT, dT, wantR, dR = reference(X, None, A, B, at, who, None, F32, *t3, N)
+    within(T, wantT, dT, "T")
+    within(R, wantR, dR, "R")
+    assert not R[sum(sizes):].any()
+    plain = X.double() @ W.double().t()
+    slack = 2 * (K + 16) * 2.0 ** -24 * (X.double().abs() @ W.double().t().abs())
+    # nobody has one; no segments; no ranks
+    T.fill_(math.nan)
+    am.amulet_adapters_mm(X, W, A, B, i32(at), T, R, adapters=i32([-1, 3, 9]), **kw)
+    assert not T.any()
+    within(R, plain, slack, "R without adapters")
+    T.fill_(math.nan)
+    R.fill_(math.nan)
+    am.amulet_adapters_mm(X, W, A, B, i32([0]), T, R, adapters=i32([]), **kw)
+    assert not T.any()
+    within(R, plain, slack, "R without segments")
+    R.fill_(math.nan)
+    am.amulet_adapters_mm(X, W, A[:, :0], B[:, :, :0], i32(at), T[:, :0], R, **kw)
+    within(R, plain, slack, "R without ranks")
+    # T alone; nothing to sum over
+    T.fill_(math.nan)
+    am.amulet_adapters_mm(X, W[:0], A, B[:, :0], i32(at), T, R[:, :0], **kw)
+    within(T, wantT, dT, "T alone")
+    am.amulet_adapters_mm(X[:, :0], W[:, :0], A[:, :, :0], B, i32(at), T, R, **kw)
+    assert not T.any() and not R.any()
+    am.amulet_adapters_mm(X[:0], W, A, B, i32(at), T[:0], R[:0], **kw)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("sizes,N,K,r", [([3, 5, 4], 40, 70, 5), ([20, 25, 20], 130, 200, 16), ([1500, 700, 1900], 4100, 136, 24)])
+def test_infinities_and_nans_stay_where_they_belong(am, sizes, N, K, r, dtype):
+    """Of an operand's infinities and NaN in other rows, or in other segments' adapters, nothing is seen; a row's own come through as in any sum."""
+    G, t3 = 3, (True, True, True)
+    X, W, A, B, scales, at, who = problem(K, sizes, None, G, N, K, r, dtype, t3, spare=2)
+    M = X.shape[0]
+    X[at[1] - 1, 3] = math.nan              # the last row of the first segment
+    X[at[2], 5] = math.inf                  # the first of the third
+    B[1, 7, 0] = math.inf                   # one column of the second adapter
+    B[1, 9, r - 1] = math.nan
+    A[2, 1, :] = math.nan                   # a rank of the third: T's column, all of R's rows
+    T, R = torch.empty(M, r, device="cuda"), torch.empty(M, N, dtype=dtype, device="cuda")
+    am.amulet_adapters_mm(X, W, A, B, i32(at), T, R, scales=scales, trans_w=True, trans_a=True, trans_b=True)
+    want = X.double() @ W.double().t()
+    for rows, g in spans(at, who, G):
+        t = float(scales[g]) * (X[rows].double() @ A[g].double().t())
+        want[rows] += t @ B[g].double().t()
+    assert torch.equal(torch.isnan(R), torch.isnan(want))
+    assert torch.equal(torch.isinf(R), torch.isinf(want)) and torch.equal(R[torch.isinf(R)].double(), want[torch.isinf(want)])
+    assert torch.isinf(R[at[1]:at[2], 7]).all()
+    assert not torch.isnan(T[at[0]:at[1] - 1]).any() and not torch.isnan(T[at[1]:at[2]]).any() and not T[at[3]:].any()
+
+
+def test_t_outside_of_the_range_of_fp16(am):
+    """X A may lie where fp16 has no values while R does not."""
+    K, N, r, M = 64, 48, 4, 20
+    g = gen(1)
+    X, W = normal(g, M, K, dtype=FP16, scale=200.0), normal(g, K, N, dtype=FP16)
+    A, B = normal(g, 1, K, r, dtype=FP16, scale=200.0), normal(g, 1, r, N, dtype=FP16, scale=2.0 ** -12)
+    T, R = torch.empty(M, r, device="cuda"), torch.empty(M, N, dtype=FP16, device="cuda")
+    am.amulet_adapters_mm(X, W, A, B, i32([0, M]), T, R)
+    wantT, dT, wantR, dR = reference(X, W, A, B, [0, M], [0], None, FP16, False, False, False, N)
+    assert float(wantT.abs().max()) > 65504
+    within(T, wantT, dT, "T")
+    within(R, wantR, dR, "R")
+
+
+def test_two_calls_give_the_same_bits(am):
+    sizes, which = [1] * 30 + [200, 90], [i % 5 for i in range(32)]
+    X, W, A, B, scales, at, _ = problem(9, sizes, which, 5, 1000, 1500, 16, BF16, (True, True, True))
+    M = X.shape[0]
+    got = []
+    for _ in range(2):
+        T, R = torch.empty(M, 16, device="cuda"), torch.empty(M, 1000, dtype=BF16, device="cuda")
+        am.amulet_adapters_mm(X, W, A, B, i32(at), T, R, adapters=i32(which), scales=scales, trans_w=True, trans_a=True, trans_b=True)
+        dB = torch.empty(5, 1000, 16, device="cuda")
+        ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+        am.amulet_adapters_wgrad(R, T, i32(at), dB, ws, adapters=i32(which))
+        got.append((T, R, dB))
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+
+
+def test_many_segments(am):
+    """More segments than a wave looks at at a time, empty ones among them."""
+    sizes = [(i * 7) % 4 for i in range(5000)]
+    G, N, K, r = 40, 72, 80, 8
+    which = [(i * 11) % 42 - 1 for i in range(5000)]
+    X, W, A, B, scales, at, who = problem(2, sizes, which, G, N, K, r, BF16, (True, True, True), spare=70)
+    M = X.shape[0]
+    T, R = torch.empty(M, r, device="cuda"), torch.empty(M, N, dtype=BF16, device="cuda")
+    am.amulet_adapters_mm(X, W, A, B, i32(at), T, R, adapters=i32(which), scales=scales, trans_w=True, trans_a=True, trans_b=True)
+    row = torch.full((M,), -1, device="cuda")
+    row[:at[-1]] = torch.repeat_interleave(i32(which).long(), i32(sizes).long())
+    row[row >= G] = -1
+    # (a row to a segment: its adapter's number)
+    wantT, dT, wantR, dR = torch.zeros(M, r, dtype=torch.float64, device="cuda"), torch.zeros(M, r, dtype=torch.float64, device="cuda"), X.double() @ W.double().t(), None
+    S = X.double().abs() @ W.double().t().abs()
+    extra = torch.zeros_like(S)
+    for g in range(G):
+        rows = (row == g).nonzero()[:, 0]
+        x, f = X[rows].double(), float(scales[g])
+        wantT[rows] = f * (x @ A[g].double().t())
+        dT[rows] = 2 * (K + 8) * 2.0 ** -24 * f * (x.abs() @ A[g].double().t().abs()) + 2.0 ** -24 * wantT[rows].abs()
+        wantR[rows] += wantT[rows] @ B[g].double().t()
+        size = wantT[rows].abs() + dT[rows]
+        S[rows] += size @ B[g].double().t().abs()
+        extra[rows] = (dT[rows] + PIECES[BF16] * size) @ B[g].double().t().abs()
+    within(T, wantT, dT, "T")
+    within(R, wantR, 2 * (K + 6 * r + 16) * 2.0 ** -24 * S + extra, "R")
+    dB, dS = torch.empty(G, N, r, device="cuda"), None
+    am.amulet_adapters_wgrad(R, T, i32(at), dB, adapters=i32(which))
+    want, slack = outer(R, T, at, which, G, F32)
+    within(dB, want, slack, "dB")
+
+
+def test_offsets_outside_and_not_ascending_touch_nothing_else(am):
+    """Results are unspecified where offsets do not ascend; what lies around them stays, and values past the ends count as the ends."""
+    N, K, r, G, M = 40, 48, 6, 4, 100
+    X, W, A, B, scales, _, _ = problem(4, [M], None, 1, N, K, r, BF16, (True, True, True))
+    A, B = A.expand(G, -1, -1).contiguous(), B.expand(G, -1, -1).contiguous()
+    for at in ([-50, 20, 40, 3000, 2 ** 31 - 1], [90, 10, 95, 0, 50], [100, 100, 0, 0, 100], [2 ** 31 - 1, -2 ** 31, 7, -3, 99]):
+        (T, t_ok), (R, r_ok) = room(M, r, dtype=F32, pad=3, shift=4), room(M, N, dtype=BF16, pad=3, shift=4)
+        (dB, d_ok) = room(G, N, r, dtype=F32, pad=3, shift=4)
+        am.amulet_adapters_mm(X, W, A, B, i32(at), T, R, trans_w=True, trans_a=True, trans_b=True)
+        t_ok()
+        r_ok()
+        am.amulet_adapters_wgrad(R, T, i32(at), dB)
+        d_ok()
+        if at[0] == -50:
+            wantT, dT, wantR, dR = reference(X, W, A, B, [0, 20, 40, 100, 100], [0, 1, 2, 3], None, BF16, True, True, True, N)
+            within(T, wantT, dT, "T")
+            within(R, wantR, dR, "R")
+
+
+# ---- the matrices' gradients
+
+def outer(X, T, at, which, G, out):
+    want = torch.zeros(G, X.shape[1], T.shape[1], dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(want)
+    rows_of = [0] * G
+    for rows, g in spans(at, which, G):
+        want[g] += X[rows].double().t() @ T[rows].double()
+        size[g] += X[rows].double().t().abs() @ T[rows].double().abs()
+        rows_of[g] += rows.stop - rows.start
+    # (each product is one of up to six of pieces)
+    slack = torch.tensor([2 * (6 * n + 64) * 2.0 ** -24 + PIECES[out] for n in rows_of], dtype=torch.float64, device="cuda")
+    return want, slack[:, None, None] * size
+
+
+OUTER = [
+    ([1], None, 1, 1, 1, 0), ([0, 3, 0], None, 3, 8, 8, 1), ([31, 33, 32], None, 3, 7, 16, 0), ([5, 9, 1, 0, 2, 70], [2, 2, 7, 0, -5, 2], 3, 130, 20, 4),
+    ([1] * 100, [i % 4 - 1 for i in range(100)], 3, 136, 17, 0), ([300, 1, 200, 100], [0, 1, 0, 0], 2, 129, 33, 9), ([4000], None, 1, 256, 16, 0),
+    ([1000, 500, 2548], [1, 0, 1], 2, 1003, 64, 3), ([20000, 100], None, 2, 64, 8, 0), ([700, 324], None, 2, 4096, 128, 0),
+]
+
+
+@pytest.mark.parametrize("trans_r", [False, True])
+@pytest.mark.parametrize("dtype,out", [(BF16, BF16), (BF16, F32), (FP16, FP16), (FP16, F32)])
+@pytest.mark.parametrize("lent", [0, 1 << 26])
+@pytest.mark.parametrize("sizes,which,G,N,r,spare", OUTER)
+def test_gradients_of_the_matrices(am, sizes, which, G, N, r, spare, dtype, out, trans_r, lent):
+    print("wgrad", sizes[:8], G, N, r, spare, dtype, out, trans_r, lent, flush=True)
+    g = gen(N * 100 + r)
+    M = sum(sizes) + spare
+    X, T = normal(g, M, N, dtype=dtype), normal(g, M, r)
+    at = offsets_of(sizes)
+    X[at[-1]:], T[at[-1]:] = math.nan, math.nan
+    R = torch.full((G, r, N) if trans_r else (G, N, r), math.nan, dtype=out, device="cuda")
+    ws = torch.full((lent,), 255, dtype=torch.uint8, device="cuda") if lent else None
+    am.amulet_adapters_wgrad(X, T, i32(at), R, ws, adapters=None if which is None else i32(which), trans_r=trans_r)
+    want, slack = outer(X, T, at, list(range(G)) if which is None else which, G, out)
+    within(R.transpose(1, 2) if trans_r else R, want, slack, "R")
+
+
+@pytest.mark.parametrize("trans_r", [False, True])
+@pytest.mark.parametrize("pad,shift", [(0, 1), (1, 0), (3, 5)])
+@pytest.mark.parametrize("sizes,which,G,N,r", [([30, 41], None, 2, 5, 3), ([100, 300], [1, 1], 2, 137, 16), ([9000], None, 1, 261, 40)])
+def test_gradients_of_the_matrices_of_views(am, sizes, which, G, N, r, pad, shift, trans_r):
+    print("wgrad views", sizes, N, r, pad, shift, trans_r, flush=True)
+    g = gen(pad + N)
+    M = 3 + sum(sizes)
+    X, T = normal(g, M, N, dtype=BF16, pad=pad, shift=shift), normal(g, M, r, pad=pad, shift=shift)
+    at = offsets_of(sizes, 3)
+    X[:3], T[:3] = math.inf, math.nan
+    R, ok = room(G, *((r, N) if trans_r else (N, r)), dtype=F32, pad=pad, shift=shift)
+    ws = torch.empty(am.amulet_adapters_wgrad_workspace_bytes(M, N, r, G), dtype=torch.uint8, device="cuda")
+    am.amulet_adapters_wgrad(X, T, i32(at), R, ws, adapters=None if which is None else i32(which), trans_r=trans_r)
+    want, slack = outer(X, T, at, list(range(G)) if which is None else which, G, F32)
+    within(R.transpose(1, 2) if trans_r else R, want, slack, "R")
+    ok()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_infinities_in_the_gradients_of_the_matrices(am, dtype):
+    """An infinity of X, or of T, in the rows of one adapter: in its outputs, with its sign, and no others."""
+    sizes, G, N, r = [50, 60, 70], 3, 40, 6
+    g = gen(6)
+    X, T = normal(g, sum(sizes), N, dtype=dtype), normal(g, sum(sizes), r)
+    T[T == 0] = 1.0
+    X[60, 4], X[60, 9], T[130, 2] = math.inf, -math.inf, math.inf
+    X[130][X[130] == 0] = 1.0
+    X[120, 30] = math.nan
+    at = offsets_of(sizes)
+    R = torch.empty(G, N, r, device="cuda")
+    am.amulet_adapters_wgrad(X, T, i32(at), R)
+    want = torch.stack([X[a:b].double().t() @ T[a:b].double() for a, b in zip(at, at[1:])])
+    assert torch.equal(torch.isnan(R), torch.isnan(want)) and torch.equal(torch.isinf(R), torch.isinf(want))
+    assert torch.equal(R[torch.isinf(R)].double(), want[torch.isinf(want)]) and torch.isinf(R).any() and torch.isfinite(R[0]).all()
+
+
+def test_gradients_without_rows_are_zeros(am):
+    X, T = torch.full((10, 50), math.nan, dtype=BF16, device="cuda"), torch.full((10, 4), math.nan, device="cuda")
+    for at, which, G in (([0, 0, 0], None, 2), ([0, 10], [-1], 2), ([0], [], 3)):
+        R = torch.full((G, 50, 4), math.nan, dtype=BF16, device="cuda")
+        am.amulet_adapters_wgrad(X, T, i32(at), R, adapters=None if which is None else i32(which))
+        assert not R.any()
+    R = torch.full((2, 50, 4), math.nan, dtype=BF16, device="cuda")
+    am.amulet_adapters_wgrad(X[:0], T[:0], i32([0, 0, 0]), R)
+    assert not R.any()
+
+
+def test_operands_of_more_than_4_gib(am):
+    """Offsets of rows past 2^32 bytes and 2^31 values: rows far apart."""
+    M, K, N, r, far = 1200, 64, 72, 16, 2_000_000
+    g = gen(8)
+    big = torch.zeros(M * far, dtype=BF16, device="cuda")
+    X = torch.as_strided(big, (M, K), (far, 1))
+    X.copy_(normal(g, M, K, dtype=BF16))
+    W, A, B = normal(g, N, K, dtype=BF16), normal(g, 2, r, K, dtype=BF16), normal(g, 2, N, r, dtype=BF16)
+    at = [0, 500, 1200]
+    T, R = torch.empty(M, r, device="cuda"), torch.empty(M, N, dtype=BF16, device="cuda")
+    am.amulet_adapters_mm(X, W, A, B, i32(at), T, R, trans_w=True, trans_a=True, trans_b=True)
+    near = X.contiguous()
+    wantT, dT, wantR, dR = reference(near, W, A, B, at, [0, 1], None, BF16, True, True, True, N)
+    within(T, wantT, dT, "T")
+    within(R, wantR, dR, "R")
+    dA = torch.empty(2, K, r, device="cuda")
+    am.amulet_adapters_wgrad(X, T, i32(at), dA)
+    want, slack = outer(near, T, at, [0, 1], 2, F32)
+    within(dA, want, slack, "dA")
+
+
+# ---- as they are used
+
+def test_on_another_stream_and_captured(am):
+    """A forward and backward pass captured once and replayed with other inputs, eager work between the replays, on a stream of its own."""
+    sizes, which, G, N, K, r = [40, 1, 0, 150], [1, 0, 1, 1], 2, 200, 264, 16
+    M = sum(sizes)
+    side = torch.cuda.Stream()
+    off, ad = i32(offsets_of(sizes)), i32(which)
+    X, W, A, B, scales, at, _ = problem(1, sizes, which, G, N, K, r, BF16, (True, True, True))
+    D = normal(gen(2), M, N, dtype=BF16)
+    out = lambda: dict(T=torch.empty(M, r, device="cuda"), R=torch.empty(M, N, dtype=BF16, device="cuda"), U=torch.empty(M, r, device="cuda"),   # noqa: E731
+                       dX=torch.empty(M, K, dtype=BF16, device="cuda"), dA=torch.empty(G, r, K, dtype=BF16, device="cuda"),
+                       dB=torch.empty(G, N, r, dtype=BF16, device="cuda"), ws=torch.empty(1 << 24, dtype=torch.uint8, device="cuda"),
+                       norm=torch.empty(1, device="cuda"), nws=torch.empty(am.amulet_grad_norm_workspace_bytes(2), dtype=torch.uint8, device="cuda"))
+
+    def step(o, stream=None):
+        am.amulet_adapters_mm(X, W, A, B, off, o["T"], o["R"], adapters=ad, scales=scales, trans_w=True, trans_a=True, trans_b=True, stream=stream)
+        am.amulet_adapters_mm(D, W, B, A, off, o["U"], o["dX"], adapters=ad, scales=scales, stream=stream)
+        am.amulet_adapters_wgrad(X, o["U"], off, o["dA"], o["ws"], adapters=ad, trans_r=True, stream=stream)
+        am.amulet_adapters_wgrad(D, o["T"], off, o["dB"], o["ws"], adapters=ad, stream=stream)
+        am.amulet_grad_norm_clip([o["dA"], o["dB"]], 1.0, o["norm"], o["nws"], stream=stream)
+
+    eager, captured = out(), out()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(captured)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(captured)
+    for n in range(4):
+        X.copy_(normal(gen(10 + n), M, K, dtype=BF16))
+        D.copy_(normal(gen(20 + n), M, N, dtype=BF16))
+        graph.replay()
+        step(eager)
+        torch.cuda.synchronize()
+        for k in ("T", "R", "U", "dX", "dA", "dB", "norm"):
+            assert torch.equal(eager[k], captured[k]), (n, k)
+        step(eager, stream=side)
+        side.synchronize()
+        assert torch.equal(eager["dB"], captured["dB"]) and torch.equal(eager["norm"], captured["norm"])
+
+
+def test_gradients_are_the_derivatives(am):
+    """dX, dA and dB of a weighted sum of R against its differences in 64 bits."""
+    sizes, which, G, N, K, r = [7, 12, 5], [1, 0, 1], 2, 40, 48, 4
+    X, W, A, B, scales, at, _ = problem(5, sizes, which, G, N, K, r, BF16, (True, True, True), spare=2)
+    M = X.shape[0]
+    D = normal(gen(6), M, N, dtype=BF16)
+    off, ad = i32(at), i32(which)
+    T, U = torch.empty(M, r, device="cuda"), torch.empty(M, r, device="cuda")
+    R, dX = torch.empty(M, N, device="cuda"), torch.empty(M, K, device="cuda")
+    dA, dB = torch.empty(G, r, K, device="cuda"), torch.empty(G, N, r, device="cuda")
+    am.amulet_adapters_mm(X, W, A, B, off, T, R, adapters=ad, scales=scales, trans_w=True, trans_a=True, trans_b=True)
+    am.amulet_adapters_mm(D, W, B, A, off, U, dX, adapters=ad, scales=scales)
+    am.amulet_adapters_wgrad(X, U, off, dA, adapters=ad, trans_r=True)
+    am.amulet_adapters_wgrad(D, T, off, dB, adapters=ad)
+
+    def loss(x, a, b):
+        y = x @ W.double().t()
+        for rows, g in spans(at, which, G):
+            y[rows] += float(scales[g]) * (x[rows] @ a[g].t()) @ b[g].t()
+        return float((y * D.double()).sum())
+
+    ops = [X.double(), A.double(), B.double()]
+    g = gen(7)
+    for n, grad in enumerate((dX, dA, dB)):
+        # the loss has no second derivative in one operand: its difference over a step is exact but for the rounding of 64 bits
+        step = torch.empty(ops[n].shape, dtype=torch.float64, device="cuda").normal_(generator=g)
+        up, down = list(ops), list(ops)
+        up[n], down[n] = ops[n] + step, ops[n] - step
+        slope = (loss(*up) - loss(*down)) / 2
+        got = float((grad.double() * step).sum())
+        # fp32 sums of at most 3 x 48 terms each, and the differences' own rounding
+        size = float((grad.double().abs() * step.abs()).sum())
+        scale = sum(float((x.abs() @ W.double().t().abs() * D.double().abs()).sum()) for x in (up[0], down[0]))
+        assert abs(got - slope) <= 2.0 ** -12 * size + 2.0 ** -40 * scale, n
