@@ -686,7 +686,7 @@ struct TileScales {
 // Stages that lie wholly inside go through the ring: S of them are requested at first, and the one barrier of a stage lies before its last
 // step, when every wave has read all of it: behind it the slot is refilled with the stage S further on, and the first fragments of the
 // next stage are read, which the same barrier certifies as landed.  What is left is loaded through registers, one stage at a time.
-// `begin(acc)` adds what the sums begin with, while the first stages are on their way.
+// `begin(acc)` adds what the sums begin with, while the first stages are on their way; every wave calls it once, before it meets the others.
 struct FromZero {
     template <class Acc>
     __device__ __forceinline__ void operator()(Acc &) const {}
@@ -886,7 +886,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
             // There is always a request, past the end for the last stage once more (nobody reads it there): every wait is the
             // same, and one loop does for all stages but the last.
             for (int q = 0; q < S; ++q) request(q, q);
-            if constexpr (BUSY) begin(acc);
+            begin(acc);
             wait_vm<LOADS * (S - 1)>();
             first();
             while (r + 1 < mine) go(yes, all_but);
@@ -898,7 +898,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
                     if (q == plain) move_back();
                     request(q, q);
                 }
-            if constexpr (BUSY) begin(acc);
+            begin(acc);
             if (mine >= S) wait_vm<LOADS * (S - 1)>();
             else wait_vm<0>();
             first();
@@ -910,7 +910,7 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
             while (r + 1 < mine) go(no, []() { wait_vm<0>(); });
             if constexpr (BUSY) last();
         }
-    } else if constexpr (BUSY) begin(acc);
+    } else begin(acc);
     if constexpr (T::ALWAYS) wait_vm<0>();   // (the requests past the end: nothing is under way when the workgroup ends)
     if constexpr (T::WK > 1 && T::NW > 1)
         for (int r = mine; r < (ringed + T::WK - 1) / T::WK; ++r) meet<T::NW>();   // (the groups that have one stage more)
