@@ -757,7 +757,7 @@ int amulet_mm_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K,
  *   X  M x K, bf16 or fp16 (`type`)      W  K x N, or N x K with trans_w; NULL: no shared matrix, R = T B
  *   A  G matrices, group_a elements apart, K x r, or r x K with trans_a      B  r x N, or N x r with trans_b
  *   scales  G values, NULL: ones         T  M x r, fp32, written (the gradients below take it)      R  fp32 or X's type
- * An adapter of a lower rank than r has zeros behind it.  r up to 65536, S and G up to 65536.
+ * An adapter of a lower rank than r has zeros behind it.  r, S and G up to 65536; the pitches of X, W, A and B as those of A, B and D above.
  * T is not rounded between the two products: R's sums take it as two bf16 values (16 bits of it) where R has 16 bits, three (all 24) where
  * it has 32, and X A, X W and T B are each summed in fp32.  (T B of fp16 operands too is made of bf16 products, B in two, exactly: T may
  * lie outside fp16's range.)

@@ -26,16 +26,29 @@ static bool matrices_apart(int64_t G, int64_t rows, int64_t cols, int64_t ld, in
     return group >= cols && ((group - cols) / ld >= rows - 1 || (ld - cols) / group >= G - 1);
 }
 
-// Shares of an adapter's rows: as many as give every compute unit a workgroup of eight waves, of 256 rows at least (a workgroup's waves then
-// have one step of 32 each), and as the workspace holds.
-static int outer_parts(int64_t M, int64_t N, int64_t r, int64_t G, size_t bytes)
+// How the gradients' sums are shared out.  Columns to a workgroup: 128, or 64 (half of a row's bytes in a request) where those would not
+// give every compute unit one.  Rows: an adapter's, or pieces of it, two workgroups of four waves to a compute unit, that the workspace has
+// room for, of 512 rows at least (fewer are not worth the second launch, 4 us).  us, whole / pieces of 512 / 1024 / 2048 rows, out of the caches:
+// 16384 x 4096 by rank 16, 4 adapters of equal rows 42 / 37 / 34 / 33, one of them with half of the rows 73 / 39 / 41 / 40; 4096 x 4096 by rank 64,
+// 8 adapters, results of 32 bits 20 / 24 / 24 / 24 and 45 / 31 / 29 / 43.
+struct OuterPlan {
+    int columns, quota;
+    int64_t pieces;
+};
+static OuterPlan outer_plan(int64_t M, int64_t N, int64_t r, int64_t G, size_t bytes)
 {
-    const int64_t ranks = (r + outer_ranks((int)r) - 1) / outer_ranks((int)r), whole = outer_blocks(N, G, 1) * ranks;
-    const int64_t room = (int64_t)(bytes / 4 / (size_t)(N * r)) / G, most = M / (256 * G);
-    int64_t parts = whole > 0 ? compute_units() / whole : 1;
-    parts = parts < most ? parts : most;
-    parts = parts < room ? parts : room;
-    return (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    const int64_t units = compute_units(), ranks = r <= 16 ? 1 : (r + 31) / 32, wide = (N + 127) / 128 * ranks;
+    OuterPlan p = {wide * G >= units || M >= 512 * 2 * G ? 128 : 64, 0, G};
+    const int64_t blocks = (N + p.columns - 1) / p.columns * ranks;
+    const int64_t fill = 2 * units / blocks, least = 512;
+    int64_t quota = fill > 0 ? (M + fill - 1) / fill : M;
+    if (quota < least) quota = least;
+    if (quota <= 0 || G > kOuterAdapters || M < 2 * quota) return p;
+    const int64_t pieces = M / quota + G;
+    if ((size_t)pieces > bytes / 4 / (size_t)(N * r)) return p;
+    p.quota = (int)quota;
+    p.pieces = pieces;
+    return p;
 }
 
 static int check_tensors(int64_t n, const int32_t *types, const int64_t *counts, const void *const *in, void *const *out)
@@ -133,19 +146,24 @@ int amulet_adapters_mm(int type, int out_type, int trans_w, int trans_a, int tra
         if (ldw > kMostPitch / 2) return AMULET_ERR_RANGE;
     }
     if (some && K > 0 && (lda < (trans_a ? K : r) || (G > 1 && group_a < 0))) return AMULET_ERR_LD;
+    if (some && K > 0 && lda > kMostPitch / 2) return AMULET_ERR_RANGE;
     if (some && N > 0 && (ldb < (trans_b ? r : N) || (G > 1 && group_b < 0))) return AMULET_ERR_LD;
+    if (some && N > 0 && ldb > kMostPitch / 2) return AMULET_ERR_RANGE;
     if (r > 0 && (M + 15) / 16 + S + 1 > kMostBlocks512 / ((r + 15) / 16)) return AMULET_ERR_RANGE;
 
     Segments rows = {};
     rows.offsets = offsets; rows.adapters = adapters;
     rows.S = some ? (int)S : 0; rows.G = some ? (int)G : 0; rows.M = (int)M;
+    // Segments of fewer rows than a matrix instruction has: their matrices come from memory, many at a time, which the larger tiles have no room for
+    bool many = some && M < 16 * S;
     UpArgs u = {};
     RowsPlan plan = {};
     if (N > 0) {
         u.mm.A = X; u.mm.lda = ldx; u.mm.B = W; u.mm.ldb = ldw; u.mm.R = R; u.mm.ldr = ldr;
         u.mm.M = (int)M; u.mm.N = (int)N; u.mm.K = W ? (int)K : 0; u.mm.G = 1; u.mm.out = out_type;
         u.rows = rows; u.T = T; u.ldt = ldt; u.B = B; u.ldb = ldb; u.group_b = group_b; u.r = (int)r; u.across = !trans_b;
-        plan = rows_plan(2, !trans_w, u.mm, M, N, 1, true);
+        plan = rows_plan(2, !trans_w, u.mm, M, N, 1, many ? EXPERTS_64x64 : EXPERTS_256x256);
+        if (plan.tile < 0 && many) { many = false; plan = rows_plan(2, !trans_w, u.mm, M, N, 1, EXPERTS_256x256); }
         if (plan.tile < 0) return AMULET_ERR_RANGE;
     }
     hipStream_t s = (hipStream_t)stream;
@@ -160,7 +178,7 @@ int amulet_adapters_mm(int type, int out_type, int trans_w, int trans_a, int tra
     if (N == 0) return AMULET_OK;
     note_kernel(kUpNames[plan.tile], M, plan.behind ? kExpertsTileCols[EXPERTS_128x128] : 0);
     auto launch = [&](int tile, int64_t blocks) {
-        return launch_status(type == AMULET_BF16 ? launch_adapters_up_bf16(tile, !trans_w, u, blocks, s) : launch_adapters_up_fp16(tile, !trans_w, u, blocks, s));
+        return launch_status(type == AMULET_BF16 ? launch_adapters_up_bf16(tile, !trans_w, many, u, blocks, s) : launch_adapters_up_fp16(tile, !trans_w, many, u, blocks, s));
     };
     if (plan.behind == 0) return launch(plan.tile, plan.blocks);
     u.mm.part_of = EXPERTS_BEFORE;
@@ -173,8 +191,8 @@ int amulet_adapters_mm(int type, int out_type, int trans_w, int trans_a, int tra
 size_t amulet_adapters_wgrad_workspace_bytes(int64_t M, int64_t N, int64_t r, int64_t G)
 {
     if (M <= 0 || N <= 0 || r <= 0 || G <= 0 || M > kMostRows || N > kMostRows || r > kMostRank || G > kMostGroups) return 0;
-    const int parts = outer_parts(M, N, r, G, ~(size_t)0 >> 1);
-    return parts < 2 ? 0 : (size_t)parts * (size_t)G * (size_t)N * (size_t)r * 4;
+    const OuterPlan p = outer_plan(M, N, r, G, ~(size_t)0 >> 1);
+    return p.quota == 0 ? 0 : (size_t)p.pieces * (size_t)N * (size_t)r * 4;
 }
 
 int amulet_adapters_wgrad(int type, int out_type, int trans_r, int64_t M, int64_t N, int64_t r, int64_t S, int64_t G,
@@ -196,13 +214,15 @@ int amulet_adapters_wgrad(int type, int out_type, int trans_r, int64_t M, int64_
     a.rows.S = M > 0 ? (int)S : 0; a.rows.G = (int)G; a.rows.M = (int)M;
     a.X = X; a.ldx = ldx; a.T = T; a.ldt = ldt; a.R = R; a.ldr = ldr; a.group_r = group_r; a.workspace = (float *)workspace;
     a.N = (int)N; a.r = (int)r; a.out = out_type; a.trans_r = trans_r != 0;
-    const int64_t ranks = (r + outer_ranks((int)r) - 1) / outer_ranks((int)r);
-    if (outer_blocks(N, G, 1) > kMostBlocks512 / ranks || G * r > kMostBlocks256 * 256 / ((N + 3) / 4)) return AMULET_ERR_RANGE;
-    a.parts = outer_parts(M, N, r, G, workspace ? workspace_bytes : 0);
-    note_kernel("adapters_wgrad", M, 0, a.parts);
+    if ((N + 63) / 64 * ((r + 15) / 16) > kMostBlocks256 / (G + M / 512) || G * r > kMostBlocks256 * 256 / ((N + 3) / 4)) return AMULET_ERR_RANGE;
+    const OuterPlan p = outer_plan(M, N, r, G, workspace ? workspace_bytes : 0);
+    a.columns = p.columns;
+    a.quota = p.quota;
+    a.pieces = (int)p.pieces;
+    note_kernel("adapters_wgrad", M, 0, p.quota > 0 ? 2 : 1);
     hipStream_t s = (hipStream_t)stream;
     const int rc = launch_status(launch_adapters_outer(type, a, s));
-    if (rc != AMULET_OK || a.parts == 1) return rc;
+    if (rc != AMULET_OK || p.quota == 0) return rc;
     return launch_status(launch_adapters_join(a, s));
 }
 

@@ -1,13 +1,12 @@
 // T[i] = scale[a(i)] X[i] A[a(i)]: a batch's rows, each by the first matrix of its adapter, M x r in fp32.
 //
-// Bound by X's bytes (many rows) or the adapters' (few).  A workgroup has up to 16 MI rows of one segment and 16 RI ranks, and its
-// eight waves share k: each takes a line of 128 bytes of every eighth, all of X's and A's fragments straight from memory into the matrix
-// instruction, and the sums are joined in LDS in the waves' order.
+// Bound by X's bytes (many rows) or the adapters' (few).  A workgroup has up to BM rows of one segment and BN ranks; its waves share
+// k, each with a ring of stages of its own in LDS (experts_tile.h), where all of it is read once from memory, and their
+// sums are joined in the waves' order.  (Fragments straight from memory instead, without LDS: neighbouring lanes of a matrix operand have rows
+// of their own, a cache line for every 16 bytes, and 8192 x 4096 by rank 64 took 48 us.)
 #include "adapters_segments.h"
 
 namespace amulet {
-
-constexpr int kDownWaves = 8;
 
 // The rows are cut at every BM-th and where a segment begins.  Cut `k` of these (in order; at one row the segments' first), up to the
 // next one: rows p0 .. p1 - 1 of segment s, or of none.
@@ -43,117 +42,77 @@ __device__ __forceinline__ void rows_of_cut(const Segments &g, int k, int lane, 
     s = at - 1;
 }
 
-template <int ELEM, int MI, int RI, bool ACROSS>
-__global__ void __launch_bounds__(64 * kDownWaves) adapters_down_kernel(const DownArgs a)
+template <class T>
+__global__ void __launch_bounds__(T::NT) adapters_down_kernel(const DownArgs a)
 {
-    constexpr int BM = 16 * MI, BK = 64;
-    __shared__ xt_f4 sums[kDownWaves][MI * RI][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    int p0, p1, s;
-    rows_of_cut<BM>(a.rows, (int)blockIdx.x, lane, p0, p1, s);
+    static_assert(!T::AKS, "k lies along X's rows");
+    static_assert(T::LDS <= 160 * 1024 && (T::WK - 1) * T::NW * T::MI * T::NI * 1024 <= T::LDS, "LDS");
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), kg = w / T::NW, wave = w % T::NW;
+    const int wm = wave / T::WN * (T::BM / T::WM), wn = wave % T::WN * (T::BN / T::WN);   // the wave's first row and rank of the tile
+    int p0, p1, s, lo, hi, g;
+    rows_of_cut<T::BM>(a.rows, (int)blockIdx.x, lane, p0, p1, s);
     p0 = __builtin_amdgcn_readfirstlane(p0);
     p1 = __builtin_amdgcn_readfirstlane(p1);
     if (p0 >= p1) return;
-    int lo, hi, g;
     segment_rows(a.rows, __builtin_amdgcn_readfirstlane(s), lo, hi, g);
     g = __builtin_amdgcn_readfirstlane(g);
-    const int r0 = (int)blockIdx.y * 16 * RI, i = lane & 15, b = lane >> 4;
+    const int from = (int)blockIdx.y * T::BN, r0 = T::BKS ? inside(from, T::BN, a.r) : from;
+    const int K = g < 0 ? 0 : a.K;
 
-    xt_f4 acc[MI][RI];
-#pragma unroll
-    for (int m = 0; m < MI; ++m)
-#pragma unroll
-        for (int n = 0; n < RI; ++n) acc[m][n] = xt_f4{0, 0, 0, 0};
-    if (g >= 0) {
-        typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
-        const char *x[MI];
-#pragma unroll
-        for (int m = 0; m < MI; ++m) {
-            const int row = p0 + m * 16 + i;
-            x[m] = (const char *)a.X + (int64_t)(row < p1 ? row : p1 - 1) * a.ldx * 2;
-        }
-        const char *const base = (const char *)a.A + (int64_t)g * a.group_a * 2;
-        const char *y[RI];
-#pragma unroll
-        for (int n = 0; n < RI; ++n) {
-            const int c = r0 + n * 16 + i;
-            const int64_t at = c < a.r ? c : a.r - 1;
-            y[n] = base + (ACROSS ? at * 2 : at * a.lda * 2);
-        }
-        auto read_x = [&](int m, int k, bool whole) -> xt_u4 {   // 8 k from k on
-            if (whole) return __builtin_bit_cast(xt_u4, *(const u4 *)(x[m] + k * 2));
-            return k < a.K ? load_unit<2>(x[m], k * 2, a.K * 2) : xt_u4{0, 0, 0, 0};
-        };
-        auto read_a = [&](int n, int k, bool whole) -> xt_u4 {
-            if constexpr (!ACROSS) {
-                if (whole) return __builtin_bit_cast(xt_u4, *(const u4 *)(y[n] + k * 2));
-                return k < a.K ? load_unit<2>(y[n], k * 2, a.K * 2) : xt_u4{0, 0, 0, 0};
-            } else {
-                uint32_t v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = whole || k + j < a.K ? *(const uint16_t *)(y[n] + (int64_t)(k + j) * a.lda * 2) : 0u;
-                return xt_u4{v[0] | (v[1] << 16), v[2] | (v[3] << 16), v[4] | (v[5] << 16), v[6] | (v[7] << 16)};
-            }
-        };
-        auto line = [&](int k0, bool whole) {
-            xt_u4 fx[2][MI], fa[2][RI];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = k0 + 32 * h + 8 * b;
-#pragma unroll
-                for (int m = 0; m < MI; ++m) fx[h][m] = read_x(m, k, whole);
-#pragma unroll
-                for (int n = 0; n < RI; ++n) fa[h][n] = read_a(n, k, whole);
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int m = 0; m < MI; ++m)
-#pragma unroll
-                    for (int n = 0; n < RI; ++n) acc[m][n] = mma16<ELEM>(fa[h][n], fx[h][m], acc[m][n]);
-        };
-        int k0 = wave * BK;
-        for (; k0 + BK <= a.K; k0 += kDownWaves * BK) line(k0, true);
-        if (k0 < a.K) line(k0, false);
+    xt_f4 acc[T::MI][T::NI];
+    auto same = [](int i) { return i; };
+    Staged<T::BM, T::ES, T::KB, T::AKS, false, T::NW, T::WIDE> sa = {};
+    Staged<T::BN, T::ES, T::KB, T::BKS, T::PERM, T::NW, false> sb = {};
+    if (K > 0) {
+        const char *const A = (const char *)a.A + (int64_t)g * a.group_a * 2;
+        sa.start_kc((const char *)a.X, a.ldx * 2, p0, p1, K, kg * T::BK, wave, lane, same, true);
+        if constexpr (T::BKS) sb.start_ks(A, a.lda * 2, nullptr, 0, r0, a.r, K, kg * T::BK, wave, lane);
+        else sb.start_kc(A, a.lda * 2, r0, a.r, K, kg * T::BK, wave, lane, same, true);
     }
-#pragma unroll
-    for (int m = 0; m < MI; ++m)
-#pragma unroll
-        for (int n = 0; n < RI; ++n) sums[wave][m * RI + n][lane] = acc[m][n];
-    __syncthreads();
+    if (!tile_sums<T>(sa, sb, 0, K, wave, kg, lane, same, TileScales(), false, acc)) return;
     const float scale = g >= 0 && a.scales ? a.scales[g] : 1.0f;
-    for (int f = wave; f < MI * RI; f += kDownWaves) {
-        xt_f4 t = sums[0][f][lane];
 #pragma unroll
-        for (int w = 1; w < kDownWaves; ++w) t += sums[w][f][lane];
-        const int row = p0 + f / RI * 16 + i, c = r0 + f % RI * 16 + 4 * b;
-        const float v[4] = {g < 0 ? 0.0f : t[0] * scale, g < 0 ? 0.0f : t[1] * scale, g < 0 ? 0.0f : t[2] * scale, g < 0 ? 0.0f : t[3] * scale};
-        if (row < p1) store_out<4>(a.T, EXPERTS_FP32, (int64_t)row * a.ldt, c, 0, a.r, v);
-    }
+    for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] *= scale;   // (zeros stay zeros: a scale of no adapter is 1)
+    store_sums<T>(acc, a.T, EXPERTS_FP32, lane, r0 + wn, from, a.r, [&](int mi) -> int64_t {
+        const int i = p0 + wm + mi * 16 + (lane & 15);
+        return i < p1 ? (int64_t)i * a.ldt : -1;
+    });
 }
 
-template <int ELEM, int MI, int RI>
-static hipError_t launch_down(const DownArgs &a, hipStream_t s)
+template <class T>
+static hipError_t launch_tile(const DownArgs &a, hipStream_t s)
 {
-    const int64_t cuts = ((int64_t)a.rows.M + 16 * MI - 1) / (16 * MI) + a.rows.S + 1;
-    const dim3 grid((unsigned)cuts, (unsigned)((a.r + 16 * RI - 1) / (16 * RI)));
-    if (a.across) adapters_down_kernel<ELEM, MI, RI, true><<<grid, dim3(64 * kDownWaves), 0, s>>>(a);
-    else adapters_down_kernel<ELEM, MI, RI, false><<<grid, dim3(64 * kDownWaves), 0, s>>>(a);
+    static const hipError_t granted = hipFuncSetAttribute((const void *)adapters_down_kernel<T>, hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
+    if (granted != hipSuccess) { (void)hipGetLastError(); return granted; }
+    const int64_t cuts = ((int64_t)a.rows.M + T::BM - 1) / T::BM + a.rows.S + 1;
+    adapters_down_kernel<T><<<dim3((unsigned)cuts, (unsigned)((a.r + T::BN - 1) / T::BN)), dim3(T::NT), T::LDS, s>>>(a);
     return hipGetLastError();
 }
-template <int ELEM>
+template <int ELEM, bool KS>
 static hipError_t launch_down(const DownArgs &a, hipStream_t s)
 {
-    const bool few = a.rows.M < 16 * (int64_t)a.rows.S;
-    if (a.r <= 16) return few ? launch_down<ELEM, 1, 1>(a, s) : launch_down<ELEM, 2, 1>(a, s);
-    if (a.r <= 32) return few ? launch_down<ELEM, 1, 2>(a, s) : launch_down<ELEM, 2, 2>(a, s);
-    return few ? launch_down<ELEM, 1, 4>(a, s) : launch_down<ELEM, 2, 4>(a, s);
+    // Rows to a workgroup: a block where segments are shorter; 32, or 64 where those would be more than one to a compute unit (an adapter's matrix is
+    // read once for as many).  us, 32 / 64 rows, rank 64, out of the caches: 8192 x 4096 of one segment 21 / 25, of 24 segments 39 / 26, 16384
+    // x 4096 34 / 33, 2048 x 4096 13 / 15.
+    const int64_t M = a.rows.M, S = a.rows.S, ranks = a.r <= 16 ? 16 : a.r <= 32 ? 32 : 64;
+    const int rows = M < 16 * S ? 16 : (M / 32 + S) * ((a.r + ranks - 1) / ranks) <= compute_units() ? 32 : 64;
+    if (a.r <= 16)
+        return rows == 16 ? launch_tile<ExpertTile<ELEM, 16, 16, 1, 1, 8, 4, false, KS>>(a, s)
+               : rows == 32 ? launch_tile<ExpertTile<ELEM, 32, 16, 1, 1, 8, 3, false, KS>>(a, s) : launch_tile<ExpertTile<ELEM, 64, 16, 1, 1, 4, 3, false, KS>>(a, s);
+    if (a.r <= 32)
+        return rows == 16 ? launch_tile<ExpertTile<ELEM, 16, 32, 1, 1, 8, 3, false, KS>>(a, s)
+               : rows == 32 ? launch_tile<ExpertTile<ELEM, 32, 32, 1, 1, 4, 4, false, KS>>(a, s) : launch_tile<ExpertTile<ELEM, 64, 32, 1, 1, 4, 3, false, KS>>(a, s);
+    return rows == 16 ? launch_tile<ExpertTile<ELEM, 16, 64, 1, 1, 4, 3, false, KS>>(a, s)
+           : rows == 32 ? launch_tile<ExpertTile<ELEM, 32, 64, 1, 1, 4, 3, false, KS>>(a, s) : launch_tile<ExpertTile<ELEM, 64, 64, 2, 2, 2, 4, false, KS>>(a, s);
 }
 
 hipError_t launch_adapters_down(int type, const DownArgs &a, hipStream_t s)
 {
     if (forced_launch_failure()) return hipErrorLaunchFailure;
-    return type == EXPERTS_BF16 ? launch_down<EXPERTS_BF16>(a, s) : launch_down<EXPERTS_FP16>(a, s);
+    if (type == EXPERTS_BF16) return a.across ? launch_down<EXPERTS_BF16, true>(a, s) : launch_down<EXPERTS_BF16, false>(a, s);
+    return a.across ? launch_down<EXPERTS_FP16, true>(a, s) : launch_down<EXPERTS_FP16, false>(a, s);
 }
 
 }  // namespace amulet

@@ -36,8 +36,8 @@ struct UpArgs {
     int64_t ldt, ldb, group_b;
     int r, across;             // across: B's storage is r x N, else N x r
 };
-hipError_t launch_adapters_up_bf16(int tile, bool w_across, const UpArgs &a, int64_t blocks, hipStream_t s);
-hipError_t launch_adapters_up_fp16(int tile, bool w_across, const UpArgs &a, int64_t blocks, hipStream_t s);
+hipError_t launch_adapters_up_bf16(int tile, bool w_across, bool many, const UpArgs &a, int64_t blocks, hipStream_t s);
+hipError_t launch_adapters_up_fp16(int tile, bool w_across, bool many, const UpArgs &a, int64_t blocks, hipStream_t s);
 
 // R[g] = sum over the rows i of adapter g of X[i]^T T[i]
 struct OuterArgs {
@@ -45,15 +45,14 @@ struct OuterArgs {
     const void *X;
     const float *T;
     void *R;
-    float *workspace;          // parts > 1: fp32 sums
+    float *workspace;          // fp32 sums of pieces
     int64_t ldx, ldt, ldr, group_r;
-    int N, r, out, trans_r, parts;
+    int N, r, out, trans_r;
+    int columns;               // of X to a workgroup: 128 or 64
+    int quota, pieces;         // rows of a piece (0: an adapter is one), the most pieces that there can be
 };
 hipError_t launch_adapters_outer(int type, const OuterArgs &a, hipStream_t s);
-// what it sums at a time: columns of X and of T to a workgroup, and rows to a step of a wave
-constexpr int kOuterColumns = 128, kOuterWaves = 8;
-inline int outer_ranks(int r) { return r <= 16 ? 16 : 32; }
-inline int64_t outer_blocks(int64_t N, int64_t G, int64_t parts) { return (N + kOuterColumns - 1) / kOuterColumns * G * parts; }
+constexpr int kOuterWaves = 4, kOuterAdapters = 1024;   // of a workgroup; the most whose rows are counted
 hipError_t launch_adapters_join(const OuterArgs &a, hipStream_t s);
 
 // The norm of several tensors' values, and the values scaled down to a largest one.  A launch has as many tensors as its

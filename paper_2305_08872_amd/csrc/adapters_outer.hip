@@ -1,26 +1,75 @@
 // R[g] = sum over the rows i of adapter g of X[i]^T T[i]: the gradients of the adapters' matrices, N x r or r x N each.
 //
-// Bound by X's bytes: T and R are a few columns wide.  A workgroup has 128 columns of X and 16 RI of T of one adapter (and, with parts, a
-// share of its rows), its eight waves take steps of 32 rows in turn and join their sums in LDS, in order.  A lane reads 16 bytes of 8
-// rows of X and turns them in registers (32 byte permutes) into 8 columns of 8 rows each, the operands of 8 matrix instructions: lane
-// i of 16 has columns 8 i + f in instruction f, so that what it ends with are neighbouring columns.  T is fp32 and is taken as two bf16 pieces
-// for results of 16 bits, three for 32 (adapters_segments.h), X of fp16 as two.
+// Bound by X's bytes: T and R are a few columns wide.  A workgroup has 16 F columns of X and 16 RI of T of one adapter, or of a piece of its
+// rows; its waves take steps of 32 rows in turn and join their sums in LDS, in order.  A lane reads 2 F bytes of 8 rows of X
+// and turns them in registers (byte permutes) into F columns of 8 rows each, the operands of F matrix instructions: lane i of 16 has
+// columns F i + f in instruction f, so that what it ends with are neighbouring columns.  T is fp32 and is taken as two bf16 pieces for
+// results of 16 bits, three for 32 (adapters_segments.h), X of fp16 as two.
 #include "adapters_segments.h"
 
 namespace amulet {
 
-template <int ELEM, int RI, int PIECES>
-__global__ void __launch_bounds__(64 * kOuterWaves) adapters_outer_kernel(const OuterArgs a)
+// How an adapter's rows are shared out: pieces of about `quota` rows, an adapter without rows one too (its zeros).  Piece k of all: its
+// adapter, which of how many it is.  False: there is none.  counts: the adapters' rows, of the workgroup's LDS.
+struct Piece {
+    int adapter, part, parts;
+};
+__device__ __forceinline__ void count_rows(const Segments &s, int *counts)
 {
-    constexpr int F = 8, OF_X = ELEM == EXPERTS_FP16 ? 2 : 1;
+    for (int g = threadIdx.x; g < s.G; g += blockDim.x) counts[g] = 0;
+    __syncthreads();
+    for (int x = threadIdx.x; x < s.S; x += blockDim.x) {
+        int lo, hi, g;
+        segment_rows(s, x, lo, hi, g);
+        if (g >= 0 && hi > lo) atomicAdd(&counts[g], hi - lo);
+    }
+    __syncthreads();
+}
+__device__ __forceinline__ int pieces_of(int rows, int quota) { return rows > 0 ? (rows + quota - 1) / quota : 1; }
+__device__ __forceinline__ bool find_piece(const int *counts, int G, int quota, int k, int lane, Piece &p)
+{
+    int before = 0;
+    for (int c = 0; c < G; c += 64) {
+        const int n = c + lane < G ? pieces_of(counts[c + lane], quota) : 0;
+        int sum = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int up = __shfl_up(sum, d);
+            if (lane >= d) sum += up;
+        }
+        const uint64_t past = __ballot(before + sum > k);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            p.adapter = c + l;
+            p.parts = __builtin_amdgcn_readlane(n, l);
+            p.part = k - (before + __builtin_amdgcn_readlane(sum, l) - p.parts);
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return false;
+}
+
+template <int ELEM, int F, int RI, int PIECES>
+__global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_per_eu(2))) adapters_outer_kernel(const OuterArgs a)
+{
+    constexpr int COLS = 16 * F, OF_X = ELEM == EXPERTS_FP16 ? 2 : 1;
+    constexpr bool AHEAD = RI == 1;   // the next step's operands on their way (with more ranks fewer workgroups would fit a compute unit)
+    __shared__ int counts[kOuterAdapters];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int i = lane & 15, b = lane >> 4;
-    const unsigned blocks = (unsigned)((a.N + kOuterColumns - 1) / kOuterColumns), piece = blockIdx.x / blocks;
-    const int c0 = (int)(blockIdx.x - piece * blocks) * kOuterColumns + 8 * i, r0 = (int)blockIdx.y * 16 * RI;
-    const int g = (int)(piece / (unsigned)a.parts), part = (int)(piece % (unsigned)a.parts);
-    // the lane's 8 columns end at X's last one
-    const int col = c0 + 8 <= a.N || a.N < 8 ? c0 : a.N - 8;
-    const int workers = kOuterWaves * a.parts, me = part * kOuterWaves + wave;
+    const unsigned blocks = (unsigned)((a.N + COLS - 1) / COLS), piece = blockIdx.x / blocks;
+    Piece p = {(int)piece, 0, 1};
+    if (a.quota > 0) {
+        count_rows(a.rows, counts);
+        if (!find_piece(counts, a.rows.G, a.quota, (int)piece, lane, p)) return;
+    }
+    const int g = p.adapter;
+    // the lane's columns c0 + f, its ranks r0 + n (of T; what it ends with: ranks of line 4 b + v)
+    const int c0 = (int)(blockIdx.x - piece * blocks) * COLS + F * i, r_block = (int)blockIdx.y * 16 * RI, r0 = r_block + RI * i;
+    // they end at X's last one
+    const int col = c0 + F <= a.N || a.N < F ? c0 : a.N - F;
+    const int workers = kOuterWaves * p.parts, me = p.part * kOuterWaves + wave;
 
     xt_f4 acc[F][RI];
 #pragma unroll
@@ -29,42 +78,87 @@ __global__ void __launch_bounds__(64 * kOuterWaves) adapters_outer_kernel(const 
         for (int n = 0; n < RI; ++n) acc[f][n] = xt_f4{0, 0, 0, 0};
 
     // one step: rows base .. base + 31, of which those below `end` are there
-    auto step = [&](int base, int end) {
-        typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
-        xt_u4 x[8];
-        float t[RI][8];
+    struct Step {
+        uint32_t x[8][F / 2];
+        float t[8][RI];
+        int left;   // rows
+    };
+    // (No branch around a load, which would be waited for in it: lanes past an edge read what lies at it.  Columns and ranks that are not
+    // there are sums of their own, which nobody stores; rows become zeros.)
+    const int c_in = a.N < F ? 0 : col < a.N - F ? col : a.N - F;
+    const bool even = a.r % RI == 0;
+    int r_in[RI];
+#pragma unroll
+    for (int n = 0; n < RI; ++n) r_in[n] = r0 + n < a.r ? r0 + n : a.r - 1;
+    const int r_even = r0 + RI <= a.r ? r0 : a.r - RI;
+    auto load = [&](Step &s, int base, int end) {
+        typedef uint32_t xs __attribute__((ext_vector_type(F / 2), aligned(2)));
+        typedef float ts __attribute__((ext_vector_type(RI), aligned(4)));
+        const char *x[8];
+        const float *t[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int row = base + 8 * b + j;
-            x[j] = xt_u4{0, 0, 0, 0};
-            const char *const from = (const char *)a.X + (int64_t)row * a.ldx * 2;
-            if (row < end && c0 < a.N) {
-                if (a.N >= 8) x[j] = __builtin_bit_cast(xt_u4, *(const u4 *)(from + (int64_t)col * 2));
-                else x[j] = load_unit<2>(from, 0, a.N * 2);
-            }
+            const int row = base + 8 * b + j, in = row < end ? row : end - 1;
+            x[j] = (const char *)a.X + (int64_t)in * a.ldx * 2;
+            t[j] = a.T + (int64_t)in * a.ldt;
+        }
+        if (a.N >= F) {
 #pragma unroll
-            for (int n = 0; n < RI; ++n) {
-                const int k = r0 + n * 16 + i;
-                t[n][j] = row < end && k < a.r ? a.T[(int64_t)row * a.ldt + k] : 0.0f;
+            for (int j = 0; j < 8; ++j) {
+                const xs v = *(const xs *)(x[j] + (int64_t)c_in * 2);
+#pragma unroll
+                for (int q = 0; q < F / 2; ++q) s.x[j][q] = v[q];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const xt_u4 v = load_unit<2>(x[j], 0, a.N * 2);
+#pragma unroll
+                for (int q = 0; q < F / 2; ++q) s.x[j][q] = v[q];
             }
         }
-        // column f of the lane's 8 rows
-        auto column = [&](int f) {
-            xt_u4 v;
+        if (RI > 1 && even) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = __builtin_amdgcn_perm(x[2 * q + 1][f / 2], x[2 * q][f / 2], f % 2 ? 0x07060302u : 0x05040100u);
-            return v;
-        };
+            for (int j = 0; j < 8; ++j) {
+                const ts v = *(const ts *)(t[j] + r_even);
+#pragma unroll
+                for (int n = 0; n < RI; ++n) s.t[j][n] = v[n];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int n = 0; n < RI; ++n) s.t[j][n] = t[j][r_in[n]];
+        }
+        s.left = end - base;
+    };
+    auto add = [&](Step &s) {
+        if (s.left < 32)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool there = 8 * b + j < s.left;
+#pragma unroll
+                for (int q = 0; q < F / 2; ++q) s.x[j][q] = there ? s.x[j][q] : 0u;
+#pragma unroll
+                for (int n = 0; n < RI; ++n) s.t[j][n] = there ? s.t[j][n] : 0.0f;
+            }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int n = 0; n < RI; ++n) s.t[j][n] = whole_nan(s.t[j][n]);
         xt_u4 pt[PIECES][RI];
 #pragma unroll
         for (int p = 0; p < PIECES; ++p)
 #pragma unroll
             for (int n = 0; n < RI; ++n)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) pt[p][n][q] = bf16_pair(piece_of(t[n][2 * q], p, PIECES), piece_of(t[n][2 * q + 1], p, PIECES));
+                for (int q = 0; q < 4; ++q) pt[p][n][q] = bf16_pair(piece_of(s.t[2 * q][n], p, PIECES), piece_of(s.t[2 * q + 1][n], p, PIECES));
 #pragma unroll
         for (int f = 0; f < F; ++f) {
-            const xt_u4 v = column(f);
+            // column f of the lane's 8 rows
+            xt_u4 v;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = __builtin_amdgcn_perm(s.x[2 * q + 1][f / 2], s.x[2 * q][f / 2], f % 2 ? 0x07060302u : 0x05040100u);
 #pragma unroll
             for (int h = 0; h < OF_X; ++h) {
                 xt_u4 w = v;
@@ -79,33 +173,69 @@ __global__ void __launch_bounds__(64 * kOuterWaves) adapters_outer_kernel(const 
         }
     };
 
-    int done = 0;   // steps of the adapter's segments so far, modulo the workers
-    auto segment = [&](int lo, int hi) {
-        const int steps = (hi - lo + 31) / 32;
-        int first = me - done;
-        if (first < 0) first += workers;
-        for (int64_t s = first; s < steps; s += workers) step(lo + (int)s * 32, hi);
-        done = (int)(((int64_t)done + steps) % workers);
-    };
-    if (!a.rows.adapters) {
-        if (g < a.rows.S) {
-            int lo, hi, adapter;
-            segment_rows(a.rows, g, lo, hi, adapter);
+    // The wave's steps: every `workers`-th of those of the adapter's segments
+    int lo = 0, hi = 0, steps = 0, s = me;   // the segment, the wave's next step of it
+    int chunk = 0, l_lo = 0, l_hi = 0;
+    uint64_t left = 0;
+    bool started = false;
+    auto next_segment = [&]() -> bool {
+        if (!a.rows.adapters) {
+            if (started || g >= a.rows.S) return false;
+            started = true;
+            int x;
+            segment_rows(a.rows, g, lo, hi, x);
             lo = __builtin_amdgcn_readfirstlane(lo);
             hi = __builtin_amdgcn_readfirstlane(hi);
-            if (hi > lo) segment(lo, hi);
+        } else {
+            while (left == 0) {
+                if (started) chunk += 64;
+                started = true;
+                if (chunk >= a.rows.S) return false;
+                int x;
+                segment_rows(a.rows, chunk + lane, l_lo, l_hi, x);
+                left = __ballot(x == g && l_hi > l_lo);
+            }
+            const int l = __builtin_ctzll(left);
+            left &= left - 1;
+            lo = __builtin_amdgcn_readlane(l_lo, l);
+            hi = __builtin_amdgcn_readlane(l_hi, l);
+        }
+        steps = hi > lo ? (hi - lo + 31) / 32 : 0;
+        return true;
+    };
+    auto next = [&](int &base) -> bool {
+        while (s >= steps) {
+            s -= steps;
+            steps = 0;
+            if (!next_segment()) return false;
+        }
+        base = lo + s * 32;
+        s += workers;
+        return true;
+    };
+    int base;
+    if constexpr (AHEAD) {
+        Step x, y;
+        bool have = next(base);
+        if (have) load(x, base, hi);
+        while (have) {
+            const bool more = next(base);
+            if (more) load(y, base, hi);
+            add(x);
+            if (!more) break;
+            have = next(base);
+            if (have) load(x, base, hi);
+            add(y);
         }
     } else {
-        for (int c = 0; c < a.rows.S; c += 64) {
-            int lo, hi, adapter;
-            segment_rows(a.rows, c + lane, lo, hi, adapter);
-            for (uint64_t left = __ballot(adapter == g && hi > lo); left; left &= left - 1) {
-                const int l = __builtin_ctzll(left);
-                segment(__builtin_amdgcn_readlane(lo, l), __builtin_amdgcn_readlane(hi, l));
-            }
+        Step x;
+        while (next(base)) {
+            load(x, base, hi);
+            add(x);
         }
     }
 
+    sums_done();
     // the waves' sums: halves onto halves, in a fixed order
     extern __shared__ __attribute__((aligned(16))) char smem[];
     xt_f4 *const sums = (xt_f4 *)smem;
@@ -125,75 +255,99 @@ __global__ void __launch_bounds__(64 * kOuterWaves) adapters_outer_kernel(const 
         __syncthreads();
     }
     if (wave != 0 || c0 >= a.N) return;
-    // a lane's columns col + f (those from c0 on are its own), ranks r0 + 16 n + 4 b + v
-    const bool whole = a.parts == 1;
+    // columns col + f (those from c0 on are the lane's own), ranks k + RI v + n: 4 RI in a row
+    const bool whole = p.parts == 1;
     void *const R = whole ? a.R : (void *)a.workspace;
     const int out = whole ? a.out : EXPERTS_FP32;
-    const int64_t group = whole ? (int64_t)g * a.group_r : ((int64_t)g * a.parts + part) * ((int64_t)a.N * a.r);
-    const bool columns_first = whole && !a.trans_r;   // (parts lie r x N)
+    const int64_t group = whole ? (int64_t)g * a.group_r : (int64_t)piece * ((int64_t)a.N * a.r);
     const int64_t ld = whole ? a.ldr : a.N;
+    const int k = r_block + RI * 4 * b;
+    if (whole && !a.trans_r) {
 #pragma unroll
-    for (int n = 0; n < RI; ++n) {
-        const int k = r0 + 16 * n + 4 * b;
-        if (k >= a.r) continue;
-        if (columns_first) {
+        for (int f = 0; f < F; ++f) {
+            if (col + f < c0 || col + f >= a.N) continue;
+            float v[4 * RI];
 #pragma unroll
-            for (int f = 0; f < F; ++f) {
-                const float v[4] = {acc[f][n][0], acc[f][n][1], acc[f][n][2], acc[f][n][3]};
-                if (col + f >= c0 && col + f < a.N) store_out<4>(R, out, group + (int64_t)(col + f) * ld, k, 0, a.r, v);
-            }
-        } else {
+            for (int q = 0; q < 4 * RI; ++q) v[q] = acc[f][q % RI][q / RI];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const float y[8] = {acc[0][n][v], acc[1][n][v], acc[2][n][v], acc[3][n][v], acc[4][n][v], acc[5][n][v], acc[6][n][v], acc[7][n][v]};
-                if (k + v < a.r) store_out<8>(R, out, group + (int64_t)(k + v) * ld, col, c0, a.N, y);
-            }
+            for (int q = 0; q < 4 * RI; q += 4) store_out<4>(R, out, group + (int64_t)(col + f) * ld, k + q, 0, a.r, v + q);
+        }
+    } else {   // (parts lie r x N)
+#pragma unroll
+        for (int q = 0; q < 4 * RI; ++q) {
+            float v[F];
+#pragma unroll
+            for (int f = 0; f < F; ++f) v[f] = acc[f][q % RI][q / RI];
+            if (k + q < a.r) store_out<F>(R, out, group + (int64_t)(k + q) * ld, col, c0, a.N, v);
         }
     }
 }
 
-template <int ELEM, int RI>
+template <int ELEM, int F, int RI>
 static hipError_t launch_outer(const OuterArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)outer_blocks(a.N, a.rows.G, a.parts), (unsigned)((a.r + 16 * RI - 1) / (16 * RI)));
-    constexpr int lds = kOuterWaves / 2 * 8 * RI * 1024;
-    auto launch = [&](auto kernel) -> hipError_t {
-        const hipError_t granted = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (granted != hipSuccess) { (void)hipGetLastError(); return granted; }
-        kernel<<<grid, dim3(64 * kOuterWaves), lds, s>>>(a);
-        return hipGetLastError();
-    };
-    return a.out == EXPERTS_FP32 ? launch(adapters_outer_kernel<ELEM, RI, 3>) : launch(adapters_outer_kernel<ELEM, RI, 2>);
+    const dim3 grid((unsigned)((a.N + 16 * F - 1) / (16 * F) * a.pieces), (unsigned)((a.r + 16 * RI - 1) / (16 * RI)));
+    constexpr int lds = kOuterWaves / 2 * F * RI * 1024;
+    static_assert(lds + kOuterAdapters * 4 <= 64 * 1024, "LDS of an ordinary launch");
+    if (a.out == EXPERTS_FP32) adapters_outer_kernel<ELEM, F, RI, 3><<<grid, dim3(64 * kOuterWaves), lds, s>>>(a);
+    else adapters_outer_kernel<ELEM, F, RI, 2><<<grid, dim3(64 * kOuterWaves), lds, s>>>(a);
+    return hipGetLastError();
+}
+template <int ELEM>
+static hipError_t launch_outer(const OuterArgs &a, hipStream_t s)
+{
+    if (a.columns == 128) return a.r <= 16 ? launch_outer<ELEM, 8, 1>(a, s) : launch_outer<ELEM, 8, 2>(a, s);
+    return a.r <= 16 ? launch_outer<ELEM, 4, 1>(a, s) : launch_outer<ELEM, 4, 2>(a, s);
 }
 hipError_t launch_adapters_outer(int type, const OuterArgs &a, hipStream_t s)
 {
     if (forced_launch_failure()) return hipErrorLaunchFailure;
-    const bool narrow = outer_ranks(a.r) == 16;
-    if (type == EXPERTS_BF16) return narrow ? launch_outer<EXPERTS_BF16, 1>(a, s) : launch_outer<EXPERTS_BF16, 2>(a, s);
-    return narrow ? launch_outer<EXPERTS_FP16, 1>(a, s) : launch_outer<EXPERTS_FP16, 2>(a, s);
+    return type == EXPERTS_BF16 ? launch_outer<EXPERTS_BF16>(a, s) : launch_outer<EXPERTS_FP16>(a, s);
 }
 
-// The parts' sums added up in order: a thread to four neighbouring columns of a rank.
+// The pieces' sums added up in order, of adapters that have several: four neighbouring columns of a rank to a thread.
 __global__ void __launch_bounds__(256) adapters_join_kernel(const OuterArgs a)
 {
+    __shared__ int counts[kOuterAdapters];
+    count_rows(a.rows, counts);
     const int64_t of_group = (int64_t)a.N * a.r;
     const int fours = (a.N + 3) / 4;
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, k = at / fours;
     const int c = (int)(at - k * fours) * 4, g = (int)(k / a.r), rank = (int)(k - (int64_t)g * a.r);
     if (g >= a.rows.G) return;
-    const float *const from = a.workspace + (int64_t)g * a.parts * of_group + (int64_t)rank * a.N + c;
+    const int parts = pieces_of(counts[g], a.quota);
+    if (parts == 1) return;
+    int first = 0;
+    for (int x = 0; x < g; ++x) first += pieces_of(counts[x], a.quota);
+    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+    // (the last columns of a row: its last four, of which the thread's are stored)
+    const int in = c + 4 <= a.N || a.N < 4 ? c : a.N - 4;
+    const float *const from = a.workspace + (int64_t)first * of_group + (int64_t)rank * a.N + in;
     float x[4] = {0, 0, 0, 0};
-    for (int p = 0; p < a.parts; ++p)
+    if (a.N >= 4) {
+        xt_f4 sum = {0, 0, 0, 0};
+        int p = 0;
+        for (; p + 4 <= parts; p += 4) {
+            f4 y[4];
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-            if (c + v < a.N) x[v] = p == 0 ? from[v] : x[v] + from[p * of_group + v];
+            for (int q = 0; q < 4; ++q) y[q] = *(const f4 *)(from + (p + q) * of_group);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum += __builtin_bit_cast(xt_f4, y[q]);
+        }
+        for (; p < parts; ++p) sum += __builtin_bit_cast(xt_f4, *(const f4 *)(from + p * of_group));
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x[v] = sum[v];
+    } else {
+        for (int p = 0; p < parts; ++p)
+            for (int v = 0; v < a.N; ++v) x[v] += from[p * of_group + v];
+    }
     const int64_t group = (int64_t)g * a.group_r;
-    if (a.trans_r) { store_out<4>(a.R, a.out, group + (int64_t)rank * a.ldr, c, 0, a.N, x); return; }
+    if (a.trans_r) { store_out<4>(a.R, a.out, group + (int64_t)rank * a.ldr, in, c, a.N, x); return; }
 #pragma unroll
     for (int v = 0; v < 4; ++v)
-        if (c + v < a.N) {
+        if (in + v >= c && in + v < a.N) {
             const float y[4] = {x[v], 0, 0, 0};
-            store_out<4>(a.R, a.out, group + (int64_t)(c + v) * a.ldr, rank, 0, rank + 1, y);
+            store_out<4>(a.R, a.out, group + (int64_t)(in + v) * a.ldr, rank, 0, rank + 1, y);
         }
 }
 hipError_t launch_adapters_join(const OuterArgs &a, hipStream_t s)

@@ -47,13 +47,22 @@ __device__ __forceinline__ float piece_rest(float x, float first)
     const float rest = x - first;
     return __builtin_fabsf(rest) > 0.0f ? rest : first * 0x1p-30f;
 }
-// piece `which` of `pieces` (2 or 3)
+// piece `which` of `pieces` (2 or 3).  (Of a NaN whose upper 7 bits of payload are zeros, which no operation makes, the first would be an infinity: a
+// caller's values pass through whole_nan().)
 __device__ __forceinline__ float piece_of(float x, int which, int pieces)
 {
-    if (x != x) return x;
     const float p0 = piece_first(x), r1 = piece_rest(x, p0);
     const float p1 = pieces > 2 ? piece_first(r1) : r1, r2 = piece_rest(r1, p1);
     return which == 0 ? p0 : which == 1 ? p1 : r2;
+}
+__device__ __forceinline__ float whole_nan(float x) { return x != x ? __builtin_nanf("") : x; }
+// Matrix instructions' results are there: for what reads them in another basic block (the compiler waits between the two where they lie in one; where
+// a branch lay between, a copy of a sum was seen to take what its register held before).
+__device__ __forceinline__ void sums_done()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 7\n\ts_nop 7" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
 }
 // two values rounded to bf16 side by side
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)

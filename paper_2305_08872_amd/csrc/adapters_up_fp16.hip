@@ -3,9 +3,9 @@
 
 namespace amulet {
 
-hipError_t launch_adapters_up_fp16(int tile, bool w_across, const UpArgs &a, int64_t blocks, hipStream_t s)
+hipError_t launch_adapters_up_fp16(int tile, bool w_across, bool many, const UpArgs &a, int64_t blocks, hipStream_t s)
 {
-    return launch_adapters_up<EXPERTS_FP16>(tile, w_across, a, blocks, s);
+    return launch_adapters_up<EXPERTS_FP16>(tile, w_across, many, a, blocks, s);
 }
 
 }  // namespace amulet

@@ -15,24 +15,21 @@
 
 namespace amulet {
 
-// Units: 8 ranks, of which an instruction has four.  Ways: the pieces of T times those of B.
+// Units: 8 ranks, of which an instruction has four.  Ways: the pieces of T times those of B.  What is read of B at a time (up to four units) is
+// taken by as many instructions as it has ways, or, with one or two units, as all of these fill, one behind the other.
 struct Ways {
     int units, ways;
-    bool packed;   // few units: an instruction's four groups of lanes have ways too, one behind the other
+    bool packed;
     __device__ __forceinline__ Ways(int n, int w) : units(n), ways(w), packed(n <= 2) {}
-    __device__ __forceinline__ int steps() const { return packed ? (units * ways + 3) / 4 : (units + 3) / 4 * ways; }
-    // of step s, in the lanes of group b: unit and way; whether there is one
-    __device__ __forceinline__ bool at(int s, int b, int &unit, int &way) const
+    __device__ __forceinline__ int reads() const { return (units + 3) / 4; }
+    __device__ __forceinline__ int of_read(int read) const { return units - 4 * read < 4 ? units - 4 * read : 4; }   // units
+    __device__ __forceinline__ int each() const { return packed ? (units * ways + 3) / 4 : ways; }                   // instructions
+    // of instruction e of a read, in the lanes of group b: unit and way; whether there is one
+    __device__ __forceinline__ bool at(int read, int e, int b, int &unit, int &way) const
     {
-        if (packed) {
-            const int x = 4 * s + b;
-            unit = units == 1 ? 0 : x & 1;
-            way = units == 1 ? x : x >> 1;
-        } else {
-            const int q = s / ways;
-            unit = 4 * q + b;
-            way = s - q * ways;
-        }
+        const int x = 4 * e + b;
+        unit = !packed ? 4 * read + b : units == 1 ? 0 : x & 1;
+        way = !packed ? e : units == 1 ? x : x >> 1;
         return unit < units && way < ways;
     }
 };
@@ -51,14 +48,20 @@ struct Adapters {
         xt_u4 v = {0, 0, 0, 0};
         if (!a.across) {
             const char *const row = b + (int64_t)n * a.ldb * 2;
-            if (there) v = load_unit<2>(row, unit * 16, a.r * 2);
+            typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+            if ((a.r & 7) == 0) {
+                v = __builtin_bit_cast(xt_u4, *(const u4 *)(row + (unit * 8 < a.r ? unit * 16 : 0)));
+                if (!there) v = xt_u4{0, 0, 0, 0};
+            } else if (there) v = load_unit<2>(row, unit * 16, a.r * 2);
         } else {
             uint32_t x[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int k = unit * 8 + j;
-                x[j] = there && k < a.r ? *(const uint16_t *)(b + ((int64_t)k * a.ldb + n) * 2) : 0u;
+                x[j] = *(const uint16_t *)(b + ((int64_t)(k < a.r ? k : a.r - 1) * a.ldb + n) * 2);
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = there && unit * 8 + j < a.r ? x[j] : 0u;
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = x[2 * j] | (x[2 * j + 1] << 16);
         }
@@ -72,31 +75,62 @@ struct Adapters {
             for (int j = 0; j < 4; ++j) v[j] = bf16_pair(piece_of(half_of<EXPERTS_FP16>(v[j], 0), which, 2), piece_of(half_of<EXPERTS_FP16>(v[j], 1), which, 2));
         return v;
     }
-    // T of the tile's rows, units u0 .. u0 + n - 1, as pieces: slot (unit * pieces + piece) has 16 bytes of every row
-    __device__ __forceinline__ void lay_out_t(char *lds, int u0, int n, int pieces) const
+    // T of the tile's rows, units u0 .. u0 + n - 1, as pieces: slot (unit * pieces + piece) has 16 bytes of every row.  A thread has two items (8
+    // ranks of a row) on their way at a time; no branch around a read: what is not there is read at the edge and becomes zeros.
+    static constexpr int T_ITEMS = 2;
+    __device__ __forceinline__ void item_of_t(int at, int n, int &line, int &unit) const
+    {
+        line = at / n;
+        unit = at - line * n;
+    }
+    __device__ __forceinline__ void read_t(float (&t)[T_ITEMS][8], int begin, int u0, int n) const
     {
         typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
-        for (int at = (int)threadIdx.x; at < n * T::BM; at += T::NT) {
-            const int line = at / n, unit = at - line * n, row = tile_row + line, k = (u0 + unit) * 8;
-            float t[8];
-            const float *const p = a.T + (int64_t)row * a.ldt + k;
-            if (row < a.rows.M && k + 8 <= a.r) {
-                const f4 x = *(const f4 *)p, y = *(const f4 *)(p + 4);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) { t[j] = x[j]; t[4 + j] = y[j]; }
+        for (int q = 0; q < T_ITEMS; ++q) {
+            int line, unit;
+            item_of_t(begin + q * T::NT < n * T::BM ? begin + q * T::NT : 0, n, line, unit);
+            const int row = tile_row + line, k = (u0 + unit) * 8;
+            const float *const p = a.T + (int64_t)(row < a.rows.M ? row : a.rows.M - 1) * a.ldt;
+            if ((a.r & 7) == 0) {
+                const f4 x = *(const f4 *)(p + k), y = *(const f4 *)(p + k + 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { t[q][j] = x[j]; t[q][4 + j] = y[j]; }
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) t[j] = row < a.rows.M && k + j < a.r ? p[j] : 0.0f;
+                for (int j = 0; j < 8; ++j) t[q][j] = p[k + j < a.r ? k + j : a.r - 1];
             }
+        }
+    }
+    __device__ __forceinline__ void write_t(char *lds, float (&t)[T_ITEMS][8], int begin, int u0, int n, int pieces) const
+    {
+#pragma unroll
+        for (int q = 0; q < T_ITEMS; ++q) {
+            if (begin + q * T::NT >= n * T::BM) return;
+            int line, unit;
+            item_of_t(begin + q * T::NT, n, line, unit);
+            const int row = tile_row + line, k = (u0 + unit) * 8;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[q][j] = row < a.rows.M && k + j < a.r ? t[q][j] : 0.0f;
             for (int piece = 0; piece < pieces; ++piece) {
                 xt_u4 v;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = bf16_pair(piece_of(t[2 * j], piece, pieces), piece_of(t[2 * j + 1], piece, pieces));
+                for (int j = 0; j < 4; ++j) v[j] = bf16_pair(piece_of(t[q][2 * j], piece, pieces), piece_of(t[q][2 * j + 1], piece, pieces));
                 *(xt_u4 *)(lds + ((unit * pieces + piece) * T::BM + line) * 16) = v;
             }
         }
     }
-    // an instruction's products added to block m, in the rows lo .. hi - 1
+    // from item `begin` of the thread's on
+    __device__ __forceinline__ void lay_out_t(char *lds, int begin, int u0, int n, int pieces) const
+    {
+        for (int at = (int)threadIdx.x + begin * T::NT; at < n * T::BM; at += T_ITEMS * T::NT) {
+            float t[T_ITEMS][8];
+            read_t(t, at, u0, n);
+            write_t(lds, t, at, u0, n, pieces);
+        }
+    }
+    // An instruction's products added to block m, in the rows lo .. hi - 1.  (Blocks that a segment has whole could do without the choice; a
+    // branch for them gained nothing, and there is to be none between a matrix instruction and what reads its result.)
     template <int mi>
     __device__ __forceinline__ void add_block(xt_f4 (&acc)[T::MI][T::NI], const char *t_at, bool there, int lo, int hi, const xt_u4 (&vb)[T::NI]) const
     {
@@ -128,7 +162,7 @@ struct Meeting {
     bool more;
     __device__ __forceinline__ void start(const Segments &g, int first, int last, int lane)
     {
-        chunk = segment_of(g, first, lane);
+        chunk = g.S <= 64 ? 0 : segment_of(g, first, lane);
         look(g, first, last, lane);
     }
     __device__ __forceinline__ void look(const Segments &g, int first, int last, int lane)
@@ -140,165 +174,353 @@ struct Meeting {
     __device__ __forceinline__ void next(const Segments &g, int first, int last, int lane) { chunk += 64; look(g, first, last, lane); }
 };
 
-// From memory: (segment, step) pairs, PAIRS of them on their way at a time; the k groups take the segments in turn
+// From memory: a batch of segments' B on its way while the one before is multiplied; the k groups take the segments in turn.  T and the first batch
+// are asked for before the first stages of X and W.  Neighbouring lanes read neighbouring bytes and hand them on by a
+// permutation (a matrix operand's lanes have columns of their own: a cache line for every 16 bytes).
 template <class T>
 struct AddFromMemory : Adapters<T> {
-    static constexpr int ROOM = T::BM >= 64 ? 32 * 1024 : 8 * 1024;   // for T, beside the ring
-    static constexpr int LDS = T::LDS + ROOM, SLOTS = ROOM / (T::BM * 16);
-    static constexpr int PAIRS = 8 / Adapters<T>::OF_B;
+    static constexpr int ROOM = T::BM >= 64 ? (T::WK > 1 ? 32 : 8) * 1024 : 8 * 1024;   // for T, beside the ring
+    static constexpr int LDS = T::LDS + ROOM, SLOTS = ROOM / (T::BM * 16), OF_B = Adapters<T>::OF_B;
+    static constexpr int AT = 4 / OF_B, T_ITEMS = Adapters<T>::T_ITEMS;   // segments of a batch
     static_assert(SLOTS >= 3, "one unit in three pieces");
-    __device__ __forceinline__ AddFromMemory(const Adapters<T> &x) : Adapters<T>(x) {}
 
-    struct Pair {
-        int adapter, lo, hi, step;
+    struct Batch {
+        xt_u4 v[AT][T::NI];
+        int lo[AT], hi[AT], n;
     };
+    // what a lane reads of B: the reads units of which all segments have the same
+    struct Lane {
+        const char *first;      // B at the wave's first column and the read's first rank
+        uint32_t off[T::NI];
+        int unit, k, from;      // its unit of a read, the read's first rank; the lane whose read is its operand
+        bool reads, whole, full;   // it reads at all; no unit is cut; every lane has one
+    };
+    mutable float t0[T_ITEMS][8];
+    mutable Meeting first;
+    mutable Batch batch;
+    int row1, pieces, units, most;
+
+    __device__ __forceinline__ AddFromMemory(const Adapters<T> &x) : Adapters<T>(x)
+    {
+        const UpArgs &a = this->a;
+        if (a.r == 0 || a.rows.S == 0) return;
+        pieces = a.mm.out == EXPERTS_FP32 ? 3 : 2;
+        units = (a.r + 7) / 8;
+        most = SLOTS / pieces;
+        row1 = this->row0 + T::MI * 16 < a.rows.M ? this->row0 + T::MI * 16 : a.rows.M;
+        this->read_t(t0, (int)threadIdx.x, 0, units < most ? units : most);
+        if (this->idle) return;
+        first.start(a.rows, this->row0, row1, this->lane);
+        met = 0;
+        fetch(lane_of(0, Ways(units < most ? units : most, pieces * OF_B), 0), first, batch);
+    }
+    mutable int met;
+
     __device__ __forceinline__ void operator()(xt_f4 (&acc)[T::MI][T::NI]) const
     {
         const UpArgs &a = this->a;
         if (a.r == 0 || a.rows.S == 0) return;
         char *const lds = xt_smem + T::LDS;
-        const int pieces = a.mm.out == EXPERTS_FP32 ? 3 : 2, units = (a.r + 7) / 8, most = SLOTS / pieces;
         for (int u0 = 0; u0 < units; u0 += most) {
             const int n = units - u0 < most ? units - u0 : most;
-            if (u0 > 0) __syncthreads();
-            this->lay_out_t(lds, u0, n, pieces);
+            if (u0 > 0) {
+                __syncthreads();
+                this->lay_out_t(lds, 0, u0, n, pieces);
+            } else {
+                this->write_t(lds, t0, (int)threadIdx.x, 0, n, pieces);
+                this->lay_out_t(lds, T_ITEMS, 0, n, pieces);
+            }
             meet<T::NW * T::WK>();
-            if (!this->idle) add(acc, lds, u0, n, pieces);
+            if (this->idle) continue;
+            const Ways ways(n, pieces * OF_B);
+            for (int read = 0; read < ways.reads(); ++read) {
+                const Lane l = lane_of(u0, ways, read);
+                if (u0 > 0 || read > 0) {
+                    first.start(a.rows, this->row0, row1, this->lane);
+                    met = 0;
+                    fetch(l, first, batch);
+                }
+                while (batch.n > 0) {
+                    Batch next;
+                    next.n = 0;
+                    if (batch.n == AT) fetch(l, first, next);
+                    multiply(acc, lds, batch, l, ways, read);
+                    if (batch.n < AT || next.n == 0) break;
+                    batch.n = 0;
+                    if (next.n == AT) fetch(l, first, batch);
+                    multiply(acc, lds, next, l, ways, read);
+                }
+            }
         }
     }
-    __device__ __forceinline__ void add(xt_f4 (&acc)[T::MI][T::NI], const char *lds, int u0, int n_units, int pieces) const
+    __device__ __forceinline__ Lane lane_of(int u0, const Ways &ways, int read) const
     {
         const UpArgs &a = this->a;
-        const int lane = this->lane, row0 = this->row0, b = lane >> 4, row1 = row0 + T::MI * 16 < a.rows.M ? row0 + T::MI * 16 : a.rows.M;
-        const Ways ways(n_units, pieces * this->OF_B);
-        const int steps = ways.steps();
-        Meeting m;
-        m.start(a.rows, row0, row1, lane);
-        int step = 0, met = 0;
-        auto next = [&](Pair &p) -> bool {
-            for (;;) {
-                if (m.which == 0) {
-                    if (!m.more) return false;
-                    m.next(a.rows, row0, row1, lane);
-                    continue;
-                }
-                if (met % T::WK != this->kg) {
-                    m.which &= m.which - 1;
-                    ++met;
-                    continue;
-                }
-                const int l = __builtin_ctzll(m.which);
-                p = {__builtin_amdgcn_readlane(m.adapter, l), __builtin_amdgcn_readlane(m.lo, l), __builtin_amdgcn_readlane(m.hi, l), step};
-                if (++step == steps) { step = 0; m.which &= m.which - 1; ++met; }
-                return true;
-            }
-        };
-        const char *const t_row = lds + (row0 - this->tile_row + (lane & 15)) * 16;
-        for (;;) {
-            Pair p[PAIRS];
-            xt_u4 vb[PAIRS][T::NI];
-            int n = 0;
-            for_each<PAIRS>([&](auto which) {
-                constexpr int q = decltype(which)::value;
-                if (n < q || !next(p[q])) return;
-                n = q + 1;
-                int unit, way;
-                const bool there = ways.at(p[q].step, b, unit, way);
-                const char *const from = (const char *)a.B + (int64_t)p[q].adapter * a.group_b * 2;
+        const int lane = this->lane, b = lane >> 4, n = ways.of_read(read);
+        Lane l;
+        const int i = a.across ? lane & 15 : n == 4 ? lane >> 2 : n == 1 ? lane : n == 2 ? lane >> 1 : lane / 3;
+        l.unit = a.across ? b : lane - i * n;
+        l.k = (u0 + 4 * read) * 8;
+        l.reads = i < 16 && l.unit < n;
+        const uint32_t ld = (uint32_t)a.ldb * 2u;
+        const int c0 = this->col0 < a.mm.N ? this->col0 : a.mm.N - 1;
+        l.first = (const char *)a.B + (a.across ? (int64_t)l.k * a.ldb + c0 : (int64_t)c0 * a.ldb + l.k) * 2;
 #pragma unroll
-                for (int ni = 0; ni < T::NI; ++ni) {
-                    const int c = this->col0 + this->column(ni, lane);
-                    vb[q][ni] = this->read_b(from, c < a.mm.N ? c : a.mm.N - 1, u0 + unit, there);
-                }
-            });
-            if (n == 0) break;
-            for_each<PAIRS>([&](auto which) {
-                constexpr int q = decltype(which)::value;
-                if (q >= n) return;
-                int unit, way;
-                const bool there = ways.at(p[q].step, b, unit, way);
-#pragma unroll
-                for (int ni = 0; ni < T::NI; ++ni) vb[q][ni] = this->piece_of_b(vb[q][ni], way % this->OF_B);
-                const char *const t_at = t_row + (there ? unit * pieces + way / this->OF_B : 0) * (T::BM * 16);
-                for_each<T::MI>([&](auto mi) { this->template add_block<decltype(mi)::value>(acc, t_at, there, p[q].lo, p[q].hi, vb[q]); });
-            });
-            if (n < PAIRS) break;
+        for (int ni = 0; ni < T::NI; ++ni) {
+            int c = this->col0 + this->column(ni, i & 15);
+            c = (c < a.mm.N ? c : a.mm.N - 1) - c0;
+            l.off[ni] = a.across ? (uint32_t)c * 2u : (uint32_t)c * ld + (l.reads ? (uint32_t)l.unit * 16u : 0u);
         }
+        l.whole = (a.r & 7) == 0;
+        l.full = l.whole && n == 4;
+        const int own = ways.packed ? (n == 1 ? 0 : b & 1) : b < n ? b : 0;
+        l.from = a.across ? (lane & 15) + 16 * own : (lane & 15) * n + own;
+        return l;
+    }
+    __device__ __forceinline__ xt_u4 load(const Lane &l, const char *base, int ni) const
+    {
+        typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+        const UpArgs &a = this->a;
+        if (!a.across) {
+            if (l.whole) return __builtin_bit_cast(xt_u4, *(const u4 *)(base + l.off[ni]));
+            xt_u4 v = {0, 0, 0, 0};
+            if (l.reads) v = load_unit<2>(base + (l.off[ni] - (uint32_t)l.unit * 16u) - l.k * 2, (l.k + l.unit * 8) * 2, a.r * 2);
+            return v;
+        }
+        const uint32_t ld = (uint32_t)a.ldb * 2u;
+        uint32_t x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int at = l.unit * 8 + j;
+            x[j] = *(const uint16_t *)(base + l.off[ni] + (uint32_t)(l.k + at < a.r ? at : a.r - 1 - l.k) * ld);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = l.k + l.unit * 8 + j < a.r ? x[j] : 0u;
+        return xt_u4{x[0] | (x[1] << 16), x[2] | (x[3] << 16), x[4] | (x[5] << 16), x[6] | (x[7] << 16)};
+    }
+    // the group's next segments' B
+    __device__ __forceinline__ void fetch(const Lane &l, Meeting &m, Batch &x) const
+    {
+        const UpArgs &a = this->a;
+        x.n = 0;
+        for_each<AT>([&](auto which) {
+            constexpr int q = decltype(which)::value;
+            if (x.n < q) return;
+            for (;;) {
+                while (m.which == 0 && m.more) m.next(a.rows, this->row0, row1, this->lane);
+                if (m.which == 0) return;
+                if (T::WK == 1 || met++ % T::WK == this->kg) break;
+                m.which &= m.which - 1;
+            }
+            const int at = __builtin_ctzll(m.which);
+            m.which &= m.which - 1;
+            x.n = q + 1;
+            x.lo[q] = __builtin_amdgcn_readlane(m.lo, at);
+            x.hi[q] = __builtin_amdgcn_readlane(m.hi, at);
+            const char *const base = l.first + (int64_t)__builtin_amdgcn_readlane(m.adapter, at) * a.group_b * 2;
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ++ni) x.v[q][ni] = load(l, base, ni);
+        });
+    }
+    __device__ __forceinline__ void multiply(xt_f4 (&acc)[T::MI][T::NI], const char *lds, const Batch &x, const Lane &l, const Ways &ways, int read) const
+    {
+        const int lane = this->lane, b = lane >> 4, each = ways.each();
+        const char *const t_row = lds + (this->row0 - this->tile_row + (lane & 15)) * 16;
+        for_each<AT>([&](auto which) {
+            constexpr int q = decltype(which)::value;
+            if (q >= x.n) return;
+            xt_u4 vb[T::NI];
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ++ni)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) vb[ni][j] = (uint32_t)__builtin_amdgcn_ds_bpermute(l.from * 4, (int)x.v[q][ni][j]);
+            for (int e = 0; e < each; ++e) {
+                int at, way;
+                const bool some = ways.at(read, e, b, at, way);
+                xt_u4 w[T::NI];
+#pragma unroll
+                for (int ni = 0; ni < T::NI; ++ni) w[ni] = this->piece_of_b(vb[ni], way % OF_B);
+                if (!l.full)
+#pragma unroll
+                    for (int ni = 0; ni < T::NI; ++ni) w[ni] = some ? w[ni] : xt_u4{0, 0, 0, 0};
+                const char *const t_at = t_row + (some ? at * pieces + way / OF_B : 0) * (T::BM * 16);
+                for_each<T::MI>([&](auto mi) { this->template add_block<decltype(mi)::value>(acc, t_at, some, x.lo[q], x.hi[q], w); });
+            }
+        });
     }
 };
 
-// Through LDS: T's pieces and B's (slot (unit * pieces + piece) of a segment has 16 bytes of every column)
+// Through LDS: T's pieces and B's (slot (unit * pieces + piece) of a segment has 16 bytes of every column).  While one batch of segments is
+// multiplied the next one's B is on its way into registers.
 template <class T>
 struct AddFromLds : Adapters<T> {
-    static constexpr int LDS = T::LDS, ROOM = T::S * T::STAGE - 1024;   // (a list of 64 segments behind it)
+    // behind the ring: the first segments that the tile meets, which its first wave looks up while the first stages are on their way
+    struct List {
+        int4 of[64];   // adapter, first row, last row + 1
+        int n, chunk, more;
+    };
+    static constexpr int LDS = T::LDS + (int)sizeof(List), ROOM = T::LDS;
     static constexpr int OF_B = Adapters<T>::OF_B;
-    __device__ __forceinline__ AddFromLds(const Adapters<T> &x) : Adapters<T>(x) {}
+    static constexpr int ITEMS = 4;   // 16 bytes of B that a thread has on their way
+    static_assert(ROOM >= (3 * T::BM + OF_B * T::BN) * 16 && ITEMS * T::NT >= T::BN, "a unit of both");
+    // T and the first segments' B are asked for before the sums begin, where there are registers for them
+    static constexpr bool AHEAD = T::BM < 256;
+    static constexpr int T_ITEMS = Adapters<T>::T_ITEMS;
+    mutable xt_u4 next[ITEMS];
+    mutable float t0[T_ITEMS][8];
+    int pieces, units, most;
+    __device__ __forceinline__ AddFromLds(const Adapters<T> &x) : Adapters<T>(x)
+    {
+        pieces = this->a.mm.out == EXPERTS_FP32 ? 3 : 2;
+        units = (this->a.r + 7) / 8;
+        most = ROOM / (pieces * T::BM * 16 + OF_B * T::BN * 16);
+        most = most < ITEMS * T::NT / T::BN ? most : ITEMS * T::NT / T::BN;
+        if (AHEAD && this->a.r > 0 && this->a.rows.S > 0) this->read_t(t0, (int)threadIdx.x, 0, units < most ? units : most);
+    }
+    // segments of a batch, one at least
+    __device__ __forceinline__ int at_once(int n_units) const
+    {
+        const int room = (ROOM - n_units * pieces * T::BM * 16) / (n_units * OF_B * T::BN * 16), items = ITEMS * T::NT / (n_units * T::BN);
+        return room < items ? room : items;
+    }
+    static __device__ __forceinline__ List *list() { return (List *)(xt_smem + T::LDS); }
+
+    __device__ __forceinline__ void write(const Meeting &m) const
+    {
+        if ((m.which >> this->lane) & 1) list()->of[__popcll(m.which & ((1ull << this->lane) - 1))] = int4{m.adapter, m.lo, m.hi, 0};
+        if (this->lane == 0) {
+            list()->n = __popcll(m.which);
+            list()->chunk = m.chunk;
+            list()->more = m.more;
+        }
+    }
+    __device__ __forceinline__ int last_row() const { return this->tile_row + T::BM < this->a.rows.M ? this->tile_row + T::BM : this->a.rows.M; }
+    // the sums' beginning: nothing is added yet
+    struct Look {
+        const AddFromLds &x;
+        __device__ __forceinline__ void operator()(xt_f4 (&)[T::MI][T::NI]) const
+        {
+            const UpArgs &a = x.a;
+            if ((!AHEAD && threadIdx.x >= 64) || a.r == 0 || a.rows.S == 0) return;
+            Meeting m;
+            m.start(a.rows, x.tile_row, x.last_row(), x.lane);
+            if (threadIdx.x < 64) x.write(m);
+            if constexpr (AHEAD) {
+                // (lane j: the j-th segment's adapter)
+                // (all lanes take part: those of no segment send to the last one, which a full list alone reads)
+                const int to = (m.which >> x.lane) & 1 ? __popcll(m.which & ((1ull << x.lane) - 1)) : 63;
+                const int adapter = __builtin_amdgcn_ds_permute(to * 4, m.adapter);
+                const int met = __popcll(m.which), n_units = x.units < x.most ? x.units : x.most, once = x.at_once(n_units);
+                x.read_batch(x.next, met < once ? met : once, 0, n_units, [&](int k) { return __shfl(adapter, k); });
+            }
+        }
+    };
+    // the first wave's: the list of the next 64 segments, or the first again
+    __device__ __forceinline__ void look(int chunk) const
+    {
+        Meeting m;
+        m.chunk = chunk;
+        m.look(this->a.rows, this->tile_row, last_row(), this->lane);
+        write(m);
+    }
 
     __device__ __forceinline__ void operator()(xt_f4 (&acc)[T::MI][T::NI]) const
     {
         const UpArgs &a = this->a;
         if (a.r == 0 || a.rows.S == 0) return;
-        const int lane = this->lane, row0 = this->tile_row, row1 = row0 + T::BM < a.rows.M ? row0 + T::BM : a.rows.M;
-        const int pieces = a.mm.out == EXPERTS_FP32 ? 3 : 2, units = (a.r + 7) / 8;
         const int t_unit = pieces * T::BM * 16, b_unit = OF_B * T::BN * 16;
-        const int most = ROOM / (t_unit + b_unit);
-        static_assert(ROOM >= (3 * T::BM + OF_B * T::BN) * 16, "a unit of both");
-        int4 *const list = (int4 *)(xt_smem + ROOM);
+        __syncthreads();   // (the ring is read no more, and the list is there)
+        const int first = __builtin_amdgcn_readfirstlane(list()->chunk);
+        if (!__builtin_amdgcn_readfirstlane(list()->n | list()->more)) return;
         for (int u0 = 0; u0 < units; u0 += most) {
-            const int n_units = units - u0 < most ? units - u0 : most;
-            __syncthreads();   // (what lies there is read no more)
-            this->lay_out_t(xt_smem, u0, n_units, pieces);
+            const int n_units = units - u0 < most ? units - u0 : most, once = at_once(n_units);
             char *const lds_b = xt_smem + n_units * t_unit;
-            const int at_once = (ROOM - n_units * t_unit) / (n_units * b_unit);   // segments, one at least
             const Ways ways(n_units, pieces * OF_B);
-            const int steps = ways.steps();
-            Meeting m;
-            m.start(a.rows, row0, row1, lane);
-            for (;;) {
-                const int met = __popcll(m.which);
-                if (threadIdx.x < 64 && ((m.which >> lane) & 1))
-                    list[__popcll(m.which & ((1ull << lane) - 1))] = int4{m.adapter, m.lo, m.hi, 0};
-                for (int s0 = 0; s0 < met; s0 += at_once) {
-                    const int n = met - s0 < at_once ? met - s0 : at_once;
-                    __syncthreads();   // the list is there; B's slots are read no more
-                    lay_out_b(lds_b, list + s0, n, u0, n_units);
+            if (u0 > 0) {
+                __syncthreads();
+                if (threadIdx.x < 64 && __builtin_amdgcn_readfirstlane(list()->chunk) != first) look(first);
+                __syncthreads();
+            }
+            for (bool begun = false;; begun = true) {
+                const int met = __builtin_amdgcn_readfirstlane(list()->n), chunk = __builtin_amdgcn_readfirstlane(list()->chunk), more = __builtin_amdgcn_readfirstlane(list()->more);
+                const auto adapter = [&](int s0) { return [s0](int k) { return list()->of[s0 + k].x; }; };
+                if (met > 0 && (!AHEAD || begun || u0 > 0)) read_batch(next, met < once ? met : once, u0, n_units, adapter(0));
+                if (!begun) {
+                    if (AHEAD && u0 == 0) this->write_t(xt_smem, t0, (int)threadIdx.x, 0, n_units, pieces);
+                    this->lay_out_t(xt_smem, AHEAD && u0 == 0 ? T_ITEMS : 0, u0, n_units, pieces);
+                }
+                for (int s0 = 0; s0 < met; s0 += once) {
+                    const int n = met - s0 < once ? met - s0 : once, left = met - s0 - n;
+                    write_batch(next, lds_b, n, n_units);
                     __syncthreads();
+                    if (left > 0) read_batch(next, left < once ? left : once, u0, n_units, adapter(s0 + n));
                     if (!this->idle)
                         for (int k = 0; k < n; ++k) {
-                            const int4 seg = list[s0 + k];
+                            const int4 seg = list()->of[s0 + k];
                             const int lo = __builtin_amdgcn_readfirstlane(seg.y), hi = __builtin_amdgcn_readfirstlane(seg.z);
-                            if (lo < this->row0 + T::MI * 16 && hi > this->row0) products(acc, lds_b + k * n_units * b_unit, lo, hi, ways, steps, pieces);
+                            if (lo < this->row0 + T::MI * 16 && hi > this->row0) products(acc, lds_b + k * n_units * b_unit, lo, hi, ways, pieces);
                         }
+                    __syncthreads();
                 }
-                if (!m.more) break;
+                if (!more) break;
                 __syncthreads();       // (the list is read no more)
-                m.next(a.rows, row0, row1, lane);
+                if (threadIdx.x < 64) look(chunk + 64);
+                __syncthreads();
             }
         }
     }
-    // B of n segments' adapters, units u0 .. u0 + units - 1, the tile's columns
-    __device__ __forceinline__ void lay_out_b(char *lds, const int4 *list, int n, int u0, int units) const
+    // which item of a batch a thread's q-th one is: segment k of it, unit, column of the tile (neighbouring threads: neighbouring addresses)
+    __device__ __forceinline__ bool item(int q, int n, int units, int &k, int &unit, int &line) const
+    {
+        const int at = (int)threadIdx.x + q * T::NT;
+        if (this->a.across) {
+            line = at % T::BN;
+            const int x = at / T::BN;
+            k = x / units;
+            unit = x - k * units;
+        } else {
+            const int x = at / units;
+            unit = at - x * units;
+            line = x % T::BN;
+            k = x / T::BN;
+        }
+        return at < n * units * T::BN;
+    }
+    // B of n segments' adapters (adapter(k): the k-th one's), units u0 .. u0 + units - 1, the tile's columns
+    template <class Adapter>
+    __device__ __forceinline__ void read_batch(xt_u4 (&v)[ITEMS], int n, int u0, int units, Adapter adapter) const
     {
         const UpArgs &a = this->a;
-        // neighbouring threads: neighbouring addresses
-        const int fast = a.across ? T::BN : units, slow = a.across ? units : T::BN;
-        for (int at = (int)threadIdx.x; at < n * units * T::BN; at += T::NT) {
-            const int x = at / fast, f = at - x * fast, k = x / slow, y = x - k * slow;
-            const int unit = a.across ? y : f, line = a.across ? f : y;
-            const int c = this->tile_col + line;
-            const xt_u4 v = this->read_b((const char *)a.B + (int64_t)list[k].x * a.group_b * 2, c < a.mm.N ? c : a.mm.N - 1, u0 + unit, true);
 #pragma unroll
-            for (int p = 0; p < OF_B; ++p) *(xt_u4 *)(lds + (((k * units + unit) * OF_B + p) * T::BN + line) * 16) = this->piece_of_b(v, p);
+        for (int q = 0; q < ITEMS; ++q) {
+            int k, unit, line;
+            const bool there = item(q, n, units, k, unit, line);
+            const int g = adapter(there ? k : 0);
+            if (!there) continue;
+            const int c = this->tile_col + line;
+            v[q] = this->read_b((const char *)a.B + (int64_t)g * a.group_b * 2, c < a.mm.N ? c : a.mm.N - 1, u0 + unit, true);
         }
     }
-    __device__ __forceinline__ void products(xt_f4 (&acc)[T::MI][T::NI], const char *lds_b, int lo, int hi, const Ways &ways, int steps, int pieces) const
+    __device__ __forceinline__ void write_batch(const xt_u4 (&v)[ITEMS], char *lds, int n, int units) const
+    {
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+            int k, unit, line;
+            if (!item(q, n, units, k, unit, line)) continue;
+#pragma unroll
+            for (int p = 0; p < OF_B; ++p) *(xt_u4 *)(lds + (((k * units + unit) * OF_B + p) * T::BN + line) * 16) = this->piece_of_b(v[q], p);
+        }
+    }
+    __device__ __forceinline__ void products(xt_f4 (&acc)[T::MI][T::NI], const char *lds_b, int lo, int hi, const Ways &ways, int pieces) const
     {
         const int lane = this->lane, b = lane >> 4;
         const char *const t_row = xt_smem + (this->row0 - this->tile_row + (lane & 15)) * 16;
+        const int each = ways.each(), steps = ways.reads() * each;
 #pragma unroll 1
         for (int s = 0; s < steps; ++s) {
             int unit, way;
-            const bool there = ways.at(s, b, unit, way);
+            const int read = s / each;
+            const bool there = ways.at(read, s - read * each, b, unit, way);
             const char *const t_at = t_row + (there ? unit * pieces + way / OF_B : 0) * (T::BM * 16);
             const char *const b_at = lds_b + ((there ? unit * OF_B + way % OF_B : 0) * T::BN + this->col0 - this->tile_col) * 16;
             xt_u4 vb[T::NI];
@@ -312,14 +534,14 @@ struct AddFromLds : Adapters<T> {
     }
 };
 
-template <class T>
-using AddAdapters = std::conditional_t<(T::WK > 1), AddFromMemory<T>, AddFromLds<T>>;
+template <class T, bool MEMORY>
+using AddAdapters = std::conditional_t<MEMORY, AddFromMemory<T>, AddFromLds<T>>;
 
-template <class T>
-__global__ void __launch_bounds__(T::NT) __attribute__((amdgpu_waves_per_eu(2))) adapters_up_kernel(const UpArgs u)
+template <class T, bool MEMORY>
+__global__ void __launch_bounds__(T::NT) __attribute__((amdgpu_waves_per_eu(!MEMORY && T::BM * T::BN <= 64 * 64 ? 3 : 2))) adapters_up_kernel(const UpArgs u)
 {
-    static_assert(!T::AKS && !T::FP8, "16-bit products by rows");
-    static_assert(AddAdapters<T>::LDS <= 160 * 1024 && (T::WK - 1) * T::NW * T::MI * T::NI * 1024 <= T::LDS, "LDS");
+    static_assert(!T::AKS && !T::FP8 && (MEMORY || T::WK == 1), "16-bit products by rows");
+    static_assert(AddAdapters<T, MEMORY>::LDS <= 160 * 1024 && (T::WK - 1) * T::NW * T::MI * T::NI * 1024 <= T::LDS, "LDS");
     const ExpertsArgs &a = u.mm;
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), kg = w / T::NW, wave = w % T::NW;
@@ -340,11 +562,11 @@ __global__ void __launch_bounds__(T::NT) __attribute__((amdgpu_waves_per_eu(2)))
         else sb.start_kc((const char *)a.B, a.ldb * T::ES, col0, a.N, a.K, kg * T::BK, wave, lane, a_row, true);
     }
     const bool idle = wave_row >= a.M;
-    const AddAdapters<T> adapters(Adapters<T>{u, row0, col0, wave_row, wave_col, lane, kg, idle});
-    if constexpr (T::WK > 1) {
+    const AddAdapters<T, MEMORY> adapters(Adapters<T>{u, row0, col0, wave_row, wave_col, lane, kg, idle});
+    if constexpr (MEMORY) {
         if (!tile_sums<T>(sa, sb, 0, a.K, wave, kg, lane, a_row, TileScales(), idle, acc, adapters)) return;
     } else {
-        tile_sums<T>(sa, sb, 0, a.K, wave, kg, lane, a_row, TileScales(), idle, acc);
+        tile_sums<T>(sa, sb, 0, a.K, wave, kg, lane, a_row, TileScales(), idle, acc, typename AddFromLds<T>::Look{adapters});
         adapters(acc);
     }
     store_sums<T>(acc, a.R, a.out, lane, wave_col, from, a.N, [&](int mi) -> int64_t {
@@ -353,35 +575,39 @@ __global__ void __launch_bounds__(T::NT) __attribute__((amdgpu_waves_per_eu(2)))
     });
 }
 
-template <class T>
+template <class T, bool MEMORY>
 inline hipError_t launch_adapters_tile(const UpArgs &a, int64_t blocks, hipStream_t s)
 {
-    constexpr int lds = AddAdapters<T>::LDS;
+    constexpr int lds = AddAdapters<T, MEMORY>::LDS;
     if (blocks <= 0) return hipSuccess;
     if (forced_launch_failure()) return hipErrorLaunchFailure;
-    static const hipError_t granted = hipFuncSetAttribute((const void *)adapters_up_kernel<T>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static const hipError_t granted = hipFuncSetAttribute((const void *)adapters_up_kernel<T, MEMORY>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (granted != hipSuccess) { (void)hipGetLastError(); return granted; }
-    adapters_up_kernel<T><<<dim3((unsigned)blocks), dim3(T::NT), lds, s>>>(a);
+    adapters_up_kernel<T, MEMORY><<<dim3((unsigned)blocks), dim3(T::NT), lds, s>>>(a);
     return hipGetLastError();
 }
 
 template <int ELEM, bool BKS>
-inline hipError_t launch_adapters_layout(int tile, const UpArgs &a, int64_t blocks, hipStream_t s)
+inline hipError_t launch_adapters_layout(int tile, bool many, const UpArgs &a, int64_t blocks, hipStream_t s)
 {
     switch (tile) {
-    case EXPERTS_256x256: return launch_adapters_tile<ExpertTile<ELEM, 256, 256, 2, 4, 1, 2, false, BKS>>(a, blocks, s);
-    case EXPERTS_128x128: return launch_adapters_tile<ExpertTile<ELEM, 128, 128, 2, 2, 1, 2, false, BKS>>(a, blocks, s);
-    case EXPERTS_64x128: return launch_adapters_tile<ExpertTile<ELEM, 64, 128, 2, 2, 1, 3, false, BKS>>(a, blocks, s);
-    case EXPERTS_64x64: return launch_adapters_tile<ExpertTile<ELEM, 64, 64, 2, 2, 1, 3, false, BKS>>(a, blocks, s);
-    case EXPERTS_64x64_K2: return launch_adapters_tile<ExpertTile<ELEM, 64, 64, 2, 2, 2, 3, false, BKS>>(a, blocks, s);
-    default: return launch_adapters_tile<ExpertTile<ELEM, 16, 32, 1, 1, 4, 3, false, BKS>>(a, blocks, s);
+    case EXPERTS_256x256: return launch_adapters_tile<ExpertTile<ELEM, 256, 256, 2, 4, 1, 2, false, BKS>, false>(a, blocks, s);
+    case EXPERTS_128x128: return launch_adapters_tile<ExpertTile<ELEM, 128, 128, 2, 2, 1, 2, false, BKS>, false>(a, blocks, s);
+    case EXPERTS_64x128: return launch_adapters_tile<ExpertTile<ELEM, 64, 128, 2, 2, 1, 3, false, BKS>, false>(a, blocks, s);
+    case EXPERTS_64x64: {
+        typedef ExpertTile<ELEM, 64, 64, 2, 2, 1, 3, false, BKS> T;
+        return many ? launch_adapters_tile<T, true>(a, blocks, s) : launch_adapters_tile<T, false>(a, blocks, s);
+    }
+    case EXPERTS_64x64_K2: return launch_adapters_tile<ExpertTile<ELEM, 64, 64, 2, 2, 2, 3, false, BKS>, true>(a, blocks, s);
+    default: return launch_adapters_tile<ExpertTile<ELEM, 16, 32, 1, 1, 4, 3, false, BKS>, true>(a, blocks, s);
     }
 }
 
+// many: segments of fewer rows than a block; the tile is EXPERTS_64x64 or smaller then
 template <int ELEM>
-inline hipError_t launch_adapters_up(int tile, bool w_across, const UpArgs &a, int64_t blocks, hipStream_t s)
+inline hipError_t launch_adapters_up(int tile, bool w_across, bool many, const UpArgs &a, int64_t blocks, hipStream_t s)
 {
-    return w_across ? launch_adapters_layout<ELEM, true>(tile, a, blocks, s) : launch_adapters_layout<ELEM, false>(tile, a, blocks, s);
+    return w_across ? launch_adapters_layout<ELEM, true>(tile, many, a, blocks, s) : launch_adapters_layout<ELEM, false>(tile, many, a, blocks, s);
 }
 
 }  // namespace amulet

@@ -77,11 +77,11 @@ static int64_t rows_blocks(int tile, int64_t M, int64_t N, int64_t G, bool group
 }
 
 // The tile with the lowest estimate of those whose workgroups one launch holds; -1: none
-static int rows_tile(int64_t M, int64_t N, int64_t K, int64_t G, int es, bool b_across, bool grouped, bool largest)
+static int rows_tile(int64_t M, int64_t N, int64_t K, int64_t G, int es, bool b_across, bool grouped, int first)
 {
     int best = -1;
     double least = 0.0;
-    for (int tile = EXPERTS_TILES - 1; tile >= (largest ? 0 : 1); --tile) {
+    for (int tile = EXPERTS_TILES - 1; tile >= first; --tile) {
         if (rows_blocks(tile, M, N, G, grouped) > kMostBlocks) continue;
         const double us = tile_us(tile, M, N, K, G < 1 ? 1 : G, es, b_across);
         if (best < 0 || us < least) { least = us; best = tile; }
@@ -127,9 +127,9 @@ static int64_t cut_blocks(ExpertsArgs &a, int64_t M, int64_t N, int64_t G, bool 
     return 2 * cuts > tried ? (blocks + 7) / 8 * 8 : 0;
 }
 
-RowsPlan rows_plan(int es, bool b_across, ExpertsArgs &a, int64_t M, int64_t N, int64_t G, bool largest)
+RowsPlan rows_plan(int es, bool b_across, ExpertsArgs &a, int64_t M, int64_t N, int64_t G, int first)
 {
-    RowsPlan p = {rows_tile(M, N, a.K, G, es, b_across, a.offsets != nullptr, largest), 0, 0};
+    RowsPlan p = {rows_tile(M, N, a.K, G, es, b_across, a.offsets != nullptr, first), 0, 0};
     if (p.tile < 0) return p;
     p.blocks = rows_blocks(p.tile, M, N, G, a.offsets != nullptr);
     p.behind = p.tile == EXPERTS_256x256 ? cut_blocks(a, M, N, G, a.offsets != nullptr, es) : 0;
@@ -141,7 +141,7 @@ static int run_rows(const char *const *names, int type, int trans_b, ExpertsArgs
     // 8-bit operands whose results keep 32 bits have no 256 x 256 tile, and that tile's offsets of A's rows have 32 bits
     const int es = type == EXPERTS_BF16 || type == EXPERTS_FP16 ? 2 : 1;
     const bool near = (a.rows ? (int64_t)a.a_rows : 256) <= 0xffffffffLL / es / (a.lda > 0 ? a.lda : 1);
-    const RowsPlan plan = rows_plan(es, !trans_b, a, M, N, G, type != EXPERTS_FP8_EXACT && near);
+    const RowsPlan plan = rows_plan(es, !trans_b, a, M, N, G, type != EXPERTS_FP8_EXACT && near ? EXPERTS_256x256 : EXPERTS_128x128);
     const int tile = plan.tile;
     if (tile < 0) return AMULET_ERR_RANGE;
     const int64_t blocks = plan.blocks, behind = plan.behind;

@@ -72,12 +72,12 @@ hipError_t launch_experts_rows_fp8(int tile, bool b_across, const ExpertsArgs &a
 // ... for results of 32 bits; no 256 x 256 tile
 hipError_t launch_experts_rows_fp8_exact(int tile, bool b_across, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
 // What a product by rows launches: `blocks` workgroups of `tile` (-1: no launch holds it), and `behind` of EXPERTS_128x128 where those take the last
-// columns (a.units and a.gap say which).  largest: the 256 x 256 tile may be taken.
+// columns (a.units and a.gap say which).  first: the largest tile that may be taken.
 struct RowsPlan {
     int tile;
     int64_t blocks, behind;
 };
-RowsPlan rows_plan(int es, bool b_across, ExpertsArgs &a, int64_t M, int64_t N, int64_t G, bool largest);
+RowsPlan rows_plan(int es, bool b_across, ExpertsArgs &a, int64_t M, int64_t N, int64_t G, int first);
 // by sums: tile EXPERTS_256x256, EXPERTS_128x128 or EXPERTS_64x64
 hipError_t launch_experts_sums(int type, int tile, const ExpertsArgs &a, int64_t blocks, hipStream_t s);
 // how its workgroups share the tiles of a group out over the XCDs, and how many there are of them
