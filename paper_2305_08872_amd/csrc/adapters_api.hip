@@ -17,7 +17,8 @@ static const int64_t kMostPitch = 0xffffffffLL / 256 - 65536;   // bytes, of the
 
 static bool known16(int type) { return type == AMULET_BF16 || type == AMULET_FP16; }
 
-static const char *const kUpNames[EXPERTS_TILES] = {"adapters_256x256", "adapters_128x128", "adapters_64x128", "adapters_64x64", "adapters_64x64_k2", "adapters_16x32"};
+static const char *const kUpNames[ADAPTERS_16x16 + 1] = {"adapters_256x256", "adapters_128x128", "adapters_64x128", "adapters_64x64", "adapters_64x64_k2", "adapters_16x32",
+                                                         "adapters_16x16"};
 
 // G matrices of rows x cols that are written: no two share an element, one behind the other or their rows in turn
 static bool matrices_apart(int64_t G, int64_t rows, int64_t cols, int64_t ld, int64_t group)
@@ -165,6 +166,8 @@ int amulet_adapters_mm(int type, int out_type, int trans_w, int trans_a, int tra
         plan = rows_plan(2, !trans_w, u.mm, M, N, 1, many ? EXPERTS_64x64 : EXPERTS_256x256);
         if (plan.tile < 0 && many) { many = false; plan = rows_plan(2, !trans_w, u.mm, M, N, 1, EXPERTS_256x256); }
         if (plan.tile < 0) return AMULET_ERR_RANGE;
+        // One row of tiles that would leave compute units without one: narrower tiles, whose eight k groups have more of W on its way
+        if (plan.tile == EXPERTS_16x32 && M <= 16 && (N + 31) / 32 < compute_units()) plan = {ADAPTERS_16x16, (N + 15) / 16 + 7 & ~(int64_t)7, 0};
     }
     hipStream_t s = (hipStream_t)stream;
     if (r > 0) {

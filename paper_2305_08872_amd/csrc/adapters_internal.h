@@ -36,6 +36,8 @@ struct UpArgs {
     int64_t ldt, ldb, group_b;
     int r, across;             // across: B's storage is r x N, else N x r
 };
+// tile: those of the products by groups, or this one: 16 x 16 with eight k groups
+enum { ADAPTERS_16x16 = EXPERTS_TILES };
 hipError_t launch_adapters_up_bf16(int tile, bool w_across, bool many, const UpArgs &a, int64_t blocks, hipStream_t s);
 hipError_t launch_adapters_up_fp16(int tile, bool w_across, bool many, const UpArgs &a, int64_t blocks, hipStream_t s);
 

@@ -203,6 +203,7 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
         steps = hi > lo ? (hi - lo + 31) / 32 : 0;
         return true;
     };
+    int base = 0, end = 0;   // the step's first row, the end of its segment
     auto next = [&](int &base) -> bool {
         while (s >= steps) {
             s -= steps;
@@ -210,27 +211,27 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
             if (!next_segment()) return false;
         }
         base = lo + s * 32;
+        end = hi;
         s += workers;
         return true;
     };
-    int base;
-    if constexpr (AHEAD) {
+    if constexpr (AHEAD) {   // (a step past the last one reads its rows again, and is not added: no branch around a read)
         Step x, y;
         bool have = next(base);
-        if (have) load(x, base, hi);
+        if (have) load(x, base, end);
         while (have) {
             const bool more = next(base);
-            if (more) load(y, base, hi);
+            load(y, base, end);
             add(x);
             if (!more) break;
             have = next(base);
-            if (have) load(x, base, hi);
+            load(x, base, end);
             add(y);
         }
     } else {
         Step x;
         while (next(base)) {
-            load(x, base, hi);
+            load(x, base, end);
             add(x);
         }
     }

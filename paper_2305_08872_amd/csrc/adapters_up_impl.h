@@ -1,13 +1,13 @@
 // R[i] = X[i] W + T[i] B[a(i)]: the products by rows of one shared matrix (experts_tile.h), to whose sums the adapters' are added.
 //
-// T is fp32 and stays so: it enters as two bf16 pieces where R has 16 bits (a rounding of 2^-15 to each value at most, under R's of 2^-8 or
+// T is fp32 and stays so: it enters the matrix instructions as two bf16 pieces where R has 16 bits (a rounding of 2^-15 to each value at most, under R's of 2^-8 or
 // 2^-11), as three, exactly, where it has 32; B of fp16 as two, exactly (fp16 products would be the shorter way, but T may lie
 // outside its range).  A workgroup lays the pieces of its rows out in LDS.  A block of 16 rows that a segment has in part takes an
 // instruction's sums over in the lanes whose row it is: nothing of another segment's operands is seen, not even an infinity times zero.
 //
-// Tiles whose k is shared by groups of waves (few rows: a decoding batch, many short segments) add the adapters while the first stages of X
-// and W are on their way: each wave takes B of eight segments at a time from memory straight into the matrix instruction.  The
-// others do it when their own sums are done and the stages' LDS is free: B of as many segments as it holds is laid out beside T.
+// That is for tiles of many rows, when their own sums are done and the stages' LDS is free: B of as many segments as it holds is laid out
+// beside T.  Tiles of few rows (whose k is shared by groups of waves) and batches of short segments take T and B from memory, row by
+// row, on the vector ALU, while the first stages of X and W are on their way.
 #ifndef AMULET_ADAPTERS_UP_IMPL_H
 #define AMULET_ADAPTERS_UP_IMPL_H
 
@@ -174,179 +174,187 @@ struct Meeting {
     __device__ __forceinline__ void next(const Segments &g, int first, int last, int lane) { chunk += 64; look(g, first, last, lane); }
 };
 
-// From memory: a batch of segments' B on its way while the one before is multiplied; the k groups take the segments in turn.  T and the first batch
-// are asked for before the first stages of X and W.  Neighbouring lanes read neighbouring bytes and hand them on by a
-// permutation (a matrix operand's lanes have columns of their own: a cache line for every 16 bytes).
+// From memory, row by row on the vector ALU: T's row times its adapter's B, in fp32.  Four lanes have 32 ranks of a column between them (so
+// that neighbouring lanes read neighbouring bytes; a matrix operand's lanes have columns of their own, a cache line for every 16 bytes),
+// and the sums go to a tile of LDS beside the ring, from where they join the others in the end.  The k groups take the rows
+// in turn; a batch of rows is on its way while the one before is multiplied, the first one is asked for before the first stages of X and W.
+// (A decoding batch has an adapter to a row, and a matrix instruction for each would have one row of 16: 192 rows by rank 32 beside 4096 x
+// 4096 took 33 us so.)
 template <class T>
-struct AddFromMemory : Adapters<T> {
-    static constexpr int ROOM = T::BM >= 64 ? (T::WK > 1 ? 32 : 8) * 1024 : 8 * 1024;   // for T, beside the ring
-    static constexpr int LDS = T::LDS + ROOM, SLOTS = ROOM / (T::BM * 16), OF_B = Adapters<T>::OF_B;
-    static constexpr int AT = 4 / OF_B, T_ITEMS = Adapters<T>::T_ITEMS;   // segments of a batch
-    static_assert(SLOTS >= 3, "one unit in three pieces");
-
+struct AddFromRows : Adapters<T> {
+    static constexpr int ROWS = T::MI * 16, LDS = T::LDS + T::BM * T::BN * 4;
+    static constexpr int AT = 2;   // rows of a batch
+    static_assert(ROWS <= 64, "a lane to a row");
+    enum { WHOLE, CUT, ACROSS };   // B along its rows, in whole units of 8 ranks or not; across
     struct Batch {
-        xt_u4 v[AT][T::NI];
-        int lo[AT], hi[AT], n;
+        xt_u4 b[AT][T::NI];
+        float t[AT][8];
+        int row[AT];   // of the wave's; -1: an empty place
     };
-    // what a lane reads of B: the reads units of which all segments have the same
-    struct Lane {
-        const char *first;      // B at the wave's first column and the read's first rank
-        uint32_t off[T::NI];
-        int unit, k, from;      // its unit of a read, the read's first rank; the lane whose read is its operand
-        bool reads, whole, full;   // it reads at all; no unit is cut; every lane has one
-    };
-    mutable float t0[T_ITEMS][8];
-    mutable Meeting first;
     mutable Batch batch;
-    int row1, pieces, units, most;
+    mutable uint64_t left;   // rows not yet taken
+    uint64_t mine;           // this group's
+    int adapter, kind;       // of row row0 + lane; -1: none
+    uint32_t off[T::NI];
+    const char *first;       // B at the wave's first column
 
-    __device__ __forceinline__ AddFromMemory(const Adapters<T> &x) : Adapters<T>(x)
+    __device__ __forceinline__ AddFromRows(const Adapters<T> &x) : Adapters<T>(x)
     {
         const UpArgs &a = this->a;
-        if (a.r == 0 || a.rows.S == 0) return;
-        pieces = a.mm.out == EXPERTS_FP32 ? 3 : 2;
-        units = (a.r + 7) / 8;
-        most = SLOTS / pieces;
-        row1 = this->row0 + T::MI * 16 < a.rows.M ? this->row0 + T::MI * 16 : a.rows.M;
-        this->read_t(t0, (int)threadIdx.x, 0, units < most ? units : most);
-        if (this->idle) return;
-        first.start(a.rows, this->row0, row1, this->lane);
-        met = 0;
-        fetch(lane_of(0, Ways(units < most ? units : most, pieces * OF_B), 0), first, batch);
-    }
-    mutable int met;
-
-    __device__ __forceinline__ void operator()(xt_f4 (&acc)[T::MI][T::NI]) const
-    {
-        const UpArgs &a = this->a;
-        if (a.r == 0 || a.rows.S == 0) return;
-        char *const lds = xt_smem + T::LDS;
-        for (int u0 = 0; u0 < units; u0 += most) {
-            const int n = units - u0 < most ? units - u0 : most;
-            if (u0 > 0) {
-                __syncthreads();
-                this->lay_out_t(lds, 0, u0, n, pieces);
-            } else {
-                this->write_t(lds, t0, (int)threadIdx.x, 0, n, pieces);
-                this->lay_out_t(lds, T_ITEMS, 0, n, pieces);
+        const int lane = this->lane, row0 = this->row0;
+        adapter = -1;
+        mine = 0;
+        if (a.r == 0 || a.rows.S == 0 || this->idle) return;
+        const int row1 = row0 + ROWS < a.rows.M ? row0 + ROWS : a.rows.M, row = row0 + lane;
+        Meeting m;
+        m.start(a.rows, row0, row1, lane);
+        for (;;) {
+            for (uint64_t some = m.which; some; some &= some - 1) {
+                const int at = __builtin_ctzll(some);
+                const int lo = __builtin_amdgcn_readlane(m.lo, at), hi = __builtin_amdgcn_readlane(m.hi, at), g = __builtin_amdgcn_readlane(m.adapter, at);
+                adapter = row >= lo && row < hi && row < row1 ? g : adapter;
             }
-            meet<T::NW * T::WK>();
-            if (this->idle) continue;
-            const Ways ways(n, pieces * OF_B);
-            for (int read = 0; read < ways.reads(); ++read) {
-                const Lane l = lane_of(u0, ways, read);
-                if (u0 > 0 || read > 0) {
-                    first.start(a.rows, this->row0, row1, this->lane);
-                    met = 0;
-                    fetch(l, first, batch);
-                }
-                while (batch.n > 0) {
-                    Batch next;
-                    next.n = 0;
-                    if (batch.n == AT) fetch(l, first, next);
-                    multiply(acc, lds, batch, l, ways, read);
-                    if (batch.n < AT || next.n == 0) break;
-                    batch.n = 0;
-                    if (next.n == AT) fetch(l, first, batch);
-                    multiply(acc, lds, next, l, ways, read);
-                }
-            }
+            if (!m.more) break;
+            m.next(a.rows, row0, row1, lane);
         }
-    }
-    __device__ __forceinline__ Lane lane_of(int u0, const Ways &ways, int read) const
-    {
-        const UpArgs &a = this->a;
-        const int lane = this->lane, b = lane >> 4, n = ways.of_read(read);
-        Lane l;
-        const int i = a.across ? lane & 15 : n == 4 ? lane >> 2 : n == 1 ? lane : n == 2 ? lane >> 1 : lane / 3;
-        l.unit = a.across ? b : lane - i * n;
-        l.k = (u0 + 4 * read) * 8;
-        l.reads = i < 16 && l.unit < n;
+        const uint64_t all = __ballot(adapter >= 0);
+        mine = T::WK == 1 ? all : __ballot(adapter >= 0 && __popcll(all & ((1ull << lane) - 1)) % T::WK == this->kg);
+        kind = a.across ? ACROSS : (a.r & 7) == 0 ? WHOLE : CUT;
         const uint32_t ld = (uint32_t)a.ldb * 2u;
         const int c0 = this->col0 < a.mm.N ? this->col0 : a.mm.N - 1;
-        l.first = (const char *)a.B + (a.across ? (int64_t)l.k * a.ldb + c0 : (int64_t)c0 * a.ldb + l.k) * 2;
+        first = (const char *)a.B + (a.across ? (int64_t)c0 : (int64_t)c0 * a.ldb) * 2;
 #pragma unroll
         for (int ni = 0; ni < T::NI; ++ni) {
-            int c = this->col0 + this->column(ni, i & 15);
+            int c = this->col0 + ni * 16 + (lane >> 2);
             c = (c < a.mm.N ? c : a.mm.N - 1) - c0;
-            l.off[ni] = a.across ? (uint32_t)c * 2u : (uint32_t)c * ld + (l.reads ? (uint32_t)l.unit * 16u : 0u);
+            off[ni] = a.across ? (uint32_t)c * 2u : (uint32_t)c * ld;
         }
-        l.whole = (a.r & 7) == 0;
-        l.full = l.whole && n == 4;
-        const int own = ways.packed ? (n == 1 ? 0 : b & 1) : b < n ? b : 0;
-        l.from = a.across ? (lane & 15) + 16 * own : (lane & 15) * n + own;
-        return l;
+        left = mine;
+        if (kind == WHOLE) fetch<WHOLE>(batch, 0);
     }
-    __device__ __forceinline__ xt_u4 load(const Lane &l, const char *base, int ni) const
+
+    // The next rows' operands, ranks k .. k + 31.  (As many reads whatever there is, and no branch around one: the wait for a batch then need
+    // not be one for the next.  An empty place reads the first row's and adapter's.)
+    template <int KIND>
+    __device__ __forceinline__ void fetch(Batch &x, int k) const
     {
+        typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
         typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
         const UpArgs &a = this->a;
-        if (!a.across) {
-            if (l.whole) return __builtin_bit_cast(xt_u4, *(const u4 *)(base + l.off[ni]));
-            xt_u4 v = {0, 0, 0, 0};
-            if (l.reads) v = load_unit<2>(base + (l.off[ni] - (uint32_t)l.unit * 16u) - l.k * 2, (l.k + l.unit * 8) * 2, a.r * 2);
-            return v;
-        }
+        const int at = k + 8 * (this->lane & 3);   // the lane's first rank
+        const bool in = at < a.r;
         const uint32_t ld = (uint32_t)a.ldb * 2u;
-        uint32_t x[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int at = l.unit * 8 + j;
-            x[j] = *(const uint16_t *)(base + l.off[ni] + (uint32_t)(l.k + at < a.r ? at : a.r - 1 - l.k) * ld);
+        for (int q = 0; q < AT; ++q) {
+            const bool there = left != 0;
+            const int row = there ? __builtin_ctzll(left) : 0;
+            left &= left - 1;
+            x.row[q] = there ? row : -1;
+            const int g = there ? __builtin_amdgcn_readlane(adapter, row) : 0;
+            const char *const base = first + (int64_t)g * a.group_b * 2;
+            const float *const t = a.T + (int64_t)(this->row0 + row) * a.ldt;
+            if constexpr (KIND == WHOLE) {
+                const f4 y = *(const f4 *)(t + (in ? at : 0)), z = *(const f4 *)(t + (in ? at : 0) + 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { x.t[q][j] = y[j]; x.t[q][4 + j] = z[j]; }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x.t[q][j] = t[at + j < a.r ? at + j : a.r - 1];
+            }
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ++ni) {
+                if constexpr (KIND == WHOLE) x.b[q][ni] = __builtin_bit_cast(xt_u4, *(const u4 *)(base + off[ni] + (in ? at * 2 : 0)));
+                else if constexpr (KIND == CUT) {
+                    x.b[q][ni] = xt_u4{0, 0, 0, 0};
+                    if (in) x.b[q][ni] = load_unit<2>(base + off[ni], at * 2, a.r * 2);
+                } else {
+                    uint32_t v[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int rank = at + j < a.r ? at + j : a.r - 1;
+                        v[j] = *(const uint16_t *)(base + (int64_t)rank * ld + off[ni]);
+                    }
+                    x.b[q][ni] = xt_u4{v[0] | (v[1] << 16), v[2] | (v[3] << 16), v[4] | (v[5] << 16), v[6] | (v[7] << 16)};
+                    __builtin_amdgcn_sched_barrier(0);   // (a batch's single values would not all have a register)
+                }
+            }
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = l.k + l.unit * 8 + j < a.r ? x[j] : 0u;
-        return xt_u4{x[0] | (x[1] << 16), x[2] | (x[3] << 16), x[4] | (x[5] << 16), x[6] | (x[7] << 16)};
     }
-    // the group's next segments' B
-    __device__ __forceinline__ void fetch(const Lane &l, Meeting &m, Batch &x) const
+    __device__ __forceinline__ float *place(int row, int c) const
+    {
+        return (float *)(xt_smem + T::LDS) + (this->row0 - this->tile_row + row) * T::BN + this->col0 - this->tile_col + c;
+    }
+    template <int KIND>
+    __device__ __forceinline__ void multiply(const Batch &x, int k) const
     {
         const UpArgs &a = this->a;
-        x.n = 0;
-        for_each<AT>([&](auto which) {
-            constexpr int q = decltype(which)::value;
-            if (x.n < q) return;
-            for (;;) {
-                while (m.which == 0 && m.more) m.next(a.rows, this->row0, row1, this->lane);
-                if (m.which == 0) return;
-                if (T::WK == 1 || met++ % T::WK == this->kg) break;
-                m.which &= m.which - 1;
-            }
-            const int at = __builtin_ctzll(m.which);
-            m.which &= m.which - 1;
-            x.n = q + 1;
-            x.lo[q] = __builtin_amdgcn_readlane(m.lo, at);
-            x.hi[q] = __builtin_amdgcn_readlane(m.hi, at);
-            const char *const base = l.first + (int64_t)__builtin_amdgcn_readlane(m.adapter, at) * a.group_b * 2;
+        const int lane = this->lane, n = a.r - k - 8 * (lane & 3);   // the lane's ranks
 #pragma unroll
-            for (int ni = 0; ni < T::NI; ++ni) x.v[q][ni] = load(l, base, ni);
-        });
+        for (int q = 0; q < AT; ++q) {
+            if (x.row[q] < 0) continue;
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ++ni) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float b = half_of<T::ELEM>(x.b[q][ni][j / 2], j % 2);
+                    if constexpr (KIND == WHOLE) sum = __builtin_fmaf(x.t[q][j], b, sum);
+                    else sum = j < n ? __builtin_fmaf(x.t[q][j], b, sum) : sum;
+                }
+                if constexpr (KIND == WHOLE) sum = n > 0 ? sum : 0.0f;
+                sum += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, sum), 0xb1, 0xf, 0xf, true));   // lanes 1 0 3 2
+                sum += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, sum), 0x4e, 0xf, 0xf, true));   // lanes 2 3 0 1
+                if ((lane & 3) == 0) {
+                    float *const to = place(x.row[q], ni * 16 + (lane >> 2));
+                    *to = k == 0 ? sum : *to + sum;
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);   // (one row's values after the other's)
+        }
     }
-    __device__ __forceinline__ void multiply(xt_f4 (&acc)[T::MI][T::NI], const char *lds, const Batch &x, const Lane &l, const Ways &ways, int read) const
+    template <int KIND>
+    __device__ __forceinline__ void rows() const
     {
-        const int lane = this->lane, b = lane >> 4, each = ways.each();
-        const char *const t_row = lds + (this->row0 - this->tile_row + (lane & 15)) * 16;
-        for_each<AT>([&](auto which) {
-            constexpr int q = decltype(which)::value;
-            if (q >= x.n) return;
-            xt_u4 vb[T::NI];
-#pragma unroll
-            for (int ni = 0; ni < T::NI; ++ni)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) vb[ni][j] = (uint32_t)__builtin_amdgcn_ds_bpermute(l.from * 4, (int)x.v[q][ni][j]);
-            for (int e = 0; e < each; ++e) {
-                int at, way;
-                const bool some = ways.at(read, e, b, at, way);
-                xt_u4 w[T::NI];
-#pragma unroll
-                for (int ni = 0; ni < T::NI; ++ni) w[ni] = this->piece_of_b(vb[ni], way % OF_B);
-                if (!l.full)
-#pragma unroll
-                    for (int ni = 0; ni < T::NI; ++ni) w[ni] = some ? w[ni] : xt_u4{0, 0, 0, 0};
-                const char *const t_at = t_row + (some ? at * pieces + way / OF_B : 0) * (T::BM * 16);
-                for_each<T::MI>([&](auto mi) { this->template add_block<decltype(mi)::value>(acc, t_at, some, x.lo[q], x.hi[q], w); });
+        for (int k = 0; k < this->a.r; k += 32) {
+            if (k > 0 || KIND != WHOLE) {
+                left = mine;
+                fetch<KIND>(batch, k);
             }
-        });
+            for (;;) {
+                Batch next;
+                if (left == 0) { multiply<KIND>(batch, k); break; }
+                fetch<KIND>(next, k);
+                multiply<KIND>(batch, k);
+                if (left == 0) { multiply<KIND>(next, k); break; }
+                fetch<KIND>(batch, k);
+                multiply<KIND>(next, k);
+            }
+        }
+    }
+    // beside the first stages
+    __device__ __forceinline__ void operator()(xt_f4 (&)[T::MI][T::NI]) const
+    {
+        if (mine == 0) return;
+        if (kind == WHOLE) rows<WHOLE>();
+        else if (kind == CUT) rows<CUT>();
+        else rows<ACROSS>();
+    }
+    // ... and the sums that they are (the k groups have met since)
+    __device__ __forceinline__ void finish(xt_f4 (&acc)[T::MI][T::NI]) const
+    {
+        if (this->a.r == 0 || this->a.rows.S == 0 || this->idle) return;
+        const int lane = this->lane;
+#pragma unroll
+        for (int mi = 0; mi < T::MI; ++mi) {
+            const int row = mi * 16 + (lane & 15);
+            const bool has = __shfl(adapter, row) >= 0;
+#pragma unroll
+            for (int ni = 0; ni < T::NI; ++ni) {
+                const xt_f4 x = *(const xt_f4 *)place(row, col_of<T>(ni, lane));
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[mi][ni][v] += has ? x[v] : 0.0f;
+            }
+        }
     }
 };
 
@@ -534,14 +542,14 @@ struct AddFromLds : Adapters<T> {
     }
 };
 
-template <class T, bool MEMORY>
-using AddAdapters = std::conditional_t<MEMORY, AddFromMemory<T>, AddFromLds<T>>;
+template <class T, bool ROWS>
+using AddAdapters = std::conditional_t<ROWS, AddFromRows<T>, AddFromLds<T>>;
 
-template <class T, bool MEMORY>
-__global__ void __launch_bounds__(T::NT) __attribute__((amdgpu_waves_per_eu(!MEMORY && T::BM * T::BN <= 64 * 64 ? 3 : 2))) adapters_up_kernel(const UpArgs u)
+template <class T, bool ROWS>
+__global__ void __launch_bounds__(T::NT) __attribute__((amdgpu_waves_per_eu(!ROWS && T::BM * T::BN <= 64 * 64 ? 3 : 2))) adapters_up_kernel(const UpArgs u)
 {
-    static_assert(!T::AKS && !T::FP8 && (MEMORY || T::WK == 1), "16-bit products by rows");
-    static_assert(AddAdapters<T, MEMORY>::LDS <= 160 * 1024 && (T::WK - 1) * T::NW * T::MI * T::NI * 1024 <= T::LDS, "LDS");
+    static_assert(!T::AKS && !T::FP8 && (ROWS || T::WK == 1), "16-bit products by rows");
+    static_assert(AddAdapters<T, ROWS>::LDS <= 160 * 1024 && (T::WK - 1) * T::NW * T::MI * T::NI * 1024 <= T::LDS, "LDS");
     const ExpertsArgs &a = u.mm;
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), kg = w / T::NW, wave = w % T::NW;
@@ -562,9 +570,10 @@ __global__ void __launch_bounds__(T::NT) __attribute__((amdgpu_waves_per_eu(!MEM
         else sb.start_kc((const char *)a.B, a.ldb * T::ES, col0, a.N, a.K, kg * T::BK, wave, lane, a_row, true);
     }
     const bool idle = wave_row >= a.M;
-    const AddAdapters<T, MEMORY> adapters(Adapters<T>{u, row0, col0, wave_row, wave_col, lane, kg, idle});
-    if constexpr (MEMORY) {
+    const AddAdapters<T, ROWS> adapters(Adapters<T>{u, row0, col0, wave_row, wave_col, lane, kg, idle});
+    if constexpr (ROWS) {
         if (!tile_sums<T>(sa, sb, 0, a.K, wave, kg, lane, a_row, TileScales(), idle, acc, adapters)) return;
+        adapters.finish(acc);
     } else {
         tile_sums<T>(sa, sb, 0, a.K, wave, kg, lane, a_row, TileScales(), idle, acc, typename AddFromLds<T>::Look{adapters});
         adapters(acc);
@@ -575,15 +584,15 @@ __global__ void __launch_bounds__(T::NT) __attribute__((amdgpu_waves_per_eu(!MEM
     });
 }
 
-template <class T, bool MEMORY>
+template <class T, bool ROWS>
 inline hipError_t launch_adapters_tile(const UpArgs &a, int64_t blocks, hipStream_t s)
 {
-    constexpr int lds = AddAdapters<T, MEMORY>::LDS;
+    constexpr int lds = AddAdapters<T, ROWS>::LDS;
     if (blocks <= 0) return hipSuccess;
     if (forced_launch_failure()) return hipErrorLaunchFailure;
-    static const hipError_t granted = hipFuncSetAttribute((const void *)adapters_up_kernel<T, MEMORY>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static const hipError_t granted = hipFuncSetAttribute((const void *)adapters_up_kernel<T, ROWS>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (granted != hipSuccess) { (void)hipGetLastError(); return granted; }
-    adapters_up_kernel<T, MEMORY><<<dim3((unsigned)blocks), dim3(T::NT), lds, s>>>(a);
+    adapters_up_kernel<T, ROWS><<<dim3((unsigned)blocks), dim3(T::NT), lds, s>>>(a);
     return hipGetLastError();
 }
 
@@ -599,7 +608,8 @@ inline hipError_t launch_adapters_layout(int tile, bool many, const UpArgs &a, i
         return many ? launch_adapters_tile<T, true>(a, blocks, s) : launch_adapters_tile<T, false>(a, blocks, s);
     }
     case EXPERTS_64x64_K2: return launch_adapters_tile<ExpertTile<ELEM, 64, 64, 2, 2, 2, 3, false, BKS>, true>(a, blocks, s);
-    default: return launch_adapters_tile<ExpertTile<ELEM, 16, 32, 1, 1, 4, 3, false, BKS>, true>(a, blocks, s);
+    case EXPERTS_16x32: return launch_adapters_tile<ExpertTile<ELEM, 16, 32, 1, 1, 4, 3, false, BKS>, true>(a, blocks, s);
+    default: return launch_adapters_tile<ExpertTile<ELEM, 16, 16, 1, 1, 8, 4, false, BKS>, true>(a, blocks, s);
     }
 }
 

@@ -121,7 +121,7 @@ def test_calls_tell_which_kernel_they_ran(lib):
     def rows(M, N, K, r=16, tw=1):
         # (the first launch makes T: refused, the second is not reached, so the name is asked of a call without ranks)
         return which(lib, lambda: mm(lib, tw=tw, M=M, N=N, K=K, r=0, ldx=K, ldw=max(N, K), ldr=N, T=None))
-    assert rows(16384, 4096, 4096) == ("adapters_256x256", 16384) and rows(256, 4096, 4096)[0] == "adapters_64x64_k2" and rows(8, 4096, 4096)[0] == "adapters_16x32"
+    assert rows(16384, 4096, 4096) == ("adapters_256x256", 16384) and rows(256, 4096, 4096)[0] == "adapters_64x64_k2" and rows(8, 4096, 4096)[0] == "adapters_16x16" and rows(40, 1024, 4096)[0] == "adapters_16x32"
     assert which(lib, lambda: mm(lib, N=0, R=None)) == ("adapters_down", 4)
     assert which(lib, lambda: wgrad(lib)) == ("adapters_wgrad", 4)
 

@@ -126,6 +126,8 @@ CASES = [
     ([700, 10, 324], None, 3, 1024, 1024, 32, 0), ([4100], None, 1, 4104, 200, 8, 0), ([2100, 1900, 96], [1, 0, 1], 2, 4096, 520, 64, 0),
     ([1500, 0, 2500, 300], None, 4, 4099, 131, 24, 50), ([1000, 2500], None, 2, 8200, 1030, 16, 600),
     ([200, 1, 55], [1, 0, 1], 2, 4096, 4096, 16, 0), ([700, 324], None, 2, 4096, 1024, 20, 0),
+    ([1] * 8, None, 8, 4096, 4096, 16, 0), ([3, 2, 0, 6], [1, -1, 0, 1], 2, 2000, 2500, 33, 1), ([1] * 14, [i % 3 for i in range(14)], 3, 1111, 4099, 72, 2),
+    ([1] * 600, [(i * 7) % 11 - 1 for i in range(600)], 9, 1024, 512, 24, 3), ([2] * 700, [(i * 5) % 4 for i in range(700)], 4, 2050, 1024, 64, 0),
 ]
 
 
@@ -154,7 +156,7 @@ def test_the_cases_above_run_every_kernel(am):
                               adapters=None if which is None else i32(which))
         seen.add(am.amulet_recent_kernel().split()[0])
         assert not R.any()
-    assert seen == {"adapters_" + t for t in ("256x256", "128x128", "64x128", "64x64", "64x64_k2", "16x32")}
+    assert seen == {"adapters_" + t for t in ("256x256", "128x128", "64x128", "64x64", "64x64_k2", "16x32", "16x16")}
 
 
 @pytest.mark.parametrize("trans", [(True, True, True), (False, False, False)])
