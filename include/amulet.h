@@ -787,7 +787,7 @@ int amulet_adapters_wgrad(int type, int out_type, int trans_r, int64_t M, int64_
 /*
  * ---- The gradients' norm ---------------------------------------------------------
  *
- * n tensors together: types[i] (amulet_type_t), counts[i] values (none is fine) one behind the other from grads[i] on, at any
+ * n tensors together: types[i] (amulet_type_t), counts[i] values (none is fine, fewer than 2^40) one behind the other from grads[i] on, at any
  * alignment of elements.  The arrays lie in host memory and are read before the call returns; the tensors and `norm` (one fp32
  * value) lie in device memory.
  *   amulet_grad_norm       norm = sqrt(sum of the squares of all values), summed in fp64 in an order that the sizes fix

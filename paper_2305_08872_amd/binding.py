@@ -1071,7 +1071,7 @@ def amulet_grad_clip(grads, max_norm: float, norm, *, outs=None, stream=None):
 
 
 def amulet_grad_norm_clip(grads, max_norm: float, norm, workspace, *, outs=None, stream=None):
-    """amulet_grad_norm and amulet_grad_clip in one call: two launches for up to 120 tensors."""
+    """amulet_grad_norm and amulet_grad_clip in one call: two launches for up to 180 tensors."""
     if _marshal is not None:
         rc = _marshal.grad_norm_clip(grads, max_norm, norm, workspace, outs, stream)
         if rc is not None:

@@ -58,18 +58,20 @@ constexpr int kOuterWaves = 4, kOuterAdapters = 1024;   // of a workgroup; the m
 hipError_t launch_adapters_join(const OuterArgs &a, hipStream_t s);
 
 // The norm of several tensors' values, and the values scaled down to a largest one.  A launch has as many tensors as its
-// arguments hold (4 KB), in chunks of kNormChunk values that its workgroups share.
-enum { NORM_TENSORS = 120, NORM_BLOCKS = 1024, NORM_JOINED = 8 };
+// arguments hold (4 KB: an address in 48 bits, a count in 40), in chunks of `chunk` values, kNormChunk or a few times as many, that its
+// workgroups share.
+enum { NORM_TENSORS = 180, NORM_BLOCKS = 2048, NORM_JOINED = 4 };
 constexpr int kNormChunk = 8192;
 struct NormTensors {
-    const void *in[NORM_TENSORS];
-    void *out[NORM_TENSORS];            // (clip only)
-    int64_t count[NORM_TENSORS];        // values
-    uint32_t first[NORM_TENSORS];       // chunks before the tensor's
-    uint8_t type[NORM_TENSORS];
-    uint32_t chunks;                    // of all of them
+    uint32_t in[NORM_TENSORS], out[NORM_TENSORS];             // (out: clip only)
+    uint32_t count[NORM_TENSORS];                             // values
+    uint32_t first[NORM_TENSORS];                             // chunks before the tensor's
+    uint16_t in_upper[NORM_TENSORS], out_upper[NORM_TENSORS];
+    uint16_t more[NORM_TENSORS];                              // upper bits of the count, from bit 8 on the type
+    uint32_t chunks, chunk;                                   // of all of them; values of one
     int n;
 };
+static_assert(sizeof(NormTensors) + 48 <= 4096, "a kernel's arguments");
 struct NormArgs {
     double *sums;                       // of squares, one for each workgroup
     int n;                              // sums of all launches

@@ -64,30 +64,69 @@ struct Values {
     }
 };
 
+// 4096 values, read by a workgroup at a time
+constexpr int kNormBatch = 4096;
+template <int TYPE>
+struct Batch {
+    typedef Values<TYPE> Vs;
+    static constexpr int AT = kNormBatch / kNormThreads / Vs::V, STEP = kNormThreads * Vs::V;
+    Vs v[AT];
+    __device__ __forceinline__ void read(const char *p, int n)   // batch n
+    {
+#pragma unroll
+        for (int q = 0; q < AT; ++q) v[q].read(p + (int64_t)(n * kNormBatch + (int)threadIdx.x * Vs::V + q * STEP) * Vs::ES);
+    }
+};
+// all(batch, its number) for the whole batches of n values, the next one on its way; some(first value) for 16 bytes of a thread, one(value) for what is left
+template <int TYPE, class All, class Some, class One>
+__device__ __forceinline__ void over_values(const char *p, int n, All all, Some some, One one)
+{
+    typedef Batch<TYPE> B;
+    const int batches = n / kNormBatch;
+    if (batches > 0) {
+        // (past the last one it is read again: no branch around a read)
+        B x, y;
+        x.read(p, 0);
+        for (int i = 0;; i += 2) {
+            y.read(p, i + 1 < batches ? i + 1 : batches - 1);
+            all(x, i);
+            if (i + 1 >= batches) break;
+            x.read(p, i + 2 < batches ? i + 2 : batches - 1);
+            all(y, i + 1);
+            if (i + 2 >= batches) break;
+        }
+    }
+    int at = batches * kNormBatch + (int)threadIdx.x * Values<TYPE>::V;
+    for (; at + Values<TYPE>::V <= n; at += B::STEP) some(at);
+    for (int i = at; i < n; ++i) one(i);
+}
+
 template <int TYPE>
 __device__ __forceinline__ double squares_of(const char *p, int n)
 {
     typedef Values<TYPE> Vs;
-    constexpr int V = Vs::V, AT = 4;
     double sum = 0.0;
-    int at = (int)threadIdx.x * V;
-    for (; at + (AT - 1) * kNormThreads * V + V <= n; at += AT * kNormThreads * V) {
-        Vs v[AT];
+    auto add = [&](const Vs &v) {
 #pragma unroll
-        for (int q = 0; q < AT; ++q) v[q].read(p + (int64_t)(at + q * kNormThreads * V) * Vs::ES);
-#pragma unroll
-        for (int q = 0; q < AT; ++q)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const double x = v[q].value(i);
-                sum = __builtin_fma(x, x, sum);
-            }
-    }
-    for (; at < n; at += kNormThreads * V)
-        for (int i = 0; i < V && at + i < n; ++i) {
-            const double x = Vs::read_one(p + (int64_t)(at + i) * Vs::ES);
+        for (int i = 0; i < Vs::V; ++i) {
+            const double x = v.value(i);
             sum = __builtin_fma(x, x, sum);
         }
+    };
+    over_values<TYPE>(p, n,
+        [&](const Batch<TYPE> &b, int) {
+#pragma unroll
+            for (int q = 0; q < Batch<TYPE>::AT; ++q) add(b.v[q]);
+        },
+        [&](int at) {
+            Vs v;
+            v.read(p + (int64_t)at * Vs::ES);
+            add(v);
+        },
+        [&](int i) {
+            const double x = Vs::read_one(p + (int64_t)i * Vs::ES);
+            sum = __builtin_fma(x, x, sum);
+        });
     return sum;
 }
 
@@ -106,28 +145,38 @@ __device__ __forceinline__ double sum_of_block(double x)
     return sum;
 }
 
-// f(tensor, its first value, how many) for the chunks of this workgroup
-template <class F>
-__device__ __forceinline__ void chunks_of_block(const NormTensors &t, F f)
+// Chunk c: its tensor's type, addresses of its values, how many they are.  BACK: each tensor's chunks from the last one on.
+struct Chunk {
+    const char *in;
+    char *out;
+    int n, type;
+};
+template <bool BACK>
+__device__ __forceinline__ Chunk chunk_of(const NormTensors &t, uint32_t c)
 {
-    for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-        const int x = __builtin_amdgcn_readfirstlane(tensor_of(t, c, threadIdx.x & 63));
-        const int64_t from = (int64_t)(c - t.first[x]) * kNormChunk, left = t.count[x] - from;
-        f(x, from, (int)(left < kNormChunk ? left : kNormChunk));
-    }
+    const int x = __builtin_amdgcn_readfirstlane(tensor_of(t, c, threadIdx.x & 63));
+    const int64_t count = ((int64_t)(t.more[x] & 255) << 32) | t.count[x], chunks = (count + t.chunk - 1) / t.chunk;
+    const int64_t at = c - t.first[x], from = (BACK ? chunks - 1 - at : at) * (int64_t)t.chunk, left = count - from;
+    Chunk y;
+    y.type = t.more[x] >> 8;
+    const int64_t bytes = from * (y.type == EXPERTS_FP32 ? 4 : 2);
+    y.in = (const char *)(((uint64_t)t.in_upper[x] << 32) | t.in[x]) + bytes;
+    y.out = (char *)(((uint64_t)t.out_upper[x] << 32) | t.out[x]) + bytes;
+    y.n = (int)(left < (int64_t)t.chunk ? left : (int64_t)t.chunk);
+    return y;
 }
 
 __global__ void __launch_bounds__(kNormThreads) norm_sums_kernel(const NormTensors t, double *sums)
 {
     double sum = 0.0;
-    chunks_of_block(t, [&](int x, int64_t from, int n) {
-        const char *const p = (const char *)t.in[x];
-        switch (t.type[x]) {
-        case EXPERTS_FP32: sum += squares_of<EXPERTS_FP32>(p + from * 4, n); break;
-        case EXPERTS_BF16: sum += squares_of<EXPERTS_BF16>(p + from * 2, n); break;
-        default: sum += squares_of<EXPERTS_FP16>(p + from * 2, n);
+    for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+        const Chunk x = chunk_of<false>(t, c);
+        switch (x.type) {
+        case EXPERTS_FP32: sum += squares_of<EXPERTS_FP32>(x.in, x.n); break;
+        case EXPERTS_BF16: sum += squares_of<EXPERTS_BF16>(x.in, x.n); break;
+        default: sum += squares_of<EXPERTS_FP16>(x.in, x.n);
         }
-    });
+    }
     sum = sum_of_block(sum);
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
 }
@@ -145,28 +194,30 @@ __global__ void __launch_bounds__(kNormThreads) norm_join_kernel(const NormArgs 
 }
 
 template <int TYPE>
-__device__ __forceinline__ void clip_values(const char *p, char *to, int n, float f)
+__device__ __forceinline__ void clip_values(const Chunk &c, float f)
 {
     typedef Values<TYPE> Vs;
-    constexpr int V = Vs::V, AT = 4;
-    int at = (int)threadIdx.x * V;
-    for (; at + (AT - 1) * kNormThreads * V + V <= n; at += AT * kNormThreads * V) {
-        Vs v[AT];
+    over_values<TYPE>(c.in, c.n,
+        [&](Batch<TYPE> &b, int n) {
 #pragma unroll
-        for (int q = 0; q < AT; ++q) v[q].read(p + (int64_t)(at + q * kNormThreads * V) * Vs::ES);
-#pragma unroll
-        for (int q = 0; q < AT; ++q) {
-            if (f != 1.0f) v[q].scale(f);
-            v[q].write(to + (int64_t)(at + q * kNormThreads * V) * Vs::ES);
-        }
-    }
-    for (; at < n; at += kNormThreads * V)
-        for (int i = 0; i < V && at + i < n; ++i) {
-            const float x = Vs::read_one(p + (int64_t)(at + i) * Vs::ES);
-            Vs::write_one(to + (int64_t)(at + i) * Vs::ES, f != 1.0f ? x * f : x);
-        }
+            for (int q = 0; q < Batch<TYPE>::AT; ++q) {
+                if (f != 1.0f) b.v[q].scale(f);
+                b.v[q].write(c.out + (int64_t)(n * kNormBatch + (int)threadIdx.x * Vs::V + q * Batch<TYPE>::STEP) * Vs::ES);
+            }
+        },
+        [&](int at) {
+            Vs v;
+            v.read(c.in + (int64_t)at * Vs::ES);
+            if (f != 1.0f) v.scale(f);
+            v.write(c.out + (int64_t)at * Vs::ES);
+        },
+        [&](int i) {
+            const float x = Vs::read_one(c.in + (int64_t)i * Vs::ES);
+            Vs::write_one(c.out + (int64_t)i * Vs::ES, f != 1.0f ? x * f : x);
+        });
 }
 
+// The chunks in the order opposite to the sums': what those read last is still in the caches.
 __global__ void __launch_bounds__(kNormThreads) norm_clip_kernel(const NormTensors t, const NormArgs a)
 {
     float norm;
@@ -178,16 +229,15 @@ __global__ void __launch_bounds__(kNormThreads) norm_clip_kernel(const NormTenso
     // (a norm that is no number or infinite changes nothing)
     const bool clipped = norm > a.most && norm < __builtin_inff();
     const float f = clipped ? a.most / norm : 1.0f;
-    chunks_of_block(t, [&](int x, int64_t from, int n) {
-        const char *const p = (const char *)t.in[x];
-        char *const to = (char *)t.out[x];
-        if (p == to && !clipped) return;
-        switch (t.type[x]) {
-        case EXPERTS_FP32: clip_values<EXPERTS_FP32>(p + from * 4, to + from * 4, n, f); break;
-        case EXPERTS_BF16: clip_values<EXPERTS_BF16>(p + from * 2, to + from * 2, n, f); break;
-        default: clip_values<EXPERTS_FP16>(p + from * 2, to + from * 2, n, f);
+    for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+        const Chunk x = chunk_of<true>(t, c);
+        if (x.in == x.out && !clipped) continue;
+        switch (x.type) {
+        case EXPERTS_FP32: clip_values<EXPERTS_FP32>(x, f); break;
+        case EXPERTS_BF16: clip_values<EXPERTS_BF16>(x, f); break;
+        default: clip_values<EXPERTS_FP16>(x, f);
         }
-    });
+    }
 }
 
 hipError_t launch_norm_sums(const NormTensors &t, double *sums, int blocks, hipStream_t s)

@@ -58,8 +58,8 @@ def check_clipped(outs, grads, want, most):
         assert ((o.double() - exact).abs() <= limit).all()
 
 
-COUNTS = [[1], [5, 0, 3], [8192], [8191, 8193, 1], [1 << 20, 17, 4096], [100003, 9, 8192 * 3], [64] * 120, [1000 + i for i in range(121)],
-          [3 * i for i in range(300)]]
+COUNTS = [[1], [5, 0, 3], [8192], [8191, 8193, 1], [1 << 20, 17, 4096], [100003, 9, 8192 * 3], [64] * 180, [1000 + i for i in range(181)],
+          [3 * i for i in range(400)]]
 
 
 @pytest.mark.parametrize("shift", [0, 1, 8])
