@@ -49,7 +49,7 @@ struct Values {
             else w[i] = pair(value(2 * i) * f, value(2 * i + 1) * f);
         }
     }
-    __device__ __forceinline__ void write(char *p) const { *(u4 *)p = w; }
+    __device__ __forceinline__ void write(char *p) const { __builtin_nontemporal_store(w, (u4 *)p); }
     // single values
     __device__ __forceinline__ static float read_one(const char *p)
     {
