@@ -316,10 +316,13 @@ __global__ void __launch_bounds__(256) adapters_join_kernel(const OuterArgs a)
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, k = at / fours;
     const int c = (int)(at - k * fours) * 4, g = (int)(k / a.r), rank = (int)(k - (int64_t)g * a.r);
     if (g >= a.rows.G) return;
-    const int parts = pieces_of(counts[g], a.quota);
+    int parts = pieces_of(counts[g], a.quota);
     if (parts == 1) return;
     int first = 0;
     for (int x = 0; x < g; ++x) first += pieces_of(counts[x], a.quota);
+    // (offsets that do not ascend may count rows twice: no more than the workspace has)
+    first = first < a.pieces ? first : a.pieces;
+    parts = first + parts <= a.pieces ? parts : a.pieces - first;
     typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
     // (the last columns of a row: its last four, of which the thread's are stored)
     const int in = c + 4 <= a.N || a.N < 4 ? c : a.N - 4;

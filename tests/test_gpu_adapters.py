@@ -319,6 +319,23 @@ def test_offsets_outside_and_not_ascending_touch_nothing_else(am):
             within(R, wantR, dR, "R")
 
 
+def test_rows_counted_twice_stay_inside_the_workspace(am):
+    """Offsets that do not ascend name rows for several adapters: more pieces than there can be room for.  What lies behind the workspace is not read."""
+    M, N, r, G = 6000, 256, 16, 8
+    X, T = normal(gen(3), M, N, dtype=BF16), normal(gen(4), M, r)
+    need = am.amulet_adapters_wgrad_workspace_bytes(M, N, r, G)
+    assert need > 0
+    whole = torch.full((need + (1 << 20),), 255, dtype=torch.uint8, device="cuda")      # (NaN as fp32)
+    (R, ok) = room(G, N, r, dtype=F32, pad=3, shift=4)
+    am.amulet_adapters_wgrad(X, T, i32([0, M, 0, M, 0, M, 0, M, 0]), R, whole[:need])
+    ok()
+    assert (whole[need:] == 255).all()
+    am.amulet_adapters_wgrad(X, T, i32([0, 0, 1000, 5000, 5000, 5000, 5500, 5600, M]), R, whole[:need])
+    want, slack = outer(X, T, [0, 0, 1000, 5000, 5000, 5000, 5500, 5600, M], list(range(G)), G, F32)
+    within(R, want, slack, "R")
+    ok()
+
+
 # ---- the matrices' gradients
 
 def outer(X, T, at, which, G, out):

@@ -1,0 +1,111 @@
+"""The example's projection with adapters, whose forward and backward passes run the operators together, against autograd in 64 bits; the
+compiled marshalling of the calls against the Python one."""
+import os
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+
+
+@pytest.fixture(scope="module")
+def ex():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import adapters
+    return adapters
+
+
+def near(a, b, rel):
+    return float((a.double() - b).norm()) <= rel * float(b.norm())
+
+
+@pytest.mark.parametrize("lengths,which,width,outputs,rank,tasks", [([1] * 6, [0, 2, -1, 1, 0, 2], 64, 96, 8, 3), ([30, 7, 0, 40], [1, -1, 0, 1], 72, 40, 5, 2),
+                                                                    ([300, 200, 700], [2, 0, 2], 136, 264, 16, 4)])
+def test_projection_against_64_bits(ex, lengths, which, width, outputs, rank, tasks):
+    print("projection", lengths, width, outputs, rank, flush=True)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(width)
+    normal = lambda *s, scale=1.0: torch.empty(s, device="cuda").normal_(0, scale, generator=g).bfloat16()   # noqa: E731
+    x, w = normal(sum(lengths), width).requires_grad_(), normal(outputs, width, scale=width ** -0.5)
+    a, b = normal(tasks, rank, width, scale=width ** -0.5).requires_grad_(), normal(tasks, outputs, rank).requires_grad_()
+    scales = torch.linspace(0.5, 2.0, tasks, device="cuda")
+    dy = normal(sum(lengths), outputs)
+    y = ex.Apply.apply(x, w, a, b, scales, ex.Rows(lengths, which))
+    dx, da, db = torch.autograd.grad(y, (x, a, b), dy)
+
+    x64, a64, b64 = (v.detach().double().requires_grad_() for v in (x, a, b))
+    out = []
+    for p, i in zip(x64.split(lengths), which):
+        out.append(p @ w.double().t())
+        if i >= 0:
+            out[-1] = out[-1] + float(scales[i]) * (p @ a64[i].t()) @ b64[i].t()
+    want = torch.cat(out)
+    wx, wa, wb = torch.autograd.grad(want, (x64, a64, b64), dy.double())
+    # one rounding to bf16 of each (2^-8 at most); sums in fp32 and T's pieces (2^-15) lie far below
+    rel = 2.0 ** -8
+    assert near(y, want.detach(), rel) and near(dx, wx, rel) and near(da, wa, rel) and near(db, wb, rel)
+    unused = [i for i in range(tasks) if not any(j == i and n for n, j in zip(lengths, which))]
+    for i in unused:
+        assert not da[i].any() and not db[i].any()
+
+    grads = [da.clone(), db.clone()]
+    total = float(torch.sqrt(sum((v.double() ** 2).sum() for v in grads)))
+    norm = ex.clip(grads, 0.25 * total)
+    assert abs(float(norm) - total) <= 2.0 ** -23 * total
+    assert near(grads[0], da.double() * 0.25, rel) and near(grads[1], db.double() * 0.25, rel)
+
+
+def test_example_runs(ex):
+    losses, y = ex.main(rows=300, width=128, outputs=96, rank=8, tasks=3, steps=3)
+    assert len(losses) == 3 and all(v == v for v in losses) and torch.isfinite(y).all()
+
+
+def test_compiled_marshalling_makes_the_same_calls(ex, monkeypatch):
+    from paper_2305_08872_amd import binding
+    if binding._marshal is None:
+        pytest.skip("the compiled module was not built")
+    am = ex.am
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")   # noqa: E731
+    x, w, a, b = torch.randn(50, 96, **bf), torch.randn(96, 200, **bf), torch.randn(3, 96, 12, **bf), torch.randn(3, 12, 200, **bf)
+    off, which, scales = i32([0, 10, 30, 50]), i32([2, -1, 0]), torch.rand(3, device="cuda")
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    out = lambda: dict(t=torch.empty(50, 12, device="cuda"), r=torch.empty(50, 200, **bf), t2=torch.empty(50, 12, device="cuda"), r2=torch.empty(50, 200, device="cuda"),   # noqa: E731
+                       d=torch.empty(3, 200, 12, device="cuda"), d2=torch.empty(3, 12, 200, **bf), n=torch.empty(1, device="cuda"), n2=torch.empty(1, device="cuda"))
+
+    def calls(o):
+        am.amulet_adapters_mm(x, w, a, b, off, o["t"], o["r"], adapters=which, scales=scales)
+        am.amulet_adapters_mm(x, None, a, b, off, o["t2"], o["r2"], stream=torch.cuda.current_stream())
+        am.amulet_adapters_wgrad(o["r"], o["t"], off, o["d"], ws, adapters=which)
+        am.amulet_adapters_wgrad(o["r"], o["t"], off, o["d2"], trans_r=True)
+        am.amulet_grad_norm([o["d"], o["d2"]], o["n"], ws)
+        am.amulet_grad_norm_clip([o["d"], o["d2"]], 3, o["n2"], ws)
+        am.amulet_grad_clip([o["d"], o["d2"]], 0.5, o["n2"])
+
+    compiled, plain = out(), out()
+    assert all(hasattr(binding._marshal, n) for n in ("adapters_mm", "adapters_wgrad", "grad_norm", "grad_norm_clip", "grad_clip"))
+    # (arguments that it takes: it answers)
+    assert binding._marshal.adapters_wgrad(x, compiled["t"].fill_(1.0), off, torch.empty(3, 96, 12, device="cuda"), None, None, False, None) == 0
+    assert binding._marshal.grad_norm([x, w], compiled["n"], ws, None) == 0
+    calls(compiled)
+    monkeypatch.setattr(binding, "_marshal", None)
+    calls(plain)
+    torch.cuda.synchronize()
+    for k in compiled:
+        assert torch.equal(compiled[k], plain[k]), k
+    with pytest.raises(ValueError):
+        am.amulet_adapters_mm(x, w, a, b[:2], off, plain["t"], plain["r"])
+    with pytest.raises(ValueError):
+        am.amulet_adapters_mm(x, w, a, b, off[:3], plain["t"], plain["r"])
+    with pytest.raises(ValueError):
+        am.amulet_adapters_mm(x, w, a.half(), b, off, plain["t"], plain["r"])
+    with pytest.raises(ValueError):
+        am.amulet_adapters_wgrad(x, plain["t"], off, plain["d"])
+    with pytest.raises(ValueError):
+        am.amulet_adapters_mm(x, w.t(), a, b, off, plain["t"], plain["r"])
+    with pytest.raises(ValueError):
+        am.amulet_grad_norm([x.cpu()], plain["n"], ws)
