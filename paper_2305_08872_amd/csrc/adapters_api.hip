@@ -41,8 +41,12 @@ static OuterPlan outer_plan(int64_t M, int64_t N, int64_t r, int64_t G, size_t b
     const int64_t units = compute_units(), ranks = r <= 16 ? 1 : (r + 31) / 32, wide = (N + 127) / 128 * ranks;
     OuterPlan p = {wide * G >= units || M >= 512 * 2 * G ? 128 : 64, 0, G};
     const int64_t blocks = (N + p.columns - 1) / p.columns * ranks;
+    // Pieces: as many as two workgroups to a compute unit make, or twice that, of which each adapter may leave one that is not full; with as many
+    // adapters, no more than keep one that has most rows from being the last.  us, of 16384 rows, 4096 columns, 4 adapters: rank 16, quota 512 / 1024 /
+    // 1366 42 / 39 / 36, rank 64 80 / 72 / 66.
     const int64_t fill = 2 * units / blocks, least = 512;
-    int64_t quota = fill > 0 ? (M + fill - 1) / fill : M;
+    const int64_t full = G >= fill ? fill : (3 * G <= fill ? fill : 2 * fill) - G;
+    int64_t quota = full > 0 ? (M + full - 1) / full : M;
     if (quota < least) quota = least;
     if (quota <= 0 || G > kOuterAdapters || M < 2 * quota) return p;
     const int64_t pieces = M / quota + G;

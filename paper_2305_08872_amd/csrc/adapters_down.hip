@@ -70,6 +70,7 @@ __global__ void __launch_bounds__(T::NT) adapters_down_kernel(const DownArgs a)
         else sb.start_kc(A, a.lda * 2, r0, a.r, K, kg * T::BK, wave, lane, same, true);
     }
     if (!tile_sums<T>(sa, sb, 0, K, wave, kg, lane, same, TileScales(), false, acc)) return;
+    sums_done();
     const float scale = g >= 0 && a.scales ? a.scales[g] : 1.0f;
 #pragma unroll
     for (int mi = 0; mi < T::MI; ++mi)
@@ -94,18 +95,22 @@ template <int ELEM, bool KS>
 static hipError_t launch_down(const DownArgs &a, hipStream_t s)
 {
     // Rows to a workgroup: a block where segments are shorter; 32, or 64 where those would be more than one to a compute unit (an adapter's matrix is
-    // read once for as many).  us, 32 / 64 rows, rank 64, out of the caches: 8192 x 4096 of one segment 21 / 25, of 24 segments 39 / 26, 16384
-    // x 4096 34 / 33, 2048 x 4096 13 / 15.
+    // read once for as many).  us, 32 / 64 rows, rank 64, out of the caches: 8192 x 4096 of one segment 21 / 25, of 24 segments 39 / 26, 2048 x
+    // 4096 13 / 15.  Blocks too, four workgroups to a compute unit, where up to 32 ranks have more than a round of 64 rows, whose last ones would
+    // be alone: 16384 x 4096 rank 16 31 / 42 us, 65536 x 4096 99 / 116, 16384 x 4096 rank 32 38 / 43.
     const int64_t M = a.rows.M, S = a.rows.S, ranks = a.r <= 16 ? 16 : a.r <= 32 ? 32 : 64;
-    const int rows = M < 16 * S ? 16 : (M / 32 + S) * ((a.r + ranks - 1) / ranks) <= compute_units() ? 32 : 64;
+    const bool rounds = M / 64 + S > compute_units();
+    const int rows = M < 16 * S ? 16 : (M / 32 + S) * ((a.r + ranks - 1) / ranks) <= compute_units() ? 32 : rounds && a.r <= 32 ? 16 : 64;
     if (a.r <= 16)
-        return rows == 16 ? launch_tile<ExpertTile<ELEM, 16, 16, 1, 1, 8, 4, false, KS>>(a, s)
+        return rows == 16 && rounds ? launch_tile<ExpertTile<ELEM, 16, 16, 1, 1, 4, 3, false, KS>>(a, s)
+               : rows == 16 ? launch_tile<ExpertTile<ELEM, 16, 16, 1, 1, 8, 4, false, KS>>(a, s)
                : rows == 32 ? launch_tile<ExpertTile<ELEM, 32, 16, 1, 1, 8, 3, false, KS>>(a, s) : launch_tile<ExpertTile<ELEM, 64, 16, 1, 1, 4, 3, false, KS>>(a, s);
     if (a.r <= 32)
-        return rows == 16 ? launch_tile<ExpertTile<ELEM, 16, 32, 1, 1, 8, 3, false, KS>>(a, s)
+        return rows == 16 && rounds ? launch_tile<ExpertTile<ELEM, 16, 32, 1, 1, 4, 3, false, KS>>(a, s)
+               : rows == 16 ? launch_tile<ExpertTile<ELEM, 16, 32, 1, 1, 8, 3, false, KS>>(a, s)
                : rows == 32 ? launch_tile<ExpertTile<ELEM, 32, 32, 1, 1, 4, 4, false, KS>>(a, s) : launch_tile<ExpertTile<ELEM, 64, 32, 1, 1, 4, 3, false, KS>>(a, s);
     return rows == 16 ? launch_tile<ExpertTile<ELEM, 16, 64, 1, 1, 4, 3, false, KS>>(a, s)
-           : rows == 32 ? launch_tile<ExpertTile<ELEM, 32, 64, 1, 1, 4, 3, false, KS>>(a, s) : launch_tile<ExpertTile<ELEM, 64, 64, 2, 2, 2, 4, false, KS>>(a, s);
+           : rows == 32 ? launch_tile<ExpertTile<ELEM, 32, 64, 1, 1, 4, 3, false, KS>>(a, s) : launch_tile<ExpertTile<ELEM, 64, 64, 2, 2, 1, 5, false, KS>>(a, s);
 }
 
 hipError_t launch_adapters_down(int type, const DownArgs &a, hipStream_t s)
