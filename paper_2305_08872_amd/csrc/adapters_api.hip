@@ -227,13 +227,15 @@ int amulet_adapters_wgrad(int type, int out_type, int trans_r, int64_t M, int64_
     if (!R || (S > 0 && M > 0 && (!offsets || !X || !T))) return AMULET_ERR_NULL;
     if (ldr < (trans_r ? N : r) || !matrices_apart(G, trans_r ? r : N, trans_r ? N : r, ldr, group_r)) return AMULET_ERR_LD;
     if (S > 0 && M > 0 && (ldx < N || ldt < r)) return AMULET_ERR_LD;
+    if (S > 0 && M > 0 && (ldx > kMostPitch / 2 || ldt > kMostPitch / 4)) return AMULET_ERR_RANGE;
     if (((uintptr_t)workspace & 15) != 0) return AMULET_ERR_WORKSPACE;
     OuterArgs a = {};
     a.rows.offsets = offsets; a.rows.adapters = adapters;
     a.rows.S = M > 0 ? (int)S : 0; a.rows.G = (int)G; a.rows.M = (int)M;
     a.X = X; a.ldx = ldx; a.T = T; a.ldt = ldt; a.R = R; a.ldr = ldr; a.group_r = group_r; a.workspace = (float *)workspace;
     a.N = (int)N; a.r = (int)r; a.out = out_type; a.trans_r = trans_r != 0;
-    if ((N + 63) / 64 * ((r + 15) / 16) > kMostBlocks256 / (G + M / 512) || G * r > kMostBlocks256 * 256 / ((N + 3) / 4)) return AMULET_ERR_RANGE;
+    if ((N + 63) / 64 > (kMostBlocks256 / ((r + 15) / 16) - 8) / (G + M / 512) || G * (trans_r ? r * ((N + 3) / 4) : N * ((r + 3) / 4)) > kMostBlocks256 * 256)
+        return AMULET_ERR_RANGE;
     const OuterPlan p = outer_plan(M, N, r, G, workspace ? workspace_bytes : 0);
     a.columns = p.columns;
     a.quota = p.quota;

@@ -54,11 +54,16 @@ template <int ELEM, int F, int RI, int PIECES>
 __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_per_eu(2))) adapters_outer_kernel(const OuterArgs a)
 {
     constexpr int COLS = 16 * F, OF_X = ELEM == EXPERTS_FP16 ? 2 : 1;
-    constexpr bool AHEAD = RI == 1;   // the next step's operands on their way (with more ranks fewer workgroups would fit a compute unit)
+    // the next step's operands on their way, where there are registers for them
+    constexpr bool AHEAD = RI == 1 || F < 8 || PIECES < 3;
     __shared__ int counts[kOuterAdapters];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int i = lane & 15, b = lane >> 4;
-    const unsigned blocks = (unsigned)((a.N + COLS - 1) / COLS), piece = blockIdx.x / blocks;
+    // (The blocks of ranks of the same rows and columns lie behind one another on the same XCD, workgroups 8 apart: its cache has X then.  Rank 64, 16384
+    // rows of 4096 columns: 44 / 51 us, half as many reads of memory.)
+    const unsigned blocks = (unsigned)((a.N + COLS - 1) / COLS), ranks = (unsigned)((a.r + 16 * RI - 1) / (16 * RI));
+    const unsigned turn = blockIdx.x >> 3, at = turn / ranks * 8 + (blockIdx.x & 7), piece = at / blocks;
+    if (piece >= (unsigned)a.pieces) return;
     Piece p = {(int)piece, 0, 1};
     if (a.quota > 0) {
         count_rows(a.rows, counts);
@@ -66,7 +71,7 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
     }
     const int g = p.adapter;
     // the lane's columns c0 + f, its ranks r0 + n (of T; what it ends with: ranks of line 4 b + v)
-    const int c0 = (int)(blockIdx.x - piece * blocks) * COLS + F * i, r_block = (int)blockIdx.y * 16 * RI, r0 = r_block + RI * i;
+    const int c0 = (int)(at - piece * blocks) * COLS + F * i, r_block = (int)(turn % ranks) * 16 * RI, r0 = r_block + RI * i;
     // they end at X's last one
     const int col = c0 + F <= a.N || a.N < F ? c0 : a.N - F;
     const int workers = kOuterWaves * p.parts, me = p.part * kOuterWaves + wave;
@@ -91,28 +96,31 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
 #pragma unroll
     for (int n = 0; n < RI; ++n) r_in[n] = r0 + n < a.r ? r0 + n : a.r - 1;
     const int r_even = r0 + RI <= a.r ? r0 : a.r - RI;
+    // (The step's first row is an address of the wave's; rows lie less than 2^32 bytes behind it, the last one that is there at most.)
+    const uint32_t x_pitch = (uint32_t)a.ldx * 2, t_pitch = (uint32_t)a.ldt * 4, x_lane = 8 * (uint32_t)b * x_pitch, t_lane = 8 * (uint32_t)b * t_pitch;
     auto load = [&](Step &s, int base, int end) {
         typedef uint32_t xs __attribute__((ext_vector_type(F / 2), aligned(2)));
         typedef float ts __attribute__((ext_vector_type(RI), aligned(4)));
-        const char *x[8];
-        const float *t[8];
+        const char *const X = (const char *)a.X + (int64_t)base * x_pitch, *const T = (const char *)a.T + (int64_t)base * t_pitch;
+        const uint32_t last = (uint32_t)(end - base < 32 ? end - base - 1 : 31), x_last = last * x_pitch, t_last = last * t_pitch;
+        uint32_t x[8], t[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int row = base + 8 * b + j, in = row < end ? row : end - 1;
-            x[j] = (const char *)a.X + (int64_t)in * a.ldx * 2;
-            t[j] = a.T + (int64_t)in * a.ldt;
+            const uint32_t x_row = x_lane + j * x_pitch, t_row = t_lane + j * t_pitch;
+            x[j] = x_row < x_last ? x_row : x_last;
+            t[j] = t_row < t_last ? t_row : t_last;
         }
         if (a.N >= F) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const xs v = *(const xs *)(x[j] + (int64_t)c_in * 2);
+                const xs v = *(const xs *)(X + (x[j] + (uint32_t)c_in * 2));
 #pragma unroll
                 for (int q = 0; q < F / 2; ++q) s.x[j][q] = v[q];
             }
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const xt_u4 v = load_unit<2>(x[j], 0, a.N * 2);
+                const xt_u4 v = load_unit<2>(X + x[j], 0, a.N * 2);
 #pragma unroll
                 for (int q = 0; q < F / 2; ++q) s.x[j][q] = v[q];
             }
@@ -120,7 +128,7 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
         if (RI > 1 && even) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const ts v = *(const ts *)(t[j] + r_even);
+                const ts v = *(const ts *)(T + (t[j] + (uint32_t)r_even * 4));
 #pragma unroll
                 for (int n = 0; n < RI; ++n) s.t[j][n] = v[n];
             }
@@ -128,7 +136,7 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int n = 0; n < RI; ++n) s.t[j][n] = t[j][r_in[n]];
+                for (int n = 0; n < RI; ++n) s.t[j][n] = *(const float *)(T + (t[j] + (uint32_t)r_in[n] * 4));
         }
         s.left = end - base;
     };
@@ -261,9 +269,9 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
     void *const R = whole ? a.R : (void *)a.workspace;
     const int out = whole ? a.out : EXPERTS_FP32;
     const int64_t group = whole ? (int64_t)g * a.group_r : (int64_t)piece * ((int64_t)a.N * a.r);
-    const int64_t ld = whole ? a.ldr : a.N;
+    const int64_t ld = whole ? a.ldr : a.trans_r ? a.N : a.r;   // (parts lie as R does)
     const int k = r_block + RI * 4 * b;
-    if (whole && !a.trans_r) {
+    if (!a.trans_r) {
 #pragma unroll
         for (int f = 0; f < F; ++f) {
             if (col + f < c0 || col + f >= a.N) continue;
@@ -273,7 +281,7 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
 #pragma unroll
             for (int q = 0; q < 4 * RI; q += 4) store_out<4>(R, out, group + (int64_t)(col + f) * ld, k + q, 0, a.r, v + q);
         }
-    } else {   // (parts lie r x N)
+    } else {
 #pragma unroll
         for (int q = 0; q < 4 * RI; ++q) {
             float v[F];
@@ -287,7 +295,8 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
 template <int ELEM, int F, int RI>
 static hipError_t launch_outer(const OuterArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)((a.N + 16 * F - 1) / (16 * F) * a.pieces), (unsigned)((a.r + 16 * RI - 1) / (16 * RI)));
+    const int64_t blocks = (a.N + 16 * F - 1) / (16 * F), ranks = (a.r + 16 * RI - 1) / (16 * RI);
+    const dim3 grid((unsigned)((blocks * a.pieces + 7) / 8 * 8 * ranks));
     constexpr int lds = kOuterWaves / 2 * F * RI * 1024;
     static_assert(lds + kOuterAdapters * 4 <= 64 * 1024, "LDS of an ordinary launch");
     if (a.out == EXPERTS_FP32) adapters_outer_kernel<ELEM, F, RI, 3><<<grid, dim3(64 * kOuterWaves), lds, s>>>(a);
@@ -306,15 +315,15 @@ hipError_t launch_adapters_outer(int type, const OuterArgs &a, hipStream_t s)
     return type == EXPERTS_BF16 ? launch_outer<EXPERTS_BF16>(a, s) : launch_outer<EXPERTS_FP16>(a, s);
 }
 
-// The pieces' sums added up in order, of adapters that have several: four neighbouring columns of a rank to a thread.
+// The pieces' sums added up in order, of adapters that have several: four neighbouring values of a matrix's line to a thread.
 __global__ void __launch_bounds__(256) adapters_join_kernel(const OuterArgs a)
 {
     __shared__ int counts[kOuterAdapters];
     count_rows(a.rows, counts);
     const int64_t of_group = (int64_t)a.N * a.r;
-    const int fours = (a.N + 3) / 4;
+    const int lines = a.trans_r ? a.r : a.N, length = a.trans_r ? a.N : a.r, fours = (length + 3) / 4;
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, k = at / fours;
-    const int c = (int)(at - k * fours) * 4, g = (int)(k / a.r), rank = (int)(k - (int64_t)g * a.r);
+    const int c = (int)(at - k * fours) * 4, g = (int)(k / lines), line = (int)(k - (int64_t)g * lines);
     if (g >= a.rows.G) return;
     int parts = pieces_of(counts[g], a.quota);
     if (parts == 1) return;
@@ -324,11 +333,11 @@ __global__ void __launch_bounds__(256) adapters_join_kernel(const OuterArgs a)
     first = first < a.pieces ? first : a.pieces;
     parts = first + parts <= a.pieces ? parts : a.pieces - first;
     typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
-    // (the last columns of a row: its last four, of which the thread's are stored)
-    const int in = c + 4 <= a.N || a.N < 4 ? c : a.N - 4;
-    const float *const from = a.workspace + (int64_t)first * of_group + (int64_t)rank * a.N + in;
+    // (a line's last four, of which the thread's are stored)
+    const int in = c + 4 <= length || length < 4 ? c : length - 4;
+    const float *const from = a.workspace + (int64_t)first * of_group + (int64_t)line * length + in;
     float x[4] = {0, 0, 0, 0};
-    if (a.N >= 4) {
+    if (length >= 4) {
         xt_f4 sum = {0, 0, 0, 0};
         int p = 0;
         for (; p + 4 <= parts; p += 4) {
@@ -343,21 +352,14 @@ __global__ void __launch_bounds__(256) adapters_join_kernel(const OuterArgs a)
         for (int v = 0; v < 4; ++v) x[v] = sum[v];
     } else {
         for (int p = 0; p < parts; ++p)
-            for (int v = 0; v < a.N; ++v) x[v] += from[p * of_group + v];
+            for (int v = 0; v < length; ++v) x[v] += from[p * of_group + v];
     }
-    const int64_t group = (int64_t)g * a.group_r;
-    if (a.trans_r) { store_out<4>(a.R, a.out, group + (int64_t)rank * a.ldr, in, c, a.N, x); return; }
-#pragma unroll
-    for (int v = 0; v < 4; ++v)
-        if (in + v >= c && in + v < a.N) {
-            const float y[4] = {x[v], 0, 0, 0};
-            store_out<4>(a.R, a.out, group + (int64_t)(in + v) * a.ldr, rank, 0, rank + 1, y);
-        }
+    store_out<4>(a.R, a.out, (int64_t)g * a.group_r + (int64_t)line * a.ldr, in, c, length, x);
 }
 hipError_t launch_adapters_join(const OuterArgs &a, hipStream_t s)
 {
     if (forced_launch_failure()) return hipErrorLaunchFailure;
-    const int64_t threads = (int64_t)a.rows.G * a.r * ((a.N + 3) / 4);
+    const int64_t threads = a.rows.G * (a.trans_r ? (int64_t)a.r * ((a.N + 3) / 4) : (int64_t)a.N * ((a.r + 3) / 4));
     adapters_join_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
