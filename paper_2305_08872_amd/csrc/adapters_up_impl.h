@@ -75,6 +75,11 @@ struct Adapters {
             for (int j = 0; j < 4; ++j) v[j] = bf16_pair(piece_of(half_of<EXPERTS_FP16>(v[j], 0), which, 2), piece_of(half_of<EXPERTS_FP16>(v[j], 1), which, 2));
         return v;
     }
+    // In LDS (AddFromLds) a slot has a unit of every line, 16 bytes each.  Its lines are turned by the unit, so that lanes that write neighbouring units
+    // of a line reach other banks (by no more than pairs of lines: a read's clocks take four lanes here and four there), and B's lie
+    // as its fragments read them.  Counted conflicts of 8192 x 8192 x 4096 with rank 64: an eighth of what lines in order have.
+    static __device__ __forceinline__ int turn(int unit) { return (unit << 1) & 15; }
+    static __device__ __forceinline__ int line_of_b(int line) { return T::PERM ? (line & ~31) | (line & 4) << 2 | (line >> 1 & 12) | (line & 3) : line; }
     // T of the tile's rows, units u0 .. u0 + n - 1, as pieces: slot (unit * pieces + piece) has 16 bytes of every row.  A thread has two items (8
     // ranks of a row) on their way at a time; no branch around a read: what is not there is read at the edge and becomes zeros.
     static constexpr int T_ITEMS = 2;
@@ -116,7 +121,7 @@ struct Adapters {
                 xt_u4 v;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = bf16_pair(piece_of(t[q][2 * j], piece, pieces), piece_of(t[q][2 * j + 1], piece, pieces));
-                *(xt_u4 *)(lds + ((unit * pieces + piece) * T::BM + line) * 16) = v;
+                *(xt_u4 *)(lds + ((unit * pieces + piece) * T::BM + (line ^ turn(unit))) * 16) = v;
             }
         }
     }
@@ -146,12 +151,6 @@ struct Adapters {
             for (int v = 0; v < 4; ++v) acc[mi][ni][v] = in ? x[v] : acc[mi][ni][v];
         }
         __builtin_amdgcn_sched_barrier(0);
-    }
-    // a lane's column of fragment ni, of the wave's
-    static __device__ __forceinline__ int column(int ni, int lane)
-    {
-        const int i = lane & 15;
-        return T::PERM ? (ni >> 1) * 32 + 8 * (i >> 2) + (i & 3) + (ni & 1) * 4 : ni * 16 + i;
     }
 };
 
@@ -516,25 +515,26 @@ struct AddFromLds : Adapters<T> {
             int k, unit, line;
             if (!item(q, n, units, k, unit, line)) continue;
 #pragma unroll
-            for (int p = 0; p < OF_B; ++p) *(xt_u4 *)(lds + (((k * units + unit) * OF_B + p) * T::BN + line) * 16) = this->piece_of_b(v[q], p);
+            for (int p = 0; p < OF_B; ++p) *(xt_u4 *)(lds + (((k * units + unit) * OF_B + p) * T::BN + (this->line_of_b(line) ^ this->turn(unit))) * 16) = this->piece_of_b(v[q], p);
         }
     }
     __device__ __forceinline__ void products(xt_f4 (&acc)[T::MI][T::NI], const char *lds_b, int lo, int hi, const Ways &ways, int pieces) const
     {
         const int lane = this->lane, b = lane >> 4;
-        const char *const t_row = xt_smem + (this->row0 - this->tile_row + (lane & 15)) * 16;
+        const char *const t_row = xt_smem + (this->row0 - this->tile_row) * 16, *const b_row = lds_b + (this->col0 - this->tile_col) * 16;
         const int each = ways.each(), steps = ways.reads() * each;
 #pragma unroll 1
         for (int s = 0; s < steps; ++s) {
             int unit, way;
             const int read = s / each;
             const bool there = ways.at(read, s - read * each, b, unit, way);
-            const char *const t_at = t_row + (there ? unit * pieces + way / OF_B : 0) * (T::BM * 16);
-            const char *const b_at = lds_b + ((there ? unit * OF_B + way % OF_B : 0) * T::BN + this->col0 - this->tile_col) * 16;
+            const int at = ((lane & 15) ^ this->turn(unit)) * 16;
+            const char *const t_at = t_row + (there ? unit * pieces + way / OF_B : 0) * (T::BM * 16) + at;
+            const char *const b_at = b_row + (there ? unit * OF_B + way % OF_B : 0) * (T::BN * 16) + at;
             xt_u4 vb[T::NI];
 #pragma unroll
             for (int ni = 0; ni < T::NI; ++ni) {
-                vb[ni] = *(const xt_u4 *)(b_at + this->column(ni, lane) * 16);
+                vb[ni] = *(const xt_u4 *)(b_at + ni * 256);
                 if (!there) vb[ni] = xt_u4{0, 0, 0, 0};
             }
             for_each<T::MI>([&](auto mi) { this->template add_block<decltype(mi)::value>(acc, t_at, there, lo, hi, vb); });
