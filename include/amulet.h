@@ -534,7 +534,10 @@ int amulet_selected_shape(int task, int64_t M, int64_t N, int64_t K);
  * <rows or tokens>"; a call whose launches are a pair has one text: " last_columns
  * <side of their tiles>" where a second launch runs the last columns of a product by
  * rows (as many as the device finds, for unlucky offsets none), and " parts <ranges>" where
- * grouped_mm_wgrad sums a group's rows in so many ranges and adds them up afterwards.  The adaptive
+ * grouped_mm_wgrad sums a group's rows in so many ranges and adds them up afterwards.  Low-rank adapters: adapters_256x256
+ * ... adapters_16x16 (the product by B and W; adapters_down where there are no columns), adapters_wgrad
+ * (" parts 2" where it may sum an adapter's rows in pieces); grad_norm, grad_clip, grad_norm_clip
+ * (" rows <tensors>").  The adaptive
  * calls make one launch per trial and one for the rest.  Static storage of the
  * calling thread, until its next call of this function.
  */
@@ -757,7 +760,9 @@ int amulet_mm_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K,
  *   X  M x K, bf16 or fp16 (`type`)      W  K x N, or N x K with trans_w; NULL: no shared matrix, R = T B
  *   A  G matrices, group_a elements apart, K x r, or r x K with trans_a      B  r x N, or N x r with trans_b
  *   scales  G values, NULL: ones         T  M x r, fp32, written (the gradients below take it)      R  fp32 or X's type
- * An adapter of a lower rank than r has zeros behind it.  r, S and G up to 65536; the pitches of X, W, A and B as those of A, B and D above.
+ * Segments cost a little even where they have no rows, and rows of the same adapter are best neighbours (one segment).
+ * An adapter of a lower rank than r has zeros behind it.  r, S and G up to 65536; the pitches of X, W, A and B as those of A, B and D above
+ * (of T too where it is read, in bytes).
  * T is not rounded between the two products: R's sums take it as two bf16 values (16 bits of it) where R has 16 bits, three (all 24) where
  * it has 32, and X A, X W and T B are each summed in fp32.  (T B of fp16 operands too is made of bf16 products, B in two, exactly: T may
  * lie outside fp16's range.)

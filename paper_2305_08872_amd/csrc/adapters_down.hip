@@ -2,7 +2,8 @@
 //
 // Bound by X's bytes (many rows) or the adapters' (few).  A workgroup has up to BM rows of one segment and BN ranks; its waves share
 // k, each with a ring of stages of its own in LDS (experts_tile.h), where all of it is read once from memory, and their
-// sums are joined in the waves' order.  (Fragments straight from memory instead, without LDS: neighbouring lanes of a matrix operand have rows
+// sums are joined in the waves' order.  us, bf16, out of the caches: 16384 x 4096 by rank 16 29 (4.7 TB/s), 8192 x 4096 by rank 64 of 24 segments 25, a wave's
+// way through its 64 stages, of which four are on their way.  (Fragments straight from memory instead, without LDS: neighbouring lanes of a matrix operand have rows
 // of their own, a cache line for every 16 bytes, and 8192 x 4096 by rank 64 took 48 us.)
 #include "adapters_segments.h"
 

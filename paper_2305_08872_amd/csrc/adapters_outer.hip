@@ -4,7 +4,8 @@
 // rows; its waves take steps of 32 rows in turn and join their sums in LDS, in order.  A lane reads 2 F bytes of 8 rows of X
 // and turns them in registers (byte permutes) into F columns of 8 rows each, the operands of F matrix instructions: lane i of 16 has
 // columns F i + f in instruction f, so that what it ends with are neighbouring columns.  T is fp32 and is taken as two bf16 pieces for
-// results of 16 bits, three for 32 (adapters_segments.h), X of fp16 as two.
+// results of 16 bits, three for 32 (adapters_segments.h), X of fp16 as two.  us, 16384 x 4096 bf16, 4 adapters, rank 16 / 32 / 64: 28 (4.8 TB/s of X) / 33 / 44,
+// and 5 to 7 to add up the pieces.
 #include "adapters_segments.h"
 
 namespace amulet {

@@ -8,6 +8,10 @@
 // That is for tiles of many rows, when their own sums are done and the stages' LDS is free: B of as many segments as it holds is laid out
 // beside T.  Tiles of few rows (whose k is shared by groups of waves) and batches of short segments take T and B from memory, row by
 // row, on the vector ALU, while the first stages of X and W are on their way.
+//
+// Bound by the shared product's operations (many rows) or W's bytes (few).  us, bf16, beside the same call without adapters: 8192 x 8192 x 4096 by
+// 24 segments, rank 64 465 / 429; 16384 x 4096 x 4096, rank 16 446 / 442; 8 x 4096 x 4096, a segment to a row, rank 16 9 of a call's 14 / 13; 208 rows of
+// as many segments, rank 32 24 / 17.
 #ifndef AMULET_ADAPTERS_UP_IMPL_H
 #define AMULET_ADAPTERS_UP_IMPL_H
 

@@ -57,6 +57,7 @@ def test_refusals_of_their_gradients(lib):
     for name in ("X", "T", "off", "R"):
         assert wgrad(lib, **{name: None}) == -3
     assert wgrad(lib, ldx=4) == -4 and wgrad(lib, ldt=2) == -4 and wgrad(lib, ldr=2) == -4 and wgrad(lib, tr=1) == -4 and wgrad(lib, gr=14) == -4
+    assert wgrad(lib, ldx=16711679 // 2 + 1) == -7 and wgrad(lib, ldt=16711679 // 4 + 1) == -7
     assert wgrad(lib, ws=ctypes.c_void_p(8), n=64) == -8
     assert wgrad(lib, G=0, S=0, R=None) == 0 and wgrad(lib, N=0, R=None) == 0 and wgrad(lib, r=0, R=None) == 0
     assert wgrad(lib, G=2 ** 16, N=2 ** 20, r=64, ldx=2 ** 20, ldt=64, ldr=64, gr=2 ** 26) == -7
