@@ -92,7 +92,7 @@ def main(rows=2048, width=512, outputs=640, rank=16, tasks=4, steps=8):
         with torch.no_grad():
             a -= 0.5 * da
             b -= 0.5 * db
-        losses.append(float(loss))
+        losses.append(float(loss.detach()))
         print("loss %.4f  gradients' norm %.3f" % (losses[-1], float(norm)))
     # a batch of single tokens
     batch = Rows([1] * 8, [i % (tasks + 1) - 1 for i in range(8)])

@@ -796,7 +796,8 @@ int amulet_adapters_wgrad(int type, int out_type, int trans_r, int64_t M, int64_
  * alignment of elements.  The arrays lie in host memory and are read before the call returns; the tensors and `norm` (one fp32
  * value) lie in device memory.
  *   amulet_grad_norm       norm = sqrt(sum of the squares of all values), summed in fp64 in an order that the sizes fix
- *   amulet_grad_clip       outs[i] = grads[i] times max_norm / norm where norm is above max_norm, else grads[i]; rounded once
+ *   amulet_grad_clip       outs[i] = grads[i] times max_norm / norm (one fp32 factor) where norm is above max_norm, else grads[i]; each
+ *                          product rounded once
  *   amulet_grad_norm_clip  both (norm is written too)
  * outs NULL: in place; outs[i] may be grads[i], and tensors overlap in no other way.  A norm that is infinite or no number changes nothing:
  * the tensors stay as they are, or are copied, and `norm` tells.  max_norm >= 0, may be infinite (AMULET_ERR_RANGE for a

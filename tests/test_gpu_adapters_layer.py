@@ -20,7 +20,8 @@ def ex():
 
 
 def near(a, b, rel):
-    return float((a.double() - b).norm()) <= rel * float(b.norm())
+    a, b = a.detach().double(), b.detach()
+    return float((a - b).norm()) <= rel * float(b.norm())
 
 
 @pytest.mark.parametrize("lengths,which,width,outputs,rank,tasks", [([1] * 6, [0, 2, -1, 1, 0, 2], 64, 96, 8, 3), ([30, 7, 0, 40], [1, -1, 0, 1], 72, 40, 5, 2),
@@ -109,3 +110,44 @@ def test_compiled_marshalling_makes_the_same_calls(ex, monkeypatch):
         am.amulet_adapters_mm(x, w.t(), a, b, off, plain["t"], plain["r"])
     with pytest.raises(ValueError):
         am.amulet_grad_norm([x.cpu()], plain["n"], ws)
+
+
+def test_a_captured_step_follows_its_inputs(ex):
+    """Forward, both gradients, their norm and clipping in one graph: replayed with other rows, other segments and other adapters, eager work between the
+    replays, every replay as the eager calls."""
+    am = ex.am
+    M, K, N, r, G, S = 700, 136, 264, 12, 3, 4
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    x, w, a, b, dy = torch.randn(M, K, **bf), torch.randn(N, K, **bf), torch.randn(G, r, K, **bf), torch.randn(G, N, r, **bf), torch.randn(M, N, **bf)
+    off, which = torch.zeros(S + 1, dtype=torch.int32, device="cuda"), torch.zeros(S, dtype=torch.int32, device="cuda")
+    space = torch.empty(max(am.amulet_adapters_wgrad_workspace_bytes(M, n, r, G) for n in (N, K)) + 1024, dtype=torch.uint8, device="cuda")
+    sums = torch.empty(am.amulet_grad_norm_workspace_bytes(2), dtype=torch.uint8, device="cuda")
+
+    def outputs():
+        return [torch.empty(M, r, device="cuda"), torch.empty(M, N, **bf), torch.empty(M, r, device="cuda"), torch.empty(M, K, **bf), torch.empty_like(a), torch.empty_like(b), torch.empty(1, device="cuda")]
+
+    def step(t, y, u, dx, da, db, norm):
+        am.amulet_adapters_mm(x, w, a, b, off, t, y, adapters=which, trans_w=True, trans_a=True, trans_b=True)
+        am.amulet_adapters_mm(dy, w, b, a, off, u, dx, adapters=which)
+        am.amulet_adapters_wgrad(x, u, off, da, space, adapters=which, trans_r=True)
+        am.amulet_adapters_wgrad(dy, t, off, db, space, adapters=which)
+        am.amulet_grad_norm_clip([da, db], 5.0, norm, sums)
+
+    captured, eager = outputs(), outputs()
+    step(*captured)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(*captured)
+    for offsets, adapters in (([0, 10, 500, 500, 690], [2, 0, 1, 2]), ([0, 0, 0, 0, 0], [0, 1, 2, 0]), ([0, 700, 700, 700, 700], [1, -1, 5, 1]), ([0, 1, 2, 3, 4], [0, -1, 0, 2])):
+        off.copy_(torch.tensor(offsets, dtype=torch.int32))
+        which.copy_(torch.tensor(adapters, dtype=torch.int32))
+        x.normal_()
+        dy.normal_()
+        step(*eager)
+        for o in captured:
+            o.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for c, e in zip(captured, eager):
+            assert torch.equal(c, e) and torch.isfinite(c).all()
