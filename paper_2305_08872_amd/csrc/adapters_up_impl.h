@@ -618,7 +618,7 @@ inline hipError_t launch_adapters_layout(int tile, bool many, const UpArgs &a, i
     }
 }
 
-// many: segments of fewer rows than a block; the tile is EXPERTS_64x64 or smaller then
+// many: segments of a few rows; the tile is EXPERTS_64x64 or smaller then
 template <int ELEM>
 inline hipError_t launch_adapters_up(int tile, bool w_across, bool many, const UpArgs &a, int64_t blocks, hipStream_t s)
 {

@@ -128,6 +128,7 @@ CASES = [
     ([200, 1, 55], [1, 0, 1], 2, 4096, 4096, 16, 0), ([700, 324], None, 2, 4096, 1024, 20, 0),
     ([1] * 8, None, 8, 4096, 4096, 16, 0), ([3, 2, 0, 6], [1, -1, 0, 1], 2, 2000, 2500, 33, 1), ([1] * 14, [i % 3 for i in range(14)], 3, 1111, 4099, 72, 2),
     ([1] * 600, [(i * 7) % 11 - 1 for i in range(600)], 9, 1024, 512, 24, 3), ([2] * 700, [(i * 5) % 4 for i in range(700)], 4, 2050, 1024, 64, 0),
+    ([1] * 200, [(i * 3) % 7 - 1 for i in range(200)], 6, 4096, 4096, 12, 8), ([40, 90, 70], [0, 1, 0], 2, 4096, 4096, 72, 8),
 ]
 
 
