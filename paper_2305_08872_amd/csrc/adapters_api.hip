@@ -172,21 +172,28 @@ int amulet_adapters_mm(int type, int out_type, int trans_w, int trans_a, int tra
     rows.offsets = offsets; rows.adapters = adapters;
     rows.S = some ? (int)S : 0; rows.G = some ? (int)G : 0; rows.M = (int)M;
     // Segments of a few rows: row by row, which the larger tiles have no room for.  us without the first product, row by row / through LDS, 1, 2, 4 and 8 rows to a
-    // segment: 1337 x 3033 x 2319 rank 32 76 / 132, 74 / 89, 73 / 67 and 72 / 57, rank 8 75 / 84, 73 / 64, 71 / 55 and 71 / 50; 208 x 4096 x 4096 rank 32 with
-    // B across 42 / 92, 42 / 58, 41 / 41, 40 / 32.
+    // segment: 1337 x 3033 x 2319 rank 32 76 / 132, 74 / 89, 73 / 67 and 72 / 57, rank 8 75 / 84, 73 / 64, 71 / 55 and 71 / 50; B across, rank 32, 94 / 173, 92 / 110,
+    // 92 / 77 and 92 / 62.  Segments shorter than a block of rows: no more than 64 of those to a tile (4 rows to a segment 77, 128 rows to a tile 130).
     bool many = some && M < 4 * S;
+    const bool brief = some && M < 16 * S;
     UpArgs u = {};
     RowsPlan plan = {};
     if (N > 0) {
         u.mm.A = X; u.mm.lda = ldx; u.mm.B = W; u.mm.ldb = ldw; u.mm.R = R; u.mm.ldr = ldr;
         u.mm.M = (int)M; u.mm.N = (int)N; u.mm.K = W ? (int)K : 0; u.mm.G = 1; u.mm.out = out_type;
         u.rows = rows; u.T = T; u.ldt = ldt; u.B = B; u.ldb = ldb; u.group_b = group_b; u.r = (int)r; u.across = !trans_b;
-        plan = rows_plan(2, !trans_w, u.mm, M, N, 1, many ? EXPERTS_64x64 : EXPERTS_256x256);
-        if (plan.tile < 0 && many) { many = false; plan = rows_plan(2, !trans_w, u.mm, M, N, 1, EXPERTS_256x256); }
+        plan = rows_plan(2, !trans_w, u.mm, M, N, 1, many ? EXPERTS_64x64 : brief ? EXPERTS_64x128 : EXPERTS_256x256);
+        if (plan.tile < 0 && brief) { many = false; plan = rows_plan(2, !trans_w, u.mm, M, N, 1, EXPERTS_256x256); }
         if (plan.tile < 0) return AMULET_ERR_RANGE;
-        // Longer segments, and B read value by value or rows of it more than twice: rather the tile without k groups, through LDS.  (208 x 4096 x 4096, 64 rows
-        // to a segment, B across, rank 8 / 32 / 64 24 / 26 / 29 us, row by row 36 / 40 / 62; along 23 / 24 / 27 and 22 / 23 / 29.)
-        if (some && !many && plan.tile == EXPERTS_64x64_K2 && (!trans_b || r % 8 != 0 || r > 64)) plan.tile = EXPERTS_64x64;   // (of as many workgroups)
+        // Longer segments, and B across, in odd ranks or read more than twice: rather the tile without k groups, through LDS.  (208 x 4096 x 4096, 64 rows to a
+        // segment, B across, rank 8 / 32 / 64 24 / 26 / 29 us, row by row 28 / 29 / 38; 8 rows to a segment 25 / 32 / 42.)
+        if (some && M >= 12 * S && plan.tile == EXPERTS_64x64_K2 && (!trans_b || r % 8 != 0 || r > 64)) plan.tile = EXPERTS_64x64;   // (of as many workgroups)
+        // (row by row two columns of B across are read at a time)
+        if (some && N < 2 && !trans_b) {
+            many = false;
+            plan = {EXPERTS_64x64, ((M + 63) / 64 + 7) / 8 * 8, 0};
+            if (plan.blocks > kMostBlocks256) return AMULET_ERR_RANGE;
+        }
         // One row of tiles that would leave compute units without one: narrower tiles, whose eight k groups have more of W on its way
         if (plan.tile == EXPERTS_16x32 && M <= 16 && (N + 31) / 32 < compute_units()) plan = {ADAPTERS_16x16, (N + 15) / 16 + 7 & ~(int64_t)7, 0};
     }

@@ -177,8 +177,9 @@ struct Meeting {
     __device__ __forceinline__ void next(const Segments &g, int first, int last, int lane) { chunk += 64; look(g, first, last, lane); }
 };
 
-// From memory, row by row on the vector ALU: T's row times its adapter's B, in fp32.  Four lanes have 32 ranks of a column between them (so
-// that neighbouring lanes read neighbouring bytes; a matrix operand's lanes have columns of their own, a cache line for every 16 bytes),
+// From memory, row by row on the vector ALU: T's row times its adapter's B, in fp32.  Four lanes have 32 ranks of a column between them, so
+// that neighbouring lanes read neighbouring bytes; a matrix operand's lanes have columns of their own, a cache line for every 16 bytes (and across,
+// two columns to a lane: 208 x 4096 x 4096, a row to a segment, rank 32 29 us, a column to a lane and value 42);
 // and the sums go to a tile of LDS beside the ring, from where they join the others in the end.  The k groups take the rows
 // in turn; a batch of rows is on its way while the one before is multiplied, the first one is asked for before the first stages of X and W.
 // (A decoding batch has an adapter to a row, and a matrix instruction for each would have one row of 16: 192 rows by rank 32 beside 4096 x
@@ -187,7 +188,7 @@ template <class T>
 struct AddFromRows : Adapters<T> {
     static constexpr int ROWS = T::MI * 16, LDS = T::LDS + T::BM * T::BN * 4;
     static constexpr int AT = 2;   // rows of a batch
-    static_assert(ROWS <= 64, "a lane to a row");
+    static_assert(ROWS <= 64 && T::NI <= 2, "a lane to a row; two columns to a lane");
     enum { WHOLE, CUT, ACROSS };   // B along its rows, in whole units of 8 ranks or not; across
     struct Batch {
         xt_u4 b[AT][T::NI];
@@ -199,7 +200,11 @@ struct AddFromRows : Adapters<T> {
     uint64_t mine;           // this group's
     int adapter, kind;       // of row row0 + lane; -1: none
     uint32_t off[T::NI];
-    const char *first;       // B at the wave's first column
+    const char *first;       // B at the wave's first column (across: at its own)
+    bool last;               // across: the lane's first column is B's last one, the second of what it reads
+    // Along, a lane has 8 ranks of columns lane / 4 + 16 ni, four lanes a column's 32; across, of NI neighbouring columns, lanes 16 apart theirs
+    template <int KIND>
+    __device__ __forceinline__ int ranks() const { return 8 * (KIND == ACROSS ? this->lane >> 4 : this->lane & 3); }
 
     __device__ __forceinline__ AddFromRows(const Adapters<T> &x) : Adapters<T>(x)
     {
@@ -225,12 +230,18 @@ struct AddFromRows : Adapters<T> {
         kind = a.across ? ACROSS : (a.r & 7) == 0 ? WHOLE : CUT;
         const uint32_t ld = (uint32_t)a.ldb * 2u;
         const int c0 = this->col0 < a.mm.N ? this->col0 : a.mm.N - 1;
-        first = (const char *)a.B + (a.across ? (int64_t)c0 : (int64_t)c0 * a.ldb) * 2;
+        first = (const char *)a.B + (a.across ? 0 : (int64_t)c0 * a.ldb) * 2;
 #pragma unroll
         for (int ni = 0; ni < T::NI; ++ni) {
             int c = this->col0 + ni * 16 + (lane >> 2);
             c = (c < a.mm.N ? c : a.mm.N - 1) - c0;
-            off[ni] = a.across ? (uint32_t)c * 2u : (uint32_t)c * ld;
+            off[ni] = (uint32_t)c * ld;
+        }
+        last = false;
+        if (a.across) {   // (B has NI columns at least)
+            const int c = this->col0 + (lane & 15) * T::NI, end = a.mm.N - T::NI;
+            last = c > end;
+            off[0] = (uint32_t)(last ? end : c) * 2u;
         }
         left = mine;
         if (kind == WHOLE) fetch<WHOLE>(batch, 0);
@@ -244,7 +255,7 @@ struct AddFromRows : Adapters<T> {
         typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
         typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
         const UpArgs &a = this->a;
-        const int at = k + 8 * (this->lane & 3);   // the lane's first rank
+        const int at = k + ranks<KIND>();   // the lane's first rank
         const bool in = at < a.r;
         const uint32_t ld = (uint32_t)a.ldb * 2u;
 #pragma unroll
@@ -270,16 +281,21 @@ struct AddFromRows : Adapters<T> {
                 else if constexpr (KIND == CUT) {
                     x.b[q][ni] = xt_u4{0, 0, 0, 0};
                     if (in) x.b[q][ni] = load_unit<2>(base + off[ni], at * 2, a.r * 2);
-                } else {
-                    uint32_t v[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int rank = at + j < a.r ? at + j : a.r - 1;
-                        v[j] = *(const uint16_t *)(base + (int64_t)rank * ld + off[ni]);
-                    }
-                    x.b[q][ni] = xt_u4{v[0] | (v[1] << 16), v[2] | (v[3] << 16), v[4] | (v[5] << 16), v[6] | (v[7] << 16)};
-                    __builtin_amdgcn_sched_barrier(0);   // (a batch's single values would not all have a register)
                 }
+            }
+            if constexpr (KIND == ACROSS) {   // (two columns of a rank, or two ranks of a column, to a word)
+                typedef uint32_t u1 __attribute__((aligned(2)));
+                uint32_t v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const char *const p = base + (int64_t)(at + j < a.r ? at + j : a.r - 1) * ld + off[0];
+                    if constexpr (T::NI > 1) v[j] = *(const u1 *)p;
+                    else v[j] = *(const uint16_t *)p;
+                }
+                if constexpr (T::NI > 1) {
+                    x.b[q][0] = xt_u4{v[0], v[1], v[2], v[3]};
+                    x.b[q][T::NI - 1] = xt_u4{v[4], v[5], v[6], v[7]};
+                } else x.b[q][0] = xt_u4{v[0] | (v[1] << 16), v[2] | (v[3] << 16), v[4] | (v[5] << 16), v[6] | (v[7] << 16)};
             }
         }
     }
@@ -291,10 +307,32 @@ struct AddFromRows : Adapters<T> {
     __device__ __forceinline__ void multiply(const Batch &x, int k) const
     {
         const UpArgs &a = this->a;
-        const int lane = this->lane, n = a.r - k - 8 * (lane & 3);   // the lane's ranks
+        const int lane = this->lane, n = a.r - k - ranks<KIND>();   // the lane's ranks
 #pragma unroll
         for (int q = 0; q < AT; ++q) {
             if (x.row[q] < 0) continue;
+            if constexpr (KIND == ACROSS) {
+                float sum[T::NI] = {};
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int c = 0; c < T::NI; ++c) {
+                        const uint32_t w = T::NI > 1 ? x.b[q][j / 4 % T::NI][j % 4] : x.b[q][0][j / 2];
+                        const float b = T::NI > 1 ? half_of<T::ELEM>(c == 0 && last ? w >> 16 : w, c) : half_of<T::ELEM>(w, j % 2);
+                        sum[c] = j < n ? __builtin_fmaf(x.t[q][j], b, sum[c]) : sum[c];
+                    }
+#pragma unroll
+                for (int c = 0; c < T::NI; ++c) {
+                    sum[c] += __shfl_xor(sum[c], 16);
+                    sum[c] += __shfl_xor(sum[c], 32);
+                    if (lane < 16) {
+                        float *const to = place(x.row[q], lane * T::NI + c);
+                        *to = k == 0 ? sum[c] : *to + sum[c];
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                continue;
+            }
 #pragma unroll
             for (int ni = 0; ni < T::NI; ++ni) {
                 float sum = 0.0f;
