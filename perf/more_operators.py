@@ -270,7 +270,7 @@ def run(s):
         return [s["norm"]]
     if op == "clip":
         am.amulet_grad_norm_clip(s["grads"], s["max_norm"], s["norm"], s["workspace"], outs=s["outs"])
-        return [s["norm"]] + [x if x.numel() else s["grads"][0][:0] for x in s["buffers"]]   # (as _joined() has it)
+        return [s["norm"]] + s["buffers"]
     t = s["trans"]
     if op == "adapters":
         am.amulet_adapters_mm(s["X"], s["W"], s["A"], s["B"], s["offsets"], s["T"], s["R"], adapters=s["adapters"], scales=s["scales"],
