@@ -71,7 +71,6 @@ __global__ void __launch_bounds__(T::NT) adapters_down_kernel(const DownArgs a)
         else sb.start_kc(A, a.lda * 2, r0, a.r, K, kg * T::BK, wave, lane, same, true);
     }
     if (!tile_sums<T>(sa, sb, 0, K, wave, kg, lane, same, TileScales(), false, acc)) return;
-    sums_done();
     const float scale = g >= 0 && a.scales ? a.scales[g] : 1.0f;
 #pragma unroll
     for (int mi = 0; mi < T::MI; ++mi)

@@ -180,6 +180,7 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
                     for (int n = 0; n < RI; ++n) acc[f][n] = mma16<EXPERTS_BF16>(pt[p][n], w, acc[f][n]);
             }
         }
+        sums_done();
     };
 
     // The wave's steps: every `workers`-th of those of the adapter's segments
@@ -245,7 +246,6 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
         }
     }
 
-    sums_done();
     // the waves' sums: halves onto halves, in a fixed order
     extern __shared__ __attribute__((aligned(16))) char smem[];
     xt_f4 *const sums = (xt_f4 *)smem;

@@ -56,14 +56,6 @@ __device__ __forceinline__ float piece_of(float x, int which, int pieces)
     return which == 0 ? p0 : which == 1 ? p1 : r2;
 }
 __device__ __forceinline__ float whole_nan(float x) { return x != x ? __builtin_nanf("") : x; }
-// Matrix instructions' results are there: for what reads them in another basic block (the compiler waits between the two where they lie in one; where
-// a branch lay between, a copy of a sum was seen to take what its register held before).
-__device__ __forceinline__ void sums_done()
-{
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_nop 7\n\ts_nop 7" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
 // two values rounded to bf16 side by side
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
 {

@@ -620,7 +620,6 @@ __global__ void __launch_bounds__(T::NT) __attribute__((amdgpu_waves_per_eu(!ROW
         tile_sums<T>(sa, sb, 0, a.K, wave, kg, lane, a_row, TileScales(), idle, acc, typename AddFromLds<T>::Look{adapters});
         adapters(acc);
     }
-    sums_done();
     store_sums<T>(acc, a.R, a.out, lane, wave_col, from, a.N, [&](int mi) -> int64_t {
         const int i = wave_row + mi * 16 + (lane & 15);
         return i < a.M ? (int64_t)i * a.ldr : -1;

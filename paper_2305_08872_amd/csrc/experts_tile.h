@@ -360,6 +360,18 @@ __device__ __forceinline__ xt_f4 mma16(xt_u4 a, xt_u4 b, xt_f4 c)
     else
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(xt_h8, a), __builtin_bit_cast(xt_h8, b), c, 0, 0, 0);
 }
+// The results of the matrix instructions before this are there (16 x 16 results of 16-bit factors: 8 wait states).  The compiler waits by itself
+// where one way leads from an instruction to a reader of its result; where ways part behind it and meet again before the reader, a loop's back edge
+// among them, it goes each block of the way back but once, so that a longer way hides a shorter one that joins it, and too few states
+// are left on that.  (Seen in its listings, tests/test_matrix_result_waits.py: at the head of a loop a copy of a sum 4 states, in another 3, behind the
+// instruction at the loop's end; and without a loop, two ways from one block to another.)  So this stands in the instructions' own block, before its
+// branch: within it the compiler's count is right.
+__device__ __forceinline__ void sums_done()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 7" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 // eight e4m3 values of a unit (its first or second half) as bf16, exactly
 __device__ __forceinline__ xt_u4 bf16_of(xt_u4 x, int half)
@@ -829,6 +841,9 @@ __device__ __forceinline__ bool tile_sums(Staged<T::BM, T::ES, T::KB, T::AKS, fa
         });
         if constexpr (AFTER && !Steps<T>::A2) f.template read_a<0>(ra, after, scale_row(after));
         if constexpr (AFTER && !Steps<T>::B2) f.template read_b<0>(rb, after + T::A_BYTES);
+        // (where the ways part: behind the last stages, and round the loops of one wave's tiles, which copy sums at their head; 8 bits:
+        // the sums are not the instructions' results)
+        if constexpr (!T::FP8 && (!AFTER || T::NW == 1)) sums_done();
     };
     constexpr auto none = [](auto, int) {};
 
