@@ -763,9 +763,8 @@ int amulet_mm_fp8(int out_type, int trans_b, int64_t M, int64_t N, int64_t K,
  * Segments cost a little even where they have no rows, and rows of the same adapter are best neighbours (one segment).
  * An adapter of a lower rank than r has zeros behind it.  r, S and G up to 65536; the pitches of X, W, A and B as those of A, B and D above
  * (of T too where it is read, in bytes).
- * T is not rounded between the two products: R's sums take it as two bf16 values (16 bits of it) where R has 16 bits, three (all 24) where
- * it has 32, and X A, X W and T B are each summed in fp32.  (T B of fp16 operands too is made of bf16 products, B in two, exactly: T may
- * lie outside fp16's range.)
+ * T is not rounded between the two products: R's sums take all 24 bits of it (as bf16 values whose sum it is), and X A, X W and T B are each
+ * summed in fp32.  (T B of fp16 operands too is made of bf16 products, B in two, exactly: T may lie outside fp16's range.)
  *
  * The rows' gradients are the same call: D for X, W read the other way, A and B exchanged and read the other way:
  *     U[i] = scales[a] D[i] B[a]^T,  dX[i] = D[i] W^T + U[i] A[a]^T

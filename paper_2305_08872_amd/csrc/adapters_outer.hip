@@ -3,8 +3,8 @@
 // Bound by X's bytes: T and R are a few columns wide.  A workgroup has 16 F columns of X and 16 RI of T of one adapter, or of a piece of its
 // rows; its waves take steps of 32 rows in turn and join their sums in LDS, in order.  A lane reads 2 F bytes of 8 rows of X
 // and turns them in registers (byte permutes) into F columns of 8 rows each, the operands of F matrix instructions: lane i of 16 has
-// columns F i + f in instruction f, so that what it ends with are neighbouring columns.  T is fp32 and is taken as two bf16 pieces for
-// results of 16 bits, three for 32 (adapters_segments.h), X of fp16 as two.  us, 16384 x 4096 bf16, 4 adapters, rank 16 / 32 / 64: 28 (4.8 TB/s of X) / 33 / 44,
+// columns F i + f in instruction f, so that what it ends with are neighbouring columns.  T is fp32 and is taken as three bf16 pieces, all
+// of its bits (adapters_segments.h), X of fp16 as two.  us, 16384 x 4096 bf16, 4 adapters, rank 16 / 32 / 64: 28 (4.8 TB/s of X) / 33 / 44,
 // and 5 to 7 to add up the pieces.
 #include "adapters_segments.h"
 
@@ -51,12 +51,12 @@ __device__ __forceinline__ bool find_piece(const int *counts, int G, int quota, 
     return false;
 }
 
-template <int ELEM, int F, int RI, int PIECES>
+template <int ELEM, int F, int RI>
 __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_per_eu(2))) adapters_outer_kernel(const OuterArgs a)
 {
     constexpr int COLS = 16 * F, OF_X = ELEM == EXPERTS_FP16 ? 2 : 1;
     // the next step's operands on their way, where there are registers for them
-    constexpr bool AHEAD = RI == 1 || F < 8 || PIECES < 3;
+    constexpr bool AHEAD = RI == 1 || F < 8;
     __shared__ int counts[kOuterAdapters];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int i = lane & 15, b = lane >> 4;
@@ -155,13 +155,13 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int n = 0; n < RI; ++n) s.t[j][n] = whole_nan(s.t[j][n]);
-        xt_u4 pt[PIECES][RI];
+        xt_u4 pt[kPieces][RI];
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p)
+        for (int p = 0; p < kPieces; ++p)
 #pragma unroll
             for (int n = 0; n < RI; ++n)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) pt[p][n][q] = bf16_pair(piece_of(s.t[2 * q][n], p, PIECES), piece_of(s.t[2 * q + 1][n], p, PIECES));
+                for (int q = 0; q < 4; ++q) pt[p][n][q] = bf16_pair(piece_of(s.t[2 * q][n], p, kPieces), piece_of(s.t[2 * q + 1][n], p, kPieces));
 #pragma unroll
         for (int f = 0; f < F; ++f) {
             // column f of the lane's 8 rows
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
 #pragma unroll
                     for (int q = 0; q < 4; ++q) w[q] = bf16_pair(piece_of(half_of<ELEM>(v[q], 0), h, 2), piece_of(half_of<ELEM>(v[q], 1), h, 2));
 #pragma unroll
-                for (int p = 0; p < PIECES; ++p)
+                for (int p = 0; p < kPieces; ++p)
 #pragma unroll
                     for (int n = 0; n < RI; ++n) acc[f][n] = mma16<EXPERTS_BF16>(pt[p][n], w, acc[f][n]);
             }
@@ -300,8 +300,7 @@ static hipError_t launch_outer(const OuterArgs &a, hipStream_t s)
     const dim3 grid((unsigned)((blocks * a.pieces + 7) / 8 * 8 * ranks));
     constexpr int lds = kOuterWaves / 2 * F * RI * 1024;
     static_assert(lds + kOuterAdapters * 4 <= 64 * 1024, "LDS of an ordinary launch");
-    if (a.out == EXPERTS_FP32) adapters_outer_kernel<ELEM, F, RI, 3><<<grid, dim3(64 * kOuterWaves), lds, s>>>(a);
-    else adapters_outer_kernel<ELEM, F, RI, 2><<<grid, dim3(64 * kOuterWaves), lds, s>>>(a);
+    adapters_outer_kernel<ELEM, F, RI><<<grid, dim3(64 * kOuterWaves), lds, s>>>(a);
     return hipGetLastError();
 }
 template <int ELEM>

@@ -1,8 +1,8 @@
 // R[i] = X[i] W + T[i] B[a(i)]: the products by rows of one shared matrix (experts_tile.h), to whose sums the adapters' are added.
 //
-// T is fp32 and stays so: it enters the matrix instructions as two bf16 pieces where R has 16 bits (a rounding of 2^-15 to each value at most, under R's of 2^-8 or
-// 2^-11), as three, exactly, where it has 32; B of fp16 as two, exactly (fp16 products would be the shorter way, but T may lie
-// outside its range).  A workgroup lays the pieces of its rows out in LDS.  A block of 16 rows that a segment has in part takes an
+// T is fp32 and stays so: it enters the matrix instructions as three bf16 pieces, all of its 24 bits (two, 16 bits, would be 3 % faster with rank 64 and
+// were seen in results of 16 bits where X W and T B cancel: up to 29 times as far off as sums of 32 bits are); B of fp16 as two, exactly (fp16
+// products would be the shorter way, but T may lie outside its range).  So a row's sums have the same bits of T whichever way they are added.  A workgroup lays the pieces of its rows out in LDS.  A block of 16 rows that a segment has in part takes an
 // instruction's sums over in the lanes whose row it is: nothing of another segment's operands is seen, not even an infinity times zero.
 //
 // That is for tiles of many rows, when their own sums are done and the stages' LDS is free: B of as many segments as it holds is laid out
@@ -111,7 +111,7 @@ struct Adapters {
             }
         }
     }
-    __device__ __forceinline__ void write_t(char *lds, float (&t)[T_ITEMS][8], int begin, int u0, int n, int pieces) const
+    __device__ __forceinline__ void write_t(char *lds, float (&t)[T_ITEMS][8], int begin, int u0, int n) const
     {
 #pragma unroll
         for (int q = 0; q < T_ITEMS; ++q) {
@@ -121,21 +121,21 @@ struct Adapters {
             const int row = tile_row + line, k = (u0 + unit) * 8;
 #pragma unroll
             for (int j = 0; j < 8; ++j) t[q][j] = row < a.rows.M && k + j < a.r ? t[q][j] : 0.0f;
-            for (int piece = 0; piece < pieces; ++piece) {
+            for (int piece = 0; piece < kPieces; ++piece) {
                 xt_u4 v;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = bf16_pair(piece_of(t[q][2 * j], piece, pieces), piece_of(t[q][2 * j + 1], piece, pieces));
-                *(xt_u4 *)(lds + ((unit * pieces + piece) * T::BM + (line ^ turn(unit))) * 16) = v;
+                for (int j = 0; j < 4; ++j) v[j] = bf16_pair(piece_of(t[q][2 * j], piece, kPieces), piece_of(t[q][2 * j + 1], piece, kPieces));
+                *(xt_u4 *)(lds + ((unit * kPieces + piece) * T::BM + (line ^ turn(unit))) * 16) = v;
             }
         }
     }
     // from item `begin` of the thread's on
-    __device__ __forceinline__ void lay_out_t(char *lds, int begin, int u0, int n, int pieces) const
+    __device__ __forceinline__ void lay_out_t(char *lds, int begin, int u0, int n) const
     {
         for (int at = (int)threadIdx.x + begin * T::NT; at < n * T::BM; at += T_ITEMS * T::NT) {
             float t[T_ITEMS][8];
             read_t(t, at, u0, n);
-            write_t(lds, t, at, u0, n, pieces);
+            write_t(lds, t, at, u0, n);
         }
     }
     // An instruction's products added to block m, in the rows lo .. hi - 1.  (Blocks that a segment has whole could do without the choice; a
@@ -411,25 +411,24 @@ struct AddFromLds : Adapters<T> {
     static constexpr int LDS = T::LDS + (int)sizeof(List), ROOM = T::LDS;
     static constexpr int OF_B = Adapters<T>::OF_B;
     static constexpr int ITEMS = 4;   // 16 bytes of B that a thread has on their way
-    static_assert(ROOM >= (3 * T::BM + OF_B * T::BN) * 16 && ITEMS * T::NT >= T::BN, "a unit of both");
+    static_assert(ROOM >= 4 * (kPieces * T::BM + OF_B * T::BN) * 16 && ITEMS * T::NT >= 4 * T::BN, "four units of both");
     // T and the first segments' B are asked for before the sums begin, where there are registers for them
     static constexpr bool AHEAD = T::BM < 256;
     static constexpr int T_ITEMS = Adapters<T>::T_ITEMS;
+    // units at a time, in fours as an instruction has them (fp16, 8192 x 8192 x 4096, rank 64 on 256 x 256 tiles, four and four of 8 / six and two: 567 / 604 us)
+    static constexpr int FIT = ROOM / (kPieces * T::BM * 16 + OF_B * T::BN * 16), ASKED = ITEMS * T::NT / T::BN, MOST = (FIT < ASKED ? FIT : ASKED) & ~3;
     mutable xt_u4 next[ITEMS];
     mutable float t0[T_ITEMS][8];
-    int pieces, units, most;
+    int units;
     __device__ __forceinline__ AddFromLds(const Adapters<T> &x) : Adapters<T>(x)
     {
-        pieces = this->a.mm.out == EXPERTS_FP32 ? 3 : 2;
         units = (this->a.r + 7) / 8;
-        most = ROOM / (pieces * T::BM * 16 + OF_B * T::BN * 16);
-        most = most < ITEMS * T::NT / T::BN ? most : ITEMS * T::NT / T::BN;
-        if (AHEAD && this->a.r > 0 && this->a.rows.S > 0) this->read_t(t0, (int)threadIdx.x, 0, units < most ? units : most);
+        if (AHEAD && this->a.r > 0 && this->a.rows.S > 0) this->read_t(t0, (int)threadIdx.x, 0, units < MOST ? units : MOST);
     }
     // segments of a batch, one at least
     __device__ __forceinline__ int at_once(int n_units) const
     {
-        const int room = (ROOM - n_units * pieces * T::BM * 16) / (n_units * OF_B * T::BN * 16), items = ITEMS * T::NT / (n_units * T::BN);
+        const int room = (ROOM - n_units * kPieces * T::BM * 16) / (n_units * OF_B * T::BN * 16), items = ITEMS * T::NT / (n_units * T::BN);
         return room < items ? room : items;
     }
     static __device__ __forceinline__ List *list() { return (List *)(xt_smem + T::LDS); }
@@ -459,7 +458,7 @@ struct AddFromLds : Adapters<T> {
                 // (all lanes take part: those of no segment send to the last one, which a full list alone reads)
                 const int to = (m.which >> x.lane) & 1 ? __popcll(m.which & ((1ull << x.lane) - 1)) : 63;
                 const int adapter = __builtin_amdgcn_ds_permute(to * 4, m.adapter);
-                const int met = __popcll(m.which), n_units = x.units < x.most ? x.units : x.most, once = x.at_once(n_units);
+                const int met = __popcll(m.which), n_units = x.units < MOST ? x.units : MOST, once = x.at_once(n_units);
                 x.read_batch(x.next, met < once ? met : once, 0, n_units, [&](int k) { return __shfl(adapter, k); });
             }
         }
@@ -477,14 +476,14 @@ struct AddFromLds : Adapters<T> {
     {
         const UpArgs &a = this->a;
         if (a.r == 0 || a.rows.S == 0) return;
-        const int t_unit = pieces * T::BM * 16, b_unit = OF_B * T::BN * 16;
+        const int t_unit = kPieces * T::BM * 16, b_unit = OF_B * T::BN * 16;
         __syncthreads();   // (the ring is read no more, and the list is there)
         const int first = __builtin_amdgcn_readfirstlane(list()->chunk);
         if (!__builtin_amdgcn_readfirstlane(list()->n | list()->more)) return;
-        for (int u0 = 0; u0 < units; u0 += most) {
-            const int n_units = units - u0 < most ? units - u0 : most, once = at_once(n_units);
+        for (int u0 = 0; u0 < units; u0 += MOST) {
+            const int n_units = units - u0 < MOST ? units - u0 : MOST, once = at_once(n_units);
             char *const lds_b = xt_smem + n_units * t_unit;
-            const Ways ways(n_units, pieces * OF_B);
+            const Ways ways(n_units, kPieces * OF_B);
             if (u0 > 0) {
                 __syncthreads();
                 if (threadIdx.x < 64 && __builtin_amdgcn_readfirstlane(list()->chunk) != first) look(first);
@@ -495,8 +494,8 @@ struct AddFromLds : Adapters<T> {
                 const auto adapter = [&](int s0) { return [s0](int k) { return list()->of[s0 + k].x; }; };
                 if (met > 0 && (!AHEAD || begun || u0 > 0)) read_batch(next, met < once ? met : once, u0, n_units, adapter(0));
                 if (!begun) {
-                    if (AHEAD && u0 == 0) this->write_t(xt_smem, t0, (int)threadIdx.x, 0, n_units, pieces);
-                    this->lay_out_t(xt_smem, AHEAD && u0 == 0 ? T_ITEMS : 0, u0, n_units, pieces);
+                    if (AHEAD && u0 == 0) this->write_t(xt_smem, t0, (int)threadIdx.x, 0, n_units);
+                    this->lay_out_t(xt_smem, AHEAD && u0 == 0 ? T_ITEMS : 0, u0, n_units);
                 }
                 for (int s0 = 0; s0 < met; s0 += once) {
                     const int n = met - s0 < once ? met - s0 : once, left = met - s0 - n;
@@ -507,7 +506,7 @@ struct AddFromLds : Adapters<T> {
                         for (int k = 0; k < n; ++k) {
                             const int4 seg = list()->of[s0 + k];
                             const int lo = __builtin_amdgcn_readfirstlane(seg.y), hi = __builtin_amdgcn_readfirstlane(seg.z);
-                            if (lo < this->row0 + T::MI * 16 && hi > this->row0) products(acc, lds_b + k * n_units * b_unit, lo, hi, ways, pieces);
+                            if (lo < this->row0 + T::MI * 16 && hi > this->row0) products(acc, lds_b + k * n_units * b_unit, lo, hi, ways);
                         }
                     __syncthreads();
                 }
@@ -560,7 +559,7 @@ struct AddFromLds : Adapters<T> {
             for (int p = 0; p < OF_B; ++p) *(xt_u4 *)(lds + (((k * units + unit) * OF_B + p) * T::BN + (this->line_of_b(line) ^ this->turn(unit))) * 16) = this->piece_of_b(v[q], p);
         }
     }
-    __device__ __forceinline__ void products(xt_f4 (&acc)[T::MI][T::NI], const char *lds_b, int lo, int hi, const Ways &ways, int pieces) const
+    __device__ __forceinline__ void products(xt_f4 (&acc)[T::MI][T::NI], const char *lds_b, int lo, int hi, const Ways &ways) const
     {
         const int lane = this->lane, b = lane >> 4;
         const char *const t_row = xt_smem + (this->row0 - this->tile_row) * 16, *const b_row = lds_b + (this->col0 - this->tile_col) * 16;
@@ -571,7 +570,7 @@ struct AddFromLds : Adapters<T> {
             const int read = s / each;
             const bool there = ways.at(read, s - read * each, b, unit, way);
             const int at = ((lane & 15) ^ this->turn(unit)) * 16;
-            const char *const t_at = t_row + (there ? unit * pieces + way / OF_B : 0) * (T::BM * 16) + at;
+            const char *const t_at = t_row + (there ? unit * kPieces + way / OF_B : 0) * (T::BM * 16) + at;
             const char *const b_at = b_row + (there ? unit * OF_B + way % OF_B : 0) * (T::BN * 16) + at;
             xt_u4 vb[T::NI];
 #pragma unroll
