@@ -26,7 +26,8 @@ __device__ __forceinline__ void count_rows(const Segments &s, int *counts)
     }
     __syncthreads();
 }
-__device__ __forceinline__ int pieces_of(int rows, int quota) { return rows > 0 ? (rows + quota - 1) / quota : 1; }
+// (rows and quota together may pass 2^31)
+__device__ __forceinline__ int pieces_of(int rows, int quota) { return rows > 0 ? (int)(((uint32_t)rows + (uint32_t)quota - 1) / (uint32_t)quota) : 1; }
 __device__ __forceinline__ bool find_piece(const int *counts, int G, int quota, int k, int lane, Piece &p)
 {
     int before = 0;
