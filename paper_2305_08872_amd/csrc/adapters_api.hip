@@ -12,7 +12,6 @@ static const int64_t kMostRows = 2147483647LL - 65536LL;   // of a dimension, as
 static const int64_t kMostGroups = 1 << 16;                // adapters, and segments
 static const int64_t kMostRank = 1 << 16;
 static const int64_t kMostBlocks256 = 0xffffffffLL / 256;  // workgroups of a launch (a grid holds 2^32 - 1 work-items) of 256 threads
-static const int64_t kMostBlocks512 = 0xffffffffLL / 512;
 static const int64_t kMostPitch = 0xffffffffLL / 256 - 65536;   // bytes, of the shared product's operands (as in the products by groups)
 
 static bool known16(int type) { return type == AMULET_BF16 || type == AMULET_FP16; }
@@ -166,7 +165,6 @@ int amulet_adapters_mm(int type, int out_type, int trans_w, int trans_a, int tra
     if (some && K > 0 && lda > kMostPitch / 2) return AMULET_ERR_RANGE;
     if (some && N > 0 && (ldb < (trans_b ? r : N) || (G > 1 && group_b < 0))) return AMULET_ERR_LD;
     if (some && N > 0 && ldb > kMostPitch / 2) return AMULET_ERR_RANGE;
-    if (r > 0 && (M + 15) / 16 + S + 1 > kMostBlocks512 / ((r + 15) / 16)) return AMULET_ERR_RANGE;
 
     Segments rows = {};
     rows.offsets = offsets; rows.adapters = adapters;
@@ -203,7 +201,9 @@ int amulet_adapters_mm(int type, int out_type, int trans_w, int trans_a, int tra
         d.rows = rows; d.X = X; d.A = A; d.scales = scales; d.T = T;
         d.ldx = ldx; d.lda = lda; d.group_a = group_a; d.ldt = ldt; d.K = (int)K; d.r = (int)r; d.across = !trans_a;
         if (N == 0) note_kernel("adapters_down", M);
-        const int rc = launch_status(launch_adapters_down(type, d, s));
+        const hipError_t e = launch_adapters_down(type, d, s);
+        if (e == hipErrorInvalidConfiguration) return AMULET_ERR_RANGE;
+        const int rc = launch_status(e);
         if (rc != AMULET_OK) return rc;
     }
     if (N == 0) return AMULET_OK;

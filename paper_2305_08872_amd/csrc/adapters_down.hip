@@ -82,12 +82,16 @@ __global__ void __launch_bounds__(T::NT) adapters_down_kernel(const DownArgs a)
     });
 }
 
+// (a dimension of a grid holds 2^32 - 1 work-items)
+static bool fits(int64_t cuts, int threads) { return cuts <= 0xffffffffLL / threads; }
+
 template <class T>
 static hipError_t launch_tile(const DownArgs &a, hipStream_t s)
 {
+    const int64_t cuts = ((int64_t)a.rows.M + T::BM - 1) / T::BM + a.rows.S + 1;
+    if (!fits(cuts, T::NT)) return hipErrorInvalidConfiguration;
     static const hipError_t granted = hipFuncSetAttribute((const void *)adapters_down_kernel<T>, hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
     if (granted != hipSuccess) { (void)hipGetLastError(); return granted; }
-    const int64_t cuts = ((int64_t)a.rows.M + T::BM - 1) / T::BM + a.rows.S + 1;
     adapters_down_kernel<T><<<dim3((unsigned)cuts, (unsigned)((a.r + T::BN - 1) / T::BN)), dim3(T::NT), T::LDS, s>>>(a);
     return hipGetLastError();
 }
@@ -99,8 +103,8 @@ static hipError_t launch_down(const DownArgs &a, hipStream_t s)
     // 4096 13 / 15.  Blocks too, four workgroups to a compute unit, where up to 32 ranks have more than a round of 64 rows, whose last ones would
     // be alone: 16384 x 4096 rank 16 31 / 42 us, 65536 x 4096 99 / 116, 16384 x 4096 rank 32 38 / 43.
     const int64_t M = a.rows.M, S = a.rows.S, ranks = a.r <= 16 ? 16 : a.r <= 32 ? 32 : 64;
-    const bool rounds = M / 64 + S > compute_units();
-    const int rows = M < 16 * S ? 16 : (M / 32 + S) * ((a.r + ranks - 1) / ranks) <= compute_units() ? 32 : rounds && a.r <= 32 ? 16 : 64;
+    const bool rounds = M / 64 + S > compute_units(), held = fits(M / 16 + S + 2, 256);
+    const int rows = M < 16 * S ? 16 : (M / 32 + S) * ((a.r + ranks - 1) / ranks) <= compute_units() ? 32 : rounds && a.r <= 32 && held ? 16 : 64;
     if (a.r <= 16)
         return rows == 16 && rounds ? launch_tile<ExpertTile<ELEM, 16, 16, 1, 1, 4, 3, false, KS>>(a, s)
                : rows == 16 ? launch_tile<ExpertTile<ELEM, 16, 16, 1, 1, 8, 4, false, KS>>(a, s)

@@ -25,6 +25,7 @@ struct DownArgs {
     int64_t ldx, lda, group_a, ldt;
     int K, r, across;          // across: A's storage has k across its rows (K x r), else r x K
 };
+// (hipErrorInvalidConfiguration, before anything is launched: no launch holds it)
 hipError_t launch_adapters_down(int type, const DownArgs &a, hipStream_t s);
 
 // R[i] = X[i] W + T[i] B[a]
