@@ -846,6 +846,8 @@ int amulet_get_deterministic(void);
  * refused launch.  n <= 0 switches it off.
  */
 void amulet_debug_fail_launches(int n);
+/* ... the k-th attempt from now on alone; those before and behind it are made (calls of several launches).  k <= 0 switches it off. */
+void amulet_debug_fail_launch(int k);
 
 /* Library version string (static storage). */
 const char *amulet_version(void);

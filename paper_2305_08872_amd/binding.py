@@ -157,6 +157,8 @@ def load_library():
     lib.amulet_get_deterministic.argtypes = []
     lib.amulet_debug_fail_launches.restype = None
     lib.amulet_debug_fail_launches.argtypes = [i32]
+    lib.amulet_debug_fail_launch.restype = None
+    lib.amulet_debug_fail_launch.argtypes = [i32]
     lib.amulet_version.restype = ctypes.c_char_p
     lib.amulet_version.argtypes = []
     sz = ctypes.c_size_t
@@ -1107,6 +1109,11 @@ def amulet_get_deterministic() -> bool:
 def amulet_debug_fail_launches(n: int) -> None:
     """Test seam: the next n kernel launches are refused on the host and reported as failed."""
     load_library().amulet_debug_fail_launches(int(n))
+
+
+def amulet_debug_fail_launch(k: int) -> None:
+    """Test seam: the k-th kernel launch from now on is refused on the host and reported as failed, no other."""
+    load_library().amulet_debug_fail_launch(int(k))
 
 
 def amulet_version() -> str:

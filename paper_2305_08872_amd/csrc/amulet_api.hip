@@ -1863,6 +1863,8 @@ int amulet_get_deterministic(void) { return k_split_allowed() ? 0 : 1; }
 
 void amulet_debug_fail_launches(int n) { g_forced_launch_failures.store(n > 0 ? n : 0, std::memory_order_relaxed); }
 
+void amulet_debug_fail_launch(int k) { g_forced_launch_failure_at.store(k > 0 ? k : 0, std::memory_order_relaxed); }
+
 const char *amulet_version(void) { return "amulet-gfx950 0.1"; }
 
 }  // extern "C"

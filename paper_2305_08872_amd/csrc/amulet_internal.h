@@ -134,11 +134,15 @@ inline bool pitch_collides(int64_t ld, int elem_bytes)
 // Test seam (amulet_debug_fail_launches): while positive, each launch attempt is refused on the
 // host, counted down, and reported as hipErrorLaunchFailure; nothing reaches the device.
 inline std::atomic<int> g_forced_launch_failures{0};
+inline std::atomic<int> g_forced_launch_failure_at{0};   // attempts up to one that fails (0: none)
 inline bool forced_launch_failure()
 {
     int n = g_forced_launch_failures.load(std::memory_order_relaxed);
     while (n > 0)
         if (g_forced_launch_failures.compare_exchange_weak(n, n - 1, std::memory_order_relaxed)) return true;
+    n = g_forced_launch_failure_at.load(std::memory_order_relaxed);
+    while (n > 0)
+        if (g_forced_launch_failure_at.compare_exchange_weak(n, n - 1, std::memory_order_relaxed)) return n == 1;
     return false;
 }
 

@@ -58,3 +58,33 @@ def test_rows_that_a_launch_holds(am, M, N, K, r):
             # (whole numbers, moved by 128 stand-ins of 2^-30 of a T below 2^6 and as many roundings of sums below 2^13, then rounded to bf16)
             want = sign * want.sum(1, keepdim=True)
             assert ((R[i:j].float() - want).abs() <= 2.0 ** -8 * want.abs() + 2 * 128 * 2.0 ** -11).all()
+
+
+def test_each_launch_of_a_call_can_be_refused(am):
+    """The status of every launch of a call comes back, not of the first alone."""
+    bf = dict(dtype=BF16, device="cuda")
+    x, w, a, b = torch.zeros(40, 64, **bf), torch.zeros(96, 64, **bf), torch.zeros(2, 8, 64, **bf), torch.zeros(2, 96, 8, **bf)
+    off, t, y = i32([0, 10, 40]), torch.zeros(40, 8, device="cuda"), torch.zeros(40, 96, **bf)
+    wide, tall = torch.zeros(2048, 1032, **bf), torch.zeros(8200, 1032, **bf)
+    wide_y, wide_t, wide_a, wide_b = torch.zeros(2048, 8200, **bf), torch.zeros(2048, 8, device="cuda"), torch.zeros(1, 8, 1032, **bf), torch.zeros(1, 8200, 8, **bf)
+    long_x, long_t, d = torch.zeros(20000, 64, **bf), torch.zeros(20000, 8, device="cuda"), torch.zeros(1, 64, 8, device="cuda")
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    grads, many, norm = [torch.zeros(10, device="cuda") for _ in range(190)], [torch.zeros(9 * 8192, device="cuda") for _ in range(1000)], torch.zeros(1, device="cuda")
+    kw = dict(trans_w=True, trans_a=True, trans_b=True)
+    calls = [(lambda: am.amulet_adapters_mm(x, w, a, b, off, t, y, **kw), 2), (lambda: am.amulet_adapters_mm(wide, tall, wide_a, wide_b, i32([0, 2048]), wide_t, wide_y, **kw), 3),
+             (lambda: am.amulet_adapters_mm(x, w, a[:, :0], b[:, :, :0], off, t[:, :0], y, **kw), 1), (lambda: am.amulet_adapters_wgrad(x, t, off, torch.empty(2, 64, 8, device="cuda")), 1),
+             (lambda: am.amulet_adapters_wgrad(long_x, long_t, i32([0, 20000]), d, ws), 2), (lambda: am.amulet_grad_norm(grads, norm, ws), 3),
+             (lambda: am.amulet_grad_norm_clip(grads, 1.0, norm, ws), 4), (lambda: am.amulet_grad_norm_clip(many, 1.0, norm, ws), 13), (lambda: am.amulet_grad_clip(grads, 1.0, norm), 2)]
+    try:
+        for n, (call, launches) in enumerate(calls):
+            for k in range(1, launches + 1):
+                am.amulet_debug_fail_launch(k)
+                with pytest.raises(am.AmuletError) as e:
+                    call()
+                assert e.value.code == -5, (n, k)
+            am.amulet_debug_fail_launch(launches + 1)
+            call()      # (as many launches as said)
+            am.amulet_debug_fail_launch(0)
+    finally:
+        am.amulet_debug_fail_launch(0)
+    torch.cuda.synchronize()
