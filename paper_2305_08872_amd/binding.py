@@ -249,9 +249,15 @@ def _mat(t, dtype, what: str):
     ld, step = t.stride()
     if cols > 1 and step != 1:
         raise ValueError("%s must have unit column stride" % what)
+    return t.data_ptr(), rows, cols, _pitch(rows, cols, ld)
+
+
+def _pitch(rows: int, cols: int, ld: int) -> int:
+    """What a call takes as the leading dimension: a tensor of one row or no values may have any; one of no elements between rows (an expanded
+    one) stays as it is, for the call to refuse."""
     if rows <= 1:
         ld = cols
-    return t.data_ptr(), rows, cols, ld if ld > 0 else 1
+    return ld if ld > 0 or (rows > 1 and cols > 0) else 1
 
 
 _N_PARAM_ROWS = {AMULET_DISCOUNT: 2, AMULET_BOOST: 1, AMULET_COUNT_GT: 1}
@@ -697,9 +703,8 @@ def _groups(t, dtype, what: str):
     gs, ld, step = t.stride()
     if cols > 1 and step != 1:
         raise ValueError("%s must have unit column stride" % what)
-    if rows <= 1:
-        ld = cols
-    return t.data_ptr(), G, rows, cols, ld if ld > 0 else 1, gs if G > 1 else rows * max(ld, 1)
+    ld = _pitch(rows, cols, ld)
+    return t.data_ptr(), G, rows, cols, ld, gs if G > 1 else rows * max(ld, 1)
 
 
 def _bytes(t, what: str):

@@ -32,6 +32,14 @@ const at::Tensor *device_tensor(PyObject *o, at::ScalarType type)
     return &t;
 }
 
+// the leading dimension: a tensor of one row or no values may have any; one of no elements between rows (an expanded one) stays as it is, for
+// the call to refuse
+int64_t pitch(int64_t rows, int64_t cols, int64_t ld)
+{
+    if (rows <= 1) ld = cols;
+    return ld > 0 || (rows > 1 && cols > 0) ? ld : 1;
+}
+
 // ... of two dimensions with unit column stride
 bool matrix(PyObject *o, at::ScalarType type, Mat &m)
 {
@@ -40,8 +48,7 @@ bool matrix(PyObject *o, at::ScalarType type, Mat &m)
     m.rows = t->size(0);
     m.cols = t->size(1);
     if (m.cols > 1 && t->stride(1) != 1) return false;
-    m.ld = m.rows <= 1 ? m.cols : t->stride(0);
-    if (m.ld <= 0) m.ld = 1;
+    m.ld = pitch(m.rows, m.cols, t->stride(0));
     m.p = t->data_ptr();
     return true;
 }
@@ -260,8 +267,7 @@ bool groups(PyObject *o, at::ScalarType type, Groups &g)
     g.rows = t->size(1);
     g.cols = t->size(2);
     if (g.cols > 1 && t->stride(2) != 1) return false;
-    g.ld = g.rows <= 1 ? g.cols : t->stride(1);
-    if (g.ld <= 0) g.ld = 1;
+    g.ld = pitch(g.rows, g.cols, t->stride(1));
     g.apart = g.n > 1 ? t->stride(0) : g.rows * g.ld;
     g.p = t->data_ptr();
     return true;
