@@ -37,7 +37,8 @@ __device__ __forceinline__ void segment_rows(const Segments &g, int s, int &lo, 
 
 // An fp32 value as a sum of bf16 ones: the first has the sign and the upper 8 bits (no rounding: it does not become infinite), the next
 // what is left.  Two keep 16 bits (all that an fp16 value has), three all 24.  A piece of which nothing is left (or of an infinity) is the one before times
-// 2^-30, far below the sum's rounding, so that a product with an infinity has its sign in every piece and is no NaN; zeros stay zeros.
+// 2^-30, far below the sum's rounding, so that a product with an infinity has its sign in every piece and is no NaN; zeros stay zeros.  (What of a value lies
+// below bf16's smallest, 2^-133, is lost: bits of values below 2^-109; a piece of one below 2^-103 may be zero, and a product of that with an infinity NaN.)
 constexpr int kPieces = 3;   // of T's values
 __device__ __forceinline__ float piece_first(float x)
 {

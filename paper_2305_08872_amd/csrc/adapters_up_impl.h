@@ -46,17 +46,15 @@ struct Adapters {
     int tile_row, tile_col, row0, col0, lane, kg;   // the tile's first row and column, the wave's
     bool idle;
 
-    // 8 ranks (from `unit` * 8 on) of column n of an adapter's matrix; zeros past the rank
-    __device__ __forceinline__ xt_u4 read_b(const char *b, int n, int unit, bool there) const
+    // 8 ranks (from `unit` * 8 on, the first there) of column n of an adapter's matrix; zeros past the rank
+    __device__ __forceinline__ xt_u4 read_b(const char *b, int n, int unit) const
     {
         xt_u4 v = {0, 0, 0, 0};
         if (!a.across) {
             const char *const row = b + (int64_t)n * a.ldb * 2;
             typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
-            if ((a.r & 7) == 0) {
-                v = __builtin_bit_cast(xt_u4, *(const u4 *)(row + (unit * 8 < a.r ? unit * 16 : 0)));
-                if (!there) v = xt_u4{0, 0, 0, 0};
-            } else if (there) v = load_unit<2>(row, unit * 16, a.r * 2);
+            if ((a.r & 7) == 0) v = __builtin_bit_cast(xt_u4, *(const u4 *)(row + unit * 16));
+            else v = load_unit<2>(row, unit * 16, a.r * 2);
         } else {
             uint32_t x[8];
 #pragma unroll
@@ -65,7 +63,7 @@ struct Adapters {
                 x[j] = *(const uint16_t *)(b + ((int64_t)(k < a.r ? k : a.r - 1) * a.ldb + n) * 2);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = there && unit * 8 + j < a.r ? x[j] : 0u;
+            for (int j = 0; j < 8; ++j) x[j] = unit * 8 + j < a.r ? x[j] : 0u;
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = x[2 * j] | (x[2 * j + 1] << 16);
         }
@@ -546,7 +544,7 @@ struct AddFromLds : Adapters<T> {
             const int g = adapter(there ? k : 0);
             if (!there) continue;
             const int c = this->tile_col + line;
-            v[q] = this->read_b((const char *)a.B + (int64_t)g * a.group_b * 2, c < a.mm.N ? c : a.mm.N - 1, u0 + unit, true);
+            v[q] = this->read_b((const char *)a.B + (int64_t)g * a.group_b * 2, c < a.mm.N ? c : a.mm.N - 1, u0 + unit);
         }
     }
     __device__ __forceinline__ void write_batch(const xt_u4 (&v)[ITEMS], char *lds, int n, int units) const

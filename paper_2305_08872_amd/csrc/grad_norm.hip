@@ -3,7 +3,7 @@
 // Bound by their bytes: read once for the norm, read again and written once to be clipped.  Squares are summed in fp64, where neither a
 // large fp32 value's overflows nor a small one's is lost: each thread's own, then a workgroup's, in an order that the sizes fix; the
 // workgroups' sums go to the workspace and are added up in order by whoever needs the norm (a workgroup of the clipping kernel each for
-// itself: 8 KB from the caches in place of a launch).  us: the norm of 2^28 bf16 values 97 (5.5 TB/s), 2^29 clipped, from the last to the first, which the
+// itself: up to 64 KB from the caches, 8 or 16 as a rule, in place of a launch).  us: the norm of 2^28 bf16 values 97 (5.5 TB/s), 2^29 clipped, from the last to the first, which the
 // caches may still have, 579 (3.2 GB of reads and writes at a copy's rate: 633).
 #include "adapters_internal.h"
 #include "experts_tile.h"
