@@ -28,7 +28,8 @@ static bool matrices_apart(int64_t G, int64_t rows, int64_t cols, int64_t ld, in
 
 // How the gradients' sums are shared out.  Columns to a workgroup: 128, or 64 (half of a row's bytes in a request) where those would not
 // give every compute unit one.  Rows: an adapter's, or pieces of it, two workgroups of four waves to a compute unit, that the workspace has
-// room for, of 512 rows at least (fewer are not worth the second launch, 4 us).  us, whole / pieces of 512 / 1024 / 2048 rows, out of the caches:
+// room for, of 512 rows at least (fewer are not worth the second launch, 4 us).  us, whole / pieces of 512 / 1024 / 2048 rows, out of the caches
+// (rank 16, here and below: T in two pieces, 1 us less than three):
 // 16384 x 4096 by rank 16, 4 adapters of equal rows 42 / 37 / 34 / 33, one of them with half of the rows 73 / 39 / 41 / 40; 4096 x 4096 by rank 64,
 // 8 adapters, results of 32 bits 20 / 24 / 24 / 24 and 45 / 31 / 29 / 43.
 struct OuterPlan {
@@ -170,8 +171,9 @@ int amulet_adapters_mm(int type, int out_type, int trans_w, int trans_a, int tra
     rows.offsets = offsets; rows.adapters = adapters;
     rows.S = some ? (int)S : 0; rows.G = some ? (int)G : 0; rows.M = (int)M;
     // Segments of a few rows: row by row, which the larger tiles have no room for.  us without the first product, row by row / through LDS, 1, 2, 4 and 8 rows to a
-    // segment: 1337 x 3033 x 2319 rank 32 76 / 132, 74 / 89, 73 / 67 and 72 / 57, rank 8 75 / 84, 73 / 64, 71 / 55 and 71 / 50; B across, rank 32, 94 / 173, 92 / 110,
-    // 92 / 77 and 92 / 62.  Segments shorter than a block of rows: no more than 64 of those to a tile (4 rows to a segment 77, 128 rows to a tile 130).
+    // segment: 1337 x 3033 x 2319 rank 32 76 / 132, 74 / 89, 73 / 72 and 72 / 59, rank 8 75 / 84, 73 / 64, 71 / 56 and 71 / 51; B across, rank 32, 94 / 173, 92 / 110,
+    // 92 / 84 and 92 / 66 (LDS at 1 and 2 rows: T in two pieces, less than three take).  Segments shorter than a block of rows: no more than 64 of those to a tile (4 rows to a
+    // segment, B across, 84; 128 rows to a tile, two pieces, 130).
     bool many = some && M < 4 * S;
     const bool brief = some && M < 16 * S;
     UpArgs u = {};
@@ -184,7 +186,7 @@ int amulet_adapters_mm(int type, int out_type, int trans_w, int trans_a, int tra
         if (plan.tile < 0 && brief) { many = false; plan = rows_plan(2, !trans_w, u.mm, M, N, 1, EXPERTS_256x256); }
         if (plan.tile < 0) return AMULET_ERR_RANGE;
         // Longer segments, and B across, in odd ranks or read more than twice: rather the tile without k groups, through LDS.  (208 x 4096 x 4096, 64 rows to a
-        // segment, B across, rank 8 / 32 / 64 24 / 26 / 29 us, row by row 28 / 29 / 38; 8 rows to a segment 25 / 32 / 42.)
+        // segment, B across, rank 8 / 32 / 64 24 / 26 / 29 us, row by row 28 / 29 / 38; 8 rows to a segment, row by row, 26 / 27 / 36, through LDS 25 / 32 / 42.)
         if (some && M >= 12 * S && plan.tile == EXPERTS_64x64_K2 && (!trans_b || r % 8 != 0 || r > 64)) plan.tile = EXPERTS_64x64;   // (of as many workgroups)
         // (row by row two columns of B across are read at a time)
         if (some && N < 2 && !trans_b) {

@@ -4,8 +4,8 @@
 // rows; its waves take steps of 32 rows in turn and join their sums in LDS, in order.  A lane reads 2 F bytes of 8 rows of X
 // and turns them in registers (byte permutes) into F columns of 8 rows each, the operands of F matrix instructions: lane i of 16 has
 // columns F i + f in instruction f, so that what it ends with are neighbouring columns.  T is fp32 and is taken as three bf16 pieces, all
-// of its bits (adapters_segments.h), X of fp16 as two.  us, 16384 x 4096 bf16, 4 adapters, rank 16 / 32 / 64: 28 (4.8 TB/s of X) / 33 / 44,
-// and 5 to 7 to add up the pieces.
+// of its bits (adapters_segments.h), X of fp16 as two.  us with the pieces' sums (5 to 7), 16384 x 4096, 4
+// adapters, out of the caches, rank 16 / 32 / 64: bf16 35 / 42 / 66 (rank 16: 4.6 TB/s of X before the sums), fp16 54 / 67 / 96.
 #include "adapters_segments.h"
 
 namespace amulet {
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(64 * kOuterWaves) __attribute__((amdgpu_waves_
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int i = lane & 15, b = lane >> 4;
     // (The blocks of ranks of the same rows and columns lie behind one another on the same XCD, workgroups 8 apart: its cache has X then.  Rank 64, 16384
-    // rows of 4096 columns: 44 / 51 us, half as many reads of memory.)
+    // rows of 4096 columns, T in two pieces: 44 / 51 us, half as many reads of memory.)
     const unsigned blocks = (unsigned)((a.N + COLS - 1) / COLS), ranks = (unsigned)((a.r + 16 * RI - 1) / (16 * RI));
     const unsigned turn = blockIdx.x >> 3, at = turn / ranks * 8 + (blockIdx.x & 7), piece = at / blocks;
     if (piece >= (unsigned)a.pieces) return;

@@ -10,8 +10,8 @@
 // row, on the vector ALU, while the first stages of X and W are on their way.
 //
 // Bound by the shared product's operations (many rows) or W's bytes (few).  us, bf16, beside the same call without adapters: 8192 x 8192 x 4096 by
-// 24 segments, rank 64 465 / 429; 16384 x 4096 x 4096, rank 16 446 / 442; 8 x 4096 x 4096, a segment to a row, rank 16 9 of a call's 14 / 13; 208 rows of
-// as many segments, rank 32 24 / 17.
+// 24 segments, rank 64 497 / 424, rank 16 451 / 426, rank 64 of fp16 562 / 444; 16384 x 4096 x 4096, rank 16 454 / 439; 4096 x 4096 x 2048 by 32 segments, rank 64, results
+// of 32 bits 88 / 65; 8 x 4096 x 4096, a segment to a row, rank 16 10.4 / 9.2; 208 rows of 192 segments, rank 32 24 / 17.
 #ifndef AMULET_ADAPTERS_UP_IMPL_H
 #define AMULET_ADAPTERS_UP_IMPL_H
 
